@@ -22,7 +22,7 @@ PROBE_PATH = os.path.join(PKG, "libomnitide_probe.so")
 ARCH = "gfx950"
 
 SOURCES = ["abi.cpp", "score.hip", "select.hip", "spans.hip", "compact.hip", "native.hip",
-           "attention.hip", "decode.hip"]
+           "attention.hip", "decode.hip", "paged_abi.cpp", "norm_rope.hip", "paged_attn.hip"]
 
 # Packed fp32 instructions are kept out of the device code (-packed-fp32-ops).
 HIP_FLAGS = ["-x", "hip", f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
