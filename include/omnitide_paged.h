@@ -137,7 +137,7 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
  * The bytes of rows that are not in use are never used (they may hold anything, NaN included); those
  * of the rows in use are finite numbers.
  * Numerics: bf16 products with float accumulation, float softmax.  Limits: n_q_heads a multiple of
- * n_kv_heads, n_seq <= 1024, scale finite.
+ * n_kv_heads, n_seq <= 1024, n_seq * max_pages * page_size * n_kv_heads <= 2^34, scale finite.
  */
 int omnitide_paged_chunk_attn(const void* q, const void* k_pool, const void* v_pool, int n_pages,
                               int page_size, const int32_t* page_table, int max_pages,
@@ -159,7 +159,7 @@ size_t omnitide_paged_chunk_attn_workspace_bytes(int n_tokens, int n_seq, int ma
  *   out         the same of out_dtype
  *   workspace   device scratch of omnitide_paged_decode_workspace_bytes() bytes; as above
  * Numerics: bf16 inputs, float accumulation and softmax, probabilities with 16 significant bits.
- * Limits: n_q * (n_q_heads / n_kv_heads) <= 16, n_seq <= 1024, scale finite.
+ * Limits: n_q * (n_q_heads / n_kv_heads) <= 16, the others as for omnitide_paged_chunk_attn.
  */
 int omnitide_paged_decode_attn(const void* q, const void* k_pool, const void* v_pool, int n_pages,
                                int page_size, const int32_t* page_table, int max_pages,

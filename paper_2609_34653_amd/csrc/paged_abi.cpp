@@ -295,9 +295,12 @@ static int paged_attn_impl(bool decode, const void* q, const void* k_pool, const
       !paged_shape_ok(n_pages, max_pages, shift, n_seq) ||
       !attn_heads_ok(n_q_heads, n_kv_heads, head_dim) || !std::isfinite(scale) ||
       static_cast<int64_t>(n_tokens) * (n_q_heads / n_kv_heads) > (1 << 28) || !aligned16(q) ||
-      !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(out))
+      !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(out) || !aligned16(workspace))
     return OMNITIDE_E_SHAPE;
   if (decode && !decode_heads_ok(n_q, n_q_heads, n_kv_heads)) return OMNITIDE_E_SHAPE;
+  // blocks of 16 rows over all sequences and KV heads are counted in 32 bits
+  if ((static_cast<int64_t>(n_seq) * max_pages * n_kv_heads << shift) > (int64_t{1} << 34))
+    return OMNITIDE_E_SHAPE;
   const int max_ctx = max_pages << shift;
   const size_t need =
       decode ? omnitide::paged_decode_workspace_bytes(n_seq, n_q, max_ctx, n_q_heads, n_kv_heads,

@@ -90,11 +90,7 @@ hipError_t launch_simple(const PagedAttnArgs& a, hipStream_t stream) {
 }  // namespace
 
 size_t paged_chunk_workspace_bytes(int, int, int, int, int, int) { return 0; }
-size_t paged_decode_workspace_bytes(int, int, int, int, int, int) { return 0; }
 hipError_t launch_paged_chunk(const PagedAttnArgs& a, hipStream_t stream) {
-  return launch_simple(a, stream);
-}
-hipError_t launch_paged_decode(const PagedAttnArgs& a, hipStream_t stream) {
   return launch_simple(a, stream);
 }
 
