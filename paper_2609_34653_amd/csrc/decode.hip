@@ -32,6 +32,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "combine.h"
+#include "mfma_tile.h"
 
 namespace omnitide {
 namespace {
@@ -43,34 +44,6 @@ constexpr int kKT = 64;                    // slots per tile of a span's tile li
 constexpr int kStep = kDecWaves * kKB;     // keys per workgroup iteration
 constexpr int kDecTargetWGs = 256;         // one eight-wave workgroup per CU
 constexpr int kMaxQG = 8;                  // query vectors per KV head (n_q * G), <= 16
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void;
-
-__device__ inline uint32_t lds_addr(const void* p) {
-  return static_cast<uint32_t>(reinterpret_cast<size_t>((const lds_void*)p));
-}
-
-// 16-byte direct global -> LDS load: lane i reads base + voff_i and writes 16 bytes at LDS byte
-// address lds_base + 16 i (uniform base in SGPRs, per-lane 32-bit offset).  Inline assembly, so
-// that the compiler's wait insertion does not treat it as a pending LDS write; the issuing wave,
-// the only reader of the region it fills, waits for it with s_waitcnt vmcnt.  One wait state is
-// required between the M0 write and the load; this file's kernels have no other M0 user.
-__device__ inline void dma16(const void* base, uint32_t voff, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(base), "s"(lds_base)
-               : "memory");
-}
-
-// Transposing 64-bit LDS read: within a 16-lane group, lane i receives element i%4 of the
-// 8-byte rows read by lanes i/4, 4+i/4, 8+i/4, 12+i/4.
-__device__ inline shortx4 ld_tr(const uint16_t* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) shortx4*)(p));
-}
 
 // 32-byte unit swizzle of a key's row in a wave's V block: the four keys one 16-lane group
 // reads (and the eight two groups read) land in distinct banks.

@@ -24,6 +24,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "mfma_tile.h"
 #include "paged.h"
 #include "paged_rows.h"
 
@@ -35,33 +36,6 @@ constexpr int kThreads = kWaves * kWave;
 constexpr int kKB = 16;                  // keys per block
 constexpr int kWGs = 512;                // shares of a large call: two workgroups on each CU
 constexpr int kMinShare = 16;            // blocks of a share at least (256 keys)
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void;
-
-__device__ inline uint32_t lds_addr(const void* p) {
-  return static_cast<uint32_t>(reinterpret_cast<size_t>((const lds_void*)p));
-}
-
-// 16-byte direct global -> LDS load: lane i reads base + voff_i and writes 16 bytes at LDS byte
-// address lds_base + 16 i.  Inline assembly, so that the compiler does not wait for it before other
-// LDS reads; the issuing wave, the only reader, waits by s_waitcnt vmcnt.  One wait state between the M0
-// write and the load; nothing else in this file uses M0.
-__device__ inline void dma16(const void* base, uint32_t voff, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(base), "s"(lds_base)
-               : "memory");
-}
-
-// Transposing 64-bit LDS read: within a 16-lane group, lane i receives element i%4 of the
-// 8-byte rows read by lanes i/4, 4+i/4, 8+i/4, 12+i/4.
-__device__ inline shortx4 ld_tr(const uint16_t* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) shortx4*)(p));
-}
 
 template <int N>
 __device__ inline void wait_vmcnt() {
