@@ -23,7 +23,7 @@ ARCH = "gfx950"
 
 SOURCES = ["abi.cpp", "score.hip", "select.hip", "spans.hip", "compact.hip", "native.hip",
            "attention.hip", "decode.hip", "paged_abi.cpp", "norm_rope.hip",
-           "paged_attn.hip", "paged_decode.hip"]
+           "paged_chunk.hip", "paged_decode.hip"]
 
 # Packed fp32 instructions are kept out of the device code (-packed-fp32-ops).
 HIP_FLAGS = ["-x", "hip", f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

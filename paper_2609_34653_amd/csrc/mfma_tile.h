@@ -94,6 +94,18 @@ __device__ inline float sum_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Stores four consecutive output values as float32, or rounded to bf16 (nearest even).
+__device__ inline void store_row4(void* out, size_t idx, bool out_bf16, floatx4 v) {
+  if (out_bf16) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + idx) =
+        bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]),
+               static_cast<__bf16>(v[3])};
+  } else {
+    *reinterpret_cast<floatx4*>(static_cast<float*>(out) + idx) = v;
+  }
+}
+
 template <int B, class T>
 __device__ inline T& pick(T& a, T& b) {
   if constexpr (B == 0) return a; else return b;

@@ -303,10 +303,11 @@ static int paged_attn_impl(bool decode, const void* q, const void* k_pool, const
     return OMNITIDE_E_SHAPE;
   const int max_ctx = max_pages << shift;
   const size_t need =
-      decode ? omnitide::paged_decode_workspace_bytes(n_seq, n_q, max_ctx, n_q_heads, n_kv_heads,
-                                                      head_dim)
-             : omnitide::paged_chunk_workspace_bytes(n_tokens, n_seq, max_ctx, n_q_heads,
-                                                     n_kv_heads, head_dim);
+      n_tokens == 0 ? 0
+      : decode      ? omnitide::paged_decode_workspace_bytes(n_seq, n_q, max_ctx, n_q_heads,
+                                                             n_kv_heads, head_dim)
+                    : omnitide::paged_chunk_workspace_bytes(n_tokens, n_seq, max_ctx, n_q_heads,
+                                                            n_kv_heads, head_dim);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return OMNITIDE_E_WORKSPACE;
   const size_t qe = static_cast<size_t>(n_tokens) * n_q_heads * head_dim;
   const size_t pool = (static_cast<size_t>(n_pages) << shift) * n_kv_heads * head_dim * 2;

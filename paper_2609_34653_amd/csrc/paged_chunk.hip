@@ -1,0 +1,647 @@
+// Chunk attention over the pages: a ragged batch of chunks, causal, grouped queries.
+//
+// Mathematics: softmax(scale q K^T) V per (token, query head) over the token's sequence up to its own
+// row, one pass over 64-key tiles with a running reference and sum per row.
+//
+//   rows      the L * G query rows (position p, head g*G + r) of a sequence and KV head are flattened
+//             as m = p*G + r and tiled kRows = 4 waves x 64 per row tile; a wave's 64 rows are two
+//             32-column blocks of the products, so one K or V operand read from LDS feeds two of
+//             them.  (With 32 rows a wave the LDS reads of a tile take as long as its products.)
+//   shares    the key tiles of all (KV head, sequence, row tile), one after the other, are cut into equal
+//             shares, one per workgroup and CU, whatever the lengths: long contexts are spread over
+//             many workgroups, short ones share one.  A share's whole row tiles are finished there; the
+//             parts of a row tile that lies in several are merged by a second kernel, in share
+//             order.  Every wave works the cuts out by itself from q_start and ctx_len (a sequence per
+//             lane), so there is no plan launch.  The work of a row tile is counted in keys, linear in its
+//             number, so a cut is found by a square root.
+//   products  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: one query column per lane,
+//             so the row statistics are lane-local; keys are permuted when K rows are read so that S^T
+//             is the B operand of the second product as it stands.
+//   pages     a wave's direct load takes 4 (d = 128) or 8 (d = 64) consecutive keys, which lie in
+//             one page, so its address is scalar; page ids come 64 groups of 16 keys at a time, one
+//             per lane.  Rows past the context are clamped to its last one and masked.
+//   softmax   fp32, base 2; exponentials against a reference that moves only when a tile sum would leave
+//             a bounded range; row sums over the rounded bf16 probabilities.
+//   loop      unrolled by two (static LDS addresses); the score products of the next tile are
+//             interleaved with this tile's exponentials.
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "mfma_tile.h"
+#include "paged.h"
+#include "paged_rows.h"
+
+namespace omnitide {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kKT = 64;                  // keys per tile
+constexpr int kNB = 2;                   // 32-row blocks per wave
+constexpr int kRows = kWaves * 32 * kNB; // query rows per row tile
+constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
+constexpr int kNumXcd = 8;
+constexpr int kOverhead = 2 * kKT;       // what a row tile costs beside its keys, in keys
+constexpr int kMinShareTiles = 4;        // tiles of a share at least
+constexpr int kSnap = 2;                 // a cut this near to a row tile's end goes to the end
+
+// Where a share begins: row tile mt of (KV head g, sequence seq), key tile `tile` of it.
+struct Cut {
+  int g, seq, mt, tile;
+};
+__device__ inline bool same_rows(const Cut& a, const Cut& b) {
+  return a.g == b.g && a.seq == b.seq && a.mt == b.mt;
+}
+__device__ inline bool before(const Cut& a, const Cut& b) {
+  if (a.g != b.g) return a.g < b.g;
+  if (a.seq != b.seq) return a.seq < b.seq;
+  if (a.mt != b.mt) return a.mt < b.mt;
+  return a.tile < b.tile;
+}
+
+// What the merge kernel needs of a share that ends a row tile begun in an earlier one (n_parts > 0).
+struct Joined {
+  int32_t n_parts, first_slot, last_share, q0, rows, mt, g, pad;
+};
+
+constexpr int kMaxSeqs = 1024;
+
+// The shares of a call, in LDS: every sequence's first token, tokens (0: none, or malformed) and
+// context, and the work (keys times G) of its chunk of 64 sequences in front of it, per KV head.
+struct PlanMem {
+  int4 seq[kMaxSeqs];
+  int64_t first[kMaxSeqs];
+  int64_t chunk[kMaxSeqs / kWave + 1];   // work in front of each chunk; the last: of all
+};
+
+// Scalars for the wave, whatever registers they were computed in.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+  const uint64_t u = static_cast<uint64_t>(x);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
+  return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
+struct Plan {
+  const PlanMem* mem;
+  int64_t per_head, total, share;
+  int G, Hkv, n_seq;
+
+  __device__ static int row_tiles(int len, int G) {
+    return static_cast<int>((static_cast<int64_t>(len) * G + kRows - 1) / kRows);
+  }
+  // work of row tiles [0, m) of a sequence with kept keys in front of its chunk
+  __device__ int64_t work(int m, int kept) const {
+    return m * (static_cast<int64_t>(G) * (kept + kOverhead)) +
+           kRows / 2 * (static_cast<int64_t>(m) * (m + 1));
+  }
+  __device__ int tiles_of(int mt, int len, int ctx) const {
+    const int last = static_cast<int>((static_cast<int64_t>(mt + 1) * kRows - 1) / G);
+    return (ctx - len + min(len - 1, last) + kKT) / kKT;
+  }
+
+  // by the whole workgroup
+  __device__ void make(PlanMem& m, const PagedBatch& b, int G_, int Hkv_, int n_wgs) {
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int cap = b.max_pages << b.page_shift;
+    G = G_;
+    Hkv = Hkv_;
+    n_seq = b.n_seq;
+    mem = &m;
+    const int n_chunks = (n_seq + kWave - 1) / kWave;
+    for (int c = wave; c < n_chunks; c += kWaves) {
+      const int i = c * kWave + lane;
+      int s0 = 0, s1 = 0, n = 0;
+      if (i < n_seq) {
+        s0 = b.q_start[i];
+        s1 = b.q_start[i + 1];
+        n = b.ctx_len[i];
+      }
+      const bool ok = s0 >= 0 && s1 > s0 && s1 <= b.n_tokens && n >= s1 - s0 && n <= cap;
+      const int len = ok ? s1 - s0 : 0;
+      const int64_t w = ok ? work(row_tiles(len, G), n - len) : 0;
+      const int64_t inc = wave_inclusive_scan(w);
+      m.seq[i] = make_int4(s0, len, n, 0);
+      m.first[i] = inc - w;
+      if (lane == kWave - 1) m.chunk[c] = inc;
+    }
+    __syncthreads();
+    int64_t sum = 0;                       // every thread adds the chunks up
+    int64_t mine = 0;
+    for (int c = 0; c < n_chunks; ++c) {
+      if (c == static_cast<int>(threadIdx.x)) mine = sum;
+      sum += m.chunk[c];
+    }
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < n_chunks) m.chunk[threadIdx.x] = mine;
+    __syncthreads();
+    per_head = uniform(sum);
+    total = per_head * Hkv;
+    const int64_t least = static_cast<int64_t>(kMinShareTiles) * kKT * G;
+    share = uniform(max(least, (total + n_wgs - 1) / n_wgs));
+  }
+
+  struct Seq {
+    int q0, len, ctx;
+  };
+  __device__ Seq seq(int s) const {
+    const int4 v = mem->seq[s];
+    return {uniform(v.x), uniform(v.y), uniform(v.z)};
+  }
+  __device__ int64_t first(int s) const {
+    return uniform(mem->chunk[s / kWave] + mem->first[s]);
+  }
+  // the next sequence with tokens from s on, n_seq if there is none
+  __device__ int next_seq(int s) const {
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int c = s / kWave; c * kWave < n_seq; ++c) {
+      const int i = c * kWave + lane;
+      const uint64_t has = __ballot(i >= s && i < n_seq && mem->seq[i].y > 0);
+      if (has != 0) return uniform(c * kWave + __ffsll(static_cast<unsigned long long>(has)) - 1);
+    }
+    return n_seq;
+  }
+  // a cut whose row tile may be one past its sequence's last, made a real one (or {Hkv, 0, 0, 0})
+  __device__ Cut settle(Cut c) const {
+    if (c.mt < row_tiles(seq(c.seq).len, G)) return c;
+    int s = next_seq(c.seq + 1), g = c.g;
+    if (s == n_seq) {
+      s = next_seq(0);
+      ++g;
+    }
+    return g < Hkv ? Cut{g, s, 0, 0} : Cut{Hkv, 0, 0, 0};
+  }
+  __device__ Cut at(int64_t x) const {
+    if (x >= total) return {Hkv, 0, 0, 0};
+    const int lane = threadIdx.x & (kWave - 1);
+    const int g = static_cast<int>(x / per_head);
+    const int64_t y = x - g * per_head;
+    int c = 0;
+    while ((c + 1) * kWave < n_seq && mem->chunk[c + 1] <= y) ++c;
+    const int i = c * kWave + lane;
+    const uint64_t hit =
+        __ballot(i < n_seq && mem->seq[i].y > 0 && mem->chunk[c] + mem->first[i] <= y);
+    const int s = uniform(c * kWave + 63 - __clzll(static_cast<long long>(hit)));
+    const Seq q = seq(s);
+    const int kept = q.ctx - q.len;
+    const int64_t z = y - first(s);
+    // kRows / 2 m^2 + bq m = z
+    const double bq = static_cast<double>(G) * (kept + kOverhead) + kRows / 2;
+    const double root = sqrt(bq * bq + 2.0 * kRows * static_cast<double>(z));
+    const int most = row_tiles(q.len, G) - 1;
+    int m = min(max(uniform(static_cast<int>(2.0 * static_cast<double>(z) / (bq + root))), 0), most);
+    while (m > 0 && work(m, kept) > z) --m;
+    while (m < most && work(m + 1, kept) <= z) ++m;
+    const int64_t w0 = work(m, kept), w1 = work(m + 1, kept);
+    const int nt = tiles_of(m, q.len, q.ctx);
+    const float part = static_cast<float>(z - w0) / static_cast<float>(w1 - w0);
+    const int tile = uniform(static_cast<int>(fminf(part, 1.f) * nt));
+    if (tile <= kSnap) return {uniform(g), s, m, 0};
+    if (tile >= nt - kSnap) return settle({uniform(g), s, m + 1, 0});
+    return {uniform(g), s, m, tile};
+  }
+  __device__ Cut share_begin(int64_t w) const {
+    const Cut c = at(min(w * share, total));
+    return {uniform(c.g), uniform(c.seq), uniform(c.mt), uniform(c.tile)};
+  }
+};
+
+template <int D>
+struct Tile {
+  static constexpr int kElems = kKT * D;
+  static constexpr int kChunks = D / 8;                             // 16-byte chunks per row
+  static constexpr int kCalls = kElems / 8 / kWave / kWaves;        // direct loads per wave
+  static constexpr int kCallKeys = kWave / kChunks;                 // keys of one load
+};
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 1) void paged_chunk_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
+    const PagedBatch b, int Hq, int Hkv, float scale_log2, void* __restrict__ out, bool out_bf16,
+    float* __restrict__ part_o, float2* __restrict__ part_ml, Joined* __restrict__ joined,
+    int32_t* __restrict__ status) {
+  using T = Tile<D>;
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * T::kElems];   // K0, K1, V0, V1
+  __shared__ PlanMem plan_mem;
+
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int col = lane & 31, h = lane >> 5;
+  const int G = Hq / Hkv;
+
+  if (blockIdx.x == 0 && wave == 0) report_batch(b, status);
+  Plan plan;
+  plan.make(plan_mem, b, G, Hkv, gridDim.x);
+  // shares next to each other (the same keys, the next rows) on one XCD: workgroups are dealt
+  // round-robin over 8
+  const int n_wg = gridDim.x;
+  const int w = (blockIdx.x % kNumXcd) * (n_wg / kNumXcd) + blockIdx.x / kNumXcd;
+  Cut cur = plan.share_begin(w);
+  const Cut end = plan.share_begin(w + 1);
+  const Cut begin = cur;
+  if (plan.total == 0 || !before(cur, end)) {
+    if (tid == 0) joined[w].n_parts = 0;
+    return;
+  }
+  if (begin.tile == 0 && tid == 0) joined[w].n_parts = 0;
+
+  const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
+  uint32_t koff[T::kCalls], voff[T::kCalls];
+  int prow[T::kCalls];                     // this lane's key within its call's keys
+#pragma unroll
+  for (int cq = 0; cq < T::kCalls; ++cq) {
+    const int lc = (wave + kWaves * cq) * kWave + lane;
+    const int key = lc / T::kChunks, pc = lc % T::kChunks;
+    prow[cq] = key % T::kCallKeys;
+    koff[cq] = prow[cq] * row_bytes + 16u * (pc ^ (kswz(key) & (T::kChunks - 1)));
+    voff[cq] = prow[cq] * row_bytes + 16u * (2 * ((pc >> 1) ^ vswz<D>(key)) + (pc & 1));
+  }
+  const uint32_t lds_wave = lds_addr(lds) + static_cast<uint32_t>(wave * kWave * 16);
+  const int krow = perm_key(col);
+  const int fk = kswz(krow) & (T::kChunks - 1);
+  const int gi = lane & 15, gq = (lane >> 4) & 1;
+  const int vsl = vswz<D>(gi >> 2);
+  const int v_lane_off = (gi >> 2) * D + 8 * ((gi & 3) >> 1) + 4 * (gi & 1);
+  constexpr int NQK = 2 * (D / 16);        // K operands per tile (two 32-key halves)
+  constexpr int EPS = 32 / NQK;            // exponentials per block and segment
+  constexpr float kSumLimit = 4294967296.f;
+
+  while (before(cur, end)) {
+    // ---- the part of one row tile
+    const auto sq = plan.seq(cur.seq);
+    const int L = sq.len, ctx = sq.ctx, kept = ctx - L, g = cur.g;
+    const int nt = plan.tiles_of(cur.mt, L, ctx);
+    const int t_begin = cur.tile;
+    const int t_end = same_rows(cur, end) ? end.tile : nt;
+    const bool whole = t_begin == 0 && t_end == nt;
+    const int slot = 2 * w + (same_rows(cur, begin) ? 0 : 1);
+    const int m0 = cur.mt * kRows;
+    const int full_lim = kept + m0 / G;    // keys <= full_lim are visible to every row
+    if (t_begin > 0 && t_end == nt && wave == 0) {
+      // the row tile ends here: tell the merge where its parts are
+      const int64_t x0 = g * plan.per_head + plan.first(cur.seq) + plan.work(cur.mt, kept);
+      int64_t w0 = x0 / plan.share;
+      const Cut start{g, cur.seq, cur.mt, 0};
+      Cut c = plan.share_begin(w0);
+      for (;;) {                           // shares that begin here with nothing in them
+        const Cut c1 = plan.share_begin(w0 + 1);
+        if (!same_rows(c1, start) || c1.tile != 0) break;
+        ++w0;
+        c = c1;
+      }
+      if (lane == 0) {
+        const int first = static_cast<int>(2 * w0) + (same_rows(c, start) && c.tile == 0 ? 0 : 1);
+        joined[w] = Joined{w - static_cast<int>(w0) + 1, first, w, sq.q0, L * G, cur.mt, g, 0};
+      }
+    } else if (t_begin > 0 && tid == 0) {
+      joined[w].n_parts = 0;
+    }
+
+    int lim[kNB];                          // last visible key of this lane's rows
+    bool row_ok[kNB];
+    size_t orow[kNB];                      // their rows of q and out
+    bf16x8 qf[kNB][D / 16];
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) {
+      const int m = m0 + (wave * kNB + nb) * 32 + col;
+      row_ok[nb] = m < L * G;
+      const int p = row_ok[nb] ? m / G : L - 1;
+      const int r = row_ok[nb] ? m % G : 0;
+      lim[nb] = kept + p;
+      orow[nb] = static_cast<size_t>(sq.q0 + p) * Hq + g * G + r;
+      const uint16_t* qrow = q + orow[nb] * D;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+        qf[nb][c] = __builtin_bit_cast(bf16x8, ld16(qrow + 16 * c + 8 * h));
+    }
+
+    // page ids of 16-key groups: group 4 * base + lane of the sequence in lane (base: a tile)
+    const int32_t* table = b.table + static_cast<size_t>(cur.seq) * b.max_pages;
+    const int groups = (ctx + 15) / 16;
+    int pages = 0, base = t_begin;
+    auto load_pages = [&](int t) {
+      const int i = 4 * t + lane;
+      int p = i < groups ? table[(i * 16) >> b.page_shift] : 0;
+      if (p < 0 || p >= b.n_pages) {
+        set_status(status, OMNITIDE_E_PAGES);
+        p = 0;
+      }
+      return p;
+    };
+    const uint8_t* k_head = reinterpret_cast<const uint8_t*>(k) + 2 * g * D;
+    const uint8_t* v_head = reinterpret_cast<const uint8_t*>(v) + 2 * g * D;
+    // direct copy of one tensor's tile t into buffer `buf` (0, 1 = K; 2, 3 = V)
+    auto issue = [&](const uint8_t* head, const uint32_t (&offs)[T::kCalls], int t, int buf) {
+      const uint32_t dst = lds_wave + static_cast<uint32_t>(buf * T::kElems * 2);
+#pragma unroll
+      for (int cq = 0; cq < T::kCalls; ++cq) {
+        const int at = t * kKT + (wave + kWaves * cq) * T::kCallKeys;
+        const int ks = min(at, ctx - 1);
+        const int page = readlane(pages, (ks >> 4) - 4 * base);
+        const uint8_t* src = head + ((static_cast<size_t>(page) << b.page_shift) +
+                                     (ks & ((1 << b.page_shift) - 1))) * row_bytes;
+        uint32_t off = offs[cq];
+        if (at + T::kCallKeys > ctx)       // rows past the context: its last one
+          off -= static_cast<uint32_t>(max(prow[cq] - (ctx - 1 - ks), 0)) * row_bytes;
+        dma16(src, off, dst + static_cast<uint32_t>(cq * kWaves * kWave * 16));
+      }
+    };
+
+    floatx16 o[kNB][D / 32];
+    float m_run[kNB], l_run[kNB];
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) {
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) o[nb][dt] = floatx16{};
+      m_run[nb] = -INFINITY;
+      l_run[nb] = 0.f;
+    }
+    auto kop = [&](const uint16_t* kb, int i) {    // K operand i: half st = i & 1, slice c = i >> 1
+      const int st = i & 1, c = i >> 1;
+      return __builtin_bit_cast(bf16x8, ld16(kb + (32 * st + krow) * D + 8 * ((2 * c + h) ^ fk)));
+    };
+
+    pages = load_pages(base);
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
+    int next_pages = 0;
+    issue(k_head, koff, t_begin, 0);
+    issue(v_head, voff, t_begin, 2);
+    if (t_begin + 1 < t_end) issue(k_head, koff, t_begin + 1, 1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    floatx16 sA[kNB][2], sB[kNB][2];
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) {
+      sA[nb][0] = floatx16{};
+      sA[nb][1] = floatx16{};
+    }
+#pragma unroll
+    for (int i = 0; i < NQK; ++i) {
+      const bf16x8 ka = kop(lds, i);
+#pragma unroll
+      for (int nb = 0; nb < kNB; ++nb) sA[nb][i & 1] = mfma(ka, qf[nb][i >> 1], sA[nb][i & 1]);
+    }
+
+    // One iteration for tile t, B = (t - t_begin) & 1: the scores of t are in s_cur; K(t+1) is in K
+    // buffer 1-B, V(t) in V buffer B.  Issues K(t+2) into K buffer B and V(t+1) into V buffer 1-B.
+    auto step = [&](auto par, int t) {
+      constexpr int B = decltype(par)::value;
+      floatx16(&s_cur)[kNB][2] = pick<B>(sA, sB);
+      floatx16(&s_nxt)[kNB][2] = pick<B>(sB, sA);
+      const uint16_t* Kn = lds + (1 - B) * T::kElems;
+      const uint16_t* Vs = lds + (2 + B) * T::kElems;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's pieces have landed
+      __syncthreads();                                   // everyone's; tile t-1 is finished
+      if (t + 2 < t_end) {
+        // ids of tiles [base, base + 16): the next 16 are asked for half-way
+        if (t + 2 - base == 8) next_pages = load_pages(base + 16);
+        if (t + 2 - base == 16) {
+          // V(t+1) still needs the old ids
+          issue(v_head, voff, t + 1, 3 - B);
+          base += 16;
+          pages = next_pages;
+          issue(k_head, koff, t + 2, B);
+        } else {
+          issue(k_head, koff, t + 2, B);
+          if (t + 1 >= base) issue(v_head, voff, t + 1, 3 - B);
+        }
+      } else if (t + 1 < t_end) {
+        issue(v_head, voff, t + 1, 3 - B);
+      }
+
+      const int j0 = t * kKT;
+      if (j0 + kKT - 1 > full_lim) {
+#pragma unroll
+        for (int nb = 0; nb < kNB; ++nb)
+#pragma unroll
+          for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (j0 + 32 * st + 16 * h + i > lim[nb]) s_cur[nb][st][i] = -INFINITY;
+      }
+
+      // segment i issues the score products of K operand i of the next tile, then EPS exponentials per
+      // block of this tile, rounds them into the P operand and adds them to the row sum.  In the last
+      // iteration the next-K buffer holds a stale tile; its scores are discarded.
+      float e[kNB][32];
+      bf16x8 pf[kNB][2][2];
+      const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+      float ls_run[kNB][2];
+#pragma unroll
+      for (int nb = 0; nb < kNB; ++nb) {
+        ls_run[nb][0] = ls_run[nb][1] = 0.f;
+        s_nxt[nb][0] = floatx16{};
+        s_nxt[nb][1] = floatx16{};
+      }
+      {
+        bf16x8 ka[2] = {kop(Kn, 0), kop(Kn, 1)};
+#pragma unroll
+        for (int i = 0; i < NQK; ++i) {
+          const bf16x8 kc = ka[i & 1];
+#pragma unroll
+          for (int nb = 0; nb < kNB; ++nb)
+            s_nxt[nb][i & 1] = mfma(kc, qf[nb][i >> 1], s_nxt[nb][i & 1]);
+          if (i + 2 < NQK) ka[i & 1] = kop(Kn, i + 2);
+#pragma unroll
+          for (int nb = 0; nb < kNB; ++nb) {
+#pragma unroll
+            for (int j = 0; j < EPS; ++j) {
+              const int x = i * EPS + j;
+              e[nb][x] = __builtin_amdgcn_exp2f(
+                  fmaf(s_cur[nb][x >> 4][x & 15], scale_log2, -m_run[nb]));
+            }
+#pragma unroll
+            for (int j = 0; j < EPS; j += 2) {
+              const int x = i * EPS + j;
+              const bf16x2 pr = {static_cast<__bf16>(e[nb][x]), static_cast<__bf16>(e[nb][x + 1])};
+              pf[nb][x >> 4][(x >> 3) & 1][x & 7] = pr[0];
+              pf[nb][x >> 4][(x >> 3) & 1][(x & 7) + 1] = pr[1];
+              ls_run[nb][(x >> 1) & 1] =
+                  __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls_run[nb][(x >> 1) & 1], false);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < kNB; ++nb) {
+        float lsum = ls_run[nb][0] + ls_run[nb][1];
+        if (__any(!(lsum < kSumLimit))) {
+          // exact tile maximum, move the reference, rescale, recompute the tile
+          float mx = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < 32; ++x) {
+            const float s = s_cur[nb][x >> 4][x & 15];
+            mx = fmaxf(mx, s == -INFINITY ? s : s * scale_log2);
+          }
+          mx = max_halves(mx);
+          const float m_new = fmaxf(m_run[nb], mx);
+          const float m_use = m_new == -INFINITY ? 0.f : m_new;
+          const float alpha = __builtin_amdgcn_exp2f(m_run[nb] - m_use);
+          l_run[nb] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt) o[nb][dt] *= alpha;
+          m_run[nb] = m_new;
+          lsum = 0.f;
+#pragma unroll
+          for (int x = 0; x < 32; ++x) {
+            const float s = s_cur[nb][x >> 4][x & 15];
+            const __bf16 p = static_cast<__bf16>(
+                s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(s, scale_log2, -m_use)));
+            pf[nb][x >> 4][(x >> 3) & 1][x & 7] = p;
+            lsum += static_cast<float>(p);
+          }
+        }
+        l_run[nb] += lsum;
+      }
+
+      // O^T += V^T P^T, the V^T operands read three products ahead
+      constexpr int NPV = 4 * (D / 32);
+      auto vop = [&](int i) {
+        const int dt = i % (D / 32), cc = (i / (D / 32)) & 1, st = i / (2 * (D / 32));
+        const int unit = (2 * dt + gq) ^ vsl;
+        const uint16_t* vp = Vs + (32 * st + 16 * h + 8 * cc) * D + 16 * unit + v_lane_off;
+        const shortx4 lo = ld_tr(vp);
+        const shortx4 hi = ld_tr(vp + 4 * D);
+        return __builtin_bit_cast(bf16x8,
+                                  __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      bf16x8 va[4] = {vop(0), vop(1), vop(2), bf16x8{}};
+#pragma unroll
+      for (int i = 0; i < NPV; ++i) {
+        if (i + 3 < NPV) va[(i + 3) % 4] = vop(i + 3);
+        const int dt = i % (D / 32), cc = (i / (D / 32)) & 1, st = i / (2 * (D / 32));
+#pragma unroll
+        for (int nb = 0; nb < kNB; ++nb) o[nb][dt] = mfma(va[i % 4], pf[nb][st][cc], o[nb][dt]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    int t = t_begin;
+    for (; t + 1 < t_end; t += 2) {
+      step(std::integral_constant<int, 0>{}, t);
+      step(std::integral_constant<int, 1>{}, t + 1);
+    }
+    if (t < t_end) step(std::integral_constant<int, 0>{}, t);
+
+    // ---- the part's result
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) {
+      const float l_tot = sum_halves(l_run[nb]);
+      if (!row_ok[nb]) continue;
+      if (whole) {
+        const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int qd = 0; qd < 4; ++qd) {
+            const size_t at = orow[nb] * D + 32 * dt + 8 * qd + 4 * h;
+            const floatx4 x = {o[nb][dt][4 * qd] * inv, o[nb][dt][4 * qd + 1] * inv,
+                               o[nb][dt][4 * qd + 2] * inv, o[nb][dt][4 * qd + 3] * inv};
+            store_row4(out, at, out_bf16, x);
+          }
+      } else {
+        const size_t prow_ = static_cast<size_t>(slot) * kRows + (wave * kNB + nb) * 32 + col;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int qd = 0; qd < 4; ++qd)
+            *reinterpret_cast<floatx4*>(part_o + prow_ * D + 32 * dt + 8 * qd + 4 * h) =
+                floatx4{o[nb][dt][4 * qd], o[nb][dt][4 * qd + 1], o[nb][dt][4 * qd + 2],
+                        o[nb][dt][4 * qd + 3]};
+        if (h == 0) part_ml[prow_] = make_float2(m_run[nb], l_tot);
+      }
+    }
+    if (t_end < nt) break;                   // the share ended inside the row tile
+    cur = plan.settle(Cut{cur.g, cur.seq, cur.mt + 1, 0});
+    cur = Cut{uniform(cur.g), uniform(cur.seq), uniform(cur.mt), 0};
+    __syncthreads();                         // the tile buffers are free again
+  }
+}
+
+// Merges the row tiles whose parts lie in several shares, in share order: workgroup (share, slice)
+// takes kSlice rows of the row tile that the share ends, if it ends one begun earlier.
+constexpr int kSlice = 32;
+template <int D>
+__global__ __launch_bounds__(kThreads) void paged_chunk_merge_kernel(
+    const float* __restrict__ part_o, const float2* __restrict__ part_ml,
+    const Joined* __restrict__ joined, int Hq, int Hkv, void* __restrict__ out, bool out_bf16) {
+  constexpr int TPR = D / 4, PER = kThreads / TPR;
+  const Joined j = joined[blockIdx.x];
+  if (j.n_parts == 0) return;
+  const int G = Hq / Hkv;
+  const int d4 = threadIdx.x % TPR;
+  for (int r = static_cast<int>(threadIdx.x) / TPR; r < kSlice; r += PER) {
+    const int rt = blockIdx.y * kSlice + r, m = j.mt * kRows + rt;
+    if (m >= j.rows) return;
+    float M = -INFINITY, den = 0.f;
+    floatx4 num = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < j.n_parts; p0 += 4) {
+      float2 ml[4];
+      floatx4 ov[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int p = p0 + c;
+        const bool in = p < j.n_parts;
+        const int slot = p == 0 ? j.first_slot : 2 * (j.last_share - j.n_parts + 1 + p);
+        const size_t row = static_cast<size_t>(slot) * kRows + rt;
+        ml[c] = in ? part_ml[row] : make_float2(-INFINITY, 0.f);
+        ov[c] = in ? *reinterpret_cast<const floatx4*>(part_o + row * D + 4 * d4)
+                   : floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+      float cm = M;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) cm = fmaxf(cm, ml[c].x);
+      if (cm == -INFINITY) continue;
+      const float a = M == -INFINITY ? 0.f : exp2f(M - cm);
+      den *= a;
+      num *= a;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float w = ml[c].x == -INFINITY ? 0.f : exp2f(ml[c].x - cm);
+        den = fmaf(w, ml[c].y, den);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) num[e] = fmaf(w, ov[c][e], num[e]);
+      }
+      M = cm;
+    }
+    const float inv = den > 0.f ? 1.f / den : 0.f;
+    const size_t at = (static_cast<size_t>(j.q0 + m / G) * Hq + j.g * G + m % G) * D + 4 * d4;
+    store_row4(out, at, out_bf16, num * inv);
+  }
+}
+
+constexpr size_t kJoinedBytes = kWGs * sizeof(Joined);
+
+template <int D>
+hipError_t launch_t(const PagedAttnArgs& a, hipStream_t stream) {
+  const PagedBatch& b = a.batch;
+  Joined* joined = static_cast<Joined*>(a.workspace);
+  float2* part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(a.workspace) + kJoinedBytes);
+  float* part_o = reinterpret_cast<float*>(part_ml + static_cast<size_t>(2 * kWGs) * kRows);
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  hipLaunchKernelGGL((paged_chunk_kernel<D>), dim3(kWGs), dim3(kThreads), 0, stream,
+                     static_cast<const uint16_t*>(a.q), static_cast<const uint16_t*>(a.k),
+                     static_cast<const uint16_t*>(a.v), b, a.n_q_heads, a.n_kv_heads, scale_log2,
+                     a.out, a.out_bf16, part_o, part_ml, joined, a.d_status);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((paged_chunk_merge_kernel<D>), dim3(kWGs, kRows / kSlice), dim3(kThreads), 0,
+                     stream, part_o, part_ml, joined, a.n_q_heads, a.n_kv_heads, a.out, a.out_bf16);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t paged_chunk_workspace_bytes(int, int, int, int, int, int head_dim) {
+  return kJoinedBytes +
+         static_cast<size_t>(2 * kWGs) * kRows * (static_cast<size_t>(head_dim) + 2) * sizeof(float);
+}
+
+hipError_t launch_paged_chunk(const PagedAttnArgs& a, hipStream_t stream) {
+  return a.head_dim == 128 ? launch_t<128>(a, stream) : launch_t<64>(a, stream);
+}
+
+}  // namespace omnitide
