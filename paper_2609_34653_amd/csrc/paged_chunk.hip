@@ -35,12 +35,13 @@
 namespace omnitide {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKT = 64;                  // keys per tile
-constexpr int kNB = 2;                   // 32-row blocks per wave
+constexpr int kNB = 1;                   // 32-row blocks per wave
 constexpr int kRows = kWaves * 32 * kNB; // query rows per row tile
 constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
+constexpr int kRing = 4;                 // tiles of each tensor in LDS
 constexpr int kNumXcd = 8;
 constexpr int kOverhead = 2 * kKT;       // what a row tile costs beside its keys, in keys
 constexpr int kMinShareTiles = 4;        // tiles of a share at least
@@ -208,6 +209,11 @@ struct Plan {
   }
 };
 
+template <int N>
+__device__ inline void wait_vmcnt() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
 template <int D>
 struct Tile {
   static constexpr int kElems = kKT * D;
@@ -217,14 +223,15 @@ struct Tile {
 };
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 1) void paged_chunk_kernel(
+__global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
     const PagedBatch b, int Hq, int Hkv, float scale_log2, void* __restrict__ out, bool out_bf16,
     float* __restrict__ part_o, float2* __restrict__ part_ml, Joined* __restrict__ joined,
     int32_t* __restrict__ status) {
   using T = Tile<D>;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * T::kElems];   // K0, K1, V0, V1
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * kRing * T::kElems];   // K, V tiles
   __shared__ PlanMem plan_mem;
+  __shared__ int32_t page_ids[kWaves][2][kWave];
 
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
@@ -265,8 +272,6 @@ __global__ __launch_bounds__(kThreads, 1) void paged_chunk_kernel(
   const int gi = lane & 15, gq = (lane >> 4) & 1;
   const int vsl = vswz<D>(gi >> 2);
   const int v_lane_off = (gi >> 2) * D + 8 * ((gi & 3) >> 1) + 4 * (gi & 1);
-  constexpr int NQK = 2 * (D / 16);        // K operands per tile (two 32-key halves)
-  constexpr int EPS = 32 / NQK;            // exponentials per block and segment
   constexpr float kSumLimit = 4294967296.f;
 
   while (before(cur, end)) {
@@ -318,165 +323,153 @@ __global__ __launch_bounds__(kThreads, 1) void paged_chunk_kernel(
         qf[nb][c] = __builtin_bit_cast(bf16x8, ld16(qrow + 16 * c + 8 * h));
     }
 
-    // page ids of 16-key groups: group 4 * base + lane of the sequence in lane (base: a tile)
+    // Ids of the 64 pages from `window` on, one per lane.  The next 64 wait in LDS, put there by a
+    // direct load when the window moved (a plain load would have the compiler wait for it, and so
+    // for the tiles asked for before it).
     const int32_t* table = b.table + static_cast<size_t>(cur.seq) * b.max_pages;
-    const int groups = (ctx + 15) / 16;
-    int pages = 0, base = t_begin;
-    auto load_pages = [&](int t) {
-      const int i = 4 * t + lane;
-      int p = i < groups ? table[(i * 16) >> b.page_shift] : 0;
+    const int last_page = (ctx - 1) >> b.page_shift;
+    int window = (t_begin * kKT) >> b.page_shift, turn = 0;
+    auto ask_pages = [&](int first) {
+      dma4(table, 4u * static_cast<uint32_t>(min(first + lane, last_page)),
+           lds_addr(&page_ids[wave][turn][0]));
+      turn ^= 1;
+    };
+    auto checked = [&](int p) {
       if (p < 0 || p >= b.n_pages) {
         set_status(status, OMNITIDE_E_PAGES);
         p = 0;
       }
       return p;
     };
+    int pages = checked(table[min(window + lane, last_page)]);
     const uint8_t* k_head = reinterpret_cast<const uint8_t*>(k) + 2 * g * D;
     const uint8_t* v_head = reinterpret_cast<const uint8_t*>(v) + 2 * g * D;
-    // direct copy of one tensor's tile t into buffer `buf` (0, 1 = K; 2, 3 = V)
-    auto issue = [&](const uint8_t* head, const uint32_t (&offs)[T::kCalls], int t, int buf) {
-      const uint32_t dst = lds_wave + static_cast<uint32_t>(buf * T::kElems * 2);
+    const int page_mask = (1 << b.page_shift) - 1;
+    // direct copy of one tensor's tile t into the ring buffer at LDS byte address dst
+    auto issue = [&](const uint8_t* head, const uint32_t (&offs)[T::kCalls], int t, uint32_t dst,
+                     int ids, int from) {
 #pragma unroll
       for (int cq = 0; cq < T::kCalls; ++cq) {
         const int at = t * kKT + (wave + kWaves * cq) * T::kCallKeys;
         const int ks = min(at, ctx - 1);
-        const int page = readlane(pages, (ks >> 4) - 4 * base);
-        const uint8_t* src = head + ((static_cast<size_t>(page) << b.page_shift) +
-                                     (ks & ((1 << b.page_shift) - 1))) * row_bytes;
+        const int page = readlane(ids, (ks >> b.page_shift) - from);
+        const uint8_t* src =
+            head + ((static_cast<size_t>(page) << b.page_shift) + (ks & page_mask)) * row_bytes;
         uint32_t off = offs[cq];
         if (at + T::kCallKeys > ctx)       // rows past the context: its last one
           off -= static_cast<uint32_t>(max(prow[cq] - (ctx - 1 - ks), 0)) * row_bytes;
         dma16(src, off, dst + static_cast<uint32_t>(cq * kWaves * kWave * 16));
       }
     };
+    auto ring = [&](int t) { return ((t - t_begin) & (kRing - 1)) * T::kElems; };
+    auto issue_k = [&](int t) { issue(k_head, koff, t, lds_wave + 2 * ring(t), pages, window); };
+    auto issue_v = [&](int t, int ids, int from) {
+      issue(v_head, voff, t, lds_wave + 2 * (kRing * T::kElems + ring(t)), ids, from);
+    };
 
     floatx16 o[kNB][D / 32];
     float m_run[kNB], l_run[kNB];
+    floatx16 sA[kNB], sB[kNB];             // scores of 32 keys, current and next in turn
+    bf16x8 pA[kNB][2], pB[kNB][2];         // probabilities of 32 keys: the operand of the products
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb) {
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) o[nb][dt] = floatx16{};
       m_run[nb] = -INFINITY;
       l_run[nb] = 0.f;
+      sA[nb] = floatx16{};
+      pB[nb][0] = pB[nb][1] = bf16x8{};
     }
-    auto kop = [&](const uint16_t* kb, int i) {    // K operand i: half st = i & 1, slice c = i >> 1
-      const int st = i & 1, c = i >> 1;
-      return __builtin_bit_cast(bf16x8, ld16(kb + (32 * st + krow) * D + 8 * ((2 * c + h) ^ fk)));
+    constexpr int NS = D / 16;             // slots of a step: K operands, and V operands
+    // K operand c of the 32 keys at kb; V operand i = (32 dims dt, 16 keys cc) of those at vb
+    auto kop = [&](const uint16_t* kb, int c) {
+      return __builtin_bit_cast(bf16x8, ld16(kb + krow * D + 8 * ((2 * c + h) ^ fk)));
+    };
+    auto vop = [&](const uint16_t* vb, int i) {
+      const int dt = i % (D / 32), cc = i / (D / 32);
+      const int unit = (2 * dt + gq) ^ vsl;
+      const uint16_t* vp = vb + (16 * h + 8 * cc) * D + 16 * unit + v_lane_off;
+      const shortx4 lo = ld_tr(vp);
+      const shortx4 hi = ld_tr(vp + 4 * D);
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
-    pages = load_pages(base);
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
-    int next_pages = 0;
-    issue(k_head, koff, t_begin, 0);
-    issue(v_head, voff, t_begin, 2);
-    if (t_begin + 1 < t_end) issue(k_head, koff, t_begin + 1, 1);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    ask_pages(window + kWave);
+    issue_k(t_begin);
+    issue_v(t_begin, pages, window);
+    if (t_begin + 1 < t_end) issue_k(t_begin + 1);
+    if (t_begin + 1 < t_end) issue_v(t_begin + 1, pages, window);
+    if (t_begin + 2 < t_end) issue_k(t_begin + 2);
+    wait_vmcnt<0>();
     __syncthreads();
-    floatx16 sA[kNB][2], sB[kNB][2];
 #pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) {
-      sA[nb][0] = floatx16{};
-      sA[nb][1] = floatx16{};
-    }
+    for (int c = 0; c < NS; ++c) {
+      const bf16x8 ka = kop(lds, c);
 #pragma unroll
-    for (int i = 0; i < NQK; ++i) {
-      const bf16x8 ka = kop(lds, i);
-#pragma unroll
-      for (int nb = 0; nb < kNB; ++nb) sA[nb][i & 1] = mfma(ka, qf[nb][i >> 1], sA[nb][i & 1]);
+      for (int nb = 0; nb < kNB; ++nb) sA[nb] = mfma(ka, qf[nb][c], sA[nb]);
     }
 
-    // One iteration for tile t, B = (t - t_begin) & 1: the scores of t are in s_cur; K(t+1) is in K
-    // buffer 1-B, V(t) in V buffer B.  Issues K(t+2) into K buffer B and V(t+1) into V buffer 1-B.
-    auto step = [&](auto par, int t) {
-      constexpr int B = decltype(par)::value;
-      floatx16(&s_cur)[kNB][2] = pick<B>(sA, sB);
-      floatx16(&s_nxt)[kNB][2] = pick<B>(sB, sA);
-      const uint16_t* Kn = lds + (1 - B) * T::kElems;
-      const uint16_t* Vs = lds + (2 + B) * T::kElems;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's pieces have landed
-      __syncthreads();                                   // everyone's; tile t-1 is finished
-      if (t + 2 < t_end) {
-        // ids of tiles [base, base + 16): the next 16 are asked for half-way
-        if (t + 2 - base == 8) next_pages = load_pages(base + 16);
-        if (t + 2 - base == 16) {
-          // V(t+1) still needs the old ids
-          issue(v_head, voff, t + 1, 3 - B);
-          base += 16;
-          pages = next_pages;
-          issue(k_head, koff, t + 2, B);
-        } else {
-          issue(k_head, koff, t + 2, B);
-          if (t + 1 >= base) issue(v_head, voff, t + 1, 3 - B);
-        }
-      } else if (t + 1 < t_end) {
-        issue(v_head, voff, t + 1, 3 - B);
-      }
-
-      const int j0 = t * kKT;
-      if (j0 + kKT - 1 > full_lim) {
+    // One step for 32 keys from key0 on, whose scores are in s_cur: their softmax, the scores of the
+    // next 32 keys (at kb) and the product of the 32 keys before (values at vb, probabilities p_prev),
+    // interleaved so that the vector units work while the matrix cores run: a wave issues in
+    // order, and one wave runs on each SIMD.  (The first step's p_prev are zeros; the last one's next
+    // scores are of a stale buffer and not used.)
+    const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+    auto step = [&](floatx16(&s_cur)[kNB], floatx16(&s_nxt)[kNB], bf16x8(&p_prev)[kNB][2],
+                    bf16x8(&p_cur)[kNB][2], const uint16_t* kb, const uint16_t* vb, int key0) {
+      if (key0 + 31 > full_lim) {
 #pragma unroll
         for (int nb = 0; nb < kNB; ++nb)
 #pragma unroll
-          for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (j0 + 32 * st + 16 * h + i > lim[nb]) s_cur[nb][st][i] = -INFINITY;
+          for (int i = 0; i < 16; ++i)
+            if (key0 + 16 * h + i > lim[nb]) s_cur[nb][i] = -INFINITY;
       }
-
-      // segment i issues the score products of K operand i of the next tile, then EPS exponentials per
-      // block of this tile, rounds them into the P operand and adds them to the row sum.  In the last
-      // iteration the next-K buffer holds a stale tile; its scores are discarded.
-      float e[kNB][32];
-      bf16x8 pf[kNB][2][2];
-      const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-      float ls_run[kNB][2];
+      constexpr int EPS = 16 / NS;         // exponentials per block and slot
+      float ls[kNB][2];
 #pragma unroll
       for (int nb = 0; nb < kNB; ++nb) {
-        ls_run[nb][0] = ls_run[nb][1] = 0.f;
-        s_nxt[nb][0] = floatx16{};
-        s_nxt[nb][1] = floatx16{};
+        ls[nb][0] = ls[nb][1] = 0.f;
+        s_nxt[nb] = floatx16{};
       }
-      {
-        bf16x8 ka[2] = {kop(Kn, 0), kop(Kn, 1)};
+      bf16x8 ka[2] = {kop(kb, 0), kop(kb, 1)};
+      bf16x8 va[2] = {vop(vb, 0), vop(vb, 1)};
 #pragma unroll
-        for (int i = 0; i < NQK; ++i) {
-          const bf16x8 kc = ka[i & 1];
+      for (int i = 0; i < NS; ++i) {
+        const bf16x8 kc = ka[i & 1], vc = va[i & 1];
+        const int dt = i % (D / 32), cc = i / (D / 32);
 #pragma unroll
-          for (int nb = 0; nb < kNB; ++nb)
-            s_nxt[nb][i & 1] = mfma(kc, qf[nb][i >> 1], s_nxt[nb][i & 1]);
-          if (i + 2 < NQK) ka[i & 1] = kop(Kn, i + 2);
+        for (int nb = 0; nb < kNB; ++nb) {
+          float e[EPS];
+          s_nxt[nb] = mfma(kc, qf[nb][i], s_nxt[nb]);
+          if (nb == kNB - 1 && i + 2 < NS) ka[i & 1] = kop(kb, i + 2);
 #pragma unroll
-          for (int nb = 0; nb < kNB; ++nb) {
+          for (int x = 0; x < EPS; ++x)
+            e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[nb][i * EPS + x], scale_log2, -m_run[nb]));
+          __builtin_amdgcn_sched_barrier(0);
+          o[nb][dt] = mfma(vc, p_prev[nb][cc], o[nb][dt]);
+          if (nb == kNB - 1 && i + 2 < NS) va[i & 1] = vop(vb, i + 2);
 #pragma unroll
-            for (int j = 0; j < EPS; ++j) {
-              const int x = i * EPS + j;
-              e[nb][x] = __builtin_amdgcn_exp2f(
-                  fmaf(s_cur[nb][x >> 4][x & 15], scale_log2, -m_run[nb]));
-            }
-#pragma unroll
-            for (int j = 0; j < EPS; j += 2) {
-              const int x = i * EPS + j;
-              const bf16x2 pr = {static_cast<__bf16>(e[nb][x]), static_cast<__bf16>(e[nb][x + 1])};
-              pf[nb][x >> 4][(x >> 3) & 1][x & 7] = pr[0];
-              pf[nb][x >> 4][(x >> 3) & 1][(x & 7) + 1] = pr[1];
-              ls_run[nb][(x >> 1) & 1] =
-                  __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls_run[nb][(x >> 1) & 1], false);
-            }
+          for (int x = 0; x < EPS; x += 2) {
+            const int at = i * EPS + x;
+            const bf16x2 pr = {static_cast<__bf16>(e[x]), static_cast<__bf16>(e[x + 1])};
+            p_cur[nb][at >> 3][at & 7] = pr[0];
+            p_cur[nb][at >> 3][(at & 7) + 1] = pr[1];
+            ls[nb][(at >> 1) & 1] =
+                __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls[nb][(at >> 1) & 1], false);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
       }
 #pragma unroll
       for (int nb = 0; nb < kNB; ++nb) {
-        float lsum = ls_run[nb][0] + ls_run[nb][1];
+        float lsum = ls[nb][0] + ls[nb][1];
         if (__any(!(lsum < kSumLimit))) {
-          // exact tile maximum, move the reference, rescale, recompute the tile
+          // exact maximum of the 32 keys, move the reference, rescale, recompute
           float mx = -INFINITY;
 #pragma unroll
-          for (int x = 0; x < 32; ++x) {
-            const float s = s_cur[nb][x >> 4][x & 15];
-            mx = fmaxf(mx, s == -INFINITY ? s : s * scale_log2);
-          }
+          for (int x = 0; x < 16; ++x)
+            mx = fmaxf(mx, s_cur[nb][x] == -INFINITY ? -INFINITY : s_cur[nb][x] * scale_log2);
           mx = max_halves(mx);
           const float m_new = fmaxf(m_run[nb], mx);
           const float m_use = m_new == -INFINITY ? 0.f : m_new;
@@ -487,44 +480,55 @@ __global__ __launch_bounds__(kThreads, 1) void paged_chunk_kernel(
           m_run[nb] = m_new;
           lsum = 0.f;
 #pragma unroll
-          for (int x = 0; x < 32; ++x) {
-            const float s = s_cur[nb][x >> 4][x & 15];
+          for (int x = 0; x < 16; ++x) {
+            const float sx = s_cur[nb][x];
             const __bf16 p = static_cast<__bf16>(
-                s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(s, scale_log2, -m_use)));
-            pf[nb][x >> 4][(x >> 3) & 1][x & 7] = p;
+                sx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(sx, scale_log2, -m_use)));
+            p_cur[nb][x >> 3][x & 7] = p;
             lsum += static_cast<float>(p);
           }
         }
         l_run[nb] += lsum;
       }
-
-      // O^T += V^T P^T, the V^T operands read three products ahead
-      constexpr int NPV = 4 * (D / 32);
-      auto vop = [&](int i) {
-        const int dt = i % (D / 32), cc = (i / (D / 32)) & 1, st = i / (2 * (D / 32));
-        const int unit = (2 * dt + gq) ^ vsl;
-        const uint16_t* vp = Vs + (32 * st + 16 * h + 8 * cc) * D + 16 * unit + v_lane_off;
-        const shortx4 lo = ld_tr(vp);
-        const shortx4 hi = ld_tr(vp + 4 * D);
-        return __builtin_bit_cast(bf16x8,
-                                  __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      };
-      bf16x8 va[4] = {vop(0), vop(1), vop(2), bf16x8{}};
-#pragma unroll
-      for (int i = 0; i < NPV; ++i) {
-        if (i + 3 < NPV) va[(i + 3) % 4] = vop(i + 3);
-        const int dt = i % (D / 32), cc = (i / (D / 32)) & 1, st = i / (2 * (D / 32));
-#pragma unroll
-        for (int nb = 0; nb < kNB; ++nb) o[nb][dt] = mfma(va[i % 4], pf[nb][st][cc], o[nb][dt]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
     };
-    int t = t_begin;
-    for (; t + 1 < t_end; t += 2) {
-      step(std::integral_constant<int, 0>{}, t);
-      step(std::integral_constant<int, 1>{}, t + 1);
+
+    const uint16_t* v_ring = lds + kRing * T::kElems;
+    const uint16_t* v_prev = v_ring + ring(t_begin);     // (any finite tile for the first step)
+    for (int t = t_begin; t < t_end; ++t) {
+      if (t > t_begin) {
+        // K(t+1) and V(t), asked for at tile t-2, have landed; what tile t-1 asked for may be in flight
+        if (t + 2 < t_end) wait_vmcnt<2 * T::kCalls>();
+        else wait_vmcnt<0>();
+        __syncthreads();                   // everyone's; tile t-1 is finished
+      }
+      if (t + 3 < t_end) {
+        const int last = min((t + 4) * kKT - 1, ctx - 1) >> b.page_shift;
+        const bool move = last - window >= kWave;        // of tile t+3
+        const int here = pages;
+        if (move) {
+          pages = checked(page_ids[wave][turn ^ 1][lane]);
+          ask_pages(window + 2 * kWave);
+        }
+        issue_v(t + 2, here, window);
+        if (move) window += kWave;
+        issue_k(t + 3);
+      } else if (t + 2 < t_end) {
+        issue_v(t + 2, pages, window);
+      }
+      const uint16_t* kt = lds + ring(t);
+      const uint16_t* vt = v_ring + ring(t);
+      step(sA, sB, pB, pA, kt + 32 * D, v_prev, t * kKT);
+      step(sB, sA, pA, pB, lds + ring(t + 1), vt, t * kKT + 32);
+      v_prev = vt + 32 * D;
     }
-    if (t < t_end) step(std::integral_constant<int, 0>{}, t);
+    // the last 32 keys' product
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const bf16x8 vc = vop(v_prev, i);
+#pragma unroll
+      for (int nb = 0; nb < kNB; ++nb)
+        o[nb][i % (D / 32)] = mfma(vc, pB[nb][i / (D / 32)], o[nb][i % (D / 32)]);
+    }
 
     // ---- the part's result
 #pragma unroll
