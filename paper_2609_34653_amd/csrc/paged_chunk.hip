@@ -344,27 +344,47 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     int pages = checked(table[min(window + lane, last_page)]);
     const uint8_t* k_head = reinterpret_cast<const uint8_t*>(k) + 2 * g * D;
     const uint8_t* v_head = reinterpret_cast<const uint8_t*>(v) + 2 * g * D;
+    // byte offset of each call's first key of tile t in a head's pool; the calls of a tile that
+    // lies in one page are a constant apart
     const int page_mask = (1 << b.page_shift) - 1;
-    // direct copy of one tensor's tile t into the ring buffer at LDS byte address dst
-    auto issue = [&](const uint8_t* head, const uint32_t (&offs)[T::kCalls], int t, uint32_t dst,
-                     int ids, int from) {
+    int64_t at_k[T::kCalls], at_v[T::kCalls];        // of the tile asked for last
+    auto locate = [&](int t) {
 #pragma unroll
       for (int cq = 0; cq < T::kCalls; ++cq) {
-        const int at = t * kKT + (wave + kWaves * cq) * T::kCallKeys;
-        const int ks = min(at, ctx - 1);
-        const int page = readlane(ids, (ks >> b.page_shift) - from);
-        const uint8_t* src =
-            head + ((static_cast<size_t>(page) << b.page_shift) + (ks & page_mask)) * row_bytes;
-        uint32_t off = offs[cq];
-        if (at + T::kCallKeys > ctx)       // rows past the context: its last one
-          off -= static_cast<uint32_t>(max(prow[cq] - (ctx - 1 - ks), 0)) * row_bytes;
-        dma16(src, off, dst + static_cast<uint32_t>(cq * kWaves * kWave * 16));
+        if (cq > 0 && b.page_shift >= 6 && (t + 1) * kKT <= ctx) {
+          at_k[cq] = at_k[0] + cq * static_cast<int64_t>(kWaves * T::kCallKeys * row_bytes);
+        } else {
+          const int ks = min(t * kKT + (wave + kWaves * cq) * T::kCallKeys, ctx - 1);
+          const int page = readlane(pages, (ks >> b.page_shift) - window);
+          at_k[cq] = ((static_cast<int64_t>(page) << b.page_shift) + (ks & page_mask)) * row_bytes;
+        }
       }
     };
-    auto ring = [&](int t) { return ((t - t_begin) & (kRing - 1)) * T::kElems; };
-    auto issue_k = [&](int t) { issue(k_head, koff, t, lds_wave + 2 * ring(t), pages, window); };
-    auto issue_v = [&](int t, int ids, int from) {
-      issue(v_head, voff, t, lds_wave + 2 * (kRing * T::kElems + ring(t)), ids, from);
+    // direct copy of one tensor's tile t into ring entry r
+    auto issue = [&](const uint8_t* head, const uint32_t (&offs)[T::kCalls],
+                     const int64_t (&at)[T::kCalls], int t, uint32_t dst) {
+      const bool inside = (t + 1) * kKT <= ctx;
+#pragma unroll
+      for (int cq = 0; cq < T::kCalls; ++cq) {
+        uint32_t off = offs[cq];
+        if (!inside) {                     // rows past the context: its last one
+          const int first = t * kKT + (wave + kWaves * cq) * T::kCallKeys;
+          off -= static_cast<uint32_t>(max(prow[cq] - (ctx - 1 - min(first, ctx - 1)), 0)) * row_bytes;
+        }
+        dma16(head + at[cq], off, dst + static_cast<uint32_t>(cq * kWaves * kWave * 16));
+      }
+    };
+    auto issue_k = [&](int t) {
+      locate(t);
+      issue(k_head, koff, at_k, t, lds_wave + ((t - t_begin) & (kRing - 1)) * (2u * T::kElems));
+    };
+    auto issue_v = [&](int t, const int64_t (&at)[T::kCalls]) {
+      issue(v_head, voff, at, t,
+            lds_wave + (kRing + ((t - t_begin) & (kRing - 1))) * (2u * T::kElems));
+    };
+    auto keep = [&]() {
+#pragma unroll
+      for (int cq = 0; cq < T::kCalls; ++cq) at_v[cq] = at_k[cq];
     };
 
     floatx16 o[kNB][D / 32];
@@ -397,10 +417,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
     ask_pages(window + kWave);
     issue_k(t_begin);
-    issue_v(t_begin, pages, window);
-    if (t_begin + 1 < t_end) issue_k(t_begin + 1);
-    if (t_begin + 1 < t_end) issue_v(t_begin + 1, pages, window);
+    issue_v(t_begin, at_k);
+    if (t_begin + 1 < t_end) {
+      issue_k(t_begin + 1);
+      issue_v(t_begin + 1, at_k);
+    }
     if (t_begin + 2 < t_end) issue_k(t_begin + 2);
+    keep();                                // at_v: of tile t+2 at tile t
     wait_vmcnt<0>();
     __syncthreads();
 #pragma unroll
@@ -417,7 +440,8 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     // scores are of a stale buffer and not used.)
     const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
     auto step = [&](floatx16(&s_cur)[kNB], floatx16(&s_nxt)[kNB], bf16x8(&p_prev)[kNB][2],
-                    bf16x8(&p_cur)[kNB][2], const uint16_t* kb, const uint16_t* vb, int key0) {
+                    bf16x8(&p_cur)[kNB][2], const uint16_t* kb, const uint16_t* vb,
+                    int key0) __attribute__((always_inline)) {
       if (key0 + 31 > full_lim) {
 #pragma unroll
         for (int nb = 0; nb < kNB; ++nb)
@@ -493,7 +517,8 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     };
 
     const uint16_t* v_ring = lds + kRing * T::kElems;
-    const uint16_t* v_prev = v_ring + ring(t_begin);     // (any finite tile for the first step)
+    const uint16_t* v_prev = v_ring + 32 * D;            // (finite, for the first step's zeros)
+    int entry = 0;                                       // (t - t_begin) % kRing
     for (int t = t_begin; t < t_end; ++t) {
       if (t > t_begin) {
         // K(t+1) and V(t), asked for at tile t-2, have landed; what tile t-1 asked for may be in flight
@@ -502,24 +527,23 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         __syncthreads();                   // everyone's; tile t-1 is finished
       }
       if (t + 3 < t_end) {
-        const int last = min((t + 4) * kKT - 1, ctx - 1) >> b.page_shift;
-        const bool move = last - window >= kWave;        // of tile t+3
-        const int here = pages;
-        if (move) {
+        issue_v(t + 2, at_v);
+        if ((min((t + 4) * kKT - 1, ctx - 1) >> b.page_shift) - window >= kWave) {
           pages = checked(page_ids[wave][turn ^ 1][lane]);
-          ask_pages(window + 2 * kWave);
+          window += kWave;
+          ask_pages(window + kWave);
         }
-        issue_v(t + 2, here, window);
-        if (move) window += kWave;
         issue_k(t + 3);
+        keep();
       } else if (t + 2 < t_end) {
-        issue_v(t + 2, pages, window);
+        issue_v(t + 2, at_v);
       }
-      const uint16_t* kt = lds + ring(t);
-      const uint16_t* vt = v_ring + ring(t);
-      step(sA, sB, pB, pA, kt + 32 * D, v_prev, t * kKT);
-      step(sB, sA, pA, pB, lds + ring(t + 1), vt, t * kKT + 32);
+      const int next = (entry + 1) & (kRing - 1);
+      const uint16_t* vt = v_ring + entry * T::kElems;
+      step(sA, sB, pB, pA, lds + entry * T::kElems + 32 * D, v_prev, t * kKT);
+      step(sB, sA, pA, pB, lds + next * T::kElems, vt, t * kKT + 32);
       v_prev = vt + 32 * D;
+      entry = next;
     }
     // the last 32 keys' product
 #pragma unroll
