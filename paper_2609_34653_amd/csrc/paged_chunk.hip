@@ -434,14 +434,16 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     }
 
     // One step for 32 keys from key0 on, whose scores are in s_cur: their softmax, the scores of the
-    // next 32 keys (at kb) and the product of the 32 keys before (values at vb, probabilities p_prev),
-    // interleaved so that the vector units work while the matrix cores run: a wave issues in
-    // order, and one wave runs on each SIMD.  (The first step's p_prev are zeros; the last one's next
-    // scores are of a stale buffer and not used.)
+    // next 32 keys and the product of the 32 keys before (probabilities p_prev), interleaved so that
+    // the vector units work while the matrix cores run: a wave issues in order.  The operands of its
+    // first two slots are in ka and va; the later ones come from kb and vb, and the next step's first
+    // two are read from kn and vn at its end.  `middle` is called half-way.  (The first step's
+    // p_prev are zeros; the last one's next scores are of stale keys and not used.)
     const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+    bf16x8 ka[2], va[2];
     auto step = [&](floatx16(&s_cur)[kNB], floatx16(&s_nxt)[kNB], bf16x8(&p_prev)[kNB][2],
                     bf16x8(&p_cur)[kNB][2], const uint16_t* kb, const uint16_t* vb,
-                    int key0) __attribute__((always_inline)) {
+                    const uint16_t* kn, const uint16_t* vn, int key0, auto middle) {
       if (key0 + 31 > full_lim) {
 #pragma unroll
         for (int nb = 0; nb < kNB; ++nb)
@@ -456,8 +458,6 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         ls[nb][0] = ls[nb][1] = 0.f;
         s_nxt[nb] = floatx16{};
       }
-      bf16x8 ka[2] = {kop(kb, 0), kop(kb, 1)};
-      bf16x8 va[2] = {vop(vb, 0), vop(vb, 1)};
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         const bf16x8 kc = ka[i & 1], vc = va[i & 1];
@@ -466,13 +466,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         for (int nb = 0; nb < kNB; ++nb) {
           float e[EPS];
           s_nxt[nb] = mfma(kc, qf[nb][i], s_nxt[nb]);
-          if (nb == kNB - 1 && i + 2 < NS) ka[i & 1] = kop(kb, i + 2);
+          if (nb == kNB - 1) ka[i & 1] = i + 2 < NS ? kop(kb, i + 2) : kop(kn, i + 2 - NS);
 #pragma unroll
           for (int x = 0; x < EPS; ++x)
             e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[nb][i * EPS + x], scale_log2, -m_run[nb]));
           __builtin_amdgcn_sched_barrier(0);
           o[nb][dt] = mfma(vc, p_prev[nb][cc], o[nb][dt]);
-          if (nb == kNB - 1 && i + 2 < NS) va[i & 1] = vop(vb, i + 2);
+          if (nb == kNB - 1) va[i & 1] = i + 2 < NS ? vop(vb, i + 2) : vop(vn, i + 2 - NS);
 #pragma unroll
           for (int x = 0; x < EPS; x += 2) {
             const int at = i * EPS + x;
@@ -483,6 +483,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
                 __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls[nb][(at >> 1) & 1], false);
           }
           __builtin_amdgcn_sched_barrier(0);
+        }
+        if (i == NS / 2 - 1) {
+          // (the first half's softmax is not to be put off to behind the branches in there)
+#pragma unroll
+          for (int nb = 0; nb < kNB; ++nb)
+            asm volatile("" : "+v"(p_cur[nb][0]), "+v"(ls[nb][0]), "+v"(ls[nb][1]));
+          middle();
         }
       }
 #pragma unroll
@@ -516,16 +523,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       }
     };
 
-    const uint16_t* v_ring = lds + kRing * T::kElems;
-    const uint16_t* v_prev = v_ring + 32 * D;            // (finite, for the first step's zeros)
-    int entry = 0;                                       // (t - t_begin) % kRing
-    for (int t = t_begin; t < t_end; ++t) {
-      if (t > t_begin) {
-        // K(t+1) and V(t), asked for at tile t-2, have landed; what tile t-1 asked for may be in flight
-        if (t + 2 < t_end) wait_vmcnt<2 * T::kCalls>();
-        else wait_vmcnt<0>();
-        __syncthreads();                   // everyone's; tile t-1 is finished
-      }
+    // In the middle of tile t's first step every wave is done with tile t-1; K(t+1) and V(t), asked for
+    // at tile t-2, have landed (what tile t-1 asked for may be in flight), which the second step
+    // needs; K(t+3) and V(t+2) are asked for, into the entries of K(t-1) and V(t-2).
+    auto turn_over = [&](int t) {
+      if (t + 2 < t_end) wait_vmcnt<2 * T::kCalls>();
+      else wait_vmcnt<0>();
+      asm volatile("s_barrier" ::: "memory");
       if (t + 3 < t_end) {
         issue_v(t + 2, at_v);
         if ((min((t + 4) * kKT - 1, ctx - 1) >> b.page_shift) - window >= kWave) {
@@ -538,10 +542,23 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       } else if (t + 2 < t_end) {
         issue_v(t + 2, at_v);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    const uint16_t* v_ring = lds + kRing * T::kElems;
+    int entry = 0;                                       // (t - t_begin) % kRing
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ka[i] = kop(lds + 32 * D, i);
+      va[i] = vop(v_ring, i);                            // (finite, for the first step's zeros)
+    }
+    const uint16_t* v_prev = v_ring;
+    for (int t = t_begin; t < t_end; ++t) {
       const int next = (entry + 1) & (kRing - 1);
+      const uint16_t* kt = lds + entry * T::kElems;
+      const uint16_t* k1 = lds + next * T::kElems;
       const uint16_t* vt = v_ring + entry * T::kElems;
-      step(sA, sB, pB, pA, lds + entry * T::kElems + 32 * D, v_prev, t * kKT);
-      step(sB, sA, pA, pB, lds + next * T::kElems, vt, t * kKT + 32);
+      step(sA, sB, pB, pA, kt + 32 * D, v_prev, k1, vt, t * kKT, [&]() { turn_over(t); });
+      step(sB, sA, pA, pB, k1, vt, k1 + 32 * D, vt + 32 * D, t * kKT + 32, []() {});
       v_prev = vt + 32 * D;
       entry = next;
     }
