@@ -66,14 +66,18 @@ struct Joined {
   int32_t n_parts, first_slot, last_share, q0, rows, mt, g, pad;
 };
 
-constexpr int kMaxSeqs = 1024;
 
-// The shares of a call, in LDS: every sequence's first token, tokens (0: none, or malformed) and
-// context, and the work (keys times G) of its chunk of 64 sequences in front of it, per KV head.
+// What the shares are made from, in LDS: every sequence's first token, tokens (0: none, or malformed),
+// context and the row tiles in front of it in its chunk of 64 sequences; the work (keys times G) in
+// front of it in its chunk; both in front of each chunk, per KV head.
+template <int SEQS>
 struct PlanMem {
-  int4 seq[kMaxSeqs];
-  int64_t first[kMaxSeqs];
-  int64_t chunk[kMaxSeqs / kWave + 1];   // work in front of each chunk; the last: of all
+  int4 seq[SEQS];
+  int64_t first[SEQS];
+  int64_t chunk[SEQS / kWave];
+  int32_t chunk_tiles[SEQS / kWave];
+  int64_t wave_max[kWaves];
+  int32_t wave_min[kWaves];
 };
 
 // Scalars for the wave, whatever registers they were computed in.
@@ -85,10 +89,17 @@ __device__ inline int64_t uniform(int64_t x) {
   return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
 }
 
+// Row tiles in order of (KV head, sequence, number).  Where they are much alike, workgroups first take
+// whole ones in rounds, n_wgs at a time, so that the workgroups of an XCD read the same keys
+// together; what is left (all of them where they are not alike) is cut into a share per workgroup:
+// each row tile into `even` equal parts where that leaves few workgroups without one, otherwise all
+// the work into equal shares.
+template <int SEQS>
 struct Plan {
-  const PlanMem* mem;
-  int64_t per_head, total, share;
-  int G, Hkv, n_seq;
+  const PlanMem<SEQS>* mem;
+  int64_t per_head, total, share, rest;  // work; rest: in front of what is cut into shares
+  int tiles_per_head, rounds, even, left;          // left: row tiles that are cut into shares
+  int G, Hkv, n_seq, n_wgs;
 
   __device__ static int row_tiles(int len, int G) {
     return static_cast<int>((static_cast<int64_t>(len) * G + kRows - 1) / kRows);
@@ -104,14 +115,18 @@ struct Plan {
   }
 
   // by the whole workgroup
-  __device__ void make(PlanMem& m, const PagedBatch& b, int G_, int Hkv_, int n_wgs) {
-    const int lane = threadIdx.x & (kWave - 1), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  __device__ void make(PlanMem<SEQS>& m, const PagedBatch& b, int G_, int Hkv_, int n_wgs_) {
+    const int tid = static_cast<int>(threadIdx.x);
+    const int lane = tid & (kWave - 1), wave = uniform(tid / kWave);
     const int cap = b.max_pages << b.page_shift;
     G = G_;
     Hkv = Hkv_;
     n_seq = b.n_seq;
+    n_wgs = n_wgs_;
     mem = &m;
     const int n_chunks = (n_seq + kWave - 1) / kWave;
+    int64_t most = 0;                      // work of the largest row tile, key tiles of the shortest
+    int fewest = INT32_MAX;
     for (int c = wave; c < n_chunks; c += kWaves) {
       const int i = c * kWave + lane;
       int s0 = 0, s1 = 0, n = 0;
@@ -122,26 +137,77 @@ struct Plan {
       }
       const bool ok = s0 >= 0 && s1 > s0 && s1 <= b.n_tokens && n >= s1 - s0 && n <= cap;
       const int len = ok ? s1 - s0 : 0;
-      const int64_t w = ok ? work(row_tiles(len, G), n - len) : 0;
-      const int64_t inc = wave_inclusive_scan(w);
-      m.seq[i] = make_int4(s0, len, n, 0);
-      m.first[i] = inc - w;
-      if (lane == kWave - 1) m.chunk[c] = inc;
+      const int rt = row_tiles(len, G);
+      const int64_t w = work(rt, n - len);
+      const int64_t inc = wave_inclusive_scan(ok ? w : 0);
+      const int tiles = wave_scan_add_i32(rt);
+      if (ok) {
+        most = max(most, w - work(rt - 1, n - len));
+        fewest = min(fewest, tiles_of(0, len, n));
+      }
+      m.seq[i] = make_int4(s0, len, n, tiles - rt);
+      m.first[i] = inc - (ok ? w : 0);
+      if (lane == kWave - 1) {
+        m.chunk[c] = inc;
+        m.chunk_tiles[c] = tiles;
+      }
+    }
+    for (int off = 1; off < kWave; off <<= 1) {
+      most = max(most, static_cast<int64_t>(__shfl_xor(static_cast<long long>(most), off, kWave)));
+      fewest = min(fewest, __shfl_xor(fewest, off, kWave));
+    }
+    if (lane == 0) {
+      m.wave_max[wave] = most;
+      m.wave_min[wave] = fewest;
     }
     __syncthreads();
-    int64_t sum = 0;                       // every thread adds the chunks up
-    int64_t mine = 0;
+    int64_t sum = 0, mine = 0;             // every thread adds the chunks up
+    int sum_tiles = 0, my_tiles = 0;
     for (int c = 0; c < n_chunks; ++c) {
-      if (c == static_cast<int>(threadIdx.x)) mine = sum;
+      if (c == tid) {
+        mine = sum;
+        my_tiles = sum_tiles;
+      }
       sum += m.chunk[c];
+      sum_tiles += m.chunk_tiles[c];
+    }
+    for (int w = 0; w < kWaves; ++w) {
+      most = max(most, m.wave_max[w]);
+      fewest = min(fewest, m.wave_min[w]);
     }
     __syncthreads();
-    if (static_cast<int>(threadIdx.x) < n_chunks) m.chunk[threadIdx.x] = mine;
+    if (tid < n_chunks) {
+      m.chunk[tid] = mine;
+      m.chunk_tiles[tid] = my_tiles;
+    }
     __syncthreads();
     per_head = uniform(sum);
     total = per_head * Hkv;
+    tiles_per_head = uniform(sum_tiles);
+    const int n_tiles = tiles_per_head * Hkv;
+    rounds = 0;
+    even = 0;
+    left = n_tiles;
+    rest = 0;
+    // alike: the largest row tile has at most 1.25 times the mean work
+    const bool alike = 4 * static_cast<double>(uniform(most)) * n_tiles <=
+                       5 * static_cast<double>(total);
+    if (n_tiles > 0 && alike) {
+      rounds = n_tiles / n_wgs;
+      left = n_tiles - rounds * n_wgs;
+      if (left > 0) {
+        const int parts_most = max(1, uniform(fewest) / kMinShareTiles);
+        const int parts = min(n_wgs / left, parts_most);
+        if (parts == parts_most || 10 * left * parts >= 9 * n_wgs) even = parts;
+        if (rounds > 0) {
+          const Cut c = row_tile(rounds * n_wgs);
+          const Seq q = seq(c.seq);
+          rest = c.g * per_head + first(c.seq) + work(c.mt, q.ctx - q.len);
+        }
+      }
+    }
     const int64_t least = static_cast<int64_t>(kMinShareTiles) * kKT * G;
-    share = uniform(max(least, (total + n_wgs - 1) / n_wgs));
+    share = uniform(max(least, (total - rest + n_wgs - 1) / n_wgs));
   }
 
   struct Seq {
@@ -174,13 +240,25 @@ struct Plan {
     }
     return g < Hkv ? Cut{g, s, 0, 0} : Cut{Hkv, 0, 0, 0};
   }
+  // row tile number i of all
+  __device__ Cut row_tile(int i) const {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int g = i / tiles_per_head, r = i - g * tiles_per_head;
+    int c = 0;
+    while ((c + 1) * kWave < n_seq && uniform(mem->chunk_tiles[c + 1]) <= r) ++c;
+    const int at = c * kWave + lane, in = r - uniform(mem->chunk_tiles[c]);
+    const uint64_t hit = __ballot(at < n_seq && mem->seq[at].y > 0 && mem->seq[at].w <= in);
+    const int s = uniform(c * kWave + 63 - __clzll(static_cast<long long>(hit)));
+    return {uniform(g), s, uniform(in - mem->seq[s].w), 0};
+  }
+  // the row tile and key tile at x units of work
   __device__ Cut at(int64_t x) const {
     if (x >= total) return {Hkv, 0, 0, 0};
     const int lane = threadIdx.x & (kWave - 1);
     const int g = static_cast<int>(x / per_head);
     const int64_t y = x - g * per_head;
     int c = 0;
-    while ((c + 1) * kWave < n_seq && mem->chunk[c + 1] <= y) ++c;
+    while ((c + 1) * kWave < n_seq && uniform(mem->chunk[c + 1]) <= y) ++c;
     const int i = c * kWave + lane;
     const uint64_t hit =
         __ballot(i < n_seq && mem->seq[i].y > 0 && mem->chunk[c] + mem->first[i] <= y);
@@ -203,9 +281,39 @@ struct Plan {
     if (tile >= nt - kSnap) return settle({uniform(g), s, m + 1, 0});
     return {uniform(g), s, m, tile};
   }
-  __device__ Cut share_begin(int64_t w) const {
-    const Cut c = at(min(w * share, total));
+  __device__ Cut share_begin(int w) const {
+    Cut c{Hkv, 0, 0, 0};
+    if (even > 0) {
+      if (w / even < left) {
+        c = row_tile(rounds * n_wgs + w / even);
+        const Seq q = seq(c.seq);
+        c.tile = static_cast<int>(static_cast<int64_t>(tiles_of(c.mt, q.len, q.ctx)) *
+                                  (w % even) / even);
+      }
+    } else if (left > 0) {
+      c = at(min(rest + w * share, total));
+    }
     return {uniform(c.g), uniform(c.seq), uniform(c.mt), uniform(c.tile)};
+  }
+  // the share whose part of row tile c (cut into several) begins it, and the part's slot
+  __device__ int first_share(Cut c, int w, int& slot) const {
+    if (even > 0) {
+      slot = 2 * (w - w % even);
+      return w - w % even;
+    }
+    const Seq q = seq(c.seq);
+    const int64_t x0 = c.g * per_head + first(c.seq) + work(c.mt, q.ctx - q.len);
+    int w0 = static_cast<int>((x0 - rest) / share);
+    c.tile = 0;
+    Cut b = share_begin(w0);
+    for (;;) {                             // shares that begin here with nothing in them
+      const Cut b1 = share_begin(w0 + 1);
+      if (!same_rows(b1, c) || b1.tile != 0) break;
+      ++w0;
+      b = b1;
+    }
+    slot = 2 * w0 + (same_rows(b, c) && b.tile == 0 ? 0 : 1);
+    return w0;
   }
 };
 
@@ -222,15 +330,16 @@ struct Tile {
   static constexpr int kCallKeys = kWave / kChunks;                 // keys of one load
 };
 
-template <int D>
+// SEQS: sequences at most.
+template <int D, int SEQS>
 __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
     const PagedBatch b, int Hq, int Hkv, float scale_log2, void* __restrict__ out, bool out_bf16,
     float* __restrict__ part_o, float2* __restrict__ part_ml, Joined* __restrict__ joined,
     int32_t* __restrict__ status) {
   using T = Tile<D>;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * kRing * T::kElems];   // K, V tiles
-  __shared__ PlanMem plan_mem;
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * kRing * T::kElems];   // K, V
+  __shared__ PlanMem<SEQS> plan_mem;
   __shared__ int32_t page_ids[kWaves][2][kWave];
 
   const int tid = threadIdx.x;
@@ -240,20 +349,15 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
   const int G = Hq / Hkv;
 
   if (blockIdx.x == 0 && wave == 0) report_batch(b, status);
-  Plan plan;
+  Plan<SEQS> plan;
   plan.make(plan_mem, b, G, Hkv, gridDim.x);
   // shares next to each other (the same keys, the next rows) on one XCD: workgroups are dealt
   // round-robin over 8
   const int n_wg = gridDim.x;
   const int w = (blockIdx.x % kNumXcd) * (n_wg / kNumXcd) + blockIdx.x / kNumXcd;
-  Cut cur = plan.share_begin(w);
-  const Cut end = plan.share_begin(w + 1);
-  const Cut begin = cur;
-  if (plan.total == 0 || !before(cur, end)) {
-    if (tid == 0) joined[w].n_parts = 0;
-    return;
-  }
-  if (begin.tile == 0 && tid == 0) joined[w].n_parts = 0;
+  const Cut begin = plan.share_begin(w), end = plan.share_begin(w + 1);
+  Cut cur = begin;
+  if (tid == 0) joined[w].n_parts = 0;
 
   const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
   uint32_t koff[T::kCalls], voff[T::kCalls];
@@ -274,36 +378,39 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
   const int v_lane_off = (gi >> 2) * D + 8 * ((gi & 3) >> 1) + 4 * (gi & 1);
   constexpr float kSumLimit = 4294967296.f;
 
-  while (before(cur, end)) {
-    // ---- the part of one row tile
-    const auto sq = plan.seq(cur.seq);
-    const int L = sq.len, ctx = sq.ctx, kept = ctx - L, g = cur.g;
-    const int nt = plan.tiles_of(cur.mt, L, ctx);
-    const int t_begin = cur.tile;
-    const int t_end = same_rows(cur, end) ? end.tile : nt;
+  for (int round = 0;; ++round) {
+    // ---- the next part: a whole row tile of a round, then what the share holds
+    const bool shared = round >= plan.rounds;
+    if (shared && !before(cur, end)) break;
+    const Cut c = shared ? cur
+                         : plan.row_tile(round * n_wg + (round & 1 ? n_wg - 1 - w : w));
+    const auto sq = plan.seq(c.seq);
+    const int L = sq.len, ctx = sq.ctx, kept = ctx - L, g = c.g;
+    const int nt = plan.tiles_of(c.mt, L, ctx);
+    const int t_begin = c.tile;
+    const int t_end = shared && same_rows(c, end) ? end.tile : nt;
     const bool whole = t_begin == 0 && t_end == nt;
-    const int slot = 2 * w + (same_rows(cur, begin) ? 0 : 1);
-    const int m0 = cur.mt * kRows;
+    const int slot = 2 * w + (same_rows(c, begin) ? 0 : 1);
+    const int m0 = c.mt * kRows;
     const int full_lim = kept + m0 / G;    // keys <= full_lim are visible to every row
     if (t_begin > 0 && t_end == nt && wave == 0) {
       // the row tile ends here: tell the merge where its parts are
-      const int64_t x0 = g * plan.per_head + plan.first(cur.seq) + plan.work(cur.mt, kept);
-      int64_t w0 = x0 / plan.share;
-      const Cut start{g, cur.seq, cur.mt, 0};
-      Cut c = plan.share_begin(w0);
-      for (;;) {                           // shares that begin here with nothing in them
-        const Cut c1 = plan.share_begin(w0 + 1);
-        if (!same_rows(c1, start) || c1.tile != 0) break;
-        ++w0;
-        c = c1;
-      }
-      if (lane == 0) {
-        const int first = static_cast<int>(2 * w0) + (same_rows(c, start) && c.tile == 0 ? 0 : 1);
-        joined[w] = Joined{w - static_cast<int>(w0) + 1, first, w, sq.q0, L * G, cur.mt, g, 0};
-      }
-    } else if (t_begin > 0 && tid == 0) {
-      joined[w].n_parts = 0;
+      int first_slot;
+      const int w0 = plan.first_share(c, w, first_slot);
+      if (lane == 0)
+        joined[w] = Joined{w - w0 + 1, first_slot, w, sq.q0, L * G, c.mt, g, 0};
     }
+
+    // on to the next part; false after the share's last
+    auto after_part = [&]() {
+      if (shared) {
+        if (t_end < nt) return false;      // it ended inside the row tile
+        cur = plan.settle(Cut{c.g, c.seq, c.mt + 1, 0});
+        cur = Cut{uniform(cur.g), uniform(cur.seq), uniform(cur.mt), 0};
+      }
+      __syncthreads();                     // the tile buffers are free again
+      return true;
+    };
 
     int lim[kNB];                          // last visible key of this lane's rows
     bool row_ok[kNB];
@@ -326,7 +433,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     // Ids of the 64 pages from `window` on, one per lane.  The next 64 wait in LDS, put there by a
     // direct load when the window moved (a plain load would have the compiler wait for it, and so
     // for the tiles asked for before it).
-    const int32_t* table = b.table + static_cast<size_t>(cur.seq) * b.max_pages;
+    const int32_t* table = b.table + static_cast<size_t>(c.seq) * b.max_pages;
     const int last_page = (ctx - 1) >> b.page_shift;
     int window = (t_begin * kKT) >> b.page_shift, turn = 0;
     auto ask_pages = [&](int first) {
@@ -552,6 +659,11 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       va[i] = vop(v_ring, i);                            // (finite, for the first step's zeros)
     }
     const uint16_t* v_prev = v_ring;
+    if (m0 + wave * 32 >= L * G) {         // a wave without rows: its share of the copies
+      for (int t = t_begin; t < t_end; ++t) turn_over(t);
+      if (!after_part()) break;
+      continue;
+    }
     for (int t = t_begin; t < t_end; ++t) {
       const int next = (entry + 1) & (kRing - 1);
       const uint16_t* kt = lds + entry * T::kElems;
@@ -599,10 +711,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         if (h == 0) part_ml[prow_] = make_float2(m_run[nb], l_tot);
       }
     }
-    if (t_end < nt) break;                   // the share ended inside the row tile
-    cur = plan.settle(Cut{cur.g, cur.seq, cur.mt + 1, 0});
-    cur = Cut{uniform(cur.g), uniform(cur.seq), uniform(cur.mt), 0};
-    __syncthreads();                         // the tile buffers are free again
+    if (!after_part()) break;
   }
 }
 
@@ -660,14 +769,14 @@ __global__ __launch_bounds__(kThreads) void paged_chunk_merge_kernel(
 
 constexpr size_t kJoinedBytes = kWGs * sizeof(Joined);
 
-template <int D>
+template <int D, int SEQS>
 hipError_t launch_t(const PagedAttnArgs& a, hipStream_t stream) {
   const PagedBatch& b = a.batch;
   Joined* joined = static_cast<Joined*>(a.workspace);
   float2* part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(a.workspace) + kJoinedBytes);
   float* part_o = reinterpret_cast<float*>(part_ml + static_cast<size_t>(2 * kWGs) * kRows);
   const float scale_log2 = a.scale * 1.4426950408889634f;
-  hipLaunchKernelGGL((paged_chunk_kernel<D>), dim3(kWGs), dim3(kThreads), 0, stream,
+  hipLaunchKernelGGL((paged_chunk_kernel<D, SEQS>), dim3(kWGs), dim3(kThreads), 0, stream,
                      static_cast<const uint16_t*>(a.q), static_cast<const uint16_t*>(a.k),
                      static_cast<const uint16_t*>(a.v), b, a.n_q_heads, a.n_kv_heads, scale_log2,
                      a.out, a.out_bf16, part_o, part_ml, joined, a.d_status);
@@ -686,7 +795,9 @@ size_t paged_chunk_workspace_bytes(int, int, int, int, int, int head_dim) {
 }
 
 hipError_t launch_paged_chunk(const PagedAttnArgs& a, hipStream_t stream) {
-  return a.head_dim == 128 ? launch_t<128>(a, stream) : launch_t<64>(a, stream);
+  if (a.batch.n_seq <= 256)
+    return a.head_dim == 128 ? launch_t<128, 256>(a, stream) : launch_t<64, 256>(a, stream);
+  return a.head_dim == 128 ? launch_t<128, 1024>(a, stream) : launch_t<64, 1024>(a, stream);
 }
 
 }  // namespace omnitide

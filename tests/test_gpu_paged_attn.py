@@ -83,6 +83,9 @@ CHUNKS = [
     ([40 + i for i in range(70)], [1 + i % 3 for i in range(70)], 32, 4, 1, 128, BF),
     ([1030], [1030], 64, 16, 4, 128, F32),                   # a prompt: no context before it
     ([9 + i % 3 for i in range(300)], [i % 3 for i in range(300)], 16, 8, 4, 64, F32),
+    ([900, 830], [600, 600], 64, 8, 8, 128, F32),            # row tiles alike, cut into even parts
+    ([1400, 1390, 1410], [700, 710, 690], 32, 32, 8, 64, F32),   # more row tiles than workgroups
+    ([2300], [2300], 64, 32, 8, 64, BF),                     # as many, of unequal work
 ]
 
 
