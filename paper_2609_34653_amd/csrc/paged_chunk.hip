@@ -76,8 +76,9 @@ struct PlanMem {
   int64_t first[SEQS];
   int64_t chunk[SEQS / kWave];
   int32_t chunk_tiles[SEQS / kWave];
-  int64_t wave_max[kWaves];
+  int64_t wave_max[kWaves], wave_sum[kWaves];
   int32_t wave_min[kWaves];
+  int64_t begin[kWGs + 1];               // work in front of each share (rounds > 0)
 };
 
 // Scalars for the wave, whatever registers they were computed in.
@@ -89,17 +90,17 @@ __device__ inline int64_t uniform(int64_t x) {
   return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
 }
 
-// Row tiles in order of (KV head, sequence, number).  Where they are much alike, workgroups first take
-// whole ones in rounds, n_wgs at a time, so that the workgroups of an XCD read the same keys
-// together; what is left (all of them where they are not alike) is cut into a share per workgroup:
-// each row tile into `even` equal parts where that leaves few workgroups without one, otherwise all
-// the work into equal shares.
+// Row tiles in order of (KV head, sequence, number).  Workgroups first take whole ones in rounds,
+// kWGs at a time, so that the workgroups of an XCD read the same keys together; what is left
+// is cut into a share per workgroup, each as large as its rounds leave room for: as many rounds
+// as leave enough to even them out.  Without rounds, row tiles that are much alike are cut into
+// `even` equal parts each where that leaves few workgroups without one, for the same reason.
 template <int SEQS>
 struct Plan {
   const PlanMem<SEQS>* mem;
   int64_t per_head, total, share, rest;  // work; rest: in front of what is cut into shares
   int tiles_per_head, rounds, even, left;          // left: row tiles that are cut into shares
-  int G, Hkv, n_seq, n_wgs;
+  int G, Hkv, n_seq;
 
   __device__ static int row_tiles(int len, int G) {
     return static_cast<int>((static_cast<int64_t>(len) * G + kRows - 1) / kRows);
@@ -115,14 +116,13 @@ struct Plan {
   }
 
   // by the whole workgroup
-  __device__ void make(PlanMem<SEQS>& m, const PagedBatch& b, int G_, int Hkv_, int n_wgs_) {
+  __device__ void make(PlanMem<SEQS>& m, const PagedBatch& b, int G_, int Hkv_) {
     const int tid = static_cast<int>(threadIdx.x);
     const int lane = tid & (kWave - 1), wave = uniform(tid / kWave);
     const int cap = b.max_pages << b.page_shift;
     G = G_;
     Hkv = Hkv_;
     n_seq = b.n_seq;
-    n_wgs = n_wgs_;
     mem = &m;
     const int n_chunks = (n_seq + kWave - 1) / kWave;
     int64_t most = 0;                      // work of the largest row tile, key tiles of the shortest
@@ -189,25 +189,83 @@ struct Plan {
     even = 0;
     left = n_tiles;
     rest = 0;
+    share = 0;
+    if (n_tiles == 0) return;
+    for (rounds = n_tiles / kWGs; rounds > 0; rounds -= (rounds + 7) / 8) {
+      left = n_tiles - rounds * kWGs;
+      rest = left > 0 ? work_before(rounds * kWGs) : total;
+      // this thread's workgroup: the work of its rounds, then its share's room up to a level
+      int64_t mine = 0;
+      if (tid < kWGs)
+        for (int r = 0; r < rounds; ++r) mine += work_of(round_tile(r, tid));
+      int64_t level = 0, top = reduce(m, tid < kWGs ? mine : 0, true);
+      bool in = tid < kWGs;
+      for (int it = 0; it < 4; ++it) {     // without those above the level so far
+        const int64_t n = reduce(m, in ? 1 : 0, false);
+        level = (total - rest + reduce(m, in ? mine : 0, false)) / max(n, static_cast<int64_t>(1)) + 1;
+        in = tid < kWGs && mine < level;
+      }
+      if (50 * top > 51 * level) continue; // too uneven: a round less
+      const int64_t room = in ? level - mine : 0;
+      const int64_t inc = wave_inclusive_scan(room);
+      if (lane == kWave - 1) m.wave_sum[wave] = inc;
+      __syncthreads();
+      int64_t before = 0;
+      for (int w = 0; w < wave; ++w) before += m.wave_sum[w];
+      if (tid <= kWGs) m.begin[tid] = before + inc - room;
+      __syncthreads();
+      return;
+    }
+    left = n_tiles;
+    rest = 0;
     // alike: the largest row tile has at most 1.25 times the mean work
     const bool alike = 4 * static_cast<double>(uniform(most)) * n_tiles <=
                        5 * static_cast<double>(total);
-    if (n_tiles > 0 && alike) {
-      rounds = n_tiles / n_wgs;
-      left = n_tiles - rounds * n_wgs;
-      if (left > 0) {
-        const int parts_most = max(1, uniform(fewest) / kMinShareTiles);
-        const int parts = min(n_wgs / left, parts_most);
-        if (parts == parts_most || 10 * left * parts >= 9 * n_wgs) even = parts;
-        if (rounds > 0) {
-          const Cut c = row_tile(rounds * n_wgs);
-          const Seq q = seq(c.seq);
-          rest = c.g * per_head + first(c.seq) + work(c.mt, q.ctx - q.len);
-        }
-      }
+    if (alike && left <= kWGs) {
+      const int parts_most = max(1, uniform(fewest) / kMinShareTiles);
+      const int parts = min(kWGs / left, parts_most);
+      if (parts == parts_most || 10 * left * parts >= 9 * kWGs) even = parts;
     }
     const int64_t least = static_cast<int64_t>(kMinShareTiles) * kKT * G;
-    share = uniform(max(least, (total - rest + n_wgs - 1) / n_wgs));
+    share = uniform(max(least, (total + kWGs - 1) / kWGs));
+  }
+
+  // sum (or maximum) over the workgroup's threads, the same for all
+  __device__ static int64_t reduce(PlanMem<SEQS>& m, int64_t x, bool maximum) {
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int64_t y = __shfl_xor(static_cast<long long>(x), off, kWave);
+      x = maximum ? max(x, y) : x + y;
+    }
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0) m.wave_max[threadIdx.x / kWave] = x;
+    __syncthreads();
+    int64_t r = m.wave_max[0];
+    for (int w = 1; w < kWaves; ++w) r = maximum ? max(r, m.wave_max[w]) : r + m.wave_max[w];
+    return uniform(r);
+  }
+  // the row tile that workgroup w takes in a round: from the other end in every second one
+  __device__ static int round_tile(int r, int w) {
+    return r * kWGs + (r & 1 ? kWGs - 1 - w : w);
+  }
+  // (sequence, number) of row tile i of a KV head, lanes apart: binary search
+  __device__ int2 find_tile(int i) const {
+    int lo = 0, hi = n_seq - 1;            // the last sequence that begins at or before i
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (mem->chunk_tiles[mid / kWave] + mem->seq[mid].w <= i) lo = mid;
+      else hi = mid - 1;
+    }
+    return make_int2(lo, i - mem->chunk_tiles[lo / kWave] - mem->seq[lo].w);
+  }
+  __device__ int64_t work_of(int i) const {
+    const int2 t = find_tile(i % tiles_per_head);
+    const int kept = mem->seq[t.x].z - mem->seq[t.x].y;
+    return work(t.y + 1, kept) - work(t.y, kept);
+  }
+  __device__ int64_t work_before(int i) const {
+    const int2 t = find_tile(i % tiles_per_head);
+    return uniform(i / tiles_per_head * per_head + mem->chunk[t.x / kWave] + mem->first[t.x] +
+                   work(t.y, mem->seq[t.x].z - mem->seq[t.x].y));
   }
 
   struct Seq {
@@ -242,14 +300,8 @@ struct Plan {
   }
   // row tile number i of all
   __device__ Cut row_tile(int i) const {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int g = i / tiles_per_head, r = i - g * tiles_per_head;
-    int c = 0;
-    while ((c + 1) * kWave < n_seq && uniform(mem->chunk_tiles[c + 1]) <= r) ++c;
-    const int at = c * kWave + lane, in = r - uniform(mem->chunk_tiles[c]);
-    const uint64_t hit = __ballot(at < n_seq && mem->seq[at].y > 0 && mem->seq[at].w <= in);
-    const int s = uniform(c * kWave + 63 - __clzll(static_cast<long long>(hit)));
-    return {uniform(g), s, uniform(in - mem->seq[s].w), 0};
+    const int2 t = find_tile(i % tiles_per_head);
+    return {uniform(i / tiles_per_head), uniform(t.x), uniform(t.y), 0};
   }
   // the row tile and key tile at x units of work
   __device__ Cut at(int64_t x) const {
@@ -285,13 +337,15 @@ struct Plan {
     Cut c{Hkv, 0, 0, 0};
     if (even > 0) {
       if (w / even < left) {
-        c = row_tile(rounds * n_wgs + w / even);
+        c = row_tile(w / even);
         const Seq q = seq(c.seq);
         c.tile = static_cast<int>(static_cast<int64_t>(tiles_of(c.mt, q.len, q.ctx)) *
                                   (w % even) / even);
       }
+    } else if (rounds > 0) {
+      c = at(min(rest + uniform(mem->begin[w]), total));
     } else if (left > 0) {
-      c = at(min(rest + w * share, total));
+      c = at(min(w * share, total));
     }
     return {uniform(c.g), uniform(c.seq), uniform(c.mt), uniform(c.tile)};
   }
@@ -303,7 +357,16 @@ struct Plan {
     }
     const Seq q = seq(c.seq);
     const int64_t x0 = c.g * per_head + first(c.seq) + work(c.mt, q.ctx - q.len);
-    int w0 = static_cast<int>((x0 - rest) / share);
+    int w0 = 0;                            // the last share that begins at or before it
+    if (rounds > 0) {
+      for (int hi = kWGs; w0 + 1 < hi;) {
+        const int mid = (w0 + hi) / 2;
+        if (uniform(mem->begin[mid]) <= x0 - rest) w0 = mid;
+        else hi = mid;
+      }
+    } else {
+      w0 = static_cast<int>(x0 / share);
+    }
     c.tile = 0;
     Cut b = share_begin(w0);
     for (;;) {                             // shares that begin here with nothing in them
@@ -350,14 +413,16 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
 
   if (blockIdx.x == 0 && wave == 0) report_batch(b, status);
   Plan<SEQS> plan;
-  plan.make(plan_mem, b, G, Hkv, gridDim.x);
+  plan.make(plan_mem, b, G, Hkv);
   // shares next to each other (the same keys, the next rows) on one XCD: workgroups are dealt
   // round-robin over 8
-  const int n_wg = gridDim.x;
-  const int w = (blockIdx.x % kNumXcd) * (n_wg / kNumXcd) + blockIdx.x / kNumXcd;
+  const int w = (blockIdx.x % kNumXcd) * (kWGs / kNumXcd) + blockIdx.x / kNumXcd;
   const Cut begin = plan.share_begin(w), end = plan.share_begin(w + 1);
   Cut cur = begin;
   if (tid == 0) joined[w].n_parts = 0;
+  // a share of nothing in the middle of a row tile: an empty part of it
+  if (!before(begin, end) && begin.tile > 0 && tid < kRows)
+    part_ml[static_cast<size_t>(2 * w) * kRows + tid] = make_float2(-INFINITY, 0.f);
 
   const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
   uint32_t koff[T::kCalls], voff[T::kCalls];
@@ -383,7 +448,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     const bool shared = round >= plan.rounds;
     if (shared && !before(cur, end)) break;
     const Cut c = shared ? cur
-                         : plan.row_tile(round * n_wg + (round & 1 ? n_wg - 1 - w : w));
+                         : plan.row_tile(Plan<SEQS>::round_tile(round, w));
     const auto sq = plan.seq(c.seq);
     const int L = sq.len, ctx = sq.ctx, kept = ctx - L, g = c.g;
     const int nt = plan.tiles_of(c.mt, L, ctx);
@@ -747,7 +812,10 @@ __global__ __launch_bounds__(kThreads) void paged_chunk_merge_kernel(
       }
       float cm = M;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) cm = fmaxf(cm, ml[c].x);
+      for (int c = 0; c < 4; ++c) {
+        cm = fmaxf(cm, ml[c].x);
+        if (ml[c].x == -INFINITY) ov[c] = floatx4{0.f, 0.f, 0.f, 0.f};   // (not written)
+      }
       if (cm == -INFINITY) continue;
       const float a = M == -INFINITY ? 0.f : exp2f(M - cm);
       den *= a;

@@ -86,6 +86,7 @@ CHUNKS = [
     ([900, 830], [600, 600], 64, 8, 8, 128, F32),            # row tiles alike, cut into even parts
     ([1400, 1390, 1410], [700, 710, 690], 32, 32, 8, 64, F32),   # more row tiles than workgroups
     ([2300], [2300], 64, 32, 8, 64, BF),                     # as many, of unequal work
+    ([3000, 600, 40, 2000], [1500, 600, 40, 1], 16, 32, 16, 64, F32),   # and of unequal sequences
 ]
 
 
