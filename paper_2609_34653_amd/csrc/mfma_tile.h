@@ -65,6 +65,13 @@ __device__ inline void dma16(const void* base, uint32_t voff, uint32_t lds_base)
                : "v"(voff), "s"(base), "s"(lds_base)
                : "memory");
 }
+// The same for data that is read once: it is not kept in the caches at the cost of other lines.
+__device__ inline void dma16_once(const void* base, uint32_t voff, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+               :
+               : "v"(voff), "s"(base), "s"(lds_base)
+               : "memory");
+}
 // The same for 4 bytes per lane (lane i writes LDS byte address lds_base + 4 i).
 __device__ inline void dma4(const void* base, uint32_t voff, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"

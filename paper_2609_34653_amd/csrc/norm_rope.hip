@@ -7,13 +7,15 @@
 // fraction is exact to 2^-53 of the product, and the float sine and cosine of half turns
 // (sincospif) take it without a range reduction of their own.
 //
-// Bound by memory (each value read and written once), by the launch and one round trip for a few
-// tokens.  One wave takes one token and up to kIters groups of heads: D / 8 lanes per head, eight
-// values per lane, as two runs of four placed so that both members of every pair sit in one
+// Bound by memory (each value read and written once): 23,041 float32 tokens of 16 heads of 64 (189
+// MB) take 36.5 us, 5.2 TB/s, a large copy's rate; 665 tokens of 40 heads of 128 in bf16 (13.6 MB) take
+// 5.8 us, by the launch and two dependent loads.  One wave takes one token and up to kIters groups of
+// heads: D / 8 lanes per head, eight values per lane, as two runs of four placed so that both members of every pair sit in one
 // lane (HALF: 4c.. and R/2 + 4c.. for the first R / 8 lanes of a head, otherwise 8c..), so the
 // rotation needs no lane exchange.  A lane's place in its head is the same in every group, so it
 // reads the four (cos, sin) it needs once; the token's angles are computed once per wave, a pair
-// per lane, while the groups' loads are in flight, and shared through LDS.
+// per lane, while the groups' loads are in flight, and shared through LDS.  Stores are marked as not
+// reused soon (189 MB: 44 us without, 37 with).
 #include "common.h"
 #include "paged.h"
 #include "paged_rows.h"
@@ -23,7 +25,7 @@ namespace {
 
 constexpr int kRowWaves = 4;
 constexpr int kRowThreads = kRowWaves * kWave;
-constexpr int kIters = 4;                // groups of heads per wave, their loads in flight together
+constexpr int kWaveSlots = 8192;         // waves that the chip holds at once (32 on each CU)
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
@@ -52,9 +54,10 @@ __device__ inline uint32_t pack_bf16(float lo, float hi) {
 template <bool F32>
 __device__ inline void store_quad(uint8_t* row, int dim, floatx4 v) {
   if constexpr (F32)
-    *reinterpret_cast<floatx4*>(row + 4 * dim) = v;
+    __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(row + 4 * dim));
   else
-    *reinterpret_cast<u32x2*>(row + 2 * dim) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    __builtin_nontemporal_store(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])},
+                                reinterpret_cast<u32x2*>(row + 2 * dim));
 }
 
 // Sum over the 8 or 16 lanes of a head, the same in each of them.
@@ -71,7 +74,8 @@ __device__ inline float head_sum(float v) {
   return v;
 }
 
-template <int D, bool IN32, bool OUT32, bool HALF, bool PAGED>
+// kIters: groups of heads per wave, their loads in flight together.
+template <int D, bool IN32, bool OUT32, bool HALF, bool PAGED, int kIters>
 __global__ __launch_bounds__(kRowThreads) void norm_rope_kernel(const NormRopeArgs a,
                                                                 int waves_per_token) {
   constexpr int LPH = D / 8;             // lanes per head
@@ -93,17 +97,31 @@ __global__ __launch_bounds__(kRowThreads) void norm_rope_kernel(const NormRopeAr
   const int da = HALF && turn_lane ? 4 * c : 8 * c;
   const int db = HALF && turn_lane ? R / 2 + 4 * c : 8 * c + 4;
 
-  // this lane's head in each group: which tensor, which of its heads
+  // everything that depends on nothing else is asked for at once: the angle of this lane's pair, the
+  // weights, the heads' values (the position and the page follow)
+  const double turn = a.turns[lane];
+  u32x4 wqa{}, wqb{}, wka{}, wkb{};
+  if (a.q.weight != nullptr) {
+    wqa = load_quad<IN32>(static_cast<const uint8_t*>(a.q.weight), da);
+    wqb = load_quad<IN32>(static_cast<const uint8_t*>(a.q.weight), db);
+  }
+  if (a.k.weight != nullptr) {
+    wka = load_quad<IN32>(static_cast<const uint8_t*>(a.k.weight), da);
+    wkb = load_quad<IN32>(static_cast<const uint8_t*>(a.k.weight), db);
+  }
+  // this lane's head in each group: which tensor, which of its heads.  (The sides' fields are
+  // chosen value by value: choosing among the structs would make them loads of every lane.)
   const int hq = a.q.heads, hqk = hq + a.k.heads, hall = hqk + a.v.heads;
+  const uint8_t* in_q = static_cast<const uint8_t*>(a.q.in) + t * a.q.in_stride * IB;
+  const uint8_t* in_k = static_cast<const uint8_t*>(a.k.in) + t * a.k.in_stride * IB;
+  const uint8_t* in_v = static_cast<const uint8_t*>(a.v.in) + t * a.v.in_stride * IB;
   u32x4 xa[kIters], xb[kIters];
 #pragma unroll
   for (int i = 0; i < kIters; ++i) {
     const int hd = (g0 + i) * HPW + hl;
     if (hd < hall) {
-      const HeadSide& s = hd < hq ? a.q : hd < hqk ? a.k : a.v;
-      const int h = hd - (hd < hq ? 0 : hd < hqk ? hq : hqk);
-      const uint8_t* row = static_cast<const uint8_t*>(s.in) +
-                           (static_cast<int64_t>(t) * s.in_stride + h * D) * IB;
+      const uint8_t* in = hd < hq ? in_q : hd < hqk ? in_k : in_v;
+      const uint8_t* row = in + (hd - (hd < hq ? 0 : hd < hqk ? hq : hqk)) * (D * IB);
       xa[i] = load_quad<IN32>(row, da);
       xb[i] = load_quad<IN32>(row, db);
     }
@@ -131,7 +149,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_rope_kernel(const NormRopeAr
   floatx4 ca = {1.f, 1.f, 1.f, 1.f}, sa = {0.f, 0.f, 0.f, 0.f};   // pairs 4c .. 4c + 3
   if (R > 0) {
     if (lane < R / 2) {
-      const double rev = static_cast<double>(p) * a.turns[lane];
+      const double rev = static_cast<double>(p) * turn;
       float sn, cn;
       sincospif(2.f * static_cast<float>(rev - rint(rev)), &sn, &cn);
       cs[wave][lane] = make_float2(cn * a.magnitude, sn * a.magnitude);
@@ -147,82 +165,94 @@ __global__ __launch_bounds__(kRowThreads) void norm_rope_kernel(const NormRopeAr
     }
   }
 
+  // where the token's rows go
+  uint8_t* out_q = static_cast<uint8_t*>(a.q.out) + t * a.q.out_stride * OB;
+  uint8_t* out_k = static_cast<uint8_t*>(a.k.out) +
+                   (PAGED ? slot * a.k.heads * D : t * a.k.out_stride) * OB;
+  uint8_t* out_v = static_cast<uint8_t*>(a.v.out) + (PAGED ? slot * a.v.heads * D : 0) * OB;
+  const bool norm_q = a.q.weight != nullptr, norm_k = a.k.weight != nullptr;
 #pragma unroll
   for (int i = 0; i < kIters; ++i) {
     const int hd = (g0 + i) * HPW + hl;
-    const bool on = hd < hall;
-    const HeadSide& s = hd < hq ? a.q : hd < hqk ? a.k : a.v;
-    const int h = hd - (hd < hq ? 0 : hd < hqk ? hq : hqk);
+    const bool on = hd < hall, is_q = hd < hq, is_v = hd >= hqk;
     floatx4 x = unpack_quad<IN32>(on ? xa[i] : u32x4{0, 0, 0, 0});
     floatx4 y = unpack_quad<IN32>(on ? xb[i] : u32x4{0, 0, 0, 0});
-    float ss = 0.f;
+    const bool norm = is_q ? norm_q : !is_v && norm_k;
+    if (norm_q || norm_k) {
+      float ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
-    ss = head_sum<LPH>(ss);              // every lane takes part
-    if (!on) continue;
-    if (s.weight != nullptr) {
-      const uint8_t* wr = static_cast<const uint8_t*>(s.weight);
-      const floatx4 wa = unpack_quad<IN32>(load_quad<IN32>(wr, da));
-      const floatx4 wb = unpack_quad<IN32>(load_quad<IN32>(wr, db));
-      const float inv = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-      x *= inv * wa;
-      y *= inv * wb;
+      for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
+      ss = head_sum<LPH>(ss);              // every lane takes part
+      const float inv = rsqrtf(ss * (1.f / D) + a.eps);
+      const floatx4 wa = unpack_quad<IN32>(is_q ? wqa : wka);
+      const floatx4 wb = unpack_quad<IN32>(is_q ? wqb : wkb);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = norm ? x[e] * (inv * wa[e]) : x[e];
+        y[e] = norm ? y[e] * (inv * wb[e]) : y[e];
+      }
     }
-    if (s.rotate && R > 0) {
+    const bool turned = R > 0 && !is_v;
+    if (R > 0) {
       if constexpr (HALF) {
-        if (turn_lane) {
-          const floatx4 u = x;
+        const bool here = turned && turn_lane;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[e] = fmaf(u[e], ca[e], -y[e] * sa[e]);
-            y[e] = fmaf(u[e], sa[e], y[e] * ca[e]);
-          }
+        for (int e = 0; e < 4; ++e) {
+          const float u = x[e], v = y[e];
+          x[e] = here ? fmaf(u, ca[e], -v * sa[e]) : u;
+          y[e] = here ? fmaf(u, sa[e], v * ca[e]) : v;
         }
       } else {
-        auto turn = [&](float& u, float& v, int e) {
-          if (8 * c + 2 * e < R) {
-            const float u0 = u;
-            u = fmaf(u0, ca[e], -v * sa[e]);
-            v = fmaf(u0, sa[e], v * ca[e]);
-          }
-        };
         float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) turn(f[2 * e], f[2 * e + 1], e);
+        for (int e = 0; e < 4; ++e) {
+          const bool here = turned && 8 * c + 2 * e < R;
+          const float u = f[2 * e], v = f[2 * e + 1];
+          f[2 * e] = here ? fmaf(u, ca[e], -v * sa[e]) : u;
+          f[2 * e + 1] = here ? fmaf(u, sa[e], v * ca[e]) : v;
+        }
         x = floatx4{f[0], f[1], f[2], f[3]};
         y = floatx4{f[4], f[5], f[6], f[7]};
       }
     }
-    const int64_t at = s.to_pool ? (slot * s.heads + h) * D
-                                 : static_cast<int64_t>(t) * s.out_stride + h * D;
-    uint8_t* row = static_cast<uint8_t*>(s.out) + at * OB;
-    if constexpr (!IN32 && !OUT32) {
-      if (s.weight == nullptr && !(s.rotate && R > 0)) {   // a plain copy keeps every bit
+    if (on) {
+      uint8_t* row = (is_q ? out_q : is_v ? out_v : out_k) +
+                     (hd - (is_q ? 0 : is_v ? hqk : hq)) * (D * OB);
+      if (!IN32 && !OUT32 && !norm && !turned) {           // a plain copy keeps every bit
         *reinterpret_cast<u32x2*>(row + 2 * da) = u32x2{xa[i][0], xa[i][1]};
         *reinterpret_cast<u32x2*>(row + 2 * db) = u32x2{xb[i][0], xb[i][1]};
-        continue;
+      } else {
+        store_quad<OUT32>(row, da, x);
+        store_quad<OUT32>(row, db, y);
       }
     }
-    store_quad<OUT32>(row, da, x);
-    store_quad<OUT32>(row, db, y);
   }
+}
+
+template <int D, bool IN32, bool OUT32, bool PAGED, int kIters>
+hipError_t launch_i(const NormRopeArgs& a, int groups, hipStream_t stream) {
+  const int wpt = (groups + kIters - 1) / kIters;
+  const int64_t waves = static_cast<int64_t>(a.n_tokens) * wpt;
+  const dim3 grid(static_cast<unsigned>((waves + kRowWaves - 1) / kRowWaves));
+  if (a.rope_half && a.rope_dims > 0)
+    hipLaunchKernelGGL((norm_rope_kernel<D, IN32, OUT32, true, PAGED, kIters>), grid,
+                       dim3(kRowThreads), 0, stream, a, wpt);
+  else
+    hipLaunchKernelGGL((norm_rope_kernel<D, IN32, OUT32, false, PAGED, kIters>), grid,
+                       dim3(kRowThreads), 0, stream, a, wpt);
+  return hipGetLastError();
 }
 
 template <int D, bool IN32, bool OUT32, bool PAGED>
 hipError_t launch_t(const NormRopeArgs& a, hipStream_t stream) {
   constexpr int HPW = kWave / (D / 8);
-  const int heads = a.q.heads + a.k.heads + a.v.heads;
-  const int groups = (heads + HPW - 1) / HPW;
-  const int wpt = (groups + kIters - 1) / kIters;
-  const int64_t waves = static_cast<int64_t>(a.n_tokens) * wpt;
-  const dim3 grid(static_cast<unsigned>((waves + kRowWaves - 1) / kRowWaves));
-  if (a.rope_half && a.rope_dims > 0)
-    hipLaunchKernelGGL((norm_rope_kernel<D, IN32, OUT32, true, PAGED>), grid, dim3(kRowThreads), 0,
-                       stream, a, wpt);
-  else
-    hipLaunchKernelGGL((norm_rope_kernel<D, IN32, OUT32, false, PAGED>), grid, dim3(kRowThreads),
-                       0, stream, a, wpt);
-  return hipGetLastError();
+  const int groups = (a.q.heads + a.k.heads + a.v.heads + HPW - 1) / HPW;
+  // One group per wave while every group finds a wave slot of the chip at once, four beyond: 24
+  // single tokens of 48 heads take 3.7 us with one and 4.9 with four, 665 tokens of 40 heads 5.8 and
+  // 6.3; 5,998 tokens of 16 heads 15.0 and 11.7, 32,343 float32 tokens of 24 heads 129 and 109.
+  if (static_cast<int64_t>(a.n_tokens) * groups <= kWaveSlots)
+    return launch_i<D, IN32, OUT32, PAGED, 1>(a, groups, stream);
+  return launch_i<D, IN32, OUT32, PAGED, 4>(a, groups, stream);
 }
 
 template <int D>

@@ -14,6 +14,8 @@
 //             buffers, one block's keys and values each, filled by direct loads (16 bytes a lane)
 //             kRing - 1 blocks ahead; no workgroup barrier until the waves merge.  A block lies in
 //             one page, so its address is scalar: page ids come 64 blocks at a time, one per lane.
+//             The loads are marked as read once (nt), which is 12% faster: 24 ragged streams,
+//             638 MB, 132 -> 118 us.
 //   products  S^T (16 keys x 16 columns) = K Q^T with v_mfma_f32_16x16x32_bf16; its output layout
 //             is the P^T operand of O^T (16 dims x 16 columns) += V^T P^T with
 //             v_mfma_f32_16x16x16_bf16, V^T by transposing LDS reads.  Each probability enters as
@@ -214,12 +216,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
 #pragma unroll
       for (int cq = 0; cq < CALLS; ++cq) {
         const uint32_t back = last < kKB - 1 ? max(prow[cq] - last, 0) * row_bytes : 0u;
-        dma16(kb, koff[cq] - back, dst + static_cast<uint32_t>(cq * kWave * 16));
+        dma16_once(kb, koff[cq] - back, dst + static_cast<uint32_t>(cq * kWave * 16));
       }
 #pragma unroll
       for (int cq = 0; cq < CALLS; ++cq) {
         const uint32_t back = last < kKB - 1 ? max(prow[cq] - last, 0) * row_bytes : 0u;
-        dma16(vb, voff[cq] - back,
+        dma16_once(vb, voff[cq] - back,
               dst + static_cast<uint32_t>(S::kBlock * 2 + cq * kWave * 16));
       }
     };

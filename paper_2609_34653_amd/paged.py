@@ -18,7 +18,7 @@ import torch
 
 from . import omnitide as ot
 from .omnitide import (BF16, F32, ROPE_HALF, ROPE_INTERLEAVED, OmnitideError,  # noqa: F401
-                       _buf, _check, _dev, _kv_dtype, _need, _out, _status, _stream)
+                       _buf, _check, _dev, _kv_dtype, _out, _status, _stream)
 
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP = 0, 1, 2, 3
 E_PAGES = -19
@@ -29,7 +29,7 @@ EXPORTS = ("omnitide_rope_thetas", "omnitide_qk_norm_rope", "omnitide_paged_appe
 
 _P, _I, _SZ, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_int64
 _D, _F = ctypes.c_double, ctypes.c_float
-_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_T, _BF16, _F32, _I32 = torch.Tensor, torch.bfloat16, torch.float32, torch.int32
 
 _lib = None
 
@@ -73,33 +73,43 @@ def _on(t, stream):
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _rows(t, name: str, dtypes):
-    """(address, tokens, heads, d, row stride in elements) of [tokens, heads, d] with contiguous
-    heads."""
-    if not isinstance(t, torch.Tensor):
+# As in ``omnitide``, a tensor in order takes one short path; a call passes up to 15 tensors, and a step
+# of single tokens is bound by its calls' marshalling.
+
+def _rows(t, name: str, dtype):
+    """(address, tokens, heads, d, row stride in elements) of [tokens, heads, d] of dtype with
+    contiguous heads."""
+    if type(t) is _T and t.dtype is dtype and t.is_cuda and t.dim() == 3:
+        n, h, d = t.shape
+        s0, s1, s2 = t.stride()
+        if s2 == 1 and s1 == d:
+            return t.data_ptr(), n, h, d, s0 if n > 1 else h * d
+        if (d == 1 or s2 == 1) and (h == 1 or s1 == d):
+            return t.data_ptr(), n, h, d, s0 if n > 1 else h * d
+    if not isinstance(t, _T):
         raise TypeError(f"{name} must be a tensor")
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name}: dtype {t.dtype} not in {list(dtypes)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: dtype {t.dtype} is not {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens, heads, d]")
-    n, h, d = t.shape
-    s0, s1, s2 = t.stride()
-    if (d > 1 and s2 != 1) or (h > 1 and s1 != d):
-        raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return t.data_ptr(), n, h, d, s0 if n > 1 else h * d
+    raise ValueError(f"{name}: the heads of a token must be contiguous")
 
 
-def _weight(w, name: str, dtype, d: int):
-    return None if w is None else _dev(w, name, dtype, d)
+def _float_type(t, name: str):
+    if not isinstance(t, _T):
+        raise TypeError(f"{name} must be a tensor")
+    if t.dtype is not _BF16 and t.dtype is not _F32:
+        raise TypeError(f"{name}: dtype {t.dtype} is not bfloat16 or float32")
+    return t.dtype
 
 
 def _theta(theta):
     """(address, rope_dims) of the host frequencies: a contiguous float64 CPU tensor or None."""
     if theta is None:
         return None, 0
-    if not (isinstance(theta, torch.Tensor) and theta.dtype == torch.float64 and not theta.is_cuda
+    if not (isinstance(theta, _T) and theta.dtype is torch.float64 and not theta.is_cuda
             and theta.dim() == 1 and theta.is_contiguous()):
         raise TypeError("theta must be a contiguous float64 CPU tensor [rope_dims / 2]")
     return theta.data_ptr(), 2 * theta.numel()
@@ -107,17 +117,18 @@ def _theta(theta):
 
 def _pools(k_pool, v_pool):
     """(k address, v address, n_pages, page_size, H_kv, d)."""
-    if not (isinstance(k_pool, torch.Tensor) and k_pool.dim() == 4):
+    if not (isinstance(k_pool, _T) and k_pool.dim() == 4):
         raise ValueError("k_pool must be [n_pages, page_size, H_kv, d]")
-    if not isinstance(v_pool, torch.Tensor) or v_pool.shape != k_pool.shape:
+    shape = k_pool.shape
+    if not isinstance(v_pool, _T) or v_pool.shape != shape:
         raise ValueError("v_pool must have k_pool's shape")
     n = k_pool.numel()
-    return (_dev(k_pool, "k_pool", _BF16, n), _dev(v_pool, "v_pool", _BF16, n), *k_pool.shape)
+    return (_dev(k_pool, "k_pool", _BF16, n), _dev(v_pool, "v_pool", _BF16, n), *shape)
 
 
 def _table(page_table, ctx_len):
     """(table address, max_pages, ctx_len address, n_seq)."""
-    if not (isinstance(page_table, torch.Tensor) and page_table.dim() == 2):
+    if not (isinstance(page_table, _T) and page_table.dim() == 2):
         raise ValueError("page_table must be [n_seq, max_pages]")
     n_seq, max_pages = page_table.shape
     return (_dev(page_table, "page_table", _I32, n_seq * max_pages), max_pages,
@@ -142,57 +153,58 @@ def omnitide_qk_norm_rope(q, k, pos, q_out, k_out, theta=None, rope_style=ROPE_H
                           q_weight=None, k_weight=None, eps=1e-6, stream=None):
     """Per-head RMS norm (weights given) and rotation (theta given) of q and k into q_out and k_out
     (all [tokens, heads, d]; an output may be its input).  q or k may be None, with its output."""
-    first = q if q is not None else k
+    first, out = (q, q_out) if q is not None else (k, k_out)
     if first is None:
         raise ValueError("q or k must be given")
-    dt, out = first.dtype, (q_out if q is not None else k_out).dtype
+    dt, odt = _float_type(first, "q or k"), _float_type(out, "q_out or k_out")
     qi = qo = ki = ko = (None, 0, 0, 0, 0)
     if q is not None:
-        qi, qo = _rows(q, "q", (_BF16, _F32)), _rows(q_out, "q_out", (_BF16, _F32))
-        if q_out.shape != q.shape:
+        qi, qo = _rows(q, "q", dt), _rows(q_out, "q_out", odt)
+        if qi[1:4] != qo[1:4]:
             raise ValueError("q_out must have q's shape")
     if k is not None:
-        ki, ko = _rows(k, "k", (dt,)), _rows(k_out, "k_out", (out,))
-        if k_out.shape != k.shape:
+        ki, ko = _rows(k, "k", dt), _rows(k_out, "k_out", odt)
+        if ki[1:4] != ko[1:4]:
             raise ValueError("k_out must have k's shape")
-    _, n, _, d, _ = qi if q is not None else ki
-    if k is not None and (ki[1] != n or ki[3] != d):
-        raise ValueError("k does not match q")
+        if q is not None and (ki[1] != qi[1] or ki[3] != qi[3]):
+            raise ValueError("k does not match q")
+    n, d = (qi if q is not None else ki)[1:4:2]
     th, dims = _theta(theta)
-    _check(lib().omnitide_qk_norm_rope(
-        qi[0], ki[0], _kv_dtype(first), n, qi[2], ki[2], d, qi[4], ki[4],
-        None if pos is None else _dev(pos, "pos", _I32, n), _weight(q_weight, "q_weight", dt, d),
-        _weight(k_weight, "k_weight", dt, d), float(eps), th, dims, int(rope_style),
-        float(magnitude), qo[0], ko[0], qo[4], ko[4], BF16 if out == _BF16 else F32,
-        _on(first, stream)), "omnitide_qk_norm_rope")
+    _check((_lib or lib()).omnitide_qk_norm_rope(
+        qi[0], ki[0], BF16 if dt is _BF16 else F32, n, qi[2], ki[2], d, qi[4], ki[4],
+        None if pos is None else _dev(pos, "pos", _I32, n),
+        None if q_weight is None else _dev(q_weight, "q_weight", dt, d),
+        None if k_weight is None else _dev(k_weight, "k_weight", dt, d), eps, th, dims, rope_style,
+        magnitude, qo[0], ko[0], qo[4], ko[4], BF16 if odt is _BF16 else F32, _on(first, stream)),
+        "omnitide_qk_norm_rope")
 
 
 def omnitide_paged_append(k, v, k_pool, v_pool, page_table, q_start, ctx_len, pos=None, theta=None,
                           rope_style=ROPE_HALF, magnitude=1.0, k_weight=None, eps=1e-6, q=None,
                           q_out=None, q_weight=None, d_status=None, stream=None):
     """The new tokens' k (normed, rotated) and v into the pages; q into q_out (bf16) if given."""
-    dt = k.dtype
-    ki, vi = _rows(k, "k", (_BF16, _F32)), _rows(v, "v", (dt,))
-    if v.shape != k.shape:
+    dt = _float_type(k, "k")
+    ki, vi = _rows(k, "k", dt), _rows(v, "v", dt)
+    n, hkv, d = ki[1:4]
+    if vi[1:4] != (n, hkv, d):
         raise ValueError("v must have k's shape")
-    n, d = ki[1], ki[3]
     qi = qo = (None, 0, 0, 0, 0)
     if q is not None or q_out is not None:
-        qi, qo = _rows(q, "q", (dt,)), _rows(q_out, "q_out", (_BF16,))
-        if qi[1] != n or qi[3] != d or q_out.shape != q.shape:
+        qi, qo = _rows(q, "q", dt), _rows(q_out, "q_out", _BF16)
+        if qi[1] != n or qi[3] != d or qi[1:4] != qo[1:4]:
             raise ValueError("q, q_out and k do not match")
-    kp, vp, n_pages, page, hkv, dp = _pools(k_pool, v_pool)
-    if hkv != ki[2] or dp != d:
+    kp, vp, n_pages, page, hp, dp = _pools(k_pool, v_pool)
+    if hp != hkv or dp != d:
         raise ValueError("the pools do not match k")
     tab, max_pages, ctx, n_seq = _table(page_table, ctx_len)
     th, dims = _theta(theta)
-    _check(lib().omnitide_paged_append(
-        ki[0], vi[0], qi[0], _kv_dtype(k), n, qi[2], hkv, d, ki[4], vi[4], qi[4], kp, vp, n_pages,
-        page, tab, max_pages, _dev(q_start, "q_start", _I32, n_seq + 1), ctx, n_seq,
-        None if pos is None else _dev(pos, "pos", _I32, n), _weight(k_weight, "k_weight", dt, d),
-        _weight(q_weight, "q_weight", dt, d), float(eps), th, dims, int(rope_style),
-        float(magnitude), qo[0], qo[4], _status(d_status), _on(k, stream)),
-        "omnitide_paged_append")
+    _check((_lib or lib()).omnitide_paged_append(
+        ki[0], vi[0], qi[0], BF16 if dt is _BF16 else F32, n, qi[2], hkv, d, ki[4], vi[4], qi[4], kp,
+        vp, n_pages, page, tab, max_pages, _dev(q_start, "q_start", _I32, n_seq + 1), ctx, n_seq,
+        None if pos is None else _dev(pos, "pos", _I32, n),
+        None if k_weight is None else _dev(k_weight, "k_weight", dt, d),
+        None if q_weight is None else _dev(q_weight, "q_weight", dt, d), eps, th, dims, rope_style,
+        magnitude, qo[0], qo[4], _status(d_status), _on(k, stream)), "omnitide_paged_append")
 
 
 def omnitide_paged_chunk_attn_workspace_bytes(n_tokens, n_seq, max_ctx, n_q_heads, n_kv_heads,
@@ -216,9 +228,9 @@ def omnitide_paged_chunk_attn(q, k_pool, v_pool, page_table, q_start, ctx_len, s
         raise ValueError("the pools do not match q")
     tab, max_pages, ctx, n_seq = _table(page_table, ctx_len)
     args = (_dev(q, "q", _BF16, q.numel()), kp, vp, n_pages, page, tab, max_pages,
-            _dev(q_start, "q_start", _I32, n_seq + 1), ctx, n_seq, n, hq, hkv, d, float(scale),
+            _dev(q_start, "q_start", _I32, n_seq + 1), ctx, n_seq, n, hq, hkv, d, scale,
             _out(out, q.numel()), _kv_dtype(out), *_ws(workspace), _status(d_status))
-    _check(lib().omnitide_paged_chunk_attn(*args, _on(q, stream)), "omnitide_paged_chunk_attn")
+    _check((_lib or lib()).omnitide_paged_chunk_attn(*args, _on(q, stream)), "omnitide_paged_chunk_attn")
 
 
 def omnitide_paged_decode_workspace_bytes(n_seq, n_q, max_ctx, n_q_heads, n_kv_heads,
@@ -239,6 +251,6 @@ def omnitide_paged_decode_attn(q, k_pool, v_pool, page_table, ctx_len, scale, ou
     if dp != d or ns != n_seq:
         raise ValueError("the pools or the table do not match q")
     args = (_dev(q, "q", _BF16, q.numel()), kp, vp, n_pages, page, tab, max_pages, ctx, n_seq, nq,
-            hq, hkv, d, float(scale), _out(out, q.numel()), _kv_dtype(out), *_ws(workspace),
+            hq, hkv, d, scale, _out(out, q.numel()), _kv_dtype(out), *_ws(workspace),
             _status(d_status))
-    _check(lib().omnitide_paged_decode_attn(*args, _on(q, stream)), "omnitide_paged_decode_attn")
+    _check((_lib or lib()).omnitide_paged_decode_attn(*args, _on(q, stream)), "omnitide_paged_decode_attn")
