@@ -44,7 +44,7 @@ constexpr int kWGs = 256;                // shares of a large call: one workgrou
 constexpr int kRing = 4;                 // tiles of each tensor in LDS
 constexpr int kNumXcd = 8;
 constexpr int kOverhead = 2 * kKT;       // what a row tile costs beside its keys, in keys
-constexpr int kMinShareTiles = 4;        // tiles of a share at least
+constexpr int kMinShareTiles = 2;        // tiles of a share at least
 constexpr int kSnap = 2;                 // a cut this near to a row tile's end goes to the end
 
 // Where a share begins: row tile mt of (KV head g, sequence seq), key tile `tile` of it.
@@ -78,6 +78,7 @@ struct PlanMem {
   int32_t chunk_tiles[SEQS / kWave];
   int64_t wave_max[kWaves], wave_sum[kWaves];
   int32_t wave_min[kWaves];
+  float wave_most[kWaves];
   int64_t begin[kWGs + 1];               // work in front of each share (rounds > 0)
 };
 
@@ -88,6 +89,14 @@ __device__ inline int64_t uniform(int64_t x) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u));
   const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
   return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
+// x / y for 0 <= x, 0 < y: by a double quotient, which is off by one at most (x / y < 2^52).
+__device__ inline int64_t div64(int64_t x, int64_t y) {
+  int64_t q = static_cast<int64_t>(static_cast<double>(x) / static_cast<double>(y));
+  if (q * y > x) --q;
+  if ((q + 1) * y <= x) ++q;
+  return q;
 }
 
 // Row tiles in order of (KV head, sequence, number).  Workgroups first take whole ones in rounds,
@@ -125,7 +134,7 @@ struct Plan {
     n_seq = b.n_seq;
     mem = &m;
     const int n_chunks = (n_seq + kWave - 1) / kWave;
-    int64_t most = 0;                      // work of the largest row tile, key tiles of the shortest
+    float most = 0.f;                      // work of the largest row tile, key tiles of the shortest
     int fewest = INT32_MAX;
     for (int c = wave; c < n_chunks; c += kWaves) {
       const int i = c * kWave + lane;
@@ -139,10 +148,10 @@ struct Plan {
       const int len = ok ? s1 - s0 : 0;
       const int rt = row_tiles(len, G);
       const int64_t w = work(rt, n - len);
-      const int64_t inc = wave_inclusive_scan(ok ? w : 0);
+      const int64_t inc = static_cast<int64_t>(wave_scan_add_u64(ok ? w : 0));
       const int tiles = wave_scan_add_i32(rt);
       if (ok) {
-        most = max(most, w - work(rt - 1, n - len));
+        most = fmaxf(most, static_cast<float>(w - work(rt - 1, n - len)));
         fewest = min(fewest, tiles_of(0, len, n));
       }
       m.seq[i] = make_int4(s0, len, n, tiles - rt);
@@ -152,12 +161,11 @@ struct Plan {
         m.chunk_tiles[c] = tiles;
       }
     }
-    for (int off = 1; off < kWave; off <<= 1) {
-      most = max(most, static_cast<int64_t>(__shfl_xor(static_cast<long long>(most), off, kWave)));
-      fewest = min(fewest, __shfl_xor(fewest, off, kWave));
-    }
+    // (floats of one sign order as their bits)
+    most = __int_as_float(wave_max_i32(__float_as_int(most)));
+    fewest = -wave_max_i32(-fewest);
     if (lane == 0) {
-      m.wave_max[wave] = most;
+      m.wave_most[wave] = most;
       m.wave_min[wave] = fewest;
     }
     __syncthreads();
@@ -172,7 +180,7 @@ struct Plan {
       sum_tiles += m.chunk_tiles[c];
     }
     for (int w = 0; w < kWaves; ++w) {
-      most = max(most, m.wave_max[w]);
+      most = fmaxf(most, m.wave_most[w]);
       fewest = min(fewest, m.wave_min[w]);
     }
     __syncthreads();
@@ -207,7 +215,7 @@ struct Plan {
       }
       if (50 * top > 51 * level) continue; // too uneven: a round less
       const int64_t room = in ? level - mine : 0;
-      const int64_t inc = wave_inclusive_scan(room);
+      const int64_t inc = static_cast<int64_t>(wave_scan_add_u64(static_cast<uint64_t>(room)));
       if (lane == kWave - 1) m.wave_sum[wave] = inc;
       __syncthreads();
       int64_t before = 0;
@@ -219,8 +227,7 @@ struct Plan {
     left = n_tiles;
     rest = 0;
     // alike: the largest row tile has at most 1.25 times the mean work
-    const bool alike = 4 * static_cast<double>(uniform(most)) * n_tiles <=
-                       5 * static_cast<double>(total);
+    const bool alike = 4.f * most * static_cast<float>(n_tiles) <= 5.f * static_cast<float>(total);
     if (alike && left <= kWGs) {
       const int parts_most = max(1, uniform(fewest) / kMinShareTiles);
       const int parts = min(kWGs / left, parts_most);
@@ -307,7 +314,7 @@ struct Plan {
   __device__ Cut at(int64_t x) const {
     if (x >= total) return {Hkv, 0, 0, 0};
     const int lane = threadIdx.x & (kWave - 1);
-    const int g = static_cast<int>(x / per_head);
+    const int g = uniform(static_cast<int>(div64(x, per_head)));
     const int64_t y = x - g * per_head;
     int c = 0;
     while ((c + 1) * kWave < n_seq && uniform(mem->chunk[c + 1]) <= y) ++c;
@@ -365,7 +372,7 @@ struct Plan {
         else hi = mid;
       }
     } else {
-      w0 = static_cast<int>(x0 / share);
+      w0 = uniform(static_cast<int>(div64(x0, share)));
     }
     c.tile = 0;
     Cut b = share_begin(w0);
