@@ -603,7 +603,9 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     }
     if (t_begin + 2 < t_end) issue_k(t_begin + 2);
     keep();                                // at_v: of tile t+2 at tile t
-    wait_vmcnt<0>();
+    // the first keys have landed; the others may be in flight (the ring's first turn waits for them)
+    if (t_begin + 2 < t_end) wait_vmcnt<4 * T::kCalls>();
+    else wait_vmcnt<0>();
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
@@ -728,9 +730,9 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       ka[i] = kop(lds + 32 * D, i);
-      va[i] = vop(v_ring, i);                            // (finite, for the first step's zeros)
+      va[i] = vop(lds, i);                 // (the first step's zeros meet the first keys: numbers)
     }
-    const uint16_t* v_prev = v_ring;
+    const uint16_t* v_prev = lds;
     if (m0 + wave * 32 >= L * G) {         // a wave without rows: its share of the copies
       for (int t = t_begin; t < t_end; ++t) turn_over(t);
       if (!after_part()) break;
