@@ -4,12 +4,13 @@
 // pass over the keys with a running reference and sum per vector.
 //
 // Bound by memory: every key and value row in use is read once.  What follows from that:
-//   shares    the 16-key blocks of all (KV head, sequence) pairs, one after the other, are cut into
-//             equal shares, one per workgroup, whatever the sequences' lengths: a long context is
-//             spread over many workgroups, short ones share one.  A share's whole sequences
-//             are finished there; the parts of a sequence that lies in several shares are merged by a
-//             second kernel, in share order.  Every wave works the shares out by itself from ctx_len
-//             (a sequence per lane, one scan), so there is no plan launch.
+//   shares    the 16-key blocks of all sequences, one after the other, are cut into equal shares, one
+//             per workgroup and KV head, whatever the sequences' lengths: a long context is
+//             spread over many workgroups, short ones share one.  The same share of all KV heads
+//             belongs to workgroups next to each other, which read the same rows together.  A
+//             share's whole sequences are finished there; the parts of a sequence that lies in several
+//             shares are merged by a second kernel, in share order.  Every wave works the shares
+//             out by itself from ctx_len (a sequence per lane, one scan): no plan launch.
 //   waves     each wave takes every fourth block of its workgroup's part and owns a ring of LDS
 //             buffers, one block's keys and values each, filled by direct loads (16 bytes a lane)
 //             kRing - 1 blocks ahead; no workgroup barrier until the waves merge.  A block lies in
@@ -45,11 +46,12 @@ __device__ inline void wait_vmcnt() {
 }
 
 // The shares of a call: sequence i = 64 n + lane holds nb[n] blocks, first[n] of its KV head's
-// blocks before it; per_head blocks per KV head; `share` blocks per workgroup.
+// blocks before it; per_head blocks per KV head; `share` blocks per workgroup.  Workgroup w takes
+// share w / H_kv of KV head w % H_kv.
 template <int NS>
 struct Shares {
   int nb[NS], first[NS], ctx[NS];
-  int per_head, total, share;
+  int per_head, share;
 };
 
 template <int NS>
@@ -70,8 +72,8 @@ __device__ inline Shares<NS> plan_shares(const PagedBatch& b, int n_kv_heads) {
     s.first[n] = s.per_head + inc - s.nb[n];
     s.per_head += readlane(inc, kWave - 1);
   }
-  s.total = s.per_head * n_kv_heads;
-  s.share = max(kMinShare, (s.total + kWGs - 1) / kWGs);
+  const int per = kWGs / n_kv_heads;
+  s.share = max(kMinShare, (s.per_head + per - 1) / per);
   return s;
 }
 
@@ -128,10 +130,10 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
       }
     }
   }
-  const int lo = static_cast<int>(min(static_cast<int64_t>(blockIdx.x) * sh.share,
-                                      static_cast<int64_t>(sh.total)));
-  const int hi = min(lo + sh.share, sh.total);
-  if (lo >= hi) return;
+  const int g = blockIdx.x % Hkv;
+  const int64_t lo64 = static_cast<int64_t>(blockIdx.x / Hkv) * sh.share;
+  if (lo64 >= sh.per_head) return;
+  const int lo = static_cast<int>(lo64), hi = min(lo + sh.share, sh.per_head);
 
   const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
   // A lane's piece cq of a block: LDS chunk cq * 64 + lane holds key (that) / CHK and, of its row,
@@ -155,16 +157,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
   const int vread = vrow * D + 4 * (c16 & 3);
 
   for (int pos = lo; pos < hi;) {
-    // the part of one (KV head, sequence) that starts at block pos
-    const int g = pos / sh.per_head, r = pos - g * sh.per_head;
+    // the part of one sequence that starts at block pos
     int seq = 0, b0 = 0, nb = 1, ctx = 1;
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      const uint64_t hit = __ballot(r >= sh.first[n] && r < sh.first[n] + sh.nb[n]);
+      const uint64_t hit = __ballot(pos >= sh.first[n] && pos < sh.first[n] + sh.nb[n]);
       if (hit != 0) {
         const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
         seq = n * kWave + l;
-        b0 = r - readlane(sh.first[n], l);
+        b0 = pos - readlane(sh.first[n], l);
         nb = readlane(sh.nb[n], l);
         ctx = readlane(sh.ctx[n], l);
       }
@@ -385,13 +386,12 @@ __global__ __launch_bounds__(kThreads) void paged_decode_merge_kernel(
     }
   }
   if (nb == 0) return;
-  first += g * sh.per_head;
   const int w0 = first / sh.share, w1 = (first + nb - 1) / sh.share;
   if (w0 == w1) return;                      // finished by its workgroup
   const int col = tok * G + head % G, nqg = nq * G;
   const int tid = threadIdx.x, ts = tid / TPR, d4 = tid % TPR;
-  // part p: workgroup w0 + p, whose first part it is unless it is that workgroup's later one
-  const int slot0 = 2 * w0 + (first == w0 * sh.share ? 0 : 1);
+  // part p: of share w0 + p, its first one except where the row begins inside the share
+  const int later0 = first == w0 * sh.share ? 0 : 1;
   const int n_parts = w1 - w0 + 1;
   float M = -INFINITY, den = 0.f;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void paged_decode_merge_kernel(
     for (int c = 0; c < PER; ++c) {
       const int p = p0 + TS * c;
       const bool in = p < n_parts;
-      const size_t r = static_cast<size_t>(p == 0 ? slot0 : 2 * (w0 + p)) * nqg + col;
+      const size_t r = static_cast<size_t>(2 * ((w0 + p) * Hkv + g) + (p == 0 ? later0 : 0)) * nqg + col;
       ml[c] = in ? part_ml[r] : make_float2(-INFINITY, 0.f);
       ov[c] = in ? *reinterpret_cast<const float4*>(part_o + r * D + 4 * d4)
                  : make_float4(0.f, 0.f, 0.f, 0.f);
