@@ -1,29 +1,43 @@
 // Chunk attention over the pages: a ragged batch of chunks, causal, grouped queries.
 //
 // Mathematics: softmax(scale q K^T) V per (token, query head) over the token's sequence up to its own
-// row, one pass over 64-key tiles with a running reference and sum per row.
+// row, one pass over the keys with a running reference and sum per row.
+//
+// What bounds it: the matrix cores.  4 d operations per query row and visible key, and at the clock
+// that the card holds under them the two products of random data reach about 1.1 PFLOP/s when nothing is
+// loaded at all (1.2 for a large matrix product; smooth data, which take less power, run a
+// sixth faster).  Bytes are few once the rows of a workgroup share each key.
 //
 //   rows      the L * G query rows (position p, head g*G + r) of a sequence and KV head are flattened
-//             as m = p*G + r and tiled kRows = 4 waves x 64 per row tile; a wave's 64 rows are two
-//             32-column blocks of the products, so one K or V operand read from LDS feeds two of
-//             them.  (With 32 rows a wave the LDS reads of a tile take as long as its products.)
-//   shares    the key tiles of all (KV head, sequence, row tile), one after the other, are cut into equal
-//             shares, one per workgroup and CU, whatever the lengths: long contexts are spread over
-//             many workgroups, short ones share one.  A share's whole row tiles are finished there; the
-//             parts of a row tile that lies in several are merged by a second kernel, in share
-//             order.  Every wave works the cuts out by itself from q_start and ctx_len (a sequence per
-//             lane), so there is no plan launch.  The work of a row tile is counted in keys, linear in its
-//             number, so a cut is found by a square root.
+//             as m = p*G + r and tiled kRows = 8 waves x 32 per row tile: one workgroup per CU, two
+//             waves per SIMD, so that one issues vector work while the other's products run.  (Four
+//             waves of 64 rows have no registers left to read ahead with; two workgroups of 4 x 32
+//             rows read every key twice and are a tenth slower on long calls.)
+//   shares    whole row tiles in rounds of kWGs, so that the workgroups of an XCD read the same keys at
+//             about the same time (L2 misses of 4 x 2,660 rows over 33,500 keys: 36 M to 8 M); the
+//             rest is cut, whatever the lengths, into a share per workgroup that evens the rounds
+//             out.  The parts of a row tile that lies in several are merged by a second kernel, in share
+//             order, so results do not depend on timing.  Every workgroup works the cuts out by
+//             itself from q_start and ctx_len, so there is no plan launch.  The work of a row tile
+//             is counted in keys, linear in its number, so a cut is found by a square root.
 //   products  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: one query column per lane,
 //             so the row statistics are lane-local; keys are permuted when K rows are read so that S^T
 //             is the B operand of the second product as it stands.
 //   pages     a wave's direct load takes 4 (d = 128) or 8 (d = 64) consecutive keys, which lie in
-//             one page, so its address is scalar; page ids come 64 groups of 16 keys at a time, one
-//             per lane.  Rows past the context are clamped to its last one and masked.
-//   softmax   fp32, base 2; exponentials against a reference that moves only when a tile sum would leave
-//             a bounded range; row sums over the rounded bf16 probabilities.
-//   loop      unrolled by two (static LDS addresses); the score products of the next tile are
-//             interleaved with this tile's exponentials.
+//             one page, so its address is scalar; page ids come 64 at a time, one per lane.  Rows
+//             past the context are clamped to its last one and masked.
+//   softmax   fp32, base 2; exponentials against a reference that moves only when the sum over 32 keys
+//             would leave a bounded range; probabilities are rounded to bf16, the operand type of the
+//             second product, and the row sums are those of the rounded ones.
+//   loop      steps of 32 keys: the softmax of this step's scores between the score products of the
+//             next one and the value products of the one before.  K and V tiles of 64 keys in rings
+//             of four, asked for two (V) and three (K) tiles ahead; the ring is turned half-way
+//             through a tile's first step, by one barrier per tile.
+//
+// Measured (bf16, d = 128, 4 query heads per KV head, 8 KV heads, pages of 64, cache larger than L2):
+//   4 chunks of 665 tokens over 33,500 keys       1,351 us, 1.06 PFLOP/s
+//   one chunk of 665 tokens over 17,290 keys        206 us, 0.88 PFLOP/s (11 us of it the merge)
+//   89 tokens over 89 keys                           17 us
 #include <algorithm>
 #include <type_traits>
 
@@ -65,7 +79,6 @@ __device__ inline bool before(const Cut& a, const Cut& b) {
 struct Joined {
   int32_t n_parts, first_slot, last_share, q0, rows, mt, g, pad;
 };
-
 
 // What the shares are made from, in LDS: every sequence's first token, tokens (0: none, or malformed),
 // context and the row tiles in front of it in its chunk of 64 sequences; the work (keys times G) in
@@ -443,11 +456,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     voff[cq] = prow[cq] * row_bytes + 16u * (2 * ((pc >> 1) ^ vswz<D>(key)) + (pc & 1));
   }
   const uint32_t lds_wave = lds_addr(lds) + static_cast<uint32_t>(wave * kWave * 16);
+  // this lane's place in the operands of 32 keys: K rows in the permuted order, V by transposing reads
+  const uint32_t lds0 = lds_addr(lds);
   const int krow = perm_key(col);
-  const int fk = kswz(krow) & (T::kChunks - 1);
+  const uint32_t k_lane = 2u * D * krow + 16u * (h ^ (kswz(krow) & (T::kChunks - 1)));
   const int gi = lane & 15, gq = (lane >> 4) & 1;
-  const int vsl = vswz<D>(gi >> 2);
-  const int v_lane_off = (gi >> 2) * D + 8 * ((gi & 3) >> 1) + 4 * (gi & 1);
+  const uint32_t v_lane = 2u * D * (16 * h + (gi >> 2)) + 32u * (gq ^ vswz<D>(gi >> 2)) +
+                          16u * ((gi & 3) >> 1) + 8u * (gi & 1);
   constexpr float kSumLimit = 4294967296.f;
 
   for (int round = 0;; ++round) {
@@ -580,16 +595,27 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       pB[nb][0] = pB[nb][1] = bf16x8{};
     }
     constexpr int NS = D / 16;             // slots of a step: K operands, and V operands
-    // K operand c of the 32 keys at kb; V operand i = (32 dims dt, 16 keys cc) of those at vb
-    auto kop = [&](const uint16_t* kb, int c) {
-      return __builtin_bit_cast(bf16x8, ld16(kb + krow * D + 8 * ((2 * c + h) ^ fk)));
+    // Operands read ahead, and their registers.  The next step's first ones are read after the ring
+    // has turned in the middle, so no further ahead than half a step.  (3 of 8 instead of 2: 1,351 us
+    // instead of 1,373 for 4 x 2,660 rows over 33,500 keys with 8 KV heads; 4: as 3.)
+    constexpr int kAhead = NS / 2 < 3 ? NS / 2 : 3, kOps = 4;
+    static_assert(kAhead <= NS / 2 && kAhead < kOps && NS % kOps == 0);
+    // K operand c of the 32 keys at LDS address kb; V operand i = (32 dims dt, 16 keys cc) of those at
+    // vb.  Rows are 2 D bytes apart and the swizzles act below that, so an operand's place is this
+    // lane's for the first with bits of its number flipped.
+    auto kop = [&](uint32_t kb, int c) {
+      return __builtin_bit_cast(
+          bf16x8, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
+                      (kb + k_lane) ^ (32u * c)));
     };
-    auto vop = [&](const uint16_t* vb, int i) {
+    auto vop = [&](uint32_t vb, int i) {
       const int dt = i % (D / 32), cc = i / (D / 32);
-      const int unit = (2 * dt + gq) ^ vsl;
-      const uint16_t* vp = vb + (16 * h + 8 * cc) * D + 16 * unit + v_lane_off;
-      const shortx4 lo = ld_tr(vp);
-      const shortx4 hi = ld_tr(vp + 4 * D);
+      const auto* vp = reinterpret_cast<__attribute__((address_space(3))) shortx4*>(
+          ((vb + v_lane) ^ (64u * dt)) + 16u * D * cc);
+      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          const_cast<__attribute__((address_space(3))) shortx4*>(vp));
+      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          const_cast<__attribute__((address_space(3))) shortx4*>(vp + D));
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
@@ -609,7 +635,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
-      const bf16x8 ka = kop(lds, c);
+      const bf16x8 ka = kop(lds0, c);
 #pragma unroll
       for (int nb = 0; nb < kNB; ++nb) sA[nb] = mfma(ka, qf[nb][c], sA[nb]);
     }
@@ -617,14 +643,15 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     // One step for 32 keys from key0 on, whose scores are in s_cur: their softmax, the scores of the
     // next 32 keys and the product of the 32 keys before (probabilities p_prev), interleaved so that
     // the vector units work while the matrix cores run: a wave issues in order.  The operands of its
-    // first two slots are in ka and va; the later ones come from kb and vb, and the next step's first
-    // two are read from kn and vn at its end.  `middle` is called half-way.  (The first step's
+    // first kAhead slots are in ka and va; the later ones come from kb and vb, and the next step's
+    // first kAhead are read from kn and vn at its end.  `middle` is called half-way.  (The first step's
     // p_prev are zeros; the last one's next scores are of stale keys and not used.)
     const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-    bf16x8 ka[2], va[2];
+    bf16x8 ka[kOps], va[kOps];
     auto step = [&](floatx16(&s_cur)[kNB], floatx16(&s_nxt)[kNB], bf16x8(&p_prev)[kNB][2],
-                    bf16x8(&p_cur)[kNB][2], const uint16_t* kb, const uint16_t* vb,
-                    const uint16_t* kn, const uint16_t* vn, int key0, auto middle) {
+                    bf16x8(&p_cur)[kNB][2], uint32_t kb, uint32_t vb,
+                    uint32_t kn, uint32_t vn, int key0,
+                    auto middle) __attribute__((always_inline)) {
       if (key0 + 31 > full_lim) {
 #pragma unroll
         for (int nb = 0; nb < kNB; ++nb)
@@ -641,19 +668,21 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       }
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        const bf16x8 kc = ka[i & 1], vc = va[i & 1];
+        const bf16x8 kc = ka[i % kOps], vc = va[i % kOps];
         const int dt = i % (D / 32), cc = i / (D / 32);
 #pragma unroll
         for (int nb = 0; nb < kNB; ++nb) {
           float e[EPS];
           s_nxt[nb] = mfma(kc, qf[nb][i], s_nxt[nb]);
-          if (nb == kNB - 1) ka[i & 1] = i + 2 < NS ? kop(kb, i + 2) : kop(kn, i + 2 - NS);
+          if (nb == kNB - 1)
+            ka[(i + kAhead) % kOps] = i + kAhead < NS ? kop(kb, i + kAhead) : kop(kn, i + kAhead - NS);
 #pragma unroll
           for (int x = 0; x < EPS; ++x)
             e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[nb][i * EPS + x], scale_log2, -m_run[nb]));
           __builtin_amdgcn_sched_barrier(0);
           o[nb][dt] = mfma(vc, p_prev[nb][cc], o[nb][dt]);
-          if (nb == kNB - 1) va[i & 1] = i + 2 < NS ? vop(vb, i + 2) : vop(vn, i + 2 - NS);
+          if (nb == kNB - 1)
+            va[(i + kAhead) % kOps] = i + kAhead < NS ? vop(vb, i + kAhead) : vop(vn, i + kAhead - NS);
 #pragma unroll
           for (int x = 0; x < EPS; x += 2) {
             const int at = i * EPS + x;
@@ -725,14 +754,15 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       }
       __builtin_amdgcn_sched_barrier(0);
     };
-    const uint16_t* v_ring = lds + kRing * T::kElems;
+    constexpr uint32_t kTileBytes = 2 * T::kElems, kHalfBytes = T::kElems;
+    const uint32_t v_ring = lds0 + kRing * kTileBytes;
     int entry = 0;                                       // (t - t_begin) % kRing
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      ka[i] = kop(lds + 32 * D, i);
-      va[i] = vop(lds, i);                 // (the first step's zeros meet the first keys: numbers)
+    for (int i = 0; i < kAhead; ++i) {
+      ka[i] = kop(lds0 + kHalfBytes, i);
+      va[i] = vop(lds0, i);                // (the first step's zeros meet the first keys: numbers)
     }
-    const uint16_t* v_prev = lds;
+    uint32_t v_prev = lds0;
     if (m0 + wave * 32 >= L * G) {         // a wave without rows: its share of the copies
       for (int t = t_begin; t < t_end; ++t) turn_over(t);
       if (!after_part()) break;
@@ -740,12 +770,11 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     }
     for (int t = t_begin; t < t_end; ++t) {
       const int next = (entry + 1) & (kRing - 1);
-      const uint16_t* kt = lds + entry * T::kElems;
-      const uint16_t* k1 = lds + next * T::kElems;
-      const uint16_t* vt = v_ring + entry * T::kElems;
-      step(sA, sB, pB, pA, kt + 32 * D, v_prev, k1, vt, t * kKT, [&]() { turn_over(t); });
-      step(sB, sA, pA, pB, k1, vt, k1 + 32 * D, vt + 32 * D, t * kKT + 32, []() {});
-      v_prev = vt + 32 * D;
+      const uint32_t kt = lds0 + entry * kTileBytes, k1 = lds0 + next * kTileBytes;
+      const uint32_t vt = v_ring + entry * kTileBytes;
+      step(sA, sB, pB, pA, kt + kHalfBytes, v_prev, k1, vt, t * kKT, [&]() { turn_over(t); });
+      step(sB, sA, pA, pB, k1, vt, k1 + kHalfBytes, vt + kHalfBytes, t * kKT + 32, []() {});
+      v_prev = vt + kHalfBytes;
       entry = next;
     }
     // the last 32 keys' product

@@ -87,6 +87,11 @@ CHUNKS = [
     ([1400, 1390, 1410], [700, 710, 690], 32, 32, 8, 64, F32),   # more row tiles than workgroups
     ([2300], [2300], 64, 32, 8, 64, BF),                     # as many, of unequal work
     ([3000, 600, 40, 2000], [1500, 600, 40, 1], 16, 32, 16, 64, F32),   # and of unequal sequences
+    ([4000, 2500], [300, 77], 256, 15, 3, 64, BF),           # 3 KV heads, 5 query heads on each
+    ([700, 3], [90, 3], 16, 32, 32, 128, F32),               # a key head per query head
+    ([1 + i % 23 for i in range(1024)], [(1 + i % 23) * (i % 5 > 0) // 2 for i in range(1024)], 16, 4,
+     1, 64, F32),
+    ([6000], [40], 16, 40, 1, 128, F32),                     # 40 query heads on one
 ]
 
 
@@ -117,6 +122,9 @@ DECODES = [
     ([300, 2], 2, 256, 14, 2, 64, F32),
     ([30 + i % 50 for i in range(260)], 1, 16, 4, 2, 64, F32),
     ([12000], 1, 64, 32, 8, 128, BF),
+    ([2900, 1, 700], 3, 32, 15, 3, 64, F32),                 # 3 KV heads; one row, three tokens
+    ([50 + i % 41 for i in range(1024)], 1, 16, 3, 3, 64, BF),
+    ([400, 90], 1, 16, 32, 32, 128, F32),
 ]
 
 
@@ -128,8 +136,13 @@ def test_decode(case):
     S = len(ctx)
     q = torch.randn(S, nq, hq, d, generator=torch.Generator().manual_seed(case)).to(BF)
     got, st = run(True, q.cuda(), kp.cuda(), vp.cuda(), table, None, ctx, d ** -0.5, out)
-    assert st == 0
+    from paper_2609_34653_amd import omnitide as ot
+    short = [0 < n < nq for n in ctx]                        # fewer rows than new tokens: refused
+    assert st == (ot.E_CAPACITY if any(short) else 0)
     for s, n in enumerate(ctx):
+        if short[s]:
+            assert torch.isnan(got[s]).all()                 # not written
+            continue
         if n == 0:
             assert (got[s] == 0).all()
             continue
@@ -349,6 +362,74 @@ def test_captured_step_replays_as_eager(decode):
         st.step(q, k, v, ds, ctx, q_out, eager, st.workspace(T, decode), decode)
         torch.cuda.synchronize()
         assert torch.equal(eager, out) and torch.equal(q_out, kept)
+
+
+def both(decode, ctx, P, hq, hkv, d, seed, new=2):
+    """Inputs of one call: (q, kp, vp, table, start, ctx)."""
+    table, n_pages = layout(ctx, P, seed)
+    kp, vp = pools(ctx, table, n_pages, P, hkv, d, seed)
+    q = torch.randn(len(ctx) * new, hq, d, generator=torch.Generator().manual_seed(seed)).to(BF)
+    q = q.view(len(ctx), new, hq, d) if decode else q
+    return q.cuda(), kp.cuda(), vp.cuda(), table, new * np.arange(len(ctx) + 1), ctx
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_sequences_share_pages(decode):
+    """Three sequences with the same first pages, each with its own tail."""
+    ctx, P, hq, hkv, d = [700, 650, 641], 64, 8, 2, 64
+    table, n_pages = layout(ctx, P, 4)
+    table[1:, :10] = table[0, :10]
+    kp, vp = (torch.randn(n_pages, P, hkv, d).to(BF) for _ in range(2))
+    q = torch.randn(6, hq, d).to(BF)
+    got, st = run(decode, (q.view(3, 2, hq, d) if decode else q).cuda(), kp.cuda(), vp.cuda(), table,
+                  [0, 2, 4, 6], ctx, 0.125, F32)
+    want, spread = op.ragged_attention(f64(q), f64(kp), f64(vp), table, [0, 2, 4, 6], ctx, 0.125)
+    assert st == 0
+    assert_near(got.view(6, hq, d), want, spread, 2.0 ** -8, F32)
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_a_sequence_of_nans_stays_alone(decode):
+    """Rows in use that are NaN and infinite spoil their own sequence, no other one, to the bit."""
+    ctx = [900, 333, 70, 500]
+    q, kp, vp, table, start, _ = both(decode, ctx, 32, 8, 2, 128, 6)
+    clean, _ = run(decode, q, kp, vp, table, start, ctx, 0.1, F32)
+    kp[table[1, :11]] = float("nan")
+    vp[table[1, :11]] = float("inf")
+    got, st = run(decode, q, kp, vp, table, start, ctx, 0.1, F32)
+    assert st == 0
+    rows = [0, 2, 3] if decode else [0, 1, 4, 5, 6, 7]
+    assert torch.equal(got[rows], clean[rows]) and torch.isfinite(clean).all()
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_two_streams_at_once(decode):
+    """Two calls in flight with a workspace each, on streams given by name, against each alone."""
+    from paper_2609_34653_amd import paged as pg
+    calls, alone = [], []
+    for seed, ctx in ((7, [5000, 300, 2000]), (8, [100, 6000, 900])):
+        q, kp, vp, table, start, _ = both(decode, ctx, 64, 16, 4, 128, seed)
+        out, st = run(decode, q, kp, vp, table, start, ctx, 0.1, BF)
+        assert st == 0
+        alone.append(out)
+        cap = table.shape[1] * 64
+        nb = (pg.omnitide_paged_decode_workspace_bytes(3, 2, cap, 16, 4, 128) if decode else
+              pg.omnitide_paged_chunk_attn_workspace_bytes(6, 3, cap, 16, 4, 128))
+        calls.append((q, kp, vp, i32(table), i32(start), i32(ctx), torch.empty_like(out),
+                      torch.empty(nb, dtype=torch.uint8, device="cuda"), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for rep in range(8):
+        for q, kp, vp, table, start, ctx, out, ws, stream in calls:
+            with torch.cuda.stream(stream):
+                out.zero_()
+            if decode:
+                pg.omnitide_paged_decode_attn(q, kp, vp, table, ctx, 0.1, out, ws, stream=stream)
+            else:
+                pg.omnitide_paged_chunk_attn(q, kp, vp, table, start, ctx, 0.1, out, ws,
+                                             stream=stream)
+    torch.cuda.synchronize()
+    for c, want in zip(calls, alone):
+        assert torch.equal(c[6], want)
 
 
 def test_zero_tokens():
