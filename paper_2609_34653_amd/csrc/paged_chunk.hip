@@ -127,10 +127,19 @@ struct Plan {
   __device__ static int row_tiles(int len, int G) {
     return static_cast<int>((static_cast<int64_t>(len) * G + kRows - 1) / kRows);
   }
-  // work of row tiles [0, m) of a sequence with kept keys in front of its chunk
-  __device__ int64_t work(int m, int kept) const {
-    return m * (static_cast<int64_t>(G) * (kept + kOverhead)) +
-           kRows / 2 * (static_cast<int64_t>(m) * (m + 1));
+  // work of row tiles [0, m) of a sequence with kept keys in front of its chunk of len tokens
+  __device__ int64_t work(int m, int kept, int len) const {
+    const int64_t each = static_cast<int64_t>(G) * (kept + kOverhead);
+    const int64_t w = m * each + kRows / 2 * (static_cast<int64_t>(m) * (m + 1));
+    // The last row tile may leave waves without rows, up to 1/20 less work each: 4 x 2,660 rows over
+    // 33,500 keys (4 waves in each last one) 1,440 us instead of 1,466, 2,660 rows over 17,290 keys
+    // 215 instead of 220.  Charged at twice that, what they cost where all row tiles are like them (8
+    // chunks over 16,384 keys: 206 us with 8 waves, 125 with 4), the latter takes 231: beside full
+    // workgroups, at the clock that those leave, they are not as fast.
+    const int64_t end = static_cast<int64_t>(len) * G;
+    if (m == 0 || static_cast<int64_t>(m) * kRows < end) return w;
+    const int waves = static_cast<int>(end - static_cast<int64_t>(m - 1) * kRows + 31) / 32;
+    return w - (each + static_cast<int64_t>(m) * kRows) * (kWaves - max(waves, 3)) / 20;
   }
   __device__ int tiles_of(int mt, int len, int ctx) const {
     const int last = static_cast<int>((static_cast<int64_t>(mt + 1) * kRows - 1) / G);
@@ -160,11 +169,11 @@ struct Plan {
       const bool ok = s0 >= 0 && s1 > s0 && s1 <= b.n_tokens && n >= s1 - s0 && n <= cap;
       const int len = ok ? s1 - s0 : 0;
       const int rt = row_tiles(len, G);
-      const int64_t w = work(rt, n - len);
+      const int64_t w = work(rt, n - len, len);
       const int64_t inc = static_cast<int64_t>(wave_scan_add_u64(ok ? w : 0));
       const int tiles = wave_scan_add_i32(rt);
       if (ok) {
-        most = fmaxf(most, static_cast<float>(w - work(rt - 1, n - len)));
+        most = fmaxf(most, static_cast<float>(w - work(rt - 1, n - len, len)));
         fewest = min(fewest, tiles_of(0, len, n));
       }
       m.seq[i] = make_int4(s0, len, n, tiles - rt);
@@ -279,13 +288,14 @@ struct Plan {
   }
   __device__ int64_t work_of(int i) const {
     const int2 t = find_tile(i % tiles_per_head);
-    const int kept = mem->seq[t.x].z - mem->seq[t.x].y;
-    return work(t.y + 1, kept) - work(t.y, kept);
+    const int len = mem->seq[t.x].y, kept = mem->seq[t.x].z - len;
+    return work(t.y + 1, kept, len) - work(t.y, kept, len);
   }
   __device__ int64_t work_before(int i) const {
     const int2 t = find_tile(i % tiles_per_head);
+    const int len = mem->seq[t.x].y, kept = mem->seq[t.x].z - len;
     return uniform(i / tiles_per_head * per_head + mem->chunk[t.x / kWave] + mem->first[t.x] +
-                   work(t.y, mem->seq[t.x].z - mem->seq[t.x].y));
+                   work(t.y, kept, len));
   }
 
   struct Seq {
@@ -338,14 +348,14 @@ struct Plan {
     const Seq q = seq(s);
     const int kept = q.ctx - q.len;
     const int64_t z = y - first(s);
-    // kRows / 2 m^2 + bq m = z
+    // kRows / 2 m^2 + bq m = z  (the last row tile's work may be less: z is then below this m's)
     const double bq = static_cast<double>(G) * (kept + kOverhead) + kRows / 2;
     const double root = sqrt(bq * bq + 2.0 * kRows * static_cast<double>(z));
     const int most = row_tiles(q.len, G) - 1;
     int m = min(max(uniform(static_cast<int>(2.0 * static_cast<double>(z) / (bq + root))), 0), most);
-    while (m > 0 && work(m, kept) > z) --m;
-    while (m < most && work(m + 1, kept) <= z) ++m;
-    const int64_t w0 = work(m, kept), w1 = work(m + 1, kept);
+    while (m > 0 && work(m, kept, q.len) > z) --m;
+    while (m < most && work(m + 1, kept, q.len) <= z) ++m;
+    const int64_t w0 = work(m, kept, q.len), w1 = work(m + 1, kept, q.len);
     const int nt = tiles_of(m, q.len, q.ctx);
     const float part = static_cast<float>(z - w0) / static_cast<float>(w1 - w0);
     const int tile = uniform(static_cast<int>(fminf(part, 1.f) * nt));
@@ -376,7 +386,7 @@ struct Plan {
       return w - w % even;
     }
     const Seq q = seq(c.seq);
-    const int64_t x0 = c.g * per_head + first(c.seq) + work(c.mt, q.ctx - q.len);
+    const int64_t x0 = c.g * per_head + first(c.seq) + work(c.mt, q.ctx - q.len, q.len);
     int w0 = 0;                            // the last share that begins at or before it
     if (rounds > 0) {
       for (int hi = kWGs; w0 + 1 < hi;) {
