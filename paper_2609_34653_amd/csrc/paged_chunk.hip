@@ -14,7 +14,7 @@
 //             waves of 64 rows have no registers left to read ahead with; two workgroups of 4 x 32
 //             rows read every key twice and are a tenth slower on long calls.)
 //   shares    whole row tiles in rounds of kWGs, so that the workgroups of an XCD read the same keys at
-//             about the same time (L2 misses of 4 x 2,660 rows over 33,500 keys: 36 M to 8 M); the
+//             about the same time (L2 misses of 4 x 2,329 tokens over 10,521 keys: 36 M to 8 M); the
 //             rest is cut, whatever the lengths, into a share per workgroup that evens the rounds
 //             out.  The parts of a row tile that lies in several are merged by a second kernel, in share
 //             order, so results do not depend on timing.  Every workgroup works the cuts out by
@@ -35,9 +35,9 @@
 //             through a tile's first step, by one barrier per tile.
 //
 // Measured (bf16, d = 128, 4 query heads per KV head, 8 KV heads, pages of 64, cache larger than L2):
-//   4 chunks of 665 tokens over 33,500 keys       1,351 us, 1.06 PFLOP/s
-//   one chunk of 665 tokens over 17,290 keys        206 us, 0.88 PFLOP/s (11 us of it the merge)
-//   89 tokens over 89 keys                           17 us
+//   4 chunks of 2,329 tokens over 10,521 keys     1,330 us, 1.07 PFLOP/s
+//   one chunk of 665 tokens over 17,048 keys        199 us, 0.92 PFLOP/s (11 us of it the merge)
+//   89 tokens over 601 keys, 4 heads, d = 64         17 us (launches, plan and merge)
 #include <algorithm>
 #include <type_traits>
 
@@ -131,9 +131,9 @@ struct Plan {
   __device__ int64_t work(int m, int kept, int len) const {
     const int64_t each = static_cast<int64_t>(G) * (kept + kOverhead);
     const int64_t w = m * each + kRows / 2 * (static_cast<int64_t>(m) * (m + 1));
-    // The last row tile may leave waves without rows, up to 1/20 less work each: 4 x 2,660 rows over
-    // 33,500 keys (4 waves in each last one) 1,440 us instead of 1,466, 2,660 rows over 17,290 keys
-    // 215 instead of 220.  Charged at twice that, what they cost where all row tiles are like them (8
+    // The last row tile may leave waves without rows, up to 1/20 less work each: 4 x 2,329 tokens
+    // over 10,521 keys (4 waves in each last one) 1,440 us instead of 1,466, 665 tokens over 17,048
+    // keys 215 instead of 220.  Charged at twice that, what they cost where all row tiles are like them (8
     // chunks over 16,384 keys: 206 us with 8 waves, 125 with 4), the latter takes 231: beside full
     // workgroups, at the clock that those leave, they are not as fast.
     const int64_t end = static_cast<int64_t>(len) * G;
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     constexpr int NS = D / 16;             // slots of a step: K operands, and V operands
     // Operands read ahead, and their registers.  The next step's first ones are read after the ring
     // has turned in the middle, so no further ahead than half a step.  (3 of 8 instead of 2: 1,351 us
-    // instead of 1,373 for 4 x 2,660 rows over 33,500 keys with 8 KV heads; 4: as 3.)
+    // instead of 1,373 for 4 x 2,329 tokens over 10,521 keys with 8 KV heads; 4: as 3.)
     constexpr int kAhead = NS / 2 < 3 ? NS / 2 : 3, kOps = 4;
     static_assert(kAhead <= NS / 2 && kAhead < kOps && NS % kOps == 0);
     // K operand c of the 32 keys at LDS address kb; V operand i = (32 dims dt, 16 keys cc) of those at
@@ -836,7 +836,8 @@ __global__ __launch_bounds__(kThreads) void paged_chunk_merge_kernel(
     const float* __restrict__ part_o, const float2* __restrict__ part_ml,
     const Joined* __restrict__ joined, int Hq, int Hkv, void* __restrict__ out, bool out_bf16) {
   constexpr int TPR = D / 4, PER = kThreads / TPR;
-  const Joined j = joined[blockIdx.x];
+  // on the XCD that wrote the parts (201 -> 199 us for 665 tokens over 17,048 keys)
+  const Joined j = joined[(blockIdx.x % kNumXcd) * (kWGs / kNumXcd) + blockIdx.x / kNumXcd];
   if (j.n_parts == 0) return;
   const int G = Hq / Hkv;
   const int d4 = threadIdx.x % TPR;
