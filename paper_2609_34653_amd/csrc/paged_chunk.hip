@@ -61,19 +61,9 @@ constexpr int kOverhead = 2 * kKT;       // what a row tile costs beside its key
 constexpr int kMinShareTiles = 2;        // tiles of a share at least
 constexpr int kSnap = 2;                 // a cut this near to a row tile's end goes to the end
 
-// Where a share begins: row tile mt of (KV head g, sequence seq), key tile `tile` of it.
-struct Cut {
-  int g, seq, mt, tile;
-};
-__device__ inline bool same_rows(const Cut& a, const Cut& b) {
-  return a.g == b.g && a.seq == b.seq && a.mt == b.mt;
-}
-__device__ inline bool before(const Cut& a, const Cut& b) {
-  if (a.g != b.g) return a.g < b.g;
-  if (a.seq != b.seq) return a.seq < b.seq;
-  if (a.mt != b.mt) return a.mt < b.mt;
-  return a.tile < b.tile;
-}
+// Where a share begins: key tile `tile` of row tile i (row tiles are numbered in order of KV head,
+// sequence and place in it), as one number that orders like them.
+__device__ inline int64_t pack_cut(int i, int tile) { return (static_cast<int64_t>(i) << 32) | tile; }
 
 // What the merge kernel needs of a share that ends a row tile begun in an earlier one (n_parts > 0).
 struct Joined {
@@ -92,7 +82,8 @@ struct PlanMem {
   int64_t wave_max[kWaves], wave_sum[kWaves];
   int32_t wave_min[kWaves];
   float wave_most[kWaves];
-  int64_t begin[kWGs + 1];               // work in front of each share (rounds > 0)
+  // each share's work in front of it (rounds > 0), then its beginning (pack_cut)
+  int64_t begin[kWGs + 1];
 };
 
 // Scalars for the wave, whatever registers they were computed in.
@@ -112,7 +103,7 @@ __device__ inline int64_t div64(int64_t x, int64_t y) {
   return q;
 }
 
-// Row tiles in order of (KV head, sequence, number).  Workgroups first take whole ones in rounds,
+// Row tiles in order of (KV head, sequence, place).  Workgroups first take whole ones in rounds,
 // kWGs at a time, so that the workgroups of an XCD read the same keys together; what is left
 // is cut into a share per workgroup, each as large as its rounds leave room for: as many rounds
 // as leave enough to even them out.  Without rounds, row tiles that are much alike are cut into
@@ -121,11 +112,12 @@ template <int SEQS>
 struct Plan {
   const PlanMem<SEQS>* mem;
   int64_t per_head, total, share, rest;  // work; rest: in front of what is cut into shares
-  int tiles_per_head, rounds, even, left;          // left: row tiles that are cut into shares
-  int G, Hkv, n_seq;
+  int tiles_per_head, n_tiles, rounds, even, left; // left: row tiles that are cut into shares
+  int G, n_seq;
 
+  // (a call's rows are at most 2^28: 32 bits hold them)
   __device__ static int row_tiles(int len, int G) {
-    return static_cast<int>((static_cast<int64_t>(len) * G + kRows - 1) / kRows);
+    return static_cast<int>(static_cast<uint32_t>(len * G + kRows - 1) / kRows);
   }
   // work of row tiles [0, m) of a sequence with kept keys in front of its chunk of len tokens
   __device__ int64_t work(int m, int kept, int len) const {
@@ -136,23 +128,23 @@ struct Plan {
     // keys 215 instead of 220.  Charged at twice that, what they cost where all row tiles are like them (8
     // chunks over 16,384 keys: 206 us with 8 waves, 125 with 4), the latter takes 231: beside full
     // workgroups, at the clock that those leave, they are not as fast.
-    const int64_t end = static_cast<int64_t>(len) * G;
-    if (m == 0 || static_cast<int64_t>(m) * kRows < end) return w;
-    const int waves = static_cast<int>(end - static_cast<int64_t>(m - 1) * kRows + 31) / 32;
-    return w - (each + static_cast<int64_t>(m) * kRows) * (kWaves - max(waves, 3)) / 20;
+    const int end = len * G;
+    if (m == 0 || m * kRows < end) return w;
+    const int waves = (end - (m - 1) * kRows + 31) >> 5;
+    return w - ((each + m * kRows) * (13 * (kWaves - max(waves, 3))) >> 8);
   }
   __device__ int tiles_of(int mt, int len, int ctx) const {
-    const int last = static_cast<int>((static_cast<int64_t>(mt + 1) * kRows - 1) / G);
-    return (ctx - len + min(len - 1, last) + kKT) / kKT;
+    const int last = static_cast<int>(static_cast<uint32_t>((mt + 1) * kRows - 1) /
+                                      static_cast<uint32_t>(G));
+    return static_cast<int>(static_cast<uint32_t>(ctx - len + min(len - 1, last) + kKT) / kKT);
   }
 
   // by the whole workgroup
-  __device__ void make(PlanMem<SEQS>& m, const PagedBatch& b, int G_, int Hkv_) {
+  __device__ void make(PlanMem<SEQS>& m, const PagedBatch& b, int G_, int Hkv) {
     const int tid = static_cast<int>(threadIdx.x);
     const int lane = tid & (kWave - 1), wave = uniform(tid / kWave);
     const int cap = b.max_pages << b.page_shift;
     G = G_;
-    Hkv = Hkv_;
     n_seq = b.n_seq;
     mem = &m;
     const int n_chunks = (n_seq + kWave - 1) / kWave;
@@ -214,13 +206,12 @@ struct Plan {
     per_head = uniform(sum);
     total = per_head * Hkv;
     tiles_per_head = uniform(sum_tiles);
-    const int n_tiles = tiles_per_head * Hkv;
+    n_tiles = tiles_per_head * Hkv;
     rounds = 0;
     even = 0;
     left = n_tiles;
     rest = 0;
     share = 0;
-    if (n_tiles == 0) return;
     for (rounds = n_tiles / kWGs; rounds > 0; rounds -= (rounds + 7) / 8) {
       left = n_tiles - rounds * kWGs;
       rest = left > 0 ? work_before(rounds * kWGs) : total;
@@ -243,14 +234,21 @@ struct Plan {
       int64_t before = 0;
       for (int w = 0; w < wave; ++w) before += m.wave_sum[w];
       if (tid <= kWGs) m.begin[tid] = before + inc - room;
-      __syncthreads();
-      return;
+      break;
     }
+    if (rounds == 0) without_rounds(fewest, most);
+    // (a thread reads and writes its own entry only)
+    if (tid <= kWGs) m.begin[tid] = cut_of(tid, m.begin[tid]);
+    __syncthreads();
+  }
+
+  // n_tiles row tiles, the shortest of `fewest` key tiles, the largest of work `most`
+  __device__ void without_rounds(int fewest, float most) {
     left = n_tiles;
     rest = 0;
     // alike: the largest row tile has at most 1.25 times the mean work
     const bool alike = 4.f * most * static_cast<float>(n_tiles) <= 5.f * static_cast<float>(total);
-    if (alike && left <= kWGs) {
+    if (alike && left > 0 && left <= kWGs) {
       const int parts_most = max(1, uniform(fewest) / kMinShareTiles);
       const int parts = min(kWGs / left, parts_most);
       if (parts == parts_most || 10 * left * parts >= 9 * kWGs) even = parts;
@@ -305,108 +303,58 @@ struct Plan {
     const int4 v = mem->seq[s];
     return {uniform(v.x), uniform(v.y), uniform(v.z)};
   }
-  __device__ int64_t first(int s) const {
-    return uniform(mem->chunk[s / kWave] + mem->first[s]);
-  }
-  // the next sequence with tokens from s on, n_seq if there is none
-  __device__ int next_seq(int s) const {
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int c = s / kWave; c * kWave < n_seq; ++c) {
-      const int i = c * kWave + lane;
-      const uint64_t has = __ballot(i >= s && i < n_seq && mem->seq[i].y > 0);
-      if (has != 0) return uniform(c * kWave + __ffsll(static_cast<unsigned long long>(has)) - 1);
+  // where share w begins, lanes apart; before: the work in front of it in what is cut
+  __device__ int64_t cut_of(int w, int64_t before) const {
+    if (even > 0) {
+      const int i = w / even;
+      if (i >= left) return pack_cut(n_tiles, 0);
+      const int2 t = find_tile(i % tiles_per_head);
+      const int4 q = mem->seq[t.x];
+      // (at most 2^24 tiles, fewer than 2^8 parts)
+      return pack_cut(i, static_cast<int>(static_cast<uint32_t>(tiles_of(t.y, q.y, q.z)) *
+                                          static_cast<uint32_t>(w - i * even) /
+                                          static_cast<uint32_t>(even)));
     }
-    return n_seq;
-  }
-  // a cut whose row tile may be one past its sequence's last, made a real one (or {Hkv, 0, 0, 0})
-  __device__ Cut settle(Cut c) const {
-    if (c.mt < row_tiles(seq(c.seq).len, G)) return c;
-    int s = next_seq(c.seq + 1), g = c.g;
-    if (s == n_seq) {
-      s = next_seq(0);
-      ++g;
-    }
-    return g < Hkv ? Cut{g, s, 0, 0} : Cut{Hkv, 0, 0, 0};
-  }
-  // row tile number i of all
-  __device__ Cut row_tile(int i) const {
-    const int2 t = find_tile(i % tiles_per_head);
-    return {uniform(i / tiles_per_head), uniform(t.x), uniform(t.y), 0};
+    const int64_t x = rounds > 0 ? rest + before : w * share;
+    return x < total ? at(x) : pack_cut(n_tiles, 0);
   }
   // the row tile and key tile at x units of work
-  __device__ Cut at(int64_t x) const {
-    if (x >= total) return {Hkv, 0, 0, 0};
-    const int lane = threadIdx.x & (kWave - 1);
-    const int g = uniform(static_cast<int>(div64(x, per_head)));
+  __device__ int64_t at(int64_t x) const {
+    const int g = static_cast<int>(div64(x, per_head));
     const int64_t y = x - g * per_head;
-    int c = 0;
-    while ((c + 1) * kWave < n_seq && uniform(mem->chunk[c + 1]) <= y) ++c;
-    const int i = c * kWave + lane;
-    const uint64_t hit =
-        __ballot(i < n_seq && mem->seq[i].y > 0 && mem->chunk[c] + mem->first[i] <= y);
-    const int s = uniform(c * kWave + 63 - __clzll(static_cast<long long>(hit)));
-    const Seq q = seq(s);
-    const int kept = q.ctx - q.len;
-    const int64_t z = y - first(s);
+    int s = 0;                             // the last sequence that begins at or before y
+    for (int hi = n_seq - 1; s < hi;) {
+      const int mid = (s + hi + 1) / 2;
+      if (mem->chunk[mid / kWave] + mem->first[mid] <= y) s = mid;
+      else hi = mid - 1;
+    }
+    const int len = mem->seq[s].y, ctx = mem->seq[s].z, kept = ctx - len;
+    const int64_t z = y - mem->chunk[s / kWave] - mem->first[s];
     // kRows / 2 m^2 + bq m = z  (the last row tile's work may be less: z is then below this m's)
     const double bq = static_cast<double>(G) * (kept + kOverhead) + kRows / 2;
     const double root = sqrt(bq * bq + 2.0 * kRows * static_cast<double>(z));
-    const int most = row_tiles(q.len, G) - 1;
-    int m = min(max(uniform(static_cast<int>(2.0 * static_cast<double>(z) / (bq + root))), 0), most);
-    while (m > 0 && work(m, kept, q.len) > z) --m;
-    while (m < most && work(m + 1, kept, q.len) <= z) ++m;
-    const int64_t w0 = work(m, kept, q.len), w1 = work(m + 1, kept, q.len);
-    const int nt = tiles_of(m, q.len, q.ctx);
+    const int most = row_tiles(len, G) - 1;
+    int m = min(max(static_cast<int>(2.0 * static_cast<double>(z) / (bq + root)), 0), most);
+    while (m > 0 && work(m, kept, len) > z) --m;
+    while (m < most && work(m + 1, kept, len) <= z) ++m;
+    const int64_t w0 = work(m, kept, len), w1 = work(m + 1, kept, len);
+    const int nt = tiles_of(m, len, ctx);
     const float part = static_cast<float>(z - w0) / static_cast<float>(w1 - w0);
-    const int tile = uniform(static_cast<int>(fminf(part, 1.f) * nt));
-    if (tile <= kSnap) return {uniform(g), s, m, 0};
-    if (tile >= nt - kSnap) return settle({uniform(g), s, m + 1, 0});
-    return {uniform(g), s, m, tile};
+    const int tile = static_cast<int>(fminf(part, 1.f) * nt);
+    const int i = g * tiles_per_head + mem->chunk_tiles[s / kWave] + mem->seq[s].w + m;
+    if (tile <= kSnap) return pack_cut(i, 0);
+    if (tile >= nt - kSnap) return pack_cut(i + 1, 0);
+    return pack_cut(i, tile);
   }
-  __device__ Cut share_begin(int w) const {
-    Cut c{Hkv, 0, 0, 0};
-    if (even > 0) {
-      if (w / even < left) {
-        c = row_tile(w / even);
-        const Seq q = seq(c.seq);
-        c.tile = static_cast<int>(static_cast<int64_t>(tiles_of(c.mt, q.len, q.ctx)) *
-                                  (w % even) / even);
-      }
-    } else if (rounds > 0) {
-      c = at(min(rest + uniform(mem->begin[w]), total));
-    } else if (left > 0) {
-      c = at(min(w * share, total));
-    }
-    return {uniform(c.g), uniform(c.seq), uniform(c.mt), uniform(c.tile)};
-  }
-  // the share whose part of row tile c (cut into several) begins it, and the part's slot
-  __device__ int first_share(Cut c, int w, int& slot) const {
-    if (even > 0) {
-      slot = 2 * (w - w % even);
-      return w - w % even;
-    }
-    const Seq q = seq(c.seq);
-    const int64_t x0 = c.g * per_head + first(c.seq) + work(c.mt, q.ctx - q.len, q.len);
-    int w0 = 0;                            // the last share that begins at or before it
-    if (rounds > 0) {
-      for (int hi = kWGs; w0 + 1 < hi;) {
-        const int mid = (w0 + hi) / 2;
-        if (uniform(mem->begin[mid]) <= x0 - rest) w0 = mid;
-        else hi = mid;
-      }
-    } else {
-      w0 = uniform(static_cast<int>(div64(x0, share)));
-    }
-    c.tile = 0;
-    Cut b = share_begin(w0);
-    for (;;) {                             // shares that begin here with nothing in them
-      const Cut b1 = share_begin(w0 + 1);
-      if (!same_rows(b1, c) || b1.tile != 0) break;
-      ++w0;
-      b = b1;
-    }
-    slot = 2 * w0 + (same_rows(b, c) && b.tile == 0 ? 0 : 1);
-    return w0;
+  __device__ int64_t share_begin(int w) const { return uniform(mem->begin[w]); }
+  // the last share up to w that begins at or before the start of row tile i
+  __device__ int first_share(int i, int w) const {
+    const int lane = threadIdx.x & (kWave - 1);
+    int n = 0;
+#pragma unroll
+    for (int c = 0; c < kWGs; c += kWave)
+      n += __popcll(__ballot(c + lane <= w && mem->begin[c + lane] <= pack_cut(i, 0)));
+    return n - 1;
   }
 };
 
@@ -447,11 +395,11 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
   // shares next to each other (the same keys, the next rows) on one XCD: workgroups are dealt
   // round-robin over 8
   const int w = (blockIdx.x % kNumXcd) * (kWGs / kNumXcd) + blockIdx.x / kNumXcd;
-  const Cut begin = plan.share_begin(w), end = plan.share_begin(w + 1);
-  Cut cur = begin;
+  const int64_t begin = plan.share_begin(w), end = plan.share_begin(w + 1);
+  int64_t cur = begin;
   if (tid == 0) joined[w].n_parts = 0;
   // a share of nothing in the middle of a row tile: an empty part of it
-  if (!before(begin, end) && begin.tile > 0 && tid < kRows)
+  if (begin == end && static_cast<int32_t>(begin) > 0 && tid < kRows)
     part_ml[static_cast<size_t>(2 * w) * kRows + tid] = make_float2(-INFINITY, 0.f);
 
   const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
@@ -478,32 +426,34 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
   for (int round = 0;; ++round) {
     // ---- the next part: a whole row tile of a round, then what the share holds
     const bool shared = round >= plan.rounds;
-    if (shared && !before(cur, end)) break;
-    const Cut c = shared ? cur
-                         : plan.row_tile(Plan<SEQS>::round_tile(round, w));
-    const auto sq = plan.seq(c.seq);
-    const int L = sq.len, ctx = sq.ctx, kept = ctx - L, g = c.g;
-    const int nt = plan.tiles_of(c.mt, L, ctx);
-    const int t_begin = c.tile;
-    const int t_end = shared && same_rows(c, end) ? end.tile : nt;
+    if (shared && cur >= end) break;
+    const int i = shared ? static_cast<int>(cur >> 32) : Plan<SEQS>::round_tile(round, w);
+    const int t_begin = shared ? static_cast<int32_t>(cur) : 0;
+    const int g = static_cast<int>(static_cast<uint32_t>(i) /
+                                   static_cast<uint32_t>(plan.tiles_per_head));
+    const int2 place = plan.find_tile(i - g * plan.tiles_per_head);
+    const int s = uniform(place.x), mt = uniform(place.y);
+    const auto sq = plan.seq(s);
+    const int L = sq.len, ctx = sq.ctx, kept = ctx - L;
+    const int nt = plan.tiles_of(mt, L, ctx);
+    const int t_end = shared && i == static_cast<int>(end >> 32) ? static_cast<int32_t>(end) : nt;
     const bool whole = t_begin == 0 && t_end == nt;
-    const int slot = 2 * w + (same_rows(c, begin) ? 0 : 1);
-    const int m0 = c.mt * kRows;
+    const int slot = 2 * w + (i == static_cast<int>(begin >> 32) ? 0 : 1);
+    const int m0 = mt * kRows;
     const int full_lim = kept + m0 / G;    // keys <= full_lim are visible to every row
     if (t_begin > 0 && t_end == nt && wave == 0) {
       // the row tile ends here: tell the merge where its parts are
-      int first_slot;
-      const int w0 = plan.first_share(c, w, first_slot);
+      const int w0 = plan.first_share(i, w);
+      const int first_slot = 2 * w0 + (plan.share_begin(w0) == pack_cut(i, 0) ? 0 : 1);
       if (lane == 0)
-        joined[w] = Joined{w - w0 + 1, first_slot, w, sq.q0, L * G, c.mt, g, 0};
+        joined[w] = Joined{w - w0 + 1, first_slot, w, sq.q0, L * G, mt, g, 0};
     }
 
     // on to the next part; false after the share's last
     auto after_part = [&]() {
       if (shared) {
         if (t_end < nt) return false;      // it ended inside the row tile
-        cur = plan.settle(Cut{c.g, c.seq, c.mt + 1, 0});
-        cur = Cut{uniform(cur.g), uniform(cur.seq), uniform(cur.mt), 0};
+        cur = pack_cut(i + 1, 0);
       }
       __syncthreads();                     // the tile buffers are free again
       return true;
@@ -530,7 +480,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     // Ids of the 64 pages from `window` on, one per lane.  The next 64 wait in LDS, put there by a
     // direct load when the window moved (a plain load would have the compiler wait for it, and so
     // for the tiles asked for before it).
-    const int32_t* table = b.table + static_cast<size_t>(c.seq) * b.max_pages;
+    const int32_t* table = b.table + static_cast<size_t>(s) * b.max_pages;
     const int last_page = (ctx - 1) >> b.page_shift;
     int window = (t_begin * kKT) >> b.page_shift, turn = 0;
     auto ask_pages = [&](int first) {
