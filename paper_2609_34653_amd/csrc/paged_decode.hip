@@ -38,16 +38,17 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKB = 16;                  // keys per block
 constexpr int kWGs = 512;                // shares of a large call: two workgroups on each CU
-constexpr int kMinShare = 16;            // blocks of a share at least (256 keys)
+constexpr int kMinShare = 16;            // work of a share at least, in blocks
+constexpr int kOverhead = 8;             // what a sequence costs beside its blocks, in blocks
 
 template <int N>
 __device__ inline void wait_vmcnt() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-// The shares of a call: sequence i = 64 n + lane holds nb[n] blocks, first[n] of its KV head's
-// blocks before it; per_head blocks per KV head; `share` blocks per workgroup.  Workgroup w takes
-// share w / H_kv of KV head w % H_kv.
+// The shares of a call: sequence i = 64 n + lane holds nb[n] blocks, work for kOverhead + nb[n] (none
+// without blocks); first[n] is its KV head's work before it, per_head all of it, `share` that of a
+// workgroup.  Workgroup w takes share w / H_kv of KV head w % H_kv.
 template <int NS>
 struct Shares {
   int nb[NS], first[NS], ctx[NS];
@@ -68,8 +69,9 @@ __device__ inline Shares<NS> plan_shares(const PagedBatch& b, int n_kv_heads) {
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
     s.nb[n] = s.ctx[n] >= b.n_q && s.ctx[n] <= cap ? (s.ctx[n] + kKB - 1) / kKB : 0;
-    const int inc = wave_scan_add_i32(s.nb[n]);
-    s.first[n] = s.per_head + inc - s.nb[n];
+    const int work = s.nb[n] > 0 ? kOverhead + s.nb[n] : 0;
+    const int inc = wave_scan_add_i32(work);
+    s.first[n] = s.per_head + inc - work;
     s.per_head += readlane(inc, kWave - 1);
   }
   const int per = kWGs / n_kv_heads;
@@ -157,23 +159,27 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
   const int vread = vrow * D + 4 * (c16 & 3);
 
   for (int pos = lo; pos < hi;) {
-    // the part of one sequence that starts at block pos
-    int seq = 0, b0 = 0, nb = 1, ctx = 1;
+    // the part of one sequence that starts at pos; its overhead comes before its blocks
+    int seq = 0, u0 = 0, nb = 1, ctx = 1;
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      const uint64_t hit = __ballot(pos >= sh.first[n] && pos < sh.first[n] + sh.nb[n]);
+      const uint64_t hit = __ballot(sh.nb[n] > 0 && pos >= sh.first[n] &&
+                                    pos < sh.first[n] + kOverhead + sh.nb[n]);
       if (hit != 0) {
         const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
         seq = n * kWave + l;
-        b0 = pos - readlane(sh.first[n], l);
+        u0 = pos - readlane(sh.first[n], l);
         nb = readlane(sh.nb[n], l);
         ctx = readlane(sh.ctx[n], l);
       }
     }
-    const int b1 = min(nb, b0 + (hi - pos));
+    const int u1 = min(kOverhead + nb, u0 + (hi - pos));
+    const int b0 = max(u0 - kOverhead, 0), b1 = max(u1 - kOverhead, 0);
+    pos += u1 - u0;
+    if (b1 == 0) break;                      // the share ends before the first block
     const bool whole = b0 == 0 && b1 == nb;
-    const int slot = 2 * static_cast<int>(blockIdx.x) + (pos == lo ? 0 : 1);
-    pos += b1 - b0;
+    // a share holds at most one part that goes on from an earlier share and one that goes on in a later
+    const int slot = 2 * static_cast<int>(blockIdx.x) + (b0 > 0 ? 0 : 1);
 
     // Q^T operand: column c16 = query vector (token c16 / G, head g*G + c16 % G)
     const bool col_ok = c16 < nqg;
@@ -386,12 +392,11 @@ __global__ __launch_bounds__(kThreads) void paged_decode_merge_kernel(
     }
   }
   if (nb == 0) return;
-  const int w0 = first / sh.share, w1 = (first + nb - 1) / sh.share;
+  const int w0 = (first + kOverhead) / sh.share, w1 = (first + kOverhead + nb - 1) / sh.share;
   if (w0 == w1) return;                      // finished by its workgroup
   const int col = tok * G + head % G, nqg = nq * G;
   const int tid = threadIdx.x, ts = tid / TPR, d4 = tid % TPR;
-  // part p: of share w0 + p, its first one except where the row begins inside the share
-  const int later0 = first == w0 * sh.share ? 0 : 1;
+  // part p: of share w0 + p
   const int n_parts = w1 - w0 + 1;
   float M = -INFINITY, den = 0.f;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -402,7 +407,8 @@ __global__ __launch_bounds__(kThreads) void paged_decode_merge_kernel(
     for (int c = 0; c < PER; ++c) {
       const int p = p0 + TS * c;
       const bool in = p < n_parts;
-      const size_t r = static_cast<size_t>(2 * ((w0 + p) * Hkv + g) + (p == 0 ? later0 : 0)) * nqg + col;
+      const size_t r =
+          static_cast<size_t>(2 * ((w0 + p) * Hkv + g) + (p == 0 ? 1 : 0)) * nqg + col;
       ml[c] = in ? part_ml[r] : make_float2(-INFINITY, 0.f);
       ov[c] = in ? *reinterpret_cast<const float4*>(part_o + r * D + 4 * d4)
                  : make_float4(0.f, 0.f, 0.f, 0.f);
