@@ -38,8 +38,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKB = 16;                  // keys per block
 constexpr int kWGs = 512;                // shares of a large call: two workgroups on each CU
-constexpr int kMinShare = 16;            // work of a share at least, in blocks
-constexpr int kOverhead = 8;             // what a sequence costs beside its blocks, in blocks
+constexpr int kMinShare = 8;             // work of a share at least, in blocks
+constexpr int kOverhead = 12;            // what a sequence costs beside its blocks, in blocks
 
 template <int N>
 __device__ inline void wait_vmcnt() {
