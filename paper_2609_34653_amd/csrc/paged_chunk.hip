@@ -59,6 +59,7 @@ constexpr int kRing = 4;                 // tiles of each tensor in LDS
 constexpr int kNumXcd = 8;
 constexpr int kOverhead = 2 * kKT;       // what a row tile costs beside its keys, in keys
 constexpr int kMinShareTiles = 2;        // tiles of a share at least
+constexpr int kNextPart = 4;             // what the next part costs a workgroup, in tiles
 constexpr int kSnap = 2;                 // a cut this near to a row tile's end goes to the end
 
 // Where a share begins: key tile `tile` of row tile i (row tiles are numbered in order of KV head,
@@ -77,11 +78,10 @@ template <int SEQS>
 struct PlanMem {
   int4 seq[SEQS];
   int64_t first[SEQS];
-  int64_t chunk[SEQS / kWave];
-  int32_t chunk_tiles[SEQS / kWave];
+  int64_t chunk[SEQS / kWave], chunk_sum[SEQS / kWave];
+  int32_t chunk_tiles[SEQS / kWave], chunk_tiles_sum[SEQS / kWave];
   int64_t wave_max[kWaves], wave_sum[kWaves];
-  int32_t wave_min[kWaves];
-  float wave_most[kWaves];
+  int4 sums[3][kWGs / kWave];
   // each share's work in front of it (rounds > 0), then its beginning (pack_cut)
   int64_t begin[kWGs + 1];
 };
@@ -106,13 +106,14 @@ __device__ inline int64_t div64(int64_t x, int64_t y) {
 // Row tiles in order of (KV head, sequence, place).  Workgroups first take whole ones in rounds,
 // kWGs at a time, so that the workgroups of an XCD read the same keys together; what is left
 // is cut into a share per workgroup, each as large as its rounds leave room for: as many rounds
-// as leave enough to even them out.  Without rounds, row tiles that are much alike are cut into
-// `even` equal parts each where that leaves few workgroups without one, for the same reason.
+// as leave enough to even them out.  Without rounds, every row tile is cut by itself into parts of
+// about one size, a workgroup each, unless the shares, which go on over the ends of row tiles, are
+// smaller by more than what it costs a workgroup to start on another part.
 template <int SEQS>
 struct Plan {
   const PlanMem<SEQS>* mem;
   int64_t per_head, total, share, rest;  // work; rest: in front of what is cut into shares
-  int tiles_per_head, n_tiles, rounds, even, left; // left: row tiles that are cut into shares
+  int tiles_per_head, n_tiles, rounds;
   int G, n_seq;
 
   // (a call's rows are at most 2^28: 32 bits hold them)
@@ -148,8 +149,6 @@ struct Plan {
     n_seq = b.n_seq;
     mem = &m;
     const int n_chunks = (n_seq + kWave - 1) / kWave;
-    float most = 0.f;                      // work of the largest row tile, key tiles of the shortest
-    int fewest = INT32_MAX;
     for (int c = wave; c < n_chunks; c += kWaves) {
       const int i = c * kWave + lane;
       int s0 = 0, s1 = 0, n = 0;
@@ -164,56 +163,33 @@ struct Plan {
       const int64_t w = work(rt, n - len, len);
       const int64_t inc = static_cast<int64_t>(wave_scan_add_u64(ok ? w : 0));
       const int tiles = wave_scan_add_i32(rt);
-      if (ok) {
-        most = fmaxf(most, static_cast<float>(w - work(rt - 1, n - len, len)));
-        fewest = min(fewest, tiles_of(0, len, n));
-      }
       m.seq[i] = make_int4(s0, len, n, tiles - rt);
       m.first[i] = inc - (ok ? w : 0);
       if (lane == kWave - 1) {
-        m.chunk[c] = inc;
-        m.chunk_tiles[c] = tiles;
+        m.chunk_sum[c] = inc;
+        m.chunk_tiles_sum[c] = tiles;
       }
     }
-    // (floats of one sign order as their bits)
-    most = __int_as_float(wave_max_i32(__float_as_int(most)));
-    fewest = -wave_max_i32(-fewest);
-    if (lane == 0) {
-      m.wave_most[wave] = most;
-      m.wave_min[wave] = fewest;
-    }
     __syncthreads();
-    int64_t sum = 0, mine = 0;             // every thread adds the chunks up
-    int sum_tiles = 0, my_tiles = 0;
+    int64_t sum = 0;                       // every thread adds the chunks up
+    int sum_tiles = 0;
     for (int c = 0; c < n_chunks; ++c) {
-      if (c == tid) {
-        mine = sum;
-        my_tiles = sum_tiles;
+      if (tid == 0) {
+        m.chunk[c] = sum;
+        m.chunk_tiles[c] = sum_tiles;
       }
-      sum += m.chunk[c];
-      sum_tiles += m.chunk_tiles[c];
-    }
-    for (int w = 0; w < kWaves; ++w) {
-      most = fmaxf(most, m.wave_most[w]);
-      fewest = min(fewest, m.wave_min[w]);
-    }
-    __syncthreads();
-    if (tid < n_chunks) {
-      m.chunk[tid] = mine;
-      m.chunk_tiles[tid] = my_tiles;
+      sum += m.chunk_sum[c];
+      sum_tiles += m.chunk_tiles_sum[c];
     }
     __syncthreads();
     per_head = uniform(sum);
     total = per_head * Hkv;
     tiles_per_head = uniform(sum_tiles);
     n_tiles = tiles_per_head * Hkv;
-    rounds = 0;
-    even = 0;
-    left = n_tiles;
     rest = 0;
     share = 0;
     for (rounds = n_tiles / kWGs; rounds > 0; rounds -= (rounds + 7) / 8) {
-      left = n_tiles - rounds * kWGs;
+      const int left = n_tiles - rounds * kWGs;
       rest = left > 0 ? work_before(rounds * kWGs) : total;
       // this thread's workgroup: the work of its rounds, then its share's room up to a level
       int64_t mine = 0;
@@ -236,27 +212,69 @@ struct Plan {
       if (tid <= kWGs) m.begin[tid] = before + inc - room;
       break;
     }
-    if (rounds == 0) without_rounds(fewest, most);
-    // (a thread reads and writes its own entry only)
-    if (tid <= kWGs) m.begin[tid] = cut_of(tid, m.begin[tid]);
+    if (rounds > 0 || !parts_of_row_tiles(m)) {
+      // (a thread reads and writes its own entry only)
+      if (tid <= kWGs) m.begin[tid] = cut_of(tid, m.begin[tid]);
+    }
     __syncthreads();
   }
 
-  // n_tiles row tiles, the shortest of `fewest` key tiles, the largest of work `most`
-  __device__ void without_rounds(int fewest, float most) {
-    left = n_tiles;
+  // no rounds: a part of a row tile per workgroup, or false for shares
+  __device__ bool parts_of_row_tiles(PlanMem<SEQS>& m) {
+    const int tid = static_cast<int>(threadIdx.x);
     rest = 0;
-    // alike: the largest row tile has at most 1.25 times the mean work
-    const bool alike = 4.f * most * static_cast<float>(n_tiles) <= 5.f * static_cast<float>(total);
-    if (alike && left > 0 && left <= kWGs) {
-      const int parts_most = max(1, uniform(fewest) / kMinShareTiles);
-      const int parts = min(kWGs / left, parts_most);
-      if (parts == parts_most || 10 * left * parts >= 9 * kWGs) even = parts;
-    }
     const int64_t least = static_cast<int64_t>(kMinShareTiles) * kKT * G;
     share = uniform(max(least, (total + kWGs - 1) / kWGs));
+    if (n_tiles == 0 || n_tiles >= kWGs) return false;
+    uint32_t nt = 0;                       // this thread's row tile
+    if (tid < n_tiles) {
+      const int2 t = find_tile(tid % tiles_per_head);
+      nt = static_cast<uint32_t>(tiles_of(t.y, mem->seq[t.x].y, mem->seq[t.x].z));
+    }
+    // the least part whose number fits, nearly: sum(ceil(nt / part)) <= sum / part + n_tiles; three
+    // between the least that there is and that are tried
+    const uint32_t sum = static_cast<uint32_t>(
+        sums<0>(m, static_cast<int>(nt), 0, 0).x);                      // (at most 2^8 times 2^24)
+    const uint32_t lo = max(static_cast<uint32_t>(kMinShareTiles), (sum + kWGs - 1) / kWGs);
+    uint32_t part = max(lo, (sum + kWGs - n_tiles - 1) / (kWGs - n_tiles));
+    if (lo < part) {
+      const uint32_t d = part - lo, p0 = lo, p1 = lo + d / 4, p2 = lo + d / 2;
+      const int4 n = sums<1>(m, static_cast<int>((nt + p0 - 1) / p0),
+                             static_cast<int>((nt + p1 - 1) / p1),
+                             static_cast<int>((nt + p2 - 1) / p2));
+      part = n.x <= kWGs ? p0 : n.y <= kWGs ? p1 : n.z <= kWGs ? p2 : part;
+    }
+    if (static_cast<int64_t>(part) * kKT * G > share + kNextPart * kKT * G) return false;
+    const uint32_t n = (nt + part - 1) / part;
+    int before = 0;
+    const int all = sums<2>(m, static_cast<int>(n), 0, 0, &before).x;
+    // (a part is a tile at least, so these rise; those of nt <= 2^24 tiles are below it)
+    const float each = static_cast<float>(nt) / static_cast<float>(max(n, 1u));
+    for (uint32_t j = 0; j < n; ++j)
+      m.begin[before + j] = pack_cut(tid, static_cast<int>(static_cast<float>(j) * each));
+    if (tid >= all && tid <= kWGs) m.begin[tid] = pack_cut(n_tiles, 0);
+    return true;
   }
 
+  // sums over the first kWGs threads, the same for all; before: of x, over the threads in front.
+  // USE: another number for each use (of its place in LDS)
+  template <int USE>
+  __device__ static int4 sums(PlanMem<SEQS>& m, int x, int y, int z, int* before = nullptr) {
+    const int wave = threadIdx.x / kWave;
+    int4 s = make_int4(wave_scan_add_i32(x), wave_scan_add_i32(y), wave_scan_add_i32(z), 0);
+    const int front = s.x - x;
+    if (threadIdx.x % kWave == kWave - 1 && threadIdx.x < kWGs) m.sums[USE][wave] = s;
+    __syncthreads();
+    s = make_int4(0, 0, 0, 0);
+    int b = front;
+    for (int w = 0; w < kWGs / kWave; ++w) {
+      const int4 t = m.sums[USE][w];
+      if (w < wave) b += t.x;
+      s = make_int4(s.x + t.x, s.y + t.y, s.z + t.z, 0);
+    }
+    if (before != nullptr) *before = b;
+    return make_int4(uniform(s.x), uniform(s.y), uniform(s.z), 0);
+  }
   // sum (or maximum) over the workgroup's threads, the same for all
   __device__ static int64_t reduce(PlanMem<SEQS>& m, int64_t x, bool maximum) {
     for (int off = 1; off < kWave; off <<= 1) {
@@ -305,16 +323,6 @@ struct Plan {
   }
   // where share w begins, lanes apart; before: the work in front of it in what is cut
   __device__ int64_t cut_of(int w, int64_t before) const {
-    if (even > 0) {
-      const int i = w / even;
-      if (i >= left) return pack_cut(n_tiles, 0);
-      const int2 t = find_tile(i % tiles_per_head);
-      const int4 q = mem->seq[t.x];
-      // (at most 2^24 tiles, fewer than 2^8 parts)
-      return pack_cut(i, static_cast<int>(static_cast<uint32_t>(tiles_of(t.y, q.y, q.z)) *
-                                          static_cast<uint32_t>(w - i * even) /
-                                          static_cast<uint32_t>(even)));
-    }
     const int64_t x = rounds > 0 ? rest + before : w * share;
     return x < total ? at(x) : pack_cut(n_tiles, 0);
   }
