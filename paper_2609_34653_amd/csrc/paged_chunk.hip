@@ -16,10 +16,11 @@
 //   shares    whole row tiles in rounds of kWGs, so that the workgroups of an XCD read the same keys at
 //             about the same time (L2 misses of 4 x 2,329 tokens over 10,521 keys: 36 M to 8 M); the
 //             rest is cut, whatever the lengths, into a share per workgroup that evens the rounds
-//             out.  The parts of a row tile that lies in several are merged by a second kernel, in share
-//             order, so results do not depend on timing.  Every workgroup works the cuts out by
-//             itself from q_start and ctx_len, so there is no plan launch.  The work of a row tile
-//             is counted in keys, linear in its number, so a cut is found by a square root.
+//             out; few row tiles are cut into parts of their own.  The parts of a row tile that lies in
+//             several are merged by a second kernel, in share order, so results do not depend on
+//             timing.  Every workgroup works all cuts out by itself from q_start and ctx_len, a
+//             thread each, so there is no plan launch.  The work of a row tile is counted in keys,
+//             linear in its number, so a cut is found by a square root.
 //   products  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: one query column per lane,
 //             so the row statistics are lane-local; keys are permuted when K rows are read so that S^T
 //             is the B operand of the second product as it stands.
@@ -36,8 +37,8 @@
 //
 // Measured (bf16, d = 128, 4 query heads per KV head, 8 KV heads, pages of 64, cache larger than L2):
 //   4 chunks of 2,329 tokens over 10,521 keys     1,330 us, 1.07 PFLOP/s
-//   one chunk of 665 tokens over 17,048 keys        199 us, 0.92 PFLOP/s (11 us of it the merge)
-//   89 tokens over 601 keys, 4 heads, d = 64         17 us (launches, plan and merge)
+//   one chunk of 665 tokens over 17,048 keys        195 us, 0.93 PFLOP/s (11 us of it the merge)
+//   89 tokens over 601 keys, 4 heads, d = 64         14 us (launches, plan, first pages and merge)
 #include <algorithm>
 #include <type_traits>
 
@@ -786,59 +787,77 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
   }
 }
 
-// Merges the row tiles whose parts lie in several shares, in share order: workgroup (share, slice)
-// takes kSlice rows of the row tile that the share ends, if it ends one begun earlier.
-constexpr int kSlice = 32;
+// One row (of D / 4 threads, four values each) from its parts, kBatch of them asked for at a time (8:
+// no better).
+template <int D>
+__device__ inline floatx4 merge_row(const Joined& j, const float* part_o, const float2* part_ml,
+                                    int row, int d4) {
+  constexpr int kBatch = 4;
+  float M = -INFINITY, den = 0.f;
+  floatx4 num = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < j.n_parts; p0 += kBatch) {
+    float2 ml[kBatch];
+    floatx4 ov[kBatch];
+#pragma unroll
+    for (int c = 0; c < kBatch; ++c) {
+      const int p = p0 + c;
+      const bool in = p < j.n_parts;
+      const int slot = p == 0 ? j.first_slot : 2 * (j.last_share - j.n_parts + 1 + p);
+      const size_t at = static_cast<size_t>(slot) * kRows + row;
+      ml[c] = in ? part_ml[at] : make_float2(-INFINITY, 0.f);
+      ov[c] = in ? *reinterpret_cast<const floatx4*>(part_o + at * D + 4 * d4)
+                 : floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    float cm = M;
+#pragma unroll
+    for (int c = 0; c < kBatch; ++c) {
+      cm = fmaxf(cm, ml[c].x);
+      if (ml[c].x == -INFINITY) ov[c] = floatx4{0.f, 0.f, 0.f, 0.f};   // (not written)
+    }
+    if (cm == -INFINITY) continue;
+    const float a = M == -INFINITY ? 0.f : exp2f(M - cm);
+    den *= a;
+    num *= a;
+#pragma unroll
+    for (int c = 0; c < kBatch; ++c) {
+      const float w = ml[c].x == -INFINITY ? 0.f : exp2f(ml[c].x - cm);
+      den = fmaf(w, ml[c].y, den);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) num[e] = fmaf(w, ov[c][e], num[e]);
+    }
+    M = cm;
+  }
+  return num * (den > 0.f ? 1.f / den : 0.f);
+}
+
+// Merges the row tiles whose parts lie in several shares, in share order: the workgroups of an XCD
+// (dealt round-robin) take those that end in the shares of that XCD, which wrote most of their parts
+// there, as many rows at a time as they have threads for.  Two workgroups per CU: a grid with one for
+// every slice of every share that may end a row tile takes 2 us longer to come to nothing where few do,
+// and a row tile of many parts (20 of 112 tokens over 3,127 keys) needs its slices small: 53 -> 32 us.
+constexpr int kMergeWGs = 512;
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_chunk_merge_kernel(
     const float* __restrict__ part_o, const float2* __restrict__ part_ml,
     const Joined* __restrict__ joined, int Hq, int Hkv, void* __restrict__ out, bool out_bf16) {
-  constexpr int TPR = D / 4, PER = kThreads / TPR;
-  // on the XCD that wrote the parts (201 -> 199 us for 665 tokens over 17,048 keys)
-  const Joined j = joined[(blockIdx.x % kNumXcd) * (kWGs / kNumXcd) + blockIdx.x / kNumXcd];
-  if (j.n_parts == 0) return;
+  constexpr int TPR = D / 4, PER = kThreads / TPR, kItems = kRows / PER;
+  constexpr int kShares = kWGs / kNumXcd;  // of an XCD
+  static_assert(kShares <= kWave);
+  const int lane = threadIdx.x & (kWave - 1);
+  const Joined* mine = joined + blockIdx.x % kNumXcd * kShares;
+  const uint64_t ends = __ballot(lane < kShares && mine[min(lane, kShares - 1)].n_parts > 0);
   const int G = Hq / Hkv;
-  const int d4 = threadIdx.x % TPR;
-  for (int r = static_cast<int>(threadIdx.x) / TPR; r < kSlice; r += PER) {
-    const int rt = blockIdx.y * kSlice + r, m = j.mt * kRows + rt;
-    if (m >= j.rows) return;
-    float M = -INFINITY, den = 0.f;
-    floatx4 num = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < j.n_parts; p0 += 4) {
-      float2 ml[4];
-      floatx4 ov[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int p = p0 + c;
-        const bool in = p < j.n_parts;
-        const int slot = p == 0 ? j.first_slot : 2 * (j.last_share - j.n_parts + 1 + p);
-        const size_t row = static_cast<size_t>(slot) * kRows + rt;
-        ml[c] = in ? part_ml[row] : make_float2(-INFINITY, 0.f);
-        ov[c] = in ? *reinterpret_cast<const floatx4*>(part_o + row * D + 4 * d4)
-                   : floatx4{0.f, 0.f, 0.f, 0.f};
-      }
-      float cm = M;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        cm = fmaxf(cm, ml[c].x);
-        if (ml[c].x == -INFINITY) ov[c] = floatx4{0.f, 0.f, 0.f, 0.f};   // (not written)
-      }
-      if (cm == -INFINITY) continue;
-      const float a = M == -INFINITY ? 0.f : exp2f(M - cm);
-      den *= a;
-      num *= a;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const float w = ml[c].x == -INFINITY ? 0.f : exp2f(ml[c].x - cm);
-        den = fmaf(w, ml[c].y, den);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) num[e] = fmaf(w, ov[c][e], num[e]);
-      }
-      M = cm;
-    }
-    const float inv = den > 0.f ? 1.f / den : 0.f;
+  for (int it = blockIdx.x / kNumXcd;; it += kMergeWGs / kNumXcd) {
+    uint64_t rest = ends;
+    for (int k = it / kItems; k > 0; --k) rest &= rest - 1;
+    if (rest == 0) return;
+    const Joined j = mine[__ffsll(static_cast<unsigned long long>(rest)) - 1];
+    const int row = it % kItems * PER + static_cast<int>(threadIdx.x) / TPR, m = j.mt * kRows + row;
+    const int d4 = threadIdx.x % TPR;
+    if (m >= j.rows) continue;
+    const floatx4 x = merge_row<D>(j, part_o, part_ml, row, d4);
     const size_t at = (static_cast<size_t>(j.q0 + m / G) * Hq + j.g * G + m % G) * D + 4 * d4;
-    store_row4(out, at, out_bf16, num * inv);
+    store_row4(out, at, out_bf16, x);
   }
 }
 
@@ -857,8 +876,8 @@ hipError_t launch_t(const PagedAttnArgs& a, hipStream_t stream) {
                      a.out, a.out_bf16, part_o, part_ml, joined, a.d_status);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_chunk_merge_kernel<D>), dim3(kWGs, kRows / kSlice), dim3(kThreads), 0,
-                     stream, part_o, part_ml, joined, a.n_q_heads, a.n_kv_heads, a.out, a.out_bf16);
+  hipLaunchKernelGGL((paged_chunk_merge_kernel<D>), dim3(kMergeWGs), dim3(kThreads), 0, stream,
+                     part_o, part_ml, joined, a.n_q_heads, a.n_kv_heads, a.out, a.out_bf16);
   return hipGetLastError();
 }
 
