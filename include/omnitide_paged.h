@@ -125,8 +125,9 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
  * omnitide_paged_chunk_attn -- grouped-query attention of a ragged batch of chunks over the pages:
  * omnitide_chunk_attn for sequences of different lengths.  For each token t of sequence s, at row
  * r = ctx_len[s] - (q_start[s + 1] - t), and query head h:
- *   out[t][h] = sum_j softmax_j(scale * <q[t][h], K_s[j][g]>) V_s[j][g],  g = h / (n_q_heads/n_kv_heads)
- *   over the sequence's rows j <= r (the chunk's own keys are in the pages already).
+ *   out[t][h] = sum_j softmax_j(scale * <q[t][h], K_s[j][g]>) V_s[j][g]
+ *   over the sequence's rows j <= r (the chunk's own keys are in the pages already), with
+ *   g = h / (n_q_heads / n_kv_heads).
  *   q           bf16 [n_tokens][n_q_heads][head_dim]
  *   out         the same of out_dtype (OMNITIDE_F32, or OMNITIDE_BF16: the float result rounded to
  *               nearest even)

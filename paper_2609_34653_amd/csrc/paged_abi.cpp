@@ -239,8 +239,11 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
   const Rows ki{k, n, n_kv_heads * d * eb, static_cast<size_t>(k_stride) * eb};
   const Rows vi{v, n, n_kv_heads * d * eb, static_cast<size_t>(v_stride) * eb};
   const Rows none{nullptr, 0, 0, 0};
-  const Rows qi = q == nullptr ? none : Rows{q, n, n_q_heads * d * eb, static_cast<size_t>(q_stride) * eb};
-  const Rows qo = q == nullptr ? none : Rows{q_out, n, n_q_heads * d * 2, static_cast<size_t>(q_out_stride) * 2};
+  const Rows qi = q == nullptr ? none
+                               : Rows{q, n, n_q_heads * d * eb, static_cast<size_t>(q_stride) * eb};
+  const Rows qo = q == nullptr
+                      ? none
+                      : Rows{q_out, n, n_q_heads * d * 2, static_cast<size_t>(q_out_stride) * 2};
   const Rows tab = flat(page_table, static_cast<size_t>(n_seq) * max_pages * 4);
   const Rows st = flat(q_start, (static_cast<size_t>(n_seq) + 1) * 4);
   const Rows cl = flat(ctx_len, static_cast<size_t>(n_seq) * 4), ps = flat(pos, n * 4);
@@ -280,11 +283,12 @@ bool decode_heads_ok(int n_q, int n_q_heads, int n_kv_heads) {
 }
 
 // The two attention calls: decode where q_start is null by design (n_q tokens per sequence).
-static int paged_attn_impl(bool decode, const void* q, const void* k_pool, const void* v_pool, int n_pages,
-              int page_size, const int32_t* page_table, int max_pages, const int32_t* q_start,
-              const int32_t* ctx_len, int n_seq, int n_tokens, int n_q, int n_q_heads,
-              int n_kv_heads, int head_dim, float scale, void* out, int out_dtype, void* workspace,
-              size_t workspace_bytes, int32_t* d_status, void* stream) {
+static int paged_attn_impl(bool decode, const void* q, const void* k_pool, const void* v_pool,
+                           int n_pages, int page_size, const int32_t* page_table, int max_pages,
+                           const int32_t* q_start, const int32_t* ctx_len, int n_seq, int n_tokens,
+                           int n_q, int n_q_heads, int n_kv_heads, int head_dim, float scale,
+                           void* out, int out_dtype, void* workspace, size_t workspace_bytes,
+                           int32_t* d_status, void* stream) {
   if (!all_set({k_pool, v_pool, page_table, ctx_len}) || (n_tokens != 0 && !all_set({q, out})))
     return OMNITIDE_E_NULL;
   if (!decode && q_start == nullptr) return OMNITIDE_E_NULL;

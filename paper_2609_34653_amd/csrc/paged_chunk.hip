@@ -4,9 +4,9 @@
 // row, one pass over the keys with a running reference and sum per row.
 //
 // What bounds it: the matrix cores.  4 d operations per query row and visible key, and at the clock
-// that the card holds under them the two products of random data reach about 1.1 PFLOP/s when nothing is
-// loaded at all (1.2 for a large matrix product; smooth data, which take less power, run a
-// sixth faster).  Bytes are few once the rows of a workgroup share each key.
+// that the card holds under them the two products of random data reach about 1.1 PFLOP/s when
+// nothing is loaded at all (1.2 for a large matrix product; smooth data, which take less power, run
+// a sixth faster).  Bytes are few once the rows of a workgroup share each key.
 //
 //   rows      the L * G query rows (position p, head g*G + r) of a sequence and KV head are flattened
 //             as m = p*G + r and tiled kRows = 8 waves x 32 per row tile: one workgroup per CU, two
@@ -53,8 +53,7 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKT = 64;                  // keys per tile
-constexpr int kNB = 1;                   // 32-row blocks per wave
-constexpr int kRows = kWaves * 32 * kNB; // query rows per row tile
+constexpr int kRows = kWaves * 32;       // query rows per row tile
 constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
 constexpr int kRing = 4;                 // tiles of each tensor in LDS
 constexpr int kNumXcd = 8;
@@ -127,9 +126,9 @@ struct Plan {
     const int64_t w = m * each + kRows / 2 * (static_cast<int64_t>(m) * (m + 1));
     // The last row tile may leave waves without rows, up to 1/20 less work each: 4 x 2,329 tokens
     // over 10,521 keys (4 waves in each last one) 1,440 us instead of 1,466, 665 tokens over 17,048
-    // keys 215 instead of 220.  Charged at twice that, what they cost where all row tiles are like them (8
-    // chunks over 16,384 keys: 206 us with 8 waves, 125 with 4), the latter takes 231: beside full
-    // workgroups, at the clock that those leave, they are not as fast.
+    // keys 215 instead of 220.  Charged at twice that, what they cost where all row tiles are like
+    // them (8 chunks over 16,384 keys: 206 us with 8 waves, 125 with 4), the latter takes 231: beside
+    // full workgroups, at the clock that those leave, they are not as fast.
     const int end = len * G;
     if (m == 0 || m * kRows < end) return w;
     const int waves = (end - (m - 1) * kRows + 31) >> 5;
@@ -468,23 +467,17 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       return true;
     };
 
-    int lim[kNB];                          // last visible key of this lane's rows
-    bool row_ok[kNB];
-    size_t orow[kNB];                      // their rows of q and out
-    bf16x8 qf[kNB][D / 16];
+    const int m = m0 + wave * 32 + col;    // this lane's row
+    const bool row_ok = m < L * G;
+    const int p = row_ok ? m / G : L - 1;
+    const int lim = kept + p;              // its last visible key
+    // its row of q and out
+    const size_t orow = static_cast<size_t>(sq.q0 + p) * Hq + g * G + (row_ok ? m % G : 0);
+    const uint16_t* qrow = q + orow * D;
+    bf16x8 qf[D / 16];
 #pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) {
-      const int m = m0 + (wave * kNB + nb) * 32 + col;
-      row_ok[nb] = m < L * G;
-      const int p = row_ok[nb] ? m / G : L - 1;
-      const int r = row_ok[nb] ? m % G : 0;
-      lim[nb] = kept + p;
-      orow[nb] = static_cast<size_t>(sq.q0 + p) * Hq + g * G + r;
-      const uint16_t* qrow = q + orow[nb] * D;
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c)
-        qf[nb][c] = __builtin_bit_cast(bf16x8, ld16(qrow + 16 * c + 8 * h));
-    }
+    for (int c = 0; c < D / 16; ++c)
+      qf[c] = __builtin_bit_cast(bf16x8, ld16(qrow + 16 * c + 8 * h));
 
     // Ids of the 64 pages from `window` on, one per lane.  The next 64 wait in LDS, put there by a
     // direct load when the window moved (a plain load would have the compiler wait for it, and so
@@ -550,19 +543,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       for (int cq = 0; cq < T::kCalls; ++cq) at_v[cq] = at_k[cq];
     };
 
-    floatx16 o[kNB][D / 32];
-    float m_run[kNB], l_run[kNB];
-    floatx16 sA[kNB], sB[kNB];             // scores of 32 keys, current and next in turn
-    bf16x8 pA[kNB][2], pB[kNB][2];         // probabilities of 32 keys: the operand of the products
+    floatx16 o[D / 32];
+    floatx16 sA = floatx16{}, sB;          // scores of 32 keys, current and next in turn
+    bf16x8 pA[2], pB[2];                   // probabilities of 32 keys: the operand of the products
+    float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) {
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) o[nb][dt] = floatx16{};
-      m_run[nb] = -INFINITY;
-      l_run[nb] = 0.f;
-      sA[nb] = floatx16{};
-      pB[nb][0] = pB[nb][1] = bf16x8{};
-    }
+    for (int dt = 0; dt < D / 32; ++dt) o[dt] = floatx16{};
+    pB[0] = pB[1] = bf16x8{};
     constexpr int NS = D / 16;             // slots of a step: K operands, and V operands
     // Operands read ahead, and their registers.  The next step's first ones are read after the ring
     // has turned in the middle, so no further ahead than half a step.  (3 of 8 instead of 2: 1,351 us
@@ -605,8 +592,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
       const bf16x8 ka = kop(lds0, c);
-#pragma unroll
-      for (int nb = 0; nb < kNB; ++nb) sA[nb] = mfma(ka, qf[nb][c], sA[nb]);
+      sA = mfma(ka, qf[c], sA);
     }
 
     // One step for 32 keys from key0 on, whose scores are in s_cur: their softmax, the scores of the
@@ -617,89 +603,72 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     // p_prev are zeros; the last one's next scores are of stale keys and not used.)
     const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
     bf16x8 ka[kOps], va[kOps];
-    auto step = [&](floatx16(&s_cur)[kNB], floatx16(&s_nxt)[kNB], bf16x8(&p_prev)[kNB][2],
-                    bf16x8(&p_cur)[kNB][2], uint32_t kb, uint32_t vb,
-                    uint32_t kn, uint32_t vn, int key0,
+    auto step = [&](floatx16& s_cur, floatx16& s_nxt, bf16x8(&p_prev)[2], bf16x8(&p_cur)[2],
+                    uint32_t kb, uint32_t vb, uint32_t kn, uint32_t vn, int key0,
                     auto middle) __attribute__((always_inline)) {
       if (key0 + 31 > full_lim) {
 #pragma unroll
-        for (int nb = 0; nb < kNB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (key0 + 16 * h + i > lim[nb]) s_cur[nb][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i)
+          if (key0 + 16 * h + i > lim) s_cur[i] = -INFINITY;
       }
-      constexpr int EPS = 16 / NS;         // exponentials per block and slot
-      float ls[kNB][2];
-#pragma unroll
-      for (int nb = 0; nb < kNB; ++nb) {
-        ls[nb][0] = ls[nb][1] = 0.f;
-        s_nxt[nb] = floatx16{};
-      }
+      constexpr int EPS = 16 / NS;         // exponentials per slot
+      float ls[2] = {0.f, 0.f};
+      s_nxt = floatx16{};
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         const bf16x8 kc = ka[i % kOps], vc = va[i % kOps];
         const int dt = i % (D / 32), cc = i / (D / 32);
+        float e[EPS];
+        s_nxt = mfma(kc, qf[i], s_nxt);
+        ka[(i + kAhead) % kOps] = i + kAhead < NS ? kop(kb, i + kAhead) : kop(kn, i + kAhead - NS);
 #pragma unroll
-        for (int nb = 0; nb < kNB; ++nb) {
-          float e[EPS];
-          s_nxt[nb] = mfma(kc, qf[nb][i], s_nxt[nb]);
-          if (nb == kNB - 1)
-            ka[(i + kAhead) % kOps] = i + kAhead < NS ? kop(kb, i + kAhead) : kop(kn, i + kAhead - NS);
+        for (int x = 0; x < EPS; ++x)
+          e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[i * EPS + x], scale_log2, -m_run));
+        __builtin_amdgcn_sched_barrier(0);
+        o[dt] = mfma(vc, p_prev[cc], o[dt]);
+        va[(i + kAhead) % kOps] = i + kAhead < NS ? vop(vb, i + kAhead) : vop(vn, i + kAhead - NS);
 #pragma unroll
-          for (int x = 0; x < EPS; ++x)
-            e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[nb][i * EPS + x], scale_log2, -m_run[nb]));
-          __builtin_amdgcn_sched_barrier(0);
-          o[nb][dt] = mfma(vc, p_prev[nb][cc], o[nb][dt]);
-          if (nb == kNB - 1)
-            va[(i + kAhead) % kOps] = i + kAhead < NS ? vop(vb, i + kAhead) : vop(vn, i + kAhead - NS);
-#pragma unroll
-          for (int x = 0; x < EPS; x += 2) {
-            const int at = i * EPS + x;
-            const bf16x2 pr = {static_cast<__bf16>(e[x]), static_cast<__bf16>(e[x + 1])};
-            p_cur[nb][at >> 3][at & 7] = pr[0];
-            p_cur[nb][at >> 3][(at & 7) + 1] = pr[1];
-            ls[nb][(at >> 1) & 1] =
-                __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls[nb][(at >> 1) & 1], false);
-          }
-          __builtin_amdgcn_sched_barrier(0);
+        for (int x = 0; x < EPS; x += 2) {
+          const int at = i * EPS + x;
+          const bf16x2 pr = {static_cast<__bf16>(e[x]), static_cast<__bf16>(e[x + 1])};
+          p_cur[at >> 3][at & 7] = pr[0];
+          p_cur[at >> 3][(at & 7) + 1] = pr[1];
+          ls[(at >> 1) & 1] =
+              __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls[(at >> 1) & 1], false);
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (i == NS / 2 - 1) {
           // (the first half's softmax is not to be put off to behind the branches in there)
-#pragma unroll
-          for (int nb = 0; nb < kNB; ++nb)
-            asm volatile("" : "+v"(p_cur[nb][0]), "+v"(ls[nb][0]), "+v"(ls[nb][1]));
+          asm volatile("" : "+v"(p_cur[0]), "+v"(ls[0]), "+v"(ls[1]));
           middle();
         }
       }
+      float lsum = ls[0] + ls[1];
+      if (__any(!(lsum < kSumLimit))) {
+        // exact maximum of the 32 keys, move the reference, rescale, recompute
+        float mx = -INFINITY;
 #pragma unroll
-      for (int nb = 0; nb < kNB; ++nb) {
-        float lsum = ls[nb][0] + ls[nb][1];
-        if (__any(!(lsum < kSumLimit))) {
-          // exact maximum of the 32 keys, move the reference, rescale, recompute
-          float mx = -INFINITY;
+        for (int x = 0; x < 16; ++x)
+          mx = fmaxf(mx, s_cur[x] == -INFINITY ? -INFINITY : s_cur[x] * scale_log2);
+        mx = max_halves(mx);
+        const float m_new = fmaxf(m_run, mx);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+        l_run *= alpha;
 #pragma unroll
-          for (int x = 0; x < 16; ++x)
-            mx = fmaxf(mx, s_cur[nb][x] == -INFINITY ? -INFINITY : s_cur[nb][x] * scale_log2);
-          mx = max_halves(mx);
-          const float m_new = fmaxf(m_run[nb], mx);
-          const float m_use = m_new == -INFINITY ? 0.f : m_new;
-          const float alpha = __builtin_amdgcn_exp2f(m_run[nb] - m_use);
-          l_run[nb] *= alpha;
+        for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
+        m_run = m_new;
+        lsum = 0.f;
 #pragma unroll
-          for (int dt = 0; dt < D / 32; ++dt) o[nb][dt] *= alpha;
-          m_run[nb] = m_new;
-          lsum = 0.f;
-#pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            const float sx = s_cur[nb][x];
-            const __bf16 p = static_cast<__bf16>(
-                sx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(sx, scale_log2, -m_use)));
-            p_cur[nb][x >> 3][x & 7] = p;
-            lsum += static_cast<float>(p);
-          }
+        for (int x = 0; x < 16; ++x) {
+          const float sx = s_cur[x];
+          const __bf16 p = static_cast<__bf16>(
+              sx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(sx, scale_log2, -m_use)));
+          p_cur[x >> 3][x & 7] = p;
+          lsum += static_cast<float>(p);
         }
-        l_run[nb] += lsum;
       }
+      l_run += lsum;
     };
 
     // In the middle of tile t's first step every wave is done with tile t-1; K(t+1) and V(t), asked for
@@ -750,38 +719,31 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
       const bf16x8 vc = vop(v_prev, i);
-#pragma unroll
-      for (int nb = 0; nb < kNB; ++nb)
-        o[nb][i % (D / 32)] = mfma(vc, pB[nb][i / (D / 32)], o[nb][i % (D / 32)]);
+      o[i % (D / 32)] = mfma(vc, pB[i / (D / 32)], o[i % (D / 32)]);
     }
 
     // ---- the part's result
+    const float l_tot = sum_halves(l_run);
+    if (row_ok && whole) {
+      const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
 #pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) {
-      const float l_tot = sum_halves(l_run[nb]);
-      if (!row_ok[nb]) continue;
-      if (whole) {
-        const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+      for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
+        for (int qd = 0; qd < 4; ++qd) {
+          const size_t at = orow * D + 32 * dt + 8 * qd + 4 * h;
+          const floatx4 x = {o[dt][4 * qd] * inv, o[dt][4 * qd + 1] * inv,
+                             o[dt][4 * qd + 2] * inv, o[dt][4 * qd + 3] * inv};
+          store_row4(out, at, out_bf16, x);
+        }
+    } else if (row_ok) {
+      const size_t at = static_cast<size_t>(slot) * kRows + wave * 32 + col;
 #pragma unroll
-          for (int qd = 0; qd < 4; ++qd) {
-            const size_t at = orow[nb] * D + 32 * dt + 8 * qd + 4 * h;
-            const floatx4 x = {o[nb][dt][4 * qd] * inv, o[nb][dt][4 * qd + 1] * inv,
-                               o[nb][dt][4 * qd + 2] * inv, o[nb][dt][4 * qd + 3] * inv};
-            store_row4(out, at, out_bf16, x);
-          }
-      } else {
-        const size_t prow_ = static_cast<size_t>(slot) * kRows + (wave * kNB + nb) * 32 + col;
+      for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-          for (int qd = 0; qd < 4; ++qd)
-            *reinterpret_cast<floatx4*>(part_o + prow_ * D + 32 * dt + 8 * qd + 4 * h) =
-                floatx4{o[nb][dt][4 * qd], o[nb][dt][4 * qd + 1], o[nb][dt][4 * qd + 2],
-                        o[nb][dt][4 * qd + 3]};
-        if (h == 0) part_ml[prow_] = make_float2(m_run[nb], l_tot);
-      }
+        for (int qd = 0; qd < 4; ++qd)
+          *reinterpret_cast<floatx4*>(part_o + at * D + 32 * dt + 8 * qd + 4 * h) =
+              floatx4{o[dt][4 * qd], o[dt][4 * qd + 1], o[dt][4 * qd + 2], o[dt][4 * qd + 3]};
+      if (h == 0) part_ml[at] = make_float2(m_run, l_tot);
     }
     if (!after_part()) break;
   }

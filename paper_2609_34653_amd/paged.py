@@ -230,7 +230,8 @@ def omnitide_paged_chunk_attn(q, k_pool, v_pool, page_table, q_start, ctx_len, s
     args = (_dev(q, "q", _BF16, q.numel()), kp, vp, n_pages, page, tab, max_pages,
             _dev(q_start, "q_start", _I32, n_seq + 1), ctx, n_seq, n, hq, hkv, d, scale,
             _out(out, q.numel()), _kv_dtype(out), *_ws(workspace), _status(d_status))
-    _check((_lib or lib()).omnitide_paged_chunk_attn(*args, _on(q, stream)), "omnitide_paged_chunk_attn")
+    _check((_lib or lib()).omnitide_paged_chunk_attn(*args, _on(q, stream)),
+           "omnitide_paged_chunk_attn")
 
 
 def omnitide_paged_decode_workspace_bytes(n_seq, n_q, max_ctx, n_q_heads, n_kv_heads,
@@ -253,4 +254,5 @@ def omnitide_paged_decode_attn(q, k_pool, v_pool, page_table, ctx_len, scale, ou
     args = (_dev(q, "q", _BF16, q.numel()), kp, vp, n_pages, page, tab, max_pages, ctx, n_seq, nq,
             hq, hkv, d, scale, _out(out, q.numel()), _kv_dtype(out), *_ws(workspace),
             _status(d_status))
-    _check((_lib or lib()).omnitide_paged_decode_attn(*args, _on(q, stream)), "omnitide_paged_decode_attn")
+    _check((_lib or lib()).omnitide_paged_decode_attn(*args, _on(q, stream)),
+           "omnitide_paged_decode_attn")
