@@ -75,16 +75,6 @@ __device__ inline uint64_t dpp_move_u64(uint64_t v) {
   const int hi = dpp_move<CTRL, ROW_MASK>(0, static_cast<int>(static_cast<uint32_t>(v >> 32)));
   return (static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo);
 }
-// Inclusive scan of a 64-bit value over the wave's lanes (modulo 2^64).
-__device__ inline uint64_t wave_scan_add_u64(uint64_t v) {
-  v += dpp_move_u64<kDppRowShr1, 0xf>(v);
-  v += dpp_move_u64<kDppRowShr2, 0xf>(v);
-  v += dpp_move_u64<kDppRowShr4, 0xf>(v);
-  v += dpp_move_u64<kDppRowShr8, 0xf>(v);
-  v += dpp_move_u64<kDppRowBcast15, 0xa>(v);
-  v += dpp_move_u64<kDppRowBcast31, 0xc>(v);
-  return v;
-}
 __device__ inline uint64_t wave_sum_u64(uint64_t v) {
   v += dpp_move_u64<kDppRowShr1, 0xf>(v);
   v += dpp_move_u64<kDppRowShr2, 0xf>(v);

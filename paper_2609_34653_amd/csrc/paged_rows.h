@@ -6,6 +6,17 @@
 
 namespace omnitide {
 
+// Inclusive scan of a 64-bit value over the wave's lanes (modulo 2^64).
+__device__ inline uint64_t wave_scan_add_u64(uint64_t v) {
+  v += dpp_move_u64<kDppRowShr1, 0xf>(v);
+  v += dpp_move_u64<kDppRowShr2, 0xf>(v);
+  v += dpp_move_u64<kDppRowShr4, 0xf>(v);
+  v += dpp_move_u64<kDppRowShr8, 0xf>(v);
+  v += dpp_move_u64<kDppRowBcast15, 0xa>(v);
+  v += dpp_move_u64<kDppRowBcast31, 0xc>(v);
+  return v;
+}
+
 // Sequence and row of a token.
 struct TokenRow {
   int seq, row;                          // seq < 0: the token belongs to no (valid) sequence
