@@ -10,8 +10,10 @@
  * omnitide_plan_spans + omnitide_compact_kv_spans (the span plan: recent units whole, boundary
  * tokens and sink prefixes of the image and audio spans of older units, a shared text budget,
  * oldest-first trimming, then compaction of the kept slots) and omnitide_decode_attn (decode
- * attention of the last few tokens over the compacted pool); omnitide_evict_native, omnitide_pack_suffix, omnitide_place_chunk and
- * omnitide_span_attn keep the native (logical-only) layout with holes instead.
+ * attention of the last few tokens over the compacted pool); omnitide_evict_native,
+ * omnitide_pack_suffix, omnitide_place_chunk and omnitide_span_attn keep the native (logical-only)
+ * layout with holes instead.  omnitide_paged.h declares the calls over a paged cache that streams
+ * of different lengths share.
  *
  * Conventions shared by every entry point
  *   - Array arguments are DEVICE pointers into memory the caller allocated (hipMalloc or a

@@ -132,9 +132,10 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
  *   out         the same of out_dtype (OMNITIDE_F32, or OMNITIDE_BF16: the float result rounded to
  *               nearest even)
  *   workspace   device scratch of omnitide_paged_chunk_attn_workspace_bytes() bytes (partial results
- *               of key ranges; may be NULL when that is 0).  The size never falls as any of its
- *               arguments but the head counts grows, so one for the largest batch serves smaller
- *               ones.  Calls that overlap in time need a workspace each.
+ *               of key ranges: 68 MB for head_dim 128, 35 MB for 64, whatever the batch; 0 and NULL
+ *               for n_tokens 0).  The size never falls as any of its arguments but the head
+ *               counts grows, so one for the largest batch serves smaller ones; nothing in it is
+ *               kept from call to call.  Calls that overlap in time need a workspace each.
  * The bytes of rows that are not in use are never used (they may hold anything, NaN included); those
  * of the rows in use are finite numbers.
  * Numerics: bf16 products with float accumulation, float softmax.  Limits: n_q_heads a multiple of

@@ -347,9 +347,9 @@ int omnitide_paged_chunk_attn(const void* q, const void* k_pool, const void* v_p
                               int n_tokens, int n_q_heads, int n_kv_heads, int head_dim,
                               float scale, void* out, int out_dtype, void* workspace,
                               size_t workspace_bytes, int32_t* d_status, void* stream) {
-  return paged_attn_impl(false, q, k_pool, v_pool, n_pages, page_size, page_table, max_pages, q_start,
-                   ctx_len, n_seq, n_tokens, 0, n_q_heads, n_kv_heads, head_dim, scale, out,
-                   out_dtype, workspace, workspace_bytes, d_status, stream);
+  return paged_attn_impl(false, q, k_pool, v_pool, n_pages, page_size, page_table, max_pages,
+                         q_start, ctx_len, n_seq, n_tokens, 0, n_q_heads, n_kv_heads, head_dim,
+                         scale, out, out_dtype, workspace, workspace_bytes, d_status, stream);
 }
 
 size_t omnitide_paged_chunk_attn_workspace_bytes(int n_tokens, int n_seq, int max_ctx,
@@ -369,9 +369,10 @@ int omnitide_paged_decode_attn(const void* q, const void* k_pool, const void* v_
                                int32_t* d_status, void* stream) {
   const int64_t tokens = static_cast<int64_t>(n_seq) * n_q;
   if (tokens < 0 || tokens > kMaxTokens) return OMNITIDE_E_SHAPE;
-  return paged_attn_impl(true, q, k_pool, v_pool, n_pages, page_size, page_table, max_pages, nullptr,
-                   ctx_len, n_seq, static_cast<int>(tokens), n_q, n_q_heads, n_kv_heads, head_dim,
-                   scale, out, out_dtype, workspace, workspace_bytes, d_status, stream);
+  return paged_attn_impl(true, q, k_pool, v_pool, n_pages, page_size, page_table, max_pages,
+                         nullptr, ctx_len, n_seq, static_cast<int>(tokens), n_q, n_q_heads,
+                         n_kv_heads, head_dim, scale, out, out_dtype, workspace, workspace_bytes,
+                         d_status, stream);
 }
 
 size_t omnitide_paged_decode_workspace_bytes(int n_seq, int n_q, int max_ctx, int n_q_heads,

@@ -204,3 +204,13 @@ def test_binding_refusals():
         pg.omnitide_qk_norm_rope(None, None, None, None, None)
     with pytest.raises(TypeError):
         pg.omnitide_qk_norm_rope(x.half(), None, None, x, None)
+
+
+def test_tensors_off_the_current_device(monkeypatch):
+    """Without a stream of theirs, tensors of another device are refused."""
+    class Tensor:
+        device = torch.device("cuda", 1)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="device 0 is the current one"):
+        pg._on(Tensor(), None)
+    assert pg._on(Tensor(), 1234) == 1234
