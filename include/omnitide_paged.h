@@ -139,7 +139,8 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
  * The bytes of rows that are not in use are never used (they may hold anything, NaN included); those
  * of the rows in use are finite numbers.
  * Numerics: bf16 products with float accumulation, float softmax.  Limits: n_q_heads a multiple of
- * n_kv_heads, n_seq <= 1024, n_seq * max_pages * page_size * n_kv_heads <= 2^34, scale finite.
+ * n_kv_heads, n_seq <= 1024, n_seq * max_pages * page_size * n_kv_heads <= 2^34, n_tokens * (n_q_heads / n_kv_heads)
+ * <= 2^28, |scale| <= 1e30 (of either sign).
  */
 int omnitide_paged_chunk_attn(const void* q, const void* k_pool, const void* v_pool, int n_pages,
                               int page_size, const int32_t* page_table, int max_pages,

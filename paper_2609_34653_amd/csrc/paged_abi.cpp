@@ -297,7 +297,7 @@ static int paged_attn_impl(bool decode, const void* q, const void* k_pool, const
   const int shift = page_shift_of(page_size);
   if (n_tokens < 0 || n_tokens > kMaxTokens || n_seq > kMaxAttnSeqs ||
       !paged_shape_ok(n_pages, max_pages, shift, n_seq) ||
-      !attn_heads_ok(n_q_heads, n_kv_heads, head_dim) || !std::isfinite(scale) ||
+      !attn_heads_ok(n_q_heads, n_kv_heads, head_dim) || !(std::fabs(scale) <= 1e30f) ||
       static_cast<int64_t>(n_tokens) * (n_q_heads / n_kv_heads) > (1 << 28) || !aligned16(q) ||
       !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(out) || !aligned16(workspace))
     return OMNITIDE_E_SHAPE;

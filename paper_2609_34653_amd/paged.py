@@ -7,8 +7,7 @@ failure; every step of the computation runs in the HIP kernels.
 Shapes: pools bf16 [n_pages, page_size, H_kv, d]; page_table int32 [n_seq, max_pages]; q_start
 int32 [n_seq + 1]; ctx_len int32 [n_seq].  Queries, keys and values of new tokens are [tokens, heads,
 d]; where a call takes row strides, parts of one fused projection (views whose heads are contiguous)
-can be passed.  Tensors of one call are on one device, the current one unless ``stream`` is a
-stream of theirs.
+can be passed.  Tensors of one call, and its ``stream`` if given, belong to the current device.
 """
 from __future__ import annotations
 
@@ -63,14 +62,12 @@ def lib() -> ctypes.CDLL:
 # ----------------------------------------------------------------------------- marshalling
 
 def _on(t, stream):
-    """The raw stream to launch on: `stream`, or the current one of t's device, which has to be the
-    current device."""
-    if stream is not None:
-        return _stream(stream)
+    """The raw stream to launch on: `stream`, or the current one; t has to be on the current
+    device."""
     dev = torch.cuda.current_device()
     if t.device.index != dev:
         raise ValueError(f"tensors on {t.device} while device {dev} is the current one")
-    return torch._C._cuda_getCurrentRawStream(dev)
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
 
 # As in ``omnitide``, a tensor in order takes one short path; a call passes up to 15 tensors, and a step

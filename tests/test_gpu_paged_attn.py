@@ -374,6 +374,19 @@ def both(decode, ctx, P, hq, hkv, d, seed, new=2):
 
 
 @pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("scale", [0.0, -0.2])
+def test_scales_that_are_not_positive(decode, scale):
+    """All keys alike, and the least score the likeliest; masked keys stay out."""
+    q, kp, vp, table, start, ctx = both(decode, [300, 65, 2], 16, 6, 2, 64, 9)
+    got, st = run(decode, q, kp, vp, table, start, ctx, scale, F32)
+    want, spread = op.ragged_attention(f64(q).reshape(6, 6, 64), f64(kp), f64(vp), table, start, ctx,
+                                       scale)
+    assert st == 0
+    # |scale| sum|q k| <= 0.2 x 100 on these inputs, as the docstring above has it
+    assert_near(got.view(6, 6, 64), want, spread, 2.0 ** -8, F32)
+
+
+@pytest.mark.parametrize("decode", [False, True])
 def test_sequences_share_pages(decode):
     """Three sequences with the same first pages, each with its own tail."""
     ctx, P, hq, hkv, d = [700, 650, 641], 64, 8, 2, 64

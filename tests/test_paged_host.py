@@ -152,7 +152,8 @@ def test_attention_refusals(L, call):
     assert call(L, od=2) == ot.E_DTYPE
     for bad in (dict(P=8), dict(P=100), dict(S=0), dict(S=1025), dict(mp=0), dict(np=0), dict(d=96),
                 dict(Hq=20), dict(Hkv=0), dict(Hkv=64, Hq=64), dict(scale=float("nan")),
-                dict(mp=1 << 24, P=128), dict(q=fake(0, 8)), dict(out=fake(6, 4))):
+                dict(mp=1 << 24, P=128), dict(q=fake(0, 8)), dict(out=fake(6, 4)),
+                dict(scale=float("inf")), dict(scale=-2e30)):
         assert call(L, **bad) == ot.E_SHAPE, bad
     for bad in (dict(out=fake(0)), dict(out=fake(1)), dict(out=fake(5)), dict(status=fake(3)),
                 dict(status=fake(6))):
@@ -207,10 +208,12 @@ def test_binding_refusals():
 
 
 def test_tensors_off_the_current_device(monkeypatch):
-    """Without a stream of theirs, tensors of another device are refused."""
+    """Tensors of another device than the current one are refused."""
     class Tensor:
         device = torch.device("cuda", 1)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    with pytest.raises(ValueError, match="device 0 is the current one"):
-        pg._on(Tensor(), None)
+    for stream in (None, 1234):
+        with pytest.raises(ValueError, match="device 0 is the current one"):
+            pg._on(Tensor(), stream)
+    Tensor.device = torch.device("cuda", 0)
     assert pg._on(Tensor(), 1234) == 1234
