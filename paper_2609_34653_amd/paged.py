@@ -64,8 +64,8 @@ def lib() -> ctypes.CDLL:
 def _on(t, stream):
     """The raw stream to launch on: `stream`, or the current one; t has to be on the current
     device."""
-    dev = torch.cuda.current_device()
-    if t.device.index != dev:
+    dev = torch._C._cuda_getDevice()
+    if t.get_device() != dev:
         raise ValueError(f"tensors on {t.device} while device {dev} is the current one")
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
@@ -114,6 +114,12 @@ def _theta(theta):
 
 def _pools(k_pool, v_pool):
     """(k address, v address, n_pages, page_size, H_kv, d)."""
+    if type(k_pool) is _T and type(v_pool) is _T:
+        shape = k_pool.shape
+        if (len(shape) == 4 and v_pool.shape == shape and k_pool.dtype is _BF16
+                and v_pool.dtype is _BF16 and k_pool.is_cuda and v_pool.is_cuda
+                and k_pool.is_contiguous() and v_pool.is_contiguous()):
+            return (k_pool.data_ptr(), v_pool.data_ptr(), *shape)
     if not (isinstance(k_pool, _T) and k_pool.dim() == 4):
         raise ValueError("k_pool must be [n_pages, page_size, H_kv, d]")
     shape = k_pool.shape
@@ -128,8 +134,12 @@ def _table(page_table, ctx_len):
     if not (isinstance(page_table, _T) and page_table.dim() == 2):
         raise ValueError("page_table must be [n_seq, max_pages]")
     n_seq, max_pages = page_table.shape
-    return (_dev(page_table, "page_table", _I32, n_seq * max_pages), max_pages,
-            _dev(ctx_len, "ctx_len", _I32, n_seq), n_seq)
+    if (type(page_table) is _T and page_table.dtype is _I32 and page_table.is_cuda
+            and page_table.is_contiguous()):
+        at = page_table.data_ptr()
+    else:
+        at = _dev(page_table, "page_table", _I32, n_seq * max_pages)
+    return at, max_pages, _dev(ctx_len, "ctx_len", _I32, n_seq), n_seq
 
 
 # ----------------------------------------------------------------------------------- calls

@@ -210,10 +210,13 @@ def test_binding_refusals():
 def test_tensors_off_the_current_device(monkeypatch):
     """Tensors of another device than the current one are refused."""
     class Tensor:
-        device = torch.device("cuda", 1)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+        device, index = "cuda:1", 1
+
+        def get_device(self):
+            return self.index
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     for stream in (None, 1234):
         with pytest.raises(ValueError, match="device 0 is the current one"):
             pg._on(Tensor(), stream)
-    Tensor.device = torch.device("cuda", 0)
+    Tensor.index = 0
     assert pg._on(Tensor(), 1234) == 1234
