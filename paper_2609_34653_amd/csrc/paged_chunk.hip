@@ -449,6 +449,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     const int slot = 2 * w + (i == static_cast<int>(begin >> 32) ? 0 : 1);
     const int m0 = mt * kRows;
     const int full_lim = kept + m0 / G;    // keys <= full_lim are visible to every row
+    const bool alone = L * G <= kRows;     // no other row tile reads these keys
     if (t_begin > 0 && t_end == nt && wave == 0) {
       // the row tile ends here: tell the merge where its parts are
       const int w0 = plan.first_share(i, w);
@@ -517,7 +518,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       }
     };
     // direct copy of one tensor's tile t into ring entry r
-    auto issue = [&](const uint8_t* head, const uint32_t (&offs)[T::kCalls],
+    auto issue = [&](auto once, const uint8_t* head, const uint32_t (&offs)[T::kCalls],
                      const int64_t (&at)[T::kCalls], int t, uint32_t dst) {
       const bool inside = (t + 1) * kKT <= ctx;
 #pragma unroll
@@ -527,15 +528,17 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
           const int first = t * kKT + (wave + kWaves * cq) * T::kCallKeys;
           off -= static_cast<uint32_t>(max(prow[cq] - (ctx - 1 - min(first, ctx - 1)), 0)) * row_bytes;
         }
-        dma16(head + at[cq], off, dst + static_cast<uint32_t>(cq * kWaves * kWave * 16));
+        const uint32_t to = dst + static_cast<uint32_t>(cq * kWaves * kWave * 16);
+        if constexpr (decltype(once)::value) dma16_once(head + at[cq], off, to);
+        else dma16(head + at[cq], off, to);
       }
     };
-    auto issue_k = [&](int t) {
+    auto issue_k = [&](auto once, int t) {
       locate(t);
-      issue(k_head, koff, at_k, t, lds_wave + ((t - t_begin) & (kRing - 1)) * (2u * T::kElems));
+      issue(once, k_head, koff, at_k, t, lds_wave + ((t - t_begin) & (kRing - 1)) * (2u * T::kElems));
     };
-    auto issue_v = [&](int t, const int64_t (&at)[T::kCalls]) {
-      issue(v_head, voff, at, t,
+    auto issue_v = [&](auto once, int t, const int64_t (&at)[T::kCalls]) {
+      issue(once, v_head, voff, at, t,
             lds_wave + (kRing + ((t - t_begin) & (kRing - 1))) * (2u * T::kElems));
     };
     auto keep = [&]() {
@@ -575,152 +578,158 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
-    asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
-    ask_pages(window + kWave);
-    issue_k(t_begin);
-    issue_v(t_begin, at_k);
-    if (t_begin + 1 < t_end) {
-      issue_k(t_begin + 1);
-      issue_v(t_begin + 1, at_k);
-    }
-    if (t_begin + 2 < t_end) issue_k(t_begin + 2);
-    keep();                                // at_v: of tile t+2 at tile t
-    // the first keys have landed; the others may be in flight (the ring's first turn waits for them)
-    if (t_begin + 2 < t_end) wait_vmcnt<4 * T::kCalls>();
-    else wait_vmcnt<0>();
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < NS; ++c) {
-      const bf16x8 ka = kop(lds0, c);
-      sA = mfma(ka, qf[c], sA);
-    }
-
-    // One step for 32 keys from key0 on, whose scores are in s_cur: their softmax, the scores of the
-    // next 32 keys and the product of the 32 keys before (probabilities p_prev), interleaved so that
-    // the vector units work while the matrix cores run: a wave issues in order.  The operands of its
-    // first kAhead slots are in ka and va; the later ones come from kb and vb, and the next step's
-    // first kAhead are read from kn and vn at its end.  `middle` is called half-way.  (The first step's
-    // p_prev are zeros; the last one's next scores are of stale keys and not used.)
-    const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-    bf16x8 ka[kOps], va[kOps];
-    auto step = [&](floatx16& s_cur, floatx16& s_nxt, bf16x8(&p_prev)[2], bf16x8(&p_cur)[2],
-                    uint32_t kb, uint32_t vb, uint32_t kn, uint32_t vn, int key0,
-                    auto middle) __attribute__((always_inline)) {
-      if (key0 + 31 > full_lim) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (key0 + 16 * h + i > lim) s_cur[i] = -INFINITY;
+    // The part's keys.  once: loaded as read once (nt), where that is so: 12% faster where memory is the
+    // bound (4 x 8 tokens over 33,000 keys 111 -> 98 us, 24 x 4 over 8,000 165 -> 145), neither faster
+    // nor slower elsewhere.
+    auto run = [&](auto once) __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
+      ask_pages(window + kWave);
+      issue_k(once, t_begin);
+      issue_v(once, t_begin, at_k);
+      if (t_begin + 1 < t_end) {
+        issue_k(once, t_begin + 1);
+        issue_v(once, t_begin + 1, at_k);
       }
-      constexpr int EPS = 16 / NS;         // exponentials per slot
-      float ls[2] = {0.f, 0.f};
-      s_nxt = floatx16{};
+      if (t_begin + 2 < t_end) issue_k(once, t_begin + 2);
+      keep();                                // at_v: of tile t+2 at tile t
+      // the first keys have landed; the others may be in flight (the ring's first turn waits for them)
+      if (t_begin + 2 < t_end) wait_vmcnt<4 * T::kCalls>();
+      else wait_vmcnt<0>();
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < NS; ++c) {
+        const bf16x8 ka = kop(lds0, c);
+        sA = mfma(ka, qf[c], sA);
+      }
+
+      // One step for 32 keys from key0 on, whose scores are in s_cur: their softmax, the scores of the
+      // next 32 keys and the product of the 32 keys before (probabilities p_prev), interleaved so that
+      // the vector units work while the matrix cores run: a wave issues in order.  The operands of its
+      // first kAhead slots are in ka and va; the later ones come from kb and vb, and the next step's
+      // first kAhead are read from kn and vn at its end.  `middle` is called half-way.  (The first step's
+      // p_prev are zeros; the last one's next scores are of stale keys and not used.)
+      const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+      bf16x8 ka[kOps], va[kOps];
+      auto step = [&](floatx16& s_cur, floatx16& s_nxt, bf16x8(&p_prev)[2], bf16x8(&p_cur)[2],
+                      uint32_t kb, uint32_t vb, uint32_t kn, uint32_t vn, int key0,
+                      auto middle) __attribute__((always_inline)) {
+        if (key0 + 31 > full_lim) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (key0 + 16 * h + i > lim) s_cur[i] = -INFINITY;
+        }
+        constexpr int EPS = 16 / NS;         // exponentials per slot
+        float ls[2] = {0.f, 0.f};
+        s_nxt = floatx16{};
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          const bf16x8 kc = ka[i % kOps], vc = va[i % kOps];
+          const int dt = i % (D / 32), cc = i / (D / 32);
+          float e[EPS];
+          s_nxt = mfma(kc, qf[i], s_nxt);
+          ka[(i + kAhead) % kOps] = i + kAhead < NS ? kop(kb, i + kAhead) : kop(kn, i + kAhead - NS);
+#pragma unroll
+          for (int x = 0; x < EPS; ++x)
+            e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[i * EPS + x], scale_log2, -m_run));
+          __builtin_amdgcn_sched_barrier(0);
+          o[dt] = mfma(vc, p_prev[cc], o[dt]);
+          va[(i + kAhead) % kOps] = i + kAhead < NS ? vop(vb, i + kAhead) : vop(vn, i + kAhead - NS);
+#pragma unroll
+          for (int x = 0; x < EPS; x += 2) {
+            const int at = i * EPS + x;
+            const bf16x2 pr = {static_cast<__bf16>(e[x]), static_cast<__bf16>(e[x + 1])};
+            p_cur[at >> 3][at & 7] = pr[0];
+            p_cur[at >> 3][(at & 7) + 1] = pr[1];
+            ls[(at >> 1) & 1] =
+                __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls[(at >> 1) & 1], false);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          if (i == NS / 2 - 1) {
+            // (the first half's softmax is not to be put off to behind the branches in there)
+            asm volatile("" : "+v"(p_cur[0]), "+v"(ls[0]), "+v"(ls[1]));
+            middle();
+          }
+        }
+        float lsum = ls[0] + ls[1];
+        if (__any(!(lsum < kSumLimit))) {
+          // exact maximum of the 32 keys, move the reference, rescale, recompute
+          float mx = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < 16; ++x)
+            mx = fmaxf(mx, s_cur[x] == -INFINITY ? -INFINITY : s_cur[x] * scale_log2);
+          mx = max_halves(mx);
+          const float m_new = fmaxf(m_run, mx);
+          const float m_use = m_new == -INFINITY ? 0.f : m_new;
+          const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+          l_run *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
+          m_run = m_new;
+          lsum = 0.f;
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const float sx = s_cur[x];
+            const __bf16 p = static_cast<__bf16>(
+                sx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(sx, scale_log2, -m_use)));
+            p_cur[x >> 3][x & 7] = p;
+            lsum += static_cast<float>(p);
+          }
+        }
+        l_run += lsum;
+      };
+
+      // In the middle of tile t's first step every wave is done with tile t-1; K(t+1) and V(t), asked for
+      // at tile t-2, have landed (what tile t-1 asked for may be in flight), which the second step
+      // needs; K(t+3) and V(t+2) are asked for, into the entries of K(t-1) and V(t-2).
+      auto turn_over = [&](int t) {
+        if (t + 2 < t_end) wait_vmcnt<2 * T::kCalls>();
+        else wait_vmcnt<0>();
+        asm volatile("s_barrier" ::: "memory");
+        if (t + 3 < t_end) {
+          issue_v(once, t + 2, at_v);
+          if ((min((t + 4) * kKT - 1, ctx - 1) >> b.page_shift) - window >= kWave) {
+            pages = checked(page_ids[wave][turn ^ 1][lane]);
+            window += kWave;
+            ask_pages(window + kWave);
+          }
+          issue_k(once, t + 3);
+          keep();
+        } else if (t + 2 < t_end) {
+          issue_v(once, t + 2, at_v);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      constexpr uint32_t kTileBytes = 2 * T::kElems, kHalfBytes = T::kElems;
+      const uint32_t v_ring = lds0 + kRing * kTileBytes;
+      int entry = 0;                                       // (t - t_begin) % kRing
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        ka[i] = kop(lds0 + kHalfBytes, i);
+        va[i] = vop(lds0, i);                // (the first step's zeros meet the first keys: numbers)
+      }
+      uint32_t v_prev = lds0;
+      if (m0 + wave * 32 >= L * G) {         // a wave without rows: its share of the copies
+        for (int t = t_begin; t < t_end; ++t) turn_over(t);
+        return;
+      }
+      for (int t = t_begin; t < t_end; ++t) {
+        const int next = (entry + 1) & (kRing - 1);
+        const uint32_t kt = lds0 + entry * kTileBytes, k1 = lds0 + next * kTileBytes;
+        const uint32_t vt = v_ring + entry * kTileBytes;
+        step(sA, sB, pB, pA, kt + kHalfBytes, v_prev, k1, vt, t * kKT, [&]() { turn_over(t); });
+        step(sB, sA, pA, pB, k1, vt, k1 + kHalfBytes, vt + kHalfBytes, t * kKT + 32, []() {});
+        v_prev = vt + kHalfBytes;
+        entry = next;
+      }
+      // the last 32 keys' product
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        const bf16x8 kc = ka[i % kOps], vc = va[i % kOps];
-        const int dt = i % (D / 32), cc = i / (D / 32);
-        float e[EPS];
-        s_nxt = mfma(kc, qf[i], s_nxt);
-        ka[(i + kAhead) % kOps] = i + kAhead < NS ? kop(kb, i + kAhead) : kop(kn, i + kAhead - NS);
-#pragma unroll
-        for (int x = 0; x < EPS; ++x)
-          e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[i * EPS + x], scale_log2, -m_run));
-        __builtin_amdgcn_sched_barrier(0);
-        o[dt] = mfma(vc, p_prev[cc], o[dt]);
-        va[(i + kAhead) % kOps] = i + kAhead < NS ? vop(vb, i + kAhead) : vop(vn, i + kAhead - NS);
-#pragma unroll
-        for (int x = 0; x < EPS; x += 2) {
-          const int at = i * EPS + x;
-          const bf16x2 pr = {static_cast<__bf16>(e[x]), static_cast<__bf16>(e[x + 1])};
-          p_cur[at >> 3][at & 7] = pr[0];
-          p_cur[at >> 3][(at & 7) + 1] = pr[1];
-          ls[(at >> 1) & 1] =
-              __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls[(at >> 1) & 1], false);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (i == NS / 2 - 1) {
-          // (the first half's softmax is not to be put off to behind the branches in there)
-          asm volatile("" : "+v"(p_cur[0]), "+v"(ls[0]), "+v"(ls[1]));
-          middle();
-        }
+        const bf16x8 vc = vop(v_prev, i);
+        o[i % (D / 32)] = mfma(vc, pB[i / (D / 32)], o[i % (D / 32)]);
       }
-      float lsum = ls[0] + ls[1];
-      if (__any(!(lsum < kSumLimit))) {
-        // exact maximum of the 32 keys, move the reference, rescale, recompute
-        float mx = -INFINITY;
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          mx = fmaxf(mx, s_cur[x] == -INFINITY ? -INFINITY : s_cur[x] * scale_log2);
-        mx = max_halves(mx);
-        const float m_new = fmaxf(m_run, mx);
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-        l_run *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
-        m_run = m_new;
-        lsum = 0.f;
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const float sx = s_cur[x];
-          const __bf16 p = static_cast<__bf16>(
-              sx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(sx, scale_log2, -m_use)));
-          p_cur[x >> 3][x & 7] = p;
-          lsum += static_cast<float>(p);
-        }
-      }
-      l_run += lsum;
     };
-
-    // In the middle of tile t's first step every wave is done with tile t-1; K(t+1) and V(t), asked for
-    // at tile t-2, have landed (what tile t-1 asked for may be in flight), which the second step
-    // needs; K(t+3) and V(t+2) are asked for, into the entries of K(t-1) and V(t-2).
-    auto turn_over = [&](int t) {
-      if (t + 2 < t_end) wait_vmcnt<2 * T::kCalls>();
-      else wait_vmcnt<0>();
-      asm volatile("s_barrier" ::: "memory");
-      if (t + 3 < t_end) {
-        issue_v(t + 2, at_v);
-        if ((min((t + 4) * kKT - 1, ctx - 1) >> b.page_shift) - window >= kWave) {
-          pages = checked(page_ids[wave][turn ^ 1][lane]);
-          window += kWave;
-          ask_pages(window + kWave);
-        }
-        issue_k(t + 3);
-        keep();
-      } else if (t + 2 < t_end) {
-        issue_v(t + 2, at_v);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    constexpr uint32_t kTileBytes = 2 * T::kElems, kHalfBytes = T::kElems;
-    const uint32_t v_ring = lds0 + kRing * kTileBytes;
-    int entry = 0;                                       // (t - t_begin) % kRing
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      ka[i] = kop(lds0 + kHalfBytes, i);
-      va[i] = vop(lds0, i);                // (the first step's zeros meet the first keys: numbers)
-    }
-    uint32_t v_prev = lds0;
-    if (m0 + wave * 32 >= L * G) {         // a wave without rows: its share of the copies
-      for (int t = t_begin; t < t_end; ++t) turn_over(t);
-      if (!after_part()) break;
-      continue;
-    }
-    for (int t = t_begin; t < t_end; ++t) {
-      const int next = (entry + 1) & (kRing - 1);
-      const uint32_t kt = lds0 + entry * kTileBytes, k1 = lds0 + next * kTileBytes;
-      const uint32_t vt = v_ring + entry * kTileBytes;
-      step(sA, sB, pB, pA, kt + kHalfBytes, v_prev, k1, vt, t * kKT, [&]() { turn_over(t); });
-      step(sB, sA, pA, pB, k1, vt, k1 + kHalfBytes, vt + kHalfBytes, t * kKT + 32, []() {});
-      v_prev = vt + kHalfBytes;
-      entry = next;
-    }
-    // the last 32 keys' product
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const bf16x8 vc = vop(v_prev, i);
-      o[i % (D / 32)] = mfma(vc, pB[i / (D / 32)], o[i % (D / 32)]);
-    }
+    if (alone) run(std::true_type{});
+    else run(std::false_type{});
 
     // ---- the part's result
     const float l_tot = sum_halves(l_run);
