@@ -578,8 +578,8 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
-    // The part's keys.  once: loaded as read once (nt), where that is so: 12% faster where memory is the
-    // bound (4 x 8 tokens over 33,000 keys 111 -> 98 us, 24 x 4 over 8,000 165 -> 145), neither faster
+    // The part's keys.  once: loaded as read once (nt), where that is so: 12% faster where memory is
+    // the bound (4 x 8 tokens over 33,000 keys 111 -> 98 us, 24 x 4 over 8,000 165 -> 145), neither faster
     // nor slower elsewhere.
     auto run = [&](auto once) __attribute__((always_inline)) {
       asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
@@ -603,11 +603,11 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       }
 
       // One step for 32 keys from key0 on, whose scores are in s_cur: their softmax, the scores of the
-      // next 32 keys and the product of the 32 keys before (probabilities p_prev), interleaved so that
-      // the vector units work while the matrix cores run: a wave issues in order.  The operands of its
-      // first kAhead slots are in ka and va; the later ones come from kb and vb, and the next step's
-      // first kAhead are read from kn and vn at its end.  `middle` is called half-way.  (The first step's
-      // p_prev are zeros; the last one's next scores are of stale keys and not used.)
+      // next 32 keys and the product of the 32 keys before (probabilities p_prev), interleaved so
+      // that the vector units work while the matrix cores run: a wave issues in order.  The operands
+      // of its first kAhead slots are in ka and va; the later ones come from kb and vb, and the next
+      // step's first kAhead are read from kn and vn at its end.  `middle` is called half-way.  (The
+      // first step's p_prev are zeros; the last one's next scores are of stale keys and not used.)
       const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
       bf16x8 ka[kOps], va[kOps];
       auto step = [&](floatx16& s_cur, floatx16& s_nxt, bf16x8(&p_prev)[2], bf16x8(&p_cur)[2],
@@ -678,9 +678,9 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         l_run += lsum;
       };
 
-      // In the middle of tile t's first step every wave is done with tile t-1; K(t+1) and V(t), asked for
-      // at tile t-2, have landed (what tile t-1 asked for may be in flight), which the second step
-      // needs; K(t+3) and V(t+2) are asked for, into the entries of K(t-1) and V(t-2).
+      // In the middle of tile t's first step every wave is done with tile t-1; K(t+1) and V(t), asked
+      // for at tile t-2, have landed (what tile t-1 asked for may be in flight), which the second
+      // step needs; K(t+3) and V(t+2) are asked for, into the entries of K(t-1) and V(t-2).
       auto turn_over = [&](int t) {
         if (t + 2 < t_end) wait_vmcnt<2 * T::kCalls>();
         else wait_vmcnt<0>();
