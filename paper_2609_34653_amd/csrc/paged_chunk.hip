@@ -559,22 +559,27 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     // instead of 1,373 for 4 x 2,329 tokens over 10,521 keys with 8 KV heads; 4: as 3.)
     constexpr int kAhead = NS / 2 < 3 ? NS / 2 : 3, kOps = 4;
     static_assert(kAhead <= NS / 2 && kAhead < kOps && NS % kOps == 0);
-    // K operand c of the 32 keys at LDS address kb; V operand i = (32 dims dt, 16 keys cc) of those at
-    // vb.  Rows are 2 D bytes apart and the swizzles act below that, so an operand's place is this
-    // lane's for the first with bits of its number flipped.
-    auto kop = [&](uint32_t kb, int c) {
+    // This lane's places in LDS of the K operands c and of the V operands of 32 dims dt, of the first 32
+    // keys of the tile that is read next; the other 32 keys are half a tile on.  Rows are 2 D bytes
+    // apart and the swizzles act below that, so they differ by bits of their number flipped.
+    constexpr uint32_t kTileBytes = 2 * T::kElems, kHalfBytes = T::kElems;
+    uint32_t kaddr[NS], vaddr[D / 32];
+#pragma unroll
+    for (int c = 0; c < NS; ++c) kaddr[c] = (lds0 + k_lane) ^ (32u * c);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) vaddr[dt] = (lds0 + v_lane) ^ (64u * dt);
+    // K operand c, and V operand i (32 dims i % (D / 32), 16 keys i / (D / 32)), of a half
+    auto kop = [&](int c, int half) __attribute__((always_inline)) {
       return __builtin_bit_cast(
           bf16x8, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
-                      (kb + k_lane) ^ (32u * c)));
+                      kaddr[c] + half * kHalfBytes));
     };
-    auto vop = [&](uint32_t vb, int i) {
+    auto vop = [&](int i, int half) __attribute__((always_inline)) {
       const int dt = i % (D / 32), cc = i / (D / 32);
-      const auto* vp = reinterpret_cast<__attribute__((address_space(3))) shortx4*>(
-          ((vb + v_lane) ^ (64u * dt)) + 16u * D * cc);
-      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          const_cast<__attribute__((address_space(3))) shortx4*>(vp));
-      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          const_cast<__attribute__((address_space(3))) shortx4*>(vp + D));
+      auto* vp = reinterpret_cast<__attribute__((address_space(3))) shortx4*>(
+          vaddr[dt] + (half * kHalfBytes + 16u * D * cc));
+      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vp);
+      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vp + D);
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
@@ -598,21 +603,34 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
       __syncthreads();
 #pragma unroll
       for (int c = 0; c < NS; ++c) {
-        const bf16x8 ka = kop(lds0, c);
+        const bf16x8 ka = kop(c, 0);
         sA = mfma(ka, qf[c], sA);
       }
 
       // One step for 32 keys from key0 on, whose scores are in s_cur: their softmax, the scores of the
       // next 32 keys and the product of the 32 keys before (probabilities p_prev), interleaved so
       // that the vector units work while the matrix cores run: a wave issues in order.  The operands
-      // of its first kAhead slots are in ka and va; the later ones come from kb and vb, and the next
-      // step's first kAhead are read from kn and vn at its end.  `middle` is called half-way.  (The
-      // first step's p_prev are zeros; the last one's next scores are of stale keys and not used.)
+      // of its first kAhead slots are in ka and va, and the next step's are read at its end.  A tile's
+      // first step reads the second halves of this tile's keys and the last one's values, its
+      // second step the first halves of the next tile's keys and this one's values: dk and dv bytes
+      // from the tiles before.  `middle` is called half-way.  (The first step's p_prev are zeros; the
+      // last one's next scores are of stale keys and not used.)
       const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
       bf16x8 ka[kOps], va[kOps];
-      auto step = [&](floatx16& s_cur, floatx16& s_nxt, bf16x8(&p_prev)[2], bf16x8(&p_cur)[2],
-                      uint32_t kb, uint32_t vb, uint32_t kn, uint32_t vn, int key0,
+      auto step = [&](auto second, floatx16& s_cur, floatx16& s_nxt, bf16x8(&p_prev)[2],
+                      bf16x8(&p_cur)[2], uint32_t dk, uint32_t dv, int key0,
                       auto middle) __attribute__((always_inline)) {
+        // operand j of this step and, from NS on, of the next one
+        auto next_k = [&](int j) __attribute__((always_inline)) {
+          const bool on = decltype(second)::value == (j < NS);     // of a new tile
+          if (on) kaddr[j % NS] += dk;
+          return kop(j % NS, on ? 0 : 1);
+        };
+        auto next_v = [&](int j) __attribute__((always_inline)) {
+          const bool on = decltype(second)::value == (j < NS);
+          if (on && j % NS < D / 32) vaddr[j % NS] += dv;
+          return vop(j % NS, on ? 0 : 1);
+        };
         if (key0 + 31 > full_lim) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -627,13 +645,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
           const int dt = i % (D / 32), cc = i / (D / 32);
           float e[EPS];
           s_nxt = mfma(kc, qf[i], s_nxt);
-          ka[(i + kAhead) % kOps] = i + kAhead < NS ? kop(kb, i + kAhead) : kop(kn, i + kAhead - NS);
+          ka[(i + kAhead) % kOps] = next_k(i + kAhead);
 #pragma unroll
           for (int x = 0; x < EPS; ++x)
             e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[i * EPS + x], scale_log2, -m_run));
           __builtin_amdgcn_sched_barrier(0);
           o[dt] = mfma(vc, p_prev[cc], o[dt]);
-          va[(i + kAhead) % kOps] = i + kAhead < NS ? vop(vb, i + kAhead) : vop(vn, i + kAhead - NS);
+          va[(i + kAhead) % kOps] = next_v(i + kAhead);
 #pragma unroll
           for (int x = 0; x < EPS; x += 2) {
             const int at = i * EPS + x;
@@ -699,32 +717,28 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         }
         __builtin_amdgcn_sched_barrier(0);
       };
-      constexpr uint32_t kTileBytes = 2 * T::kElems, kHalfBytes = T::kElems;
-      const uint32_t v_ring = lds0 + kRing * kTileBytes;
-      int entry = 0;                                       // (t - t_begin) % kRing
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        ka[i] = kop(lds0 + kHalfBytes, i);
-        va[i] = vop(lds0, i);                // (the first step's zeros meet the first keys: numbers)
+        ka[i] = kop(i, 1);
+        va[i] = vop(i, 1);                 // (the first step's zeros meet the first keys: numbers)
       }
-      uint32_t v_prev = lds0;
       if (m0 + wave * 32 >= L * G) {         // a wave without rows: its share of the copies
         for (int t = t_begin; t < t_end; ++t) turn_over(t);
         return;
       }
+      int entry = 0;                       // (t - t_begin) % kRing
+      uint32_t dv = kRing * kTileBytes;    // from the first keys to the first values
       for (int t = t_begin; t < t_end; ++t) {
-        const int next = (entry + 1) & (kRing - 1);
-        const uint32_t kt = lds0 + entry * kTileBytes, k1 = lds0 + next * kTileBytes;
-        const uint32_t vt = v_ring + entry * kTileBytes;
-        step(sA, sB, pB, pA, kt + kHalfBytes, v_prev, k1, vt, t * kKT, [&]() { turn_over(t); });
-        step(sB, sA, pA, pB, k1, vt, k1 + kHalfBytes, vt + kHalfBytes, t * kKT + 32, []() {});
-        v_prev = vt + kHalfBytes;
-        entry = next;
+        const uint32_t dk = entry < kRing - 1 ? kTileBytes : -(kRing - 1) * kTileBytes;
+        step(std::false_type{}, sA, sB, pB, pA, dk, dv, t * kKT, [&]() { turn_over(t); });
+        step(std::true_type{}, sB, sA, pA, pB, dk, dv, t * kKT + 32, []() {});
+        dv = dk;
+        entry = (entry + 1) & (kRing - 1);
       }
       // the last 32 keys' product
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        const bf16x8 vc = vop(v_prev, i);
+        const bf16x8 vc = vop(i, 1);
         o[i % (D / 32)] = mfma(vc, pB[i / (D / 32)], o[i % (D / 32)]);
       }
     };
