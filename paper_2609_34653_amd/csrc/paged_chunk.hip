@@ -555,9 +555,9 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     pB[0] = pB[1] = bf16x8{};
     constexpr int NS = D / 16;             // slots of a step: K operands, and V operands
     // Operands read ahead, and their registers.  The next step's first ones are read after the ring
-    // has turned in the middle, so no further ahead than half a step.  (3 of 8 instead of 2: 1,351 us
-    // instead of 1,373 for 4 x 2,329 tokens over 10,521 keys with 8 KV heads; 4: as 3.)
-    constexpr int kAhead = NS / 2 < 3 ? NS / 2 : 3, kOps = 4;
+    // has turned in the middle, so no further ahead than half a step.  (1: 1,445 us instead of 1,420
+    // for 4 x 2,329 tokens over 10,521 keys with 8 KV heads; 3: 1,425.)
+    constexpr int kAhead = 2, kOps = 4;
     static_assert(kAhead <= NS / 2 && kAhead < kOps && NS % kOps == 0);
     // This lane's places in LDS of the K operands c and of the V operands of 32 dims dt, of the first 32
     // keys of the tile that is read next; the other 32 keys are half a tile on.  Rows are 2 D bytes
@@ -641,21 +641,19 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         s_nxt = floatx16{};
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
+          // both products first, then vector work while the other wave's run (between the two: 1%
+          // slower; four products at once as well)
           const bf16x8 kc = ka[i % kOps], vc = va[i % kOps];
-          const int dt = i % (D / 32), cc = i / (D / 32);
-          float e[EPS];
           s_nxt = mfma(kc, qf[i], s_nxt);
+          o[i % (D / 32)] = mfma(vc, p_prev[i / (D / 32)], o[i % (D / 32)]);
           ka[(i + kAhead) % kOps] = next_k(i + kAhead);
-#pragma unroll
-          for (int x = 0; x < EPS; ++x)
-            e[x] = __builtin_amdgcn_exp2f(fmaf(s_cur[i * EPS + x], scale_log2, -m_run));
-          __builtin_amdgcn_sched_barrier(0);
-          o[dt] = mfma(vc, p_prev[cc], o[dt]);
           va[(i + kAhead) % kOps] = next_v(i + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int x = 0; x < EPS; x += 2) {
-            const int at = i * EPS + x;
-            const bf16x2 pr = {static_cast<__bf16>(e[x]), static_cast<__bf16>(e[x + 1])};
+          for (int at = i * EPS; at < (i + 1) * EPS; at += 2) {
+            const float e0 = __builtin_amdgcn_exp2f(fmaf(s_cur[at], scale_log2, -m_run));
+            const float e1 = __builtin_amdgcn_exp2f(fmaf(s_cur[at + 1], scale_log2, -m_run));
+            const bf16x2 pr = {static_cast<__bf16>(e0), static_cast<__bf16>(e1)};
             p_cur[at >> 3][at & 7] = pr[0];
             p_cur[at >> 3][(at & 7) + 1] = pr[1];
             ls[(at >> 1) & 1] =
