@@ -57,7 +57,8 @@ constexpr int kRows = kWaves * 32;       // query rows per row tile
 constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
 constexpr int kRing = 4;                 // tiles of each tensor in LDS
 constexpr int kNumXcd = 8;
-constexpr int kOverhead = 2 * kKT;       // what a row tile costs beside its keys, in keys
+constexpr int kOverhead = 4 * kKT;       // what a row tile costs before its keys, in keys
+constexpr int kLight = 10;               // what a wave without rows saves, in 1/256 of a tile
 constexpr int kMinShareTiles = 2;        // tiles of a share at least
 constexpr int kNextPart = 4;             // what the next part costs a workgroup, in tiles
 constexpr int kSnap = 2;                 // a cut this near to a row tile's end goes to the end
@@ -95,9 +96,9 @@ __device__ inline int64_t uniform(int64_t x) {
   return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
 }
 
-// x / y for 0 <= x, 0 < y: by a double quotient, which is off by one at most (x / y < 2^52).
-__device__ inline int64_t div64(int64_t x, int64_t y) {
-  int64_t q = static_cast<int64_t>(static_cast<double>(x) / static_cast<double>(y));
+// x / y for 0 <= x, 0 < y, x / y < 2^20: by a float quotient, which is off by one at most.
+__device__ inline int div_small(int64_t x, int64_t y) {
+  int q = static_cast<int>(static_cast<float>(x) / static_cast<float>(y));
   if (q * y > x) --q;
   if ((q + 1) * y <= x) ++q;
   return q;
@@ -124,15 +125,16 @@ struct Plan {
   __device__ int64_t work(int m, int kept, int len) const {
     const int64_t each = static_cast<int64_t>(G) * (kept + kOverhead);
     const int64_t w = m * each + kRows / 2 * (static_cast<int64_t>(m) * (m + 1));
-    // The last row tile may leave waves without rows, up to 1/20 less work each: 4 x 2,329 tokens
-    // over 10,521 keys (4 waves in each last one) 1,440 us instead of 1,466, 665 tokens over 17,048
-    // keys 215 instead of 220.  Charged at twice that, what they cost where all row tiles are like
-    // them (8 chunks over 16,384 keys: 206 us with 8 waves, 125 with 4), the latter takes 231: beside
-    // full workgroups, at the clock that those leave, they are not as fast.
+    // The last row tile may leave waves without rows.  Its tiles take 0.71 of a full one's cycles with 4
+    // waves of 8 and 0.66 with one, alone on its SIMD; counted as 0.84 and 0.80, since such shares
+    // are longer and wait for more keys at once (kLight 7: 195 us for 665 tokens over 17,048 keys, 10:
+    // 191, 13: 190, 18: 188.5; 8 ragged chunks 178, 180, 185, 184; seven of 275-517 tokens over
+    // 4,601-6,581 268, 267, 267, 277).
     const int end = len * G;
     if (m == 0 || m * kRows < end) return w;
     const int waves = (end - (m - 1) * kRows + 31) >> 5;
-    return w - ((each + m * kRows) * (13 * (kWaves - max(waves, 3))) >> 8);
+    const int64_t keys = static_cast<int64_t>(G) * kept + m * kRows;
+    return w - (keys * (kLight * (kWaves - max(waves, 3))) >> 8);
   }
   __device__ int tiles_of(int mt, int len, int ctx) const {
     const int last = static_cast<int>(static_cast<uint32_t>((mt + 1) * kRows - 1) /
@@ -277,12 +279,14 @@ struct Plan {
   }
   // sum (or maximum) over the workgroup's threads, the same for all
   __device__ static int64_t reduce(PlanMem<SEQS>& m, int64_t x, bool maximum) {
-    for (int off = 1; off < kWave; off <<= 1) {
-      const int64_t y = __shfl_xor(static_cast<long long>(x), off, kWave);
-      x = maximum ? max(x, y) : x + y;
+    if (maximum) {
+      for (int off = 1; off < kWave; off <<= 1)
+        x = max(x, static_cast<int64_t>(__shfl_xor(static_cast<long long>(x), off, kWave)));
+    } else {
+      x = static_cast<int64_t>(wave_scan_add_u64(static_cast<uint64_t>(x)));
     }
     __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0) m.wave_max[threadIdx.x / kWave] = x;
+    if ((threadIdx.x & (kWave - 1)) == kWave - 1) m.wave_max[threadIdx.x / kWave] = x;
     __syncthreads();
     int64_t r = m.wave_max[0];
     for (int w = 1; w < kWaves; ++w) r = maximum ? max(r, m.wave_max[w]) : r + m.wave_max[w];
@@ -328,7 +332,7 @@ struct Plan {
   }
   // the row tile and key tile at x units of work
   __device__ int64_t at(int64_t x) const {
-    const int g = static_cast<int>(div64(x, per_head));
+    const int g = div_small(x, per_head);
     const int64_t y = x - g * per_head;
     int s = 0;                             // the last sequence that begins at or before y
     for (int hi = n_seq - 1; s < hi;) {
@@ -338,17 +342,20 @@ struct Plan {
     }
     const int len = mem->seq[s].y, ctx = mem->seq[s].z, kept = ctx - len;
     const int64_t z = y - mem->chunk[s / kWave] - mem->first[s];
-    // kRows / 2 m^2 + bq m = z  (the last row tile's work may be less: z is then below this m's)
-    const double bq = static_cast<double>(G) * (kept + kOverhead) + kRows / 2;
-    const double root = sqrt(bq * bq + 2.0 * kRows * static_cast<double>(z));
+    // kRows / 2 m^2 + bq m = z, in float, then exactly (the last row tile's work may be less)
+    const float bq = static_cast<float>(G) * static_cast<float>(kept + kOverhead) + kRows / 2;
+    const float root = sqrtf(bq * bq + 2.f * kRows * static_cast<float>(z));
     const int most = row_tiles(len, G) - 1;
-    int m = min(max(static_cast<int>(2.0 * static_cast<double>(z) / (bq + root)), 0), most);
+    int m = min(static_cast<int>(2.f * static_cast<float>(z) / (bq + root)), most);
     while (m > 0 && work(m, kept, len) > z) --m;
     while (m < most && work(m + 1, kept, len) <= z) ++m;
-    const int64_t w0 = work(m, kept, len), w1 = work(m + 1, kept, len);
+    // its overhead comes before its keys
+    const int64_t w0 = work(m, kept, len) + static_cast<int64_t>(G) * kOverhead;
+    const int64_t w1 = work(m + 1, kept, len);
     const int nt = tiles_of(m, len, ctx);
-    const float part = static_cast<float>(z - w0) / static_cast<float>(w1 - w0);
-    const int tile = static_cast<int>(fminf(part, 1.f) * nt);
+    const float part = static_cast<float>(max(z - w0, static_cast<int64_t>(0))) /
+                       static_cast<float>(w1 - w0);
+    const int tile = static_cast<int>(fminf(part, 1.f) * static_cast<float>(nt));
     const int i = g * tiles_per_head + mem->chunk_tiles[s / kWave] + mem->seq[s].w + m;
     if (tile <= kSnap) return pack_cut(i, 0);
     if (tile >= nt - kSnap) return pack_cut(i + 1, 0);
