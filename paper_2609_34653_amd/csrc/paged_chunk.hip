@@ -36,7 +36,7 @@
 //             through a tile's first step, by one barrier per tile.
 //
 // Measured (bf16, d = 128, 4 query heads per KV head, 8 KV heads, pages of 64, cache larger than L2):
-//   4 chunks of 2,329 tokens over 10,521 keys     1,300-1,420 us by box, 1.0-1.1 PFLOP/s
+//   4 chunks of 2,329 tokens over 10,521 keys     1,300-1,420 us by card, 1.0-1.1 PFLOP/s
 //   one chunk of 665 tokens over 17,048 keys        188-217 us (11 us of it the merge)
 //   89 tokens over 601 keys, 4 heads, d = 64         14 us (launches, plan, first pages and merge)
 #include <algorithm>
