@@ -80,12 +80,15 @@ int page_shift_of(int page_size) {
   return -1;
 }
 
-// Rotary and norm arguments shared by the two calls; fills the launch arguments.
+// Head size, rotary and norm arguments shared by the two calls; fills the launch arguments (whose table
+// of pairs bounds rope_dims, whatever head sizes there are).
 int rope_args(const double* theta, int rope_dims, int rope_style, float magnitude, float eps,
               bool any_norm, int head_dim, NormRopeArgs& a) {
+  if (!head_dim_ok(head_dim)) return OMNITIDE_E_SHAPE;
   if (rope_dims != 0) {
     if (!(rope_style == OMNITIDE_ROPE_HALF || rope_style == OMNITIDE_ROPE_INTERLEAVED) ||
         rope_dims < 2 || rope_dims % 2 != 0 || rope_dims > head_dim ||
+        rope_dims > 2 * omnitide::kMaxRopePairs ||
         (rope_style == OMNITIDE_ROPE_HALF && rope_dims % 8 != 0) || !std::isfinite(magnitude))
       return OMNITIDE_E_SHAPE;
     for (int j = 0; j < rope_dims / 2; ++j) {
@@ -158,8 +161,7 @@ int omnitide_qk_norm_rope(const void* q, const void* k, int dtype, int n_tokens,
   const bool nq = q != nullptr && q_weight != nullptr, nk = k != nullptr && k_weight != nullptr;
   const int e = rope_args(theta, rope_dims, rope_style, magnitude, eps, nq || nk, head_dim, a);
   if (e != OMNITIDE_OK) return e;
-  if (n_tokens < 0 || n_tokens > kMaxTokens || !head_dim_ok(head_dim) ||
-      (n_tokens != 0 && rope_dims == 0 && !nq && !nk))
+  if (n_tokens < 0 || n_tokens > kMaxTokens || (n_tokens != 0 && rope_dims == 0 && !nq && !nk))
     return OMNITIDE_E_SHAPE;
   if (q != nullptr && (n_q_heads < 1 || n_q_heads > kMaxHeads ||
                        !stride_ok(q_stride, n_q_heads, head_dim, eb) ||
@@ -222,7 +224,7 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
   const int e = rope_args(theta, rope_dims, rope_style, magnitude, eps, nq || nk, head_dim, a);
   if (e != OMNITIDE_OK) return e;
   const int shift = page_shift_of(page_size);
-  if (n_tokens < 0 || n_tokens > kMaxTokens || !head_dim_ok(head_dim) || n_kv_heads < 1 ||
+  if (n_tokens < 0 || n_tokens > kMaxTokens || n_kv_heads < 1 ||
       static_cast<int64_t>(n_kv_heads) * head_dim > OMNITIDE_MAX_ROW_ELEMS ||
       !paged_shape_ok(n_pages, max_pages, shift, n_seq) ||
       !stride_ok(k_stride, n_kv_heads, head_dim, eb) ||

@@ -129,6 +129,19 @@ def test_append_refusals(L):
     assert ap(L, n=0) == ot.OK and ap(L, n=0, k=None, v=None, q=None, qo=None) == ot.OK
 
 
+@pytest.mark.parametrize("d", [256, 192, 1 << 20])
+@pytest.mark.parametrize("style", [0, 1])
+def test_heads_and_rotations_beyond_the_table(L, d, style):
+    """Head sizes that are not offered, rotated as a whole: refused before a frequency is copied (the
+    launch arguments hold those of 128 dimensions)."""
+    R = min(d, 256)
+    theta = (ctypes.c_double * (R // 2))(*[0.5] * (R // 2))
+    for r in (R, 136):
+        rot = dict(th=ctypes.cast(theta, P), R=r, style=style, d=d)
+        assert nr(L, qs=32 * d, ks=8 * d, qos=32 * d, kos=8 * d, **rot) == ot.E_SHAPE
+        assert ap(L, ks=8 * d, vs=8 * d, qs=32 * d, qos=32 * d, **rot) == ot.E_SHAPE
+
+
 def chunk(L, **kw):
     a = dict(q=fake(0), kp=fake(1), vp=fake(2), np=300, P=64, tab=fake(3), mp=270, st=fake(4),
              ctx=fake(5), S=3, n=700, Hq=32, Hkv=8, d=128, scale=0.1, out=fake(6), od=0, ws=fake(7),
