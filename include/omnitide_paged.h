@@ -30,7 +30,10 @@
  *   Device checks: OMNITIDE_E_PAGES for offsets out of order or a page id outside [0, n_pages)
  *   among the entries in use; OMNITIDE_E_CAPACITY for a sequence whose ctx_len is below its number
  *   of tokens or above max_pages * page_size (its tokens' outputs are then not written, nor its
- *   rows).  Limits: n_seq >= 1, max_pages >= 1, max_pages * page_size <= 2^30,
+ *   rows).  A page whose id is bad is neither read nor written, and no other one in its place: a new
+ *   token whose row lies there leaves the pools and q_out as they were, and the attention outputs of
+ *   the tokens that see a row of it are NaN, whether d_status is given or not; the other tokens', of
+ *   the same sequence too, are right.  Limits: n_seq >= 1, max_pages >= 1, max_pages * page_size <= 2^30,
  *   n_tokens <= 2^24, head_dim in {64, 128}, n_kv_heads * head_dim <= 4096.  A call with n_tokens 0
  *   does nothing (its per-token pointers may be NULL).
  */

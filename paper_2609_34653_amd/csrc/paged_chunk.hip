@@ -498,14 +498,23 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
            lds_addr(&page_ids[wave][turn][0]));
       turn ^= 1;
     };
-    auto checked = [&](int p) {
-      if (p < 0 || p >= b.n_pages) {
-        set_status(status, OMNITIDE_E_PAGES);
-        p = 0;
+    // A bad page spoils every row that sees it (below).  The rows that do not have its keys masked, but
+    // meet its values with probabilities of zero, so the page in front of it, all of whose rows are
+    // in use, stands in its place; before the part's first page there is none, nor a row that sees
+    // keys of the part and not this page.
+    int bad_row = INT32_MAX;               // the first row of the part's first bad page
+    auto checked = [&](int p, int before) {
+      const uint64_t bad = __ballot(p < 0 || p >= b.n_pages);
+      if (bad != 0) {
+        const int l = __ffsll(static_cast<unsigned long long>(bad)) - 1;
+        if (lane == 0) set_status(status, OMNITIDE_E_PAGES);
+        bad_row = min(bad_row, (window + l) << b.page_shift);
+        const int good = l > 0 ? readlane(p, l - 1) : before;
+        p = lane < l ? p : good;
       }
       return p;
     };
-    int pages = checked(table[min(window + lane, last_page)]);
+    int pages = checked(table[min(window + lane, last_page)], 0);
     const uint8_t* k_head = reinterpret_cast<const uint8_t*>(k) + 2 * g * D;
     const uint8_t* v_head = reinterpret_cast<const uint8_t*>(v) + 2 * g * D;
     // byte offset of each call's first key of tile t in a head's pool; the calls of a tile that
@@ -711,8 +720,8 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         if (t + 3 < t_end) {
           issue_v(once, t + 2, at_v);
           if ((min((t + 4) * kKT - 1, ctx - 1) >> b.page_shift) - window >= kWave) {
-            pages = checked(page_ids[wave][turn ^ 1][lane]);
             window += kWave;
+            pages = checked(page_ids[wave][turn ^ 1][lane], readlane(pages, kWave - 1));
             ask_pages(window + kWave);
           }
           issue_k(once, t + 3);
@@ -751,9 +760,11 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     else run(std::false_type{});
 
     // ---- the part's result
-    const float l_tot = sum_halves(l_run);
+    // (a sum that is no number spoils the row to the end)
+    const bool spoilt = lim >= bad_row;
+    const float l_tot = spoilt ? __builtin_nanf("") : sum_halves(l_run);
     if (row_ok && whole) {
-      const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+      const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -771,7 +782,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         for (int qd = 0; qd < 4; ++qd)
           *reinterpret_cast<floatx4*>(part_o + at * D + 32 * dt + 8 * qd + 4 * h) =
               floatx4{o[dt][4 * qd], o[dt][4 * qd + 1], o[dt][4 * qd + 2], o[dt][4 * qd + 3]};
-      if (h == 0) part_ml[at] = make_float2(m_run, l_tot);
+      if (h == 0) part_ml[at] = make_float2(spoilt ? 0.f : m_run, l_tot);
     }
     if (!after_part()) break;
   }
@@ -817,7 +828,7 @@ __device__ inline floatx4 merge_row(const Joined& j, const float* part_o, const 
     }
     M = cm;
   }
-  return num * (den > 0.f ? 1.f / den : 0.f);
+  return num * (den == 0.f ? 0.f : 1.f / den);
 }
 
 // Merges the row tiles whose parts lie in several shares, in share order: the workgroups of an XCD

@@ -205,19 +205,25 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
         qf[kc] = __builtin_bit_cast(bf16x8, w);
       }
     }
-    const int n_it = (b1 - b0 - wave + kWaves - 1) / kWaves;    // this wave's blocks
+    int n_it = (b1 - b0 - wave + kWaves - 1) / kWaves;          // this wave's blocks
+    int bad_row = INT32_MAX;                 // the first row of this wave's first block of a bad page
     const int32_t* table = b.table + static_cast<size_t>(seq) * b.max_pages;
     int pages = 0;                           // page of block it, in lane it % 64
+    auto block_of = [&](int it) { return b0 + wave + kWaves * it; };
+    // A block of a bad page is the wave's end: the vectors that see it are spoilt (below), and the others
+    // see no later one either, so nothing is read in its place.
     auto load_pages = [&](int it) {
       const int i = it + lane;
-      int p = i < n_it ? table[((b0 + wave + kWaves * i) * kKB) >> b.page_shift] : 0;
-      if (p < 0 || p >= b.n_pages) {
-        set_status(status, OMNITIDE_E_PAGES);
-        p = 0;
+      const bool in = i < n_it;
+      const int p = in ? table[(block_of(i) * kKB) >> b.page_shift] : 0;
+      const uint64_t bad = __ballot(in && (p < 0 || p >= b.n_pages));
+      if (bad != 0) {
+        if (lane == 0) set_status(status, OMNITIDE_E_PAGES);
+        n_it = it + __ffsll(static_cast<unsigned long long>(bad)) - 1;
+        bad_row = block_of(n_it) * kKB;
       }
       pages = p;
     };
-    auto block_of = [&](int it) { return b0 + wave + kWaves * it; };
     // issue block `it` into ring entry e
     auto issue = [&](int it, int e) {
       const int key0 = block_of(it) * kKB;
@@ -327,11 +333,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
           }
           // the reads of this entry have returned before it is filled again
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          issue(it + RING, e);
+          if (it + RING < n_it) issue(it + RING, e);
         }
       }
     }
 
+    if (lim >= bad_row) {                    // a sum that is no number spoils the column to the end
+      m_run = 0.f;
+      l_run = __builtin_nanf("");
+    }
     // merge the waves: per column the reference, the sum over the four lane groups, and O^T
     const float l_col = l_run + __shfl_xor(l_run, 16, kWave) + __shfl_xor(l_run, 32, kWave) +
                         __shfl_xor(l_run, 48, kWave);
@@ -366,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
       if (whole) {
         const size_t at =
             ((static_cast<size_t>(seq) * nq + qi / G) * Hq + g * G + qi % G) * D + d;
-        const float x = den > 0.f ? num / den : 0.f;
+        const float x = den == 0.f ? 0.f : num / den;
         if (out_bf16) static_cast<__bf16*>(out)[at] = static_cast<__bf16>(x);
         else static_cast<float*>(out)[at] = x;
       } else {
@@ -458,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void paged_decode_merge_kernel(
     d1 = fmaf(w, sml[t].y, d1);
   }
   const size_t at = static_cast<size_t>(row) * D + tid;
-  const float x = d1 > 0.f ? n1 / d1 : 0.f;
+  const float x = d1 == 0.f ? 0.f : n1 / d1;
   if (out_bf16) static_cast<__bf16*>(out)[at] = static_cast<__bf16>(x);
   else static_cast<float*>(out)[at] = x;
 }

@@ -226,6 +226,50 @@ def test_device_refusals(decode, what):
         assert torch.isnan(got[2:]).all()                    # not written
 
 
+BAD_PAGES = [
+    # (decode, ctx, new, page, hq, hkv, d, (sequence, page of it, id) ...)
+    (True, [300, 498], [4, 4], 16, 4, 1, 64, (1, 31, -1)),            # seen by the last two tokens
+    (True, [90, 2000, 40], [1, 1, 1], 16, 16, 2, 128, (1, 0, 1 << 30), (2, 2, -(1 << 31))),
+    (True, [12000, 700], [2, 2], 64, 32, 8, 128, (0, 100, -5)),       # in one of many shares
+    (True, [3000, 64], [8, 8], 256, 8, 8, 64, (0, 10, 1 << 20), (0, 11, 1 << 20)),
+    (False, [1500, 200], [700, 30], 16, 8, 8, 64, (0, 70, -1)),       # among the second 64 pages
+    (False, [1500, 200], [700, 30], 16, 8, 8, 128, (0, 64, 1 << 30)),         # the first of them
+    (False, [1500, 200], [700, 30], 16, 8, 8, 64, (0, 63, -1), (0, 64, -1), (1, 0, -7)),
+    (False, [6000, 77], [40, 5], 16, 4, 1, 64, (0, 373, -1)),         # short parts
+    (False, [6000, 77], [40, 5], 16, 4, 1, 128, (0, 200, -1)),        # all tokens, in one part
+    (False, [1000, 900], [600, 1], 256, 8, 2, 128, (0, 2, 1 << 30)),
+    (False, [1400, 1390], [700, 710], 16, 32, 16, 128, (1, 80, -1)),  # whole row tiles
+    (False, [130, 129, 64], [130, 129, 64], 64, 4, 2, 64, (0, 1, -1), (1, 2, -1)),
+]
+
+
+@pytest.mark.parametrize("case", range(len(BAD_PAGES)))
+def test_rows_of_a_bad_page(case):
+    """Tokens that see a row of a page that is not there come out as NaN; every other one, of the same
+    sequence too, comes out right: no other page's rows are attended to in its place."""
+    from paper_2609_34653_amd import paged as pg
+    decode, ctx, new, P, hq, hkv, d, *bad = BAD_PAGES[case]
+    table, n_pages = layout(ctx, P, case)
+    kp, vp = pools(ctx, table, n_pages, P, hkv, d, case)
+    start = np.concatenate([[0], np.cumsum(new)])
+    q = torch.randn(int(start[-1]), hq, d, generator=torch.Generator().manual_seed(case)).to(BF)
+    want, spread = op.ragged_attention(f64(q), f64(kp), f64(vp), table, start, ctx, d ** -0.5)
+    spoilt = np.zeros(len(q), bool)
+    for s, page, no in bad:
+        table[s, page] = no
+        row = ctx[s] - new[s] + np.arange(new[s])
+        spoilt[start[s]:start[s + 1]] |= row >= page * P
+    assert spoilt.any() and not spoilt.all()
+    for dtype in (F32, BF):
+        got, st = run(decode, (q.view(len(ctx), -1, hq, d) if decode else q).cuda(), kp.cuda(),
+                      vp.cuda(), table, start, ctx, d ** -0.5, dtype)
+        assert st == pg.E_PAGES
+        got = got.view(want.shape)
+        assert torch.isnan(got[torch.from_numpy(spoilt).cuda()]).all()
+        keep = torch.from_numpy(~spoilt).cuda()
+        assert_near(got[keep], want[~spoilt], spread[~spoilt], 2.0 ** -8, dtype)
+
+
 @pytest.mark.parametrize("decode", [False, True])
 def test_past_four_gigabytes(decode):
     """Pages whose byte offset passes 32 bits, and their order reversed."""
