@@ -27,8 +27,8 @@
  *               ctx_len[s] - (q_start[s + 1] - t).  0 <= q_start[0] <= ... <= q_start[n_seq] <=
  *               n_tokens; a sequence may have no token.  Tokens in front of q_start[0] and from
  *               q_start[n_seq] on (a padded batch) are neither read nor written anywhere.
- *   Device checks: OMNITIDE_E_PAGES for offsets out of order or a page id outside [0, n_pages)
- *   among the entries in use; OMNITIDE_E_CAPACITY for a sequence whose ctx_len is below its number
+ *   Device checks: OMNITIDE_E_PAGES for offsets out of order (of sequences that then overlap, one at
+ *   most has a token) or a page id outside [0, n_pages) among the entries in use; OMNITIDE_E_CAPACITY for a sequence whose ctx_len is below its number
  *   of tokens or above max_pages * page_size (its tokens' outputs are then not written, nor its
  *   rows).  A page whose id is bad is neither read nor written, and no other one in its place: a new
  *   token whose row lies there leaves the pools and q_out as they were, and the attention outputs of

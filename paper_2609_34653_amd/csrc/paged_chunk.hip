@@ -159,7 +159,16 @@ struct Plan {
         s1 = b.q_start[i + 1];
         n = b.ctx_len[i];
       }
-      const bool ok = s0 >= 0 && s1 > s0 && s1 <= b.n_tokens && n >= s1 - s0 && n <= cap;
+      // No token has two sequences: one that starts in front of an earlier offset has none (or offsets
+      // out of order would give the call many times the work and the counts here no bound).
+      int front = 0;
+      if (__any(s1 < s0)) front = wave_exclusive_max_i32(s0, 0);
+      if (c > 0) {
+        int before = 0;
+        for (int j = lane; j < c * kWave; j += kWave) before = max(before, b.q_start[j]);
+        front = max(front, wave_max_i32(before));
+      }
+      const bool ok = s0 >= front && s1 > s0 && s1 <= b.n_tokens && n >= s1 - s0 && n <= cap;
       const int len = ok ? s1 - s0 : 0;
       const int rt = row_tiles(len, G);
       const int64_t w = work(rt, n - len, len);

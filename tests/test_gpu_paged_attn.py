@@ -226,6 +226,31 @@ def test_device_refusals(decode, what):
         assert torch.isnan(got[2:]).all()                    # not written
 
 
+@pytest.mark.parametrize("start", [[0, 7, 3, 9], [0, 5, 0, 5, 0, 5], [2, 1 << 30, 3, 4], [-3, 4, 8],
+                                   [0] + 99 * [6] + [2] + 39 * [8]], ids=len)
+def test_overlapping_offsets(start):
+    """A sequence that starts in front of an earlier offset has no tokens: no output is written by two,
+    and the work is bounded by the tokens."""
+    from paper_2609_34653_amd import paged as pg
+    n_seq, T, hq, hkv, d, P = len(start) - 1, 9, 4, 2, 64, 16
+    ctx = [40 + 3 * (i % 7) for i in range(n_seq)]
+    table, n_pages = layout(ctx, P, n_seq)
+    kp, vp = pools(ctx, table, n_pages, P, hkv, d, n_seq)
+    q = torch.randn(T, hq, d, generator=torch.Generator().manual_seed(n_seq)).to(BF)
+    got, st = run(False, q.cuda(), kp.cuda(), vp.cuda(), table, start, ctx, 0.125, F32)
+    assert st == pg.E_PAGES
+    written, top = np.zeros(T, bool), 0
+    for s in range(n_seq):
+        a, b = start[s:s + 2]
+        if top <= a < b <= T:
+            want, spread = op.ragged_attention(f64(q[a:b]), f64(kp), f64(vp), table[s:s + 1],
+                                               [0, b - a], [ctx[s]], 0.125)
+            assert_near(got[a:b], want, spread, 2.0 ** -8, F32)
+            written[a:b] = True
+        top = max(top, a)
+    assert torch.isnan(got[torch.from_numpy(~written).cuda()]).all()
+
+
 BAD_PAGES = [
     # (decode, ctx, new, page, hq, hkv, d, (sequence, page of it, id) ...)
     (True, [300, 498], [4, 4], 16, 4, 1, 64, (1, 31, -1)),            # seen by the last two tokens
