@@ -233,3 +233,71 @@ def test_tensors_off_the_current_device(monkeypatch):
             pg._on(Tensor(), stream)
     Tensor.index = 0
     assert pg._on(Tensor(), 1234) == 1234
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that says it is on device `number`."""
+    is_cuda, number = property(lambda self: True), 0
+
+    def get_device(self):
+        return self.number
+
+
+def far(t, number=0):
+    t = t.as_subclass(OnDevice)
+    t.number = number
+    return t
+
+
+class Calls:
+    """Stands for the library: every call succeeds and touches nothing."""
+
+    def __init__(self):
+        self.made = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.made.append((name, a)) or 0
+
+
+def tensors(n=3, hq=4, hkv=2, d=64, pages=5, P=16):
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)      # noqa: E731
+    rope = dict(q=bf(n, hq, d), k=bf(n, hkv, d), pos=i(n), q_out=bf(n, hq, d), k_out=bf(n, hkv, d),
+                q_weight=bf(d), k_weight=bf(d))
+    cache = dict(k_pool=bf(pages, P, hkv, d), v_pool=bf(pages, P, hkv, d), page_table=i(2, 3),
+                 ctx_len=i(2), d_status=i(1))
+    ws = torch.zeros(8, dtype=torch.uint8)
+    append = dict(k=bf(n, hkv, d), v=bf(n, hkv, d), q_start=i(3), pos=i(n), k_weight=bf(d), q=bf(n, hq, d),
+                  q_out=bf(n, hq, d), q_weight=bf(d), **cache)
+    chunk = dict(q=bf(n, hq, d), q_start=i(3), out=bf(n, hq, d), workspace=ws, **cache)
+    decode = dict(q=bf(2, 1, hq, d), out=bf(2, 1, hq, d), workspace=ws, **cache)
+    return dict(omnitide_qk_norm_rope=rope, omnitide_paged_append=append,
+                omnitide_paged_chunk_attn=chunk, omnitide_paged_decode_attn=decode)
+
+
+@pytest.mark.parametrize("name", list(tensors()))
+def test_one_tensor_on_another_device(monkeypatch, name):
+    """Each tensor of each call in turn, and the stream: refused before the library is called; Tensor's
+    subclasses are tensors."""
+    calls = Calls()
+    monkeypatch.setattr(pg, "_lib", calls)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 77 + dev, raising=False)
+    args = {k: far(v) for k, v in tensors()[name].items()}
+    call, more = getattr(pg, name), {} if "attn" not in name else dict(scale=1.0)
+    call(**args, **more)
+    assert calls.made.pop()[1][-1] == 77
+    for k, v in args.items():
+        with pytest.raises(ValueError, match="on device|current one"):
+            call(**{**args, k: far(v, 1)}, **more)
+        with pytest.raises(ValueError):                     # a host tensor
+            call(**{**args, k: v.as_subclass(torch.Tensor)}, **more)
+
+    class Stream:
+        device, device_index, cuda_stream = "cuda:1", 1, 1234
+    with pytest.raises(ValueError, match="stream"):
+        call(**args, **more, stream=Stream())
+    assert not calls.made
+    Stream.device_index = 0
+    call(**args, **more, stream=Stream())
+    assert calls.made.pop()[1][-1] == 1234
