@@ -86,7 +86,8 @@ int omnitide_rope_thetas(double rope_base, int rope_dims, int scaling, double fa
  *   theta        HOST double [rope_dims / 2] (omnitide_rope_thetas, or the caller's own)
  *   rope_dims    0 (no rotation), or even, 2..head_dim; a multiple of 8 with OMNITIDE_ROPE_HALF
  * Strides are at least heads * head_dim elements and a multiple of 16 bytes.
- * Precision: sum of squares, norm and rotation in float; the angle in double, reduced to one turn
+ * Precision: sum of squares, norm and rotation in float (heads whose squares leave its range are scaled
+ * by a power of two first); the angle in double, reduced to one turn
  * before its float sine and cosine; one rounding (nearest even) to out_dtype at the end: within half
  * a unit in the last place of the exact result plus 2^-19 of the length of the (normed) pair, for
  * |pos * theta_j| up to 2^31.

@@ -179,17 +179,29 @@ __global__ __launch_bounds__(kRowThreads) void norm_rope_kernel(const NormRopeAr
     floatx4 y = unpack_quad<IN32>(on ? xb[i] : u32x4{0, 0, 0, 0});
     const bool norm = is_q ? norm_q : !is_v && norm_k;
     if (norm_q || norm_k) {
-      float ss = 0.f;
+      auto mean_square = [&](float eps) {
+        float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
-      ss = head_sum<LPH>(ss);              // every lane takes part
-      const float inv = rsqrtf(ss * (1.f / D) + a.eps);
+        for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
+        return head_sum<LPH>(ss) * (1.f / D) + eps;        // every lane takes part
+      };
+      float ms = mean_square(a.eps);
+      // A head whose squares leave float's range, though the head does not: the same of 2^100 or 2^-100
+      // times its values (0 and infinity stay what they are).  At most 0.1 us of a call of few tokens.
+      const bool small = ms <= 0x1p-100f, large = ms >= 0x1p120f;
+      if (__builtin_expect(__any(norm && (small || large)), 0)) {
+        const float by = small ? 0x1p100f : large ? 0x1p-100f : 1.f;
+        x *= norm ? by : 1.f;
+        y *= norm ? by : 1.f;
+        ms = mean_square(a.eps * by * by);
+      }
+      const float inv = rsqrtf(ms);
       const floatx4 wa = unpack_quad<IN32>(is_q ? wqa : wka);
       const floatx4 wb = unpack_quad<IN32>(is_q ? wqb : wkb);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[e] = norm ? x[e] * (inv * wa[e]) : x[e];
-        y[e] = norm ? y[e] * (inv * wb[e]) : y[e];
+        x[e] = norm ? x[e] * inv * wa[e] : x[e];           // (|x inv| <= sqrt(D), whatever w is)
+        y[e] = norm ? y[e] * inv * wb[e] : y[e];
       }
     }
     const bool turned = R > 0 && !is_v;

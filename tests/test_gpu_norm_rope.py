@@ -120,6 +120,35 @@ def test_norm_rope_in_place_one_side_and_padding(dtype, style):
     assert not torch.equal(y[~pad.cuda()], x[~pad.cuda()])
 
 
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (F32, BF), (BF, BF)])
+@pytest.mark.parametrize("eps", [0.0, 1e-6, 1e-34, 1e30])
+def test_norm_over_the_range_of_float(dtype, out, eps):
+    """Heads of one wave of every size from denormal numbers to the largest, whose squares float holds or
+    not, beside each other; small and large weights; rotated."""
+    from paper_2609_34653_amd import paged as pg
+    hq, hkv, d, T = 26, 3, 64, 3
+    x, (wq, wk) = fused(T, hq, hkv, d, dtype, 9)
+    power = np.array([-126, -110, -100, -90, -80, -66, -60, -51, -50, -49, -45, -30, 0, 1, 30, 45, 55, 58,
+                      59, 60, 61, 63, 64, 80, 100, 122])
+    scale = torch.tensor(np.ldexp(1.0, np.concatenate([power, [-60, 0, 64], np.zeros(hkv, int)])),
+                         dtype=torch.float32, device="cuda")[:, None]
+    unit = x.float() / x.float().abs().amax(-1, keepdim=True)
+    x = (unit * scale).to(dtype)
+    wq, wk = (wq.float() * 2.0 ** -90).to(dtype), (wk.float() * 2.0 ** 90).to(dtype)
+    q, k = x[:, :hq], x[:, hq:hq + hkv]
+    th = pg.omnitide_rope_thetas(1.0e4, 32)
+    pos = np.array([0, 77, 70001])
+    qo = torch.full((T, hq, d), float("nan"), dtype=out, device="cuda")
+    ko = torch.full((T, hkv, d), float("nan"), dtype=out, device="cuda")
+    pg.omnitide_qk_norm_rope(q, k, i32(pos), qo, ko, th, 0, 1.0, wq, wk, eps)
+    torch.cuda.synchronize()
+    e = float(np.float32(eps))
+    for got, src, w in ((qo, q, f64(wq)), (ko, k, f64(wk))):
+        want = op.norm_rope(f64(src), w, e, th, pos, "half")
+        plain = op.norm_rope(f64(src), w, e, None, pos, "half")
+        assert_close(got, want, plain, 32, "half", out)
+
+
 def test_zero_tokens():
     from paper_2609_34653_amd import paged as pg
     e = torch.empty(0, 4, 64, dtype=BF, device="cuda")
