@@ -26,7 +26,8 @@
  *               sequence s and are its last rows: token t sits at row
  *               ctx_len[s] - (q_start[s + 1] - t).  0 <= q_start[0] <= ... <= q_start[n_seq] <=
  *               n_tokens; a sequence may have no token.  Tokens in front of q_start[0] and from
- *               q_start[n_seq] on (a padded batch) are neither read nor written anywhere.
+ *               q_start[n_seq] on (a padded batch) are no sequence's: nothing is written for them,
+ *               and their rows of q, k and v, which have to be there, may hold anything.
  *   Device checks: OMNITIDE_E_PAGES for offsets out of order (of sequences that then overlap, one at
  *   most has a token) or a page id outside [0, n_pages) among the entries in use; OMNITIDE_E_CAPACITY for a sequence whose ctx_len is below its number
  *   of tokens or above max_pages * page_size (its tokens' outputs are then not written, nor its

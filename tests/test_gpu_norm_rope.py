@@ -286,6 +286,42 @@ def test_append_device_refusals(what):
         assert (kp[1, 0:4] == 1).all() and int((kp != 0).sum()) == 4 * 64
 
 
+def test_append_leaves_what_is_not_its_own():
+    """Padding rows of NaN in front and behind, and a sequence whose page is bad: neither the pools' other
+    rows nor q_out see them; the tokens beside them are as without."""
+    from paper_2609_34653_amd import paged as pg
+    ctx, new, P, hq, hkv, d = [40, 35, 9], [3, 4, 9], 16, 8, 2, 64
+    table, n_pages = layout(ctx, P, 8)
+    start = np.concatenate([[0], np.cumsum(new)]) + 5
+    T = int(start[-1]) + 4
+    x, (wq, wk) = fused(T, hq, hkv, d, BF, 8)
+    th = pg.omnitide_rope_thetas(1.0e4, d)
+
+    def run(x, table):
+        kp, vp = torch.full((2, n_pages, P, hkv, d), 2.0, dtype=BF, device="cuda")
+        qo = torch.full((T, hq, d), 7.0, dtype=BF, device="cuda")
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        pg.omnitide_paged_append(x[:, hq:hq + hkv], x[:, hq + hkv:], kp, vp, i32(table), i32(start),
+                                 i32(ctx), theta=th, k_weight=wk, q=x[:, :hq], q_out=qo, q_weight=wq,
+                                 d_status=st)
+        torch.cuda.synchronize()
+        return kp, vp, qo, int(st.item())
+    want = run(x, table)
+    padded = x.clone()
+    padded[:5] = float("nan")
+    padded[int(start[-1]):] = float("inf")
+    got = run(padded, table)
+    assert got[3] == want[3] == 0 and all(torch.equal(a, b) for a, b in zip(got[:3], want[:3]))
+    bad = table.copy()
+    bad[1, 2] = n_pages                                      # rows 32..34: the last three of four tokens
+    got = run(x, bad)
+    tokens, page = slice(int(start[2]) - 3, int(start[2])), int(table[1, 2])
+    for g, w, at, keep in zip(got, want, (page, page, tokens), (2.0, 2.0, 7.0)):
+        w[at] = keep
+        assert torch.equal(g, w)
+    assert got[3] == pg.E_PAGES
+
+
 def test_append_past_four_gigabytes():
     """Slots whose byte offset passes 32 bits."""
     from paper_2609_34653_amd import paged as pg
