@@ -111,6 +111,25 @@ def test_chunk(case):
     assert torch.isnan(got[0]).all() and torch.isnan(got[int(start[-1]):]).all()
 
 
+SMALLER = len(CHUNKS)
+CHUNKS += [
+    # d = 128: a whole row tile per workgroup, 8 to 64 more cut into shares, past 64 pages on the way; two
+    # whole ones and half as many more
+    ([1400, 1390, 1410], [700, 710, 690], 16, 32, 8, 128, F32),
+    ([1700, 400, 2200], [1200, 30, 1050], 16, 32, 16, 128, BF),
+    ([2113], [1088], 32, 64, 16, 128, F32),
+    ([640, 600], [600, 600], 64, 128, 32, 128, F32),
+    ([4700, 2300], [33, 65], 16, 16, 2, 128, F32),           # parts of a few tiles, and past 64 pages
+    ([9300], [7], 16, 8, 8, 128, BF),
+]
+
+
+@pytest.mark.parametrize("case", range(SMALLER, len(CHUNKS)))
+def test_chunk_large_heads(case):
+    """Rounds of whole row tiles, shares after them and many pages at d = 128."""
+    test_chunk(case)
+
+
 DECODES = [
     ([1], 1, 16, 4, 1, 64, F32),
     ([777], 1, 64, 32, 8, 128, F32),
@@ -149,6 +168,53 @@ def test_decode(case):
         want, spread = op.ragged_attention(f64(q[s]), f64(kp), f64(vp), table[s:s + 1], [0, nq], [n],
                                            d ** -0.5)
         assert_near(got[s], want, spread, 2.0 ** -16, out)
+
+
+LONG = [
+    # (ctx, nq, page, KV heads, d, out): blocks of 16 keys of a share (two workgroups' per CU over the KV
+    # heads), so a quarter of them of a wave
+    ([18001, 9003, 8101], 2, 16, 64, 64, F32),      # 279: 70, 70, 70 and 69 blocks of a wave
+    ([35400, 777], 1, 32, 64, 64, BF),              # 286: 72, 72, 71, 71
+    ([30001, 5701, 17], 1, 16, 64, 64, F32),        # 284: 71 each
+    ([40001, 33100], 1, 16, 32, 128, F32),          # 288: 72 each, two blocks in flight of each
+    ([69703, 300, 17], 1, 64, 32, 128, BF),         # 276: 69 each
+]
+
+
+@pytest.mark.parametrize("bad", [False, True])
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_decode_long_shares(case, bad):
+    """Waves with more blocks than the 64 page ids they hold, and many turns of their rings, which begin
+    and end at every place of the ring; with a bad page among the second 64 ids."""
+    from paper_2609_34653_amd import paged as pg
+    ctx, nq, P, hkv, d, out = LONG[case]
+    share = max(8, -(-sum(12 + -(-n // 16) for n in ctx) // (512 // hkv)))
+    assert share - 12 > 4 * 64                              # so the first part has more than 64 of a wave
+    table, n_pages = layout(ctx, P, case)
+    g = torch.Generator(device="cuda").manual_seed(case)
+    kp, vp = (torch.randn(n_pages, P, hkv, d, generator=g, device="cuda", dtype=BF) for _ in range(2))
+    for s, n in enumerate(ctx):
+        if n % P:
+            kp[table[s, n // P], n % P:] = float("nan")
+            vp[table[s, n // P], n % P:] = float("inf")
+    q = torch.randn(len(ctx), nq, hkv, d, generator=g, device="cuda").to(BF)
+    given = table.copy()
+    if bad:
+        given[0, (4 * 65 + 2) * 16 // P] = -1
+    got, st = run(True, q, kp, vp, given, None, ctx, d ** -0.5, out)
+    assert st == (pg.E_PAGES if bad else 0)
+    heads = [0, 1, hkv // 2, hkv - 1]
+    for s, n in enumerate(ctx):
+        if bad and s == 0:
+            assert torch.isnan(got[s]).all()
+            continue
+        pages = torch.from_numpy(table[s, :-(-n // P)]).long().cuda()
+        k, v = (f64(p[pages][:, :, heads].flatten(0, 1)[:n]) for p in (kp, vp))
+        qs = f64(q[s][:, heads])
+        want = oracle.chunk_attention(qs, k, v, d ** -0.5)
+        spread = oracle.chunk_attention(qs, k, np.abs(v), d ** -0.5) + np.abs(want)
+        assert_near(got[s][:, heads], want, spread, 2.0 ** -16, out)
+        assert torch.isfinite(got[s]).all()
 
 
 @pytest.mark.parametrize("decode", [False, True])
