@@ -509,21 +509,22 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     };
     // A bad page spoils every row that sees it (below).  The rows that do not have its keys masked, but
     // meet its values with probabilities of zero, so the page in front of it, all of whose rows are
-    // in use, stands in its place; before the part's first page there is none, nor a row that sees
-    // keys of the part and not this page.
+    // in use, stands in its place; before the part's first page there is none (page 0 is loaded), nor a
+    // row that sees keys of the part and not this page.
     int bad_row = INT32_MAX;               // the first row of the part's first bad page
-    auto checked = [&](int p, int before) {
+    int pages = 0;
+    auto checked = [&](int p) {
       const uint64_t bad = __ballot(p < 0 || p >= b.n_pages);
       if (bad != 0) {
         const int l = __ffsll(static_cast<unsigned long long>(bad)) - 1;
         if (lane == 0) set_status(status, OMNITIDE_E_PAGES);
         bad_row = min(bad_row, (window + l) << b.page_shift);
-        const int good = l > 0 ? readlane(p, l - 1) : before;
+        const int good = l > 0 ? readlane(p, l - 1) : readlane(pages, kWave - 1);
         p = lane < l ? p : good;
       }
       return p;
     };
-    int pages = checked(table[min(window + lane, last_page)], 0);
+    pages = checked(table[min(window + lane, last_page)]);
     const uint8_t* k_head = reinterpret_cast<const uint8_t*>(k) + 2 * g * D;
     const uint8_t* v_head = reinterpret_cast<const uint8_t*>(v) + 2 * g * D;
     // byte offset of each call's first key of tile t in a head's pool; the calls of a tile that
@@ -730,7 +731,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
           issue_v(once, t + 2, at_v);
           if ((min((t + 4) * kKT - 1, ctx - 1) >> b.page_shift) - window >= kWave) {
             window += kWave;
-            pages = checked(page_ids[wave][turn ^ 1][lane], readlane(pages, kWave - 1));
+            pages = checked(page_ids[wave][turn ^ 1][lane]);
             ask_pages(window + kWave);
           }
           issue_k(once, t + 3);
