@@ -143,9 +143,12 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
  *               kept from call to call.  Calls that overlap in time need a workspace each.
  * The bytes of rows that are not in use are never used (they may hold anything, NaN included); those
  * of the rows in use are finite numbers.
- * Numerics: bf16 products with float accumulation, float softmax.  Limits: n_q_heads a multiple of
- * n_kv_heads, n_seq <= 1024, n_seq * max_pages * page_size * n_kv_heads <= 2^34, n_tokens * (n_q_heads / n_kv_heads)
- * <= 2^28, |scale| <= 1e30 (of either sign).
+ * Numerics: bf16 products with float accumulation, float softmax statistics; each probability rounded
+ * to bf16 for its product with the values (so is it in omnitide_chunk_attn), the sum that of the
+ * rounded ones: out is off by at most 2^-8 sum_j p_j |v_j - out| for it, 1.6e-3 of out in root mean square on
+ * random data (omnitide_paged_decode_attn keeps 16 bits of them).  Limits: n_q_heads a multiple of
+ * n_kv_heads, n_seq <= 1024, n_seq * max_pages * page_size * n_kv_heads <= 2^34, n_tokens *
+ * (n_q_heads / n_kv_heads) <= 2^28, |scale| <= 1e30 (of either sign).
  */
 int omnitide_paged_chunk_attn(const void* q, const void* k_pool, const void* v_pool, int n_pages,
                               int page_size, const int32_t* page_table, int max_pages,
