@@ -28,15 +28,16 @@
  *               n_tokens; a sequence may have no token.  Tokens in front of q_start[0] and from
  *               q_start[n_seq] on (a padded batch) are no sequence's: nothing is written for them,
  *               and their rows of q, k and v, which have to be there, may hold anything.
- *   Device checks: OMNITIDE_E_PAGES for offsets out of order (of sequences that then overlap, one at
- *   most has a token) or a page id outside [0, n_pages) among the entries in use; OMNITIDE_E_CAPACITY for a sequence whose ctx_len is below its number
- *   of tokens or above max_pages * page_size (its tokens' outputs are then not written, nor its
- *   rows).  A page whose id is bad is neither read nor written, and no other one in its place: a new
- *   token whose row lies there leaves the pools and q_out as they were, and the attention outputs of
- *   the tokens that see a row of it are NaN, whether d_status is given or not; the other tokens', of
- *   the same sequence too, are right.  Limits: n_seq >= 1, max_pages >= 1, max_pages * page_size <= 2^30,
- *   n_tokens <= 2^24, head_dim in {64, 128}, n_kv_heads * head_dim <= 4096.  A call with n_tokens 0
- *   does nothing (its per-token pointers may be NULL).
+ *   Device checks: OMNITIDE_E_PAGES for offsets out of order (a token then has one sequence at most) or
+ *   a page id outside [0, n_pages) among the entries in use; OMNITIDE_E_CAPACITY for a sequence whose
+ *   ctx_len is below its number of tokens or above max_pages * page_size (its tokens' outputs are then
+ *   not written, nor its rows).  Nothing is written to a page whose id is bad and no other page is
+ *   attended to for it: a new token whose row lies there leaves the pools and q_out as they were, and
+ *   the attention outputs of the tokens that see a row of it are NaN, whether d_status is given or
+ *   not; the other tokens', of the same sequence too, are right.
+ *   Limits: n_seq >= 1, max_pages >= 1, max_pages * page_size <= 2^30, n_tokens <= 2^24, head_dim in
+ *   {64, 128}, n_kv_heads * head_dim <= 4096.  A call with n_tokens 0 does nothing (its per-token
+ *   pointers may be NULL).
  */
 #ifndef OMNITIDE_PAGED_H
 #define OMNITIDE_PAGED_H
