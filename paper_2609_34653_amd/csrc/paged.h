@@ -20,15 +20,13 @@ struct PagedBatch {
 };
 
 // One of the tensors a token's heads come from: `heads` heads of the row, in and out strides in
-// elements, the norm's weight (null: no norm), whether it is rotated.
+// elements, the norm's weight (null: no norm).
 struct HeadSide {
   const void* in = nullptr;
   void* out = nullptr;                 // rows by token, or the pool
   int64_t in_stride = 0, out_stride = 0;
   const void* weight = nullptr;
   int heads = 0;
-  bool rotate = false;
-  bool to_pool = false;
 };
 
 struct NormRopeArgs {

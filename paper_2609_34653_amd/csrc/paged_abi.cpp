@@ -192,9 +192,9 @@ int omnitide_qk_norm_rope(const void* q, const void* k, int dtype, int n_tokens,
     return OMNITIDE_E_ALIAS;
   if (n_tokens == 0) return OMNITIDE_OK;
   a.q = HeadSide{q, q_out, q_stride, q_out_stride, nq ? q_weight : nullptr,
-                 q != nullptr ? n_q_heads : 0, true, false};
+                 q != nullptr ? n_q_heads : 0};
   a.k = HeadSide{k, k_out, k_stride, k_out_stride, nk ? k_weight : nullptr,
-                 k != nullptr ? n_kv_heads : 0, true, false};
+                 k != nullptr ? n_kv_heads : 0};
   a.in_f32 = dtype == OMNITIDE_F32;
   a.out_f32 = out_dtype == OMNITIDE_F32;
   a.n_tokens = n_tokens;
@@ -258,9 +258,9 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
     return OMNITIDE_E_ALIAS;
   if (n_tokens == 0) return OMNITIDE_OK;
   a.q = HeadSide{q, q_out, q_stride, q_out_stride, nq ? q_weight : nullptr,
-                 q != nullptr ? n_q_heads : 0, true, false};
-  a.k = HeadSide{k, k_pool, k_stride, 0, k_weight, n_kv_heads, true, true};
-  a.v = HeadSide{v, v_pool, v_stride, 0, nullptr, n_kv_heads, false, true};
+                 q != nullptr ? n_q_heads : 0};
+  a.k = HeadSide{k, k_pool, k_stride, 0, k_weight, n_kv_heads};
+  a.v = HeadSide{v, v_pool, v_stride, 0, nullptr, n_kv_heads};
   a.in_f32 = dtype == OMNITIDE_F32;
   a.out_f32 = false;
   a.n_tokens = n_tokens;

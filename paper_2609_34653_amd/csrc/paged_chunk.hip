@@ -44,7 +44,6 @@
 //   4 chunks of 2,329 tokens over 10,521 keys     1,300-1,420 us by card, 1.0-1.1 PFLOP/s
 //   one chunk of 665 tokens over 17,048 keys        188-217 us (11 us of it the merge)
 //   89 tokens over 601 keys, 4 heads, d = 64         14 us (launches, plan, first pages and merge)
-#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -386,11 +385,6 @@ struct Plan {
     return n - 1;
   }
 };
-
-template <int N>
-__device__ inline void wait_vmcnt() {
-  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
-}
 
 template <int D>
 struct Tile {

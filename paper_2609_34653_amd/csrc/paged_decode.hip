@@ -29,9 +29,6 @@
 // Measured (bf16, d = 128): 96 streams of 200-60,000 rows, 2 KV heads, pages of 16 (1.12 GB) 183 us, 6.1
 // TB/s; 24 streams, 2 tokens each, 8 KV heads (638 MB) 111 us, 5.7 TB/s; one stream of 16,948 rows (69
 // MB) 18.4-19.2 us, 3.7 TB/s: two launches, three dependent loads and four or five blocks per wave.
-#include <algorithm>
-#include <type_traits>
-
 #include "common.h"
 #include "mfma_tile.h"
 #include "paged.h"
@@ -49,11 +46,6 @@ constexpr int kWGs = 512;                // shares of a large call: two workgrou
 // 1.003.)
 constexpr int kMinShare = 8;
 constexpr int kOverhead = 12;
-
-template <int N>
-__device__ inline void wait_vmcnt() {
-  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
-}
 
 // The shares of a call: sequence i = 64 n + lane holds nb[n] blocks, work for kOverhead + nb[n] (none
 // without blocks); first[n] is its KV head's work before it, per_head all of it, `share` that of a

@@ -1,4 +1,4 @@
-// Device-side lookups of a paged batch shared by the paged-cache kernels.
+// Device-side lookups of a paged batch and waits, shared by the paged-cache kernels.
 #pragma once
 
 #include "common.h"
@@ -15,6 +15,12 @@ __device__ inline uint64_t wave_scan_add_u64(uint64_t v) {
   v += dpp_move_u64<kDppRowBcast15, 0xa>(v);
   v += dpp_move_u64<kDppRowBcast31, 0xc>(v);
   return v;
+}
+
+// Waits until at most N of the wave's loads and stores of global memory are on their way.
+template <int N>
+__device__ inline void wait_vmcnt() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
 // Sequence and row of a token.
