@@ -35,8 +35,8 @@
  *   attended to for it: a new token whose row lies there leaves the pools and q_out as they were, and
  *   the attention outputs of the tokens that see a row of it are NaN, whether d_status is given or
  *   not; the other tokens', of the same sequence too, are right.
- *   Limits: n_seq >= 1, max_pages >= 1, max_pages * page_size <= 2^30, n_tokens <= 2^24, head_dim in
- *   {64, 128}, n_kv_heads * head_dim <= 4096.  A call with n_tokens 0 does nothing (its per-token
+ *   Limits: n_seq >= 1, max_pages >= 1, max_pages * page_size <= 2^30, n_seq * max_pages < 2^31,
+ *   n_tokens <= 2^24, head_dim in {64, 128}, n_kv_heads * head_dim <= 4096, n_q_heads <= 4096.  A call with n_tokens 0 does nothing (its per-token
  *   pointers may be NULL).
  */
 #ifndef OMNITIDE_PAGED_H
@@ -87,7 +87,8 @@ int omnitide_rope_thetas(double rope_base, int rope_dims, int scaling, double fa
  *                as they were.  May be NULL with rope_dims == 0 (no padding then)
  *   theta        HOST double [rope_dims / 2] (omnitide_rope_thetas, or the caller's own)
  *   rope_dims    0 (no rotation), or even, 2..head_dim; a multiple of 8 with OMNITIDE_ROPE_HALF
- * Strides are at least heads * head_dim elements and a multiple of 16 bytes.
+ * Strides are at least heads * head_dim elements, at most 2^31, and a multiple of 16 bytes; q and k have
+ * at most 4096 heads each.
  * Precision: sum of squares, norm and rotation in float (heads whose squares leave its range are scaled
  * by a power of two first); the angle in double, reduced to one turn
  * before its float sine and cosine; one rounding (nearest even) to out_dtype at the end: within half

@@ -200,12 +200,11 @@ def _table(page_table, ctx_len, dev: int):
 def omnitide_rope_thetas(rope_base, rope_dims, scaling=ROPE_PLAIN, factor=1.0, original_len=0.0,
                          ramp_slow=1.0, ramp_fast=32.0) -> torch.Tensor:
     """Rotary frequencies (float64, CPU, [rope_dims / 2]) for the calls below; a host function."""
-    n = max(0, int(rope_dims) // 2)
-    theta = torch.empty(max(1, n), dtype=torch.float64)
-    _check(lib().omnitide_rope_thetas(float(rope_base), int(rope_dims), int(scaling), float(factor),
-                                      float(original_len), float(ramp_slow), float(ramp_fast),
-                                      theta.data_ptr() if n <= 64 else None),
-           "omnitide_rope_thetas")
+    dims = int(rope_dims)
+    theta = torch.empty(max(1, min(dims, 128) // 2), dtype=torch.float64)   # the library refuses others
+    _check(lib().omnitide_rope_thetas(float(rope_base), max(-1, min(dims, 1 << 20)), int(scaling),
+                                      float(factor), float(original_len), float(ramp_slow),
+                                      float(ramp_fast), theta.data_ptr()), "omnitide_rope_thetas")
     return theta
 
 

@@ -63,6 +63,13 @@ def test_rope_thetas_refusals(bad):
     assert e.value.code in (ot.E_SHAPE, ot.E_NULL)
 
 
+@pytest.mark.parametrize("dims", [130, 256, 1 << 30, (1 << 32) + 64, 7, 0, -2])
+def test_rope_dims_refused_as_a_size(dims):
+    with pytest.raises(pg.OmnitideError) as e:
+        pg.omnitide_rope_thetas(1.0e4, dims)
+    assert e.value.code == ot.E_SHAPE
+
+
 # -------------------------------------------------------------------------------- refusals
 
 THETA = (ctypes.c_double * 64)(*[0.5] * 64)
