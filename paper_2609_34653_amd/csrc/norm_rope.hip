@@ -179,23 +179,25 @@ __global__ __launch_bounds__(kRowThreads) void norm_rope_kernel(const NormRopeAr
     floatx4 y = unpack_quad<IN32>(on ? xb[i] : u32x4{0, 0, 0, 0});
     const bool norm = is_q ? norm_q : !is_v && norm_k;
     if (norm_q || norm_k) {
-      auto mean_square = [&](float eps) {
+      auto mean_square = [&](floatx4 u, floatx4 v, float eps) {   // every lane takes part
         float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
-        return head_sum<LPH>(ss) * (1.f / D) + eps;        // every lane takes part
+        for (int e = 0; e < 4; ++e) ss = fmaf(u[e], u[e], fmaf(v[e], v[e], ss));
+        return head_sum<LPH>(ss) * (1.f / D) + eps;
       };
-      float ms = mean_square(a.eps);
-      // A head whose squares leave float's range, though the head does not: the same of 2^100 or 2^-100
-      // times its values (0 and infinity stay what they are).  At most 0.1 us of a call of few tokens.
+      const float ms = mean_square(x, y, a.eps);
+      float inv = rsqrtf(ms);
+      // A head whose squares leave float's range, though it does not itself: the same of 2^100 times a
+      // small one (exact) and of 2^-100 times a large one, whose values stay (0 and infinity do,
+      // too).  At most 0.1 us of a call of few tokens.
       const bool small = ms <= 0x1p-100f, large = ms >= 0x1p120f;
       if (__builtin_expect(__any(norm && (small || large)), 0)) {
         const float by = small ? 0x1p100f : large ? 0x1p-100f : 1.f;
-        x *= norm ? by : 1.f;
-        y *= norm ? by : 1.f;
-        ms = mean_square(a.eps * by * by);
+        inv = rsqrtf(mean_square(x * by, y * by, a.eps * by * by));
+        x *= norm && small ? by : 1.f;
+        y *= norm && small ? by : 1.f;
+        inv *= large ? by : 1.f;
       }
-      const float inv = rsqrtf(ms);
       const floatx4 wa = unpack_quad<IN32>(is_q ? wqa : wka);
       const floatx4 wb = unpack_quad<IN32>(is_q ? wqb : wkb);
 #pragma unroll

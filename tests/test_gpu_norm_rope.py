@@ -149,6 +149,30 @@ def test_norm_over_the_range_of_float(dtype, out, eps):
         assert_close(got, want, plain, 32, "half", out)
 
 
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF, BF)])
+def test_norm_of_heads_of_unlike_values(dtype, out):
+    """Pairs of tiny values beside a large one keep their bits: 2^-56 to 2^-16 beside 2^70, 2^-149 and up
+    beside 2^-62, and beside 1."""
+    from paper_2609_34653_amd import paged as pg
+    T, h, d = 5, 9, 64
+    x, (w, _) = fused(T, h, 0, d, F32, 11)
+    x = x / x.abs().amax(-1, keepdim=True)
+    at = torch.arange(d, device="cuda") % 32                 # both values of a pair are of one size
+    x = x * torch.ldexp(torch.ones(1, device="cuda"), -16 - 2 * (at % 20))
+    x[..., [3, 35]] = 1.5 * 2.0 ** 70
+    x[:, 3:6] *= 2.0 ** -60                                  # sizes 2^-76..2^-114 beside 2^10
+    x[:, 6:] *= 2.0 ** -72
+    x[:, 6:] *= 2.0 ** -60                                   # denormal numbers beside 2^-62
+    x = x.to(dtype)
+    th = pg.omnitide_rope_thetas(1.0e4, d)
+    pos, w = np.array([0, 1, 9, 700, 70001]), w.to(dtype)
+    o = torch.full((T, h, d), float("nan"), dtype=out, device="cuda")
+    pg.omnitide_qk_norm_rope(x, None, i32(pos), o, None, th, 0, 1.0, w, None, 0.0)
+    torch.cuda.synchronize()
+    want = op.norm_rope(f64(x), f64(w), 0.0, th, pos, "half")
+    assert_close(o, want, op.norm_rope(f64(x), f64(w), 0.0, None, pos, "half"), d, "half", out)
+
+
 def test_zero_tokens():
     from paper_2609_34653_amd import paged as pg
     e = torch.empty(0, 4, 64, dtype=BF, device="cuda")
