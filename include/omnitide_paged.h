@@ -36,8 +36,8 @@
  *   the attention outputs of the tokens that see a row of it are NaN, whether d_status is given or
  *   not; the other tokens', of the same sequence too, are right.
  *   Limits: n_seq >= 1, max_pages >= 1, max_pages * page_size <= 2^30, n_seq * max_pages < 2^31,
- *   n_tokens <= 2^24, head_dim in {64, 128}, n_kv_heads * head_dim <= 4096, n_q_heads <= 4096.  A call with n_tokens 0 does nothing (its per-token
- *   pointers may be NULL).
+ *   n_tokens <= 2^24, head_dim in {64, 128}, n_kv_heads * head_dim <= 4096, n_q_heads <= 4096.  A call
+ *   with n_tokens 0 does nothing (its per-token pointers may be NULL).
  */
 #ifndef OMNITIDE_PAGED_H
 #define OMNITIDE_PAGED_H

@@ -8,14 +8,15 @@
 // (sincospif) take it without a range reduction of their own.
 //
 // Bound by memory (each value read and written once): 23,041 float32 tokens of 16 heads of 64 (189
-// MB) take 36.5 us, 5.2 TB/s, a large copy's rate; 665 tokens of 40 heads of 128 in bf16 (13.6 MB) take
-// 5.8 us, by the launch and two dependent loads.  One wave takes one token and up to kIters groups of
-// heads: D / 8 lanes per head, eight values per lane, as two runs of four placed so that both members
-// of every pair sit in one lane (HALF: 4c.. and R/2 + 4c.. for the first R / 8 lanes of a head,
-// otherwise 8c..), so the rotation needs no lane exchange.  A lane's place in its head is the same
-// in every group, so it reads the four (cos, sin) it needs once; the token's angles are computed
-// once per wave, a pair per lane, while the groups' loads are in flight, and shared through LDS.
-// Stores are marked as not reused soon (189 MB: 44 us without, 37 with).
+// MB) take 36.6 us (with three sets of inputs in turn 40.8), 5.2 TB/s, a large copy's rate; 665
+// tokens of 40 heads of 128 in bf16 (13.6 MB) take 5.7 us, by the launch and two dependent loads.
+// One wave takes one token and up to kIters groups of heads: D / 8 lanes per head, eight values per
+// lane, as two runs of four placed so that both members of every pair sit in one lane (HALF: 4c..
+// and R/2 + 4c.. for the first R / 8 lanes of a head, otherwise 8c..), so the rotation needs no
+// lane exchange.  A lane's place in its head is the same in every group, so it reads the four (cos,
+// sin) it needs once; the token's angles are computed once per wave, a pair per lane, while the
+// groups' loads are in flight, and shared through LDS. Stores are marked as not reused soon (189
+// MB: 44 us without, 37 with).
 #include "common.h"
 #include "paged.h"
 #include "paged_rows.h"
