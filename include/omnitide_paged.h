@@ -19,8 +19,8 @@
  *               order.  page_size is 16, 32, 64, 128 or 256.
  *   page_table  int32 [n_seq][max_pages]: page of rows [i * page_size, (i + 1) * page_size) of
  *               each sequence.  Only the entries of the rows in use are read (the others may hold
- *               anything).  Sequences may share pages that are only read; a page written by two
- *               sequences of one append holds either's row.
+ *               anything).  Sequences may share pages that are only read; a row written by two
+ *               sequences of one append holds values of both, each either's.
  *   ctx_len     int32 [n_seq]: rows of each sequence in use, the call's new tokens included
  *   q_start     int32 [n_seq + 1]: the batch's tokens [q_start[s], q_start[s + 1]) belong to
  *               sequence s and are its last rows: token t sits at row

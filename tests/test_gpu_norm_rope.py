@@ -310,6 +310,25 @@ def test_append_device_refusals(what):
         assert (kp[1, 0:4] == 1).all() and int((kp != 0).sum()) == 4 * 64
 
 
+def test_append_to_one_row_by_many():
+    """Sequences whose new tokens share a row of a page: each value is one of theirs, their own rows are
+    whole."""
+    from paper_2609_34653_amd import paged as pg
+    n_seq, P, hkv, d = 300, 16, 8, 128
+    table = np.stack([np.zeros(n_seq, int), 1 + np.arange(n_seq)], 1)     # page 0 is everybody's
+    start, ctx = 2 * np.arange(n_seq + 1), np.full(n_seq, 17)             # rows 15 (shared) and 16 (own)
+    no = torch.arange(2 * n_seq, device="cuda").to(torch.float32)
+    k = no[:, None, None].expand(2 * n_seq, hkv, d).contiguous()
+    kp, vp = torch.full((2, n_seq + 1, P, hkv, d), -5.0, dtype=BF, device="cuda")
+    pg.omnitide_paged_append(k, -k, kp, vp, i32(table), i32(start), i32(ctx))
+    torch.cuda.synchronize()
+    first, own = (no[i::2].to(BF) for i in (0, 1))
+    assert torch.isin(kp[0, 15], first).all() and torch.isin(vp[0, 15], -first).all()
+    assert (kp[1:, 0] == own[:, None, None]).all() and (vp[1:, 0] == -own[:, None, None]).all()
+    kp[0, 15], vp[0, 15], kp[1:, 0], vp[1:, 0] = -5.0, -5.0, -5.0, -5.0
+    assert (kp == -5.0).all() and (vp == -5.0).all()
+
+
 def test_append_leaves_what_is_not_its_own():
     """Padding rows of NaN in front and behind, and a sequence whose page is bad: neither the pools' other
     rows nor q_out see them; the tokens beside them are as without."""
