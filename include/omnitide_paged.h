@@ -144,7 +144,7 @@ int omnitide_paged_append(const void* k, const void* v, const void* q, int dtype
  *               counts grows, so one for the largest batch serves smaller ones; nothing in it is
  *               kept from call to call.  Calls that overlap in time need a workspace each.
  * The bytes of rows that are not in use are never used (they may hold anything, NaN included); those
- * of the rows in use are finite numbers.
+ * of the rows in use are finite numbers (a token that sees a key of NaN comes out as NaN).
  * Numerics: bf16 products with float accumulation, float softmax statistics; each probability rounded
  * to bf16 for its product with the values (so is it in omnitide_chunk_attn), the sum that of the
  * rounded ones: out is off by at most 2^-8 sum_j p_j |v_j - out| for it, 1.6e-3 of out in root mean square on

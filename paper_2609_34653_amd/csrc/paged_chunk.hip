@@ -769,9 +769,9 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
     else run(std::false_type{});
 
     // ---- the part's result
-    // (a sum that is no number spoils the row to the end)
-    const bool spoilt = lim >= bad_row;
-    const float l_tot = spoilt ? __builtin_nanf("") : sum_halves(l_run);
+    // A sum that is no number (of a bad page, or of keys that are none) spoils the row to the end: it
+    // counts in the merge whatever references there are.
+    const float l_tot = lim >= bad_row ? __builtin_nanf("") : sum_halves(l_run);
     if (row_ok && whole) {
       const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
 #pragma unroll
@@ -791,7 +791,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void paged_chunk_kernel(
         for (int qd = 0; qd < 4; ++qd)
           *reinterpret_cast<floatx4*>(part_o + at * D + 32 * dt + 8 * qd + 4 * h) =
               floatx4{o[dt][4 * qd], o[dt][4 * qd + 1], o[dt][4 * qd + 2], o[dt][4 * qd + 3]};
-      if (h == 0) part_ml[at] = make_float2(spoilt ? 0.f : m_run, l_tot);
+      if (h == 0) part_ml[at] = make_float2(l_tot == l_tot ? m_run : 0.f, l_tot);
     }
     if (!after_part()) break;
   }

@@ -330,17 +330,16 @@ __global__ __launch_bounds__(kThreads, 2) void paged_decode_kernel(
       }
     }
 
-    if (lim >= bad_row) {                    // a sum that is no number spoils the column to the end
-      m_run = 0.f;
-      l_run = __builtin_nanf("");
-    }
-    // merge the waves: per column the reference, the sum over the four lane groups, and O^T
+    // merge the waves: per column the reference, the sum over the four lane groups, and O^T.  A sum that is
+    // no number (of a bad page, or of keys that are none) spoils the column to the end: it counts
+    // whatever references there are.
+    if (lim >= bad_row) l_run = __builtin_nanf("");
     const float l_col = l_run + __shfl_xor(l_run, 16, kWave) + __shfl_xor(l_run, 32, kWave) +
                         __shfl_xor(l_run, 48, kWave);
     __syncthreads();                         // every wave is done with its ring
     float* so = reinterpret_cast<float*>(smem);
     if (g4 == 0) {
-      sm[wave][c16] = m_run;
+      sm[wave][c16] = l_col == l_col ? m_run : 0.f;
       sl[wave][c16] = l_col;
     }
     if (c16 < NC) {

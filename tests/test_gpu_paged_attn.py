@@ -551,6 +551,26 @@ def test_a_sequence_of_nans_stays_alone(decode):
 
 
 @pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("rows", [slice(0, 1), slice(640, 700), slice(0, None)])
+def test_keys_that_are_no_numbers_are_not_lost(decode, rows):
+    """A token that sees such keys comes out as NaN, be they one, a share's or all of them; never as
+    zeros."""
+    ctx = [2500, 90, 700]
+    q, kp, vp, table, start, _ = both(decode, ctx, 16, 8, 2, 64, 12)
+    clean, _ = run(decode, q, kp, vp, table, start, ctx, 0.1, F32)
+    for s in (0, 2):
+        r = np.arange(ctx[s])[rows]
+        kp[table[s, r // 16], r % 16] = float("nan")
+    got, st = run(decode, q, kp, vp, table, start, ctx, 0.1, F32)
+    assert st == 0
+    got, clean = got.view(3, 2, 8, 64), clean.view(3, 2, 8, 64)
+    for s in (0, 2):
+        assert torch.isnan(got[s, 1]).all()
+        assert torch.isnan(got[s, 0]).all() or ctx[s] - 1 <= rows.start
+    assert torch.equal(got[1], clean[1])
+
+
+@pytest.mark.parametrize("decode", [False, True])
 def test_two_streams_at_once(decode):
     """Two calls in flight with a workspace each, on streams given by name, against each alone."""
     from paper_2609_34653_amd import paged as pg
