@@ -1,0 +1,492 @@
+// Decode attention over latent rows (the absorbed form): the last n_q tokens of each sequence, all heads on
+// one key of R + 64 values whose first R are the value as well.
+//
+// Mathematics: softmax(scale q K^T) C per sequence for its n_q * H query vectors, K = (C, E) the rows of the
+// cache, one pass over them with a running reference and sum per vector.
+//
+// Bound by memory while a workgroup has up to about 64 vectors (2 (2 R + 64) operations per vector for
+// 2 (R + 64) bytes), by its LDS reads with 128.  What follows from that:
+//   rows      vectors in row tiles of 16, one per wave: its queries (R + 64 wide) and its output (R wide) take 72
+//             and 128 registers for R = 512, so two waves share a SIMD.  (32 vectors per wave would halve the
+//             LDS reads; their output alone takes all 256 accumulation registers and the scores
+//             have none.)  2, 4 or 8 row tiles per workgroup; with 2 and 4 two key groups of waves share out
+//             the keys.
+//   shares    as in paged decode: the 32-key blocks of all sequences, one after the other, cut into equal
+//             shares, one per workgroup and row group, a fixed cost counted for each sequence; the parts of
+//             a sequence that lies in several shares are merged by a second kernel, in share order.
+//   keys      one tile of 32 keys serves both products: 16-byte chunks XOR-swizzled by the key so that both
+//             the row reads of K and the transposing reads of C touch distinct banks.  Steps of two tiles,
+//             two steps in LDS, one barrier per step.
+//   products  S^T (16 keys x 16 vectors, twice) = K Q^T and O^T (16 dims x 16 vectors) = C^T P^T with
+//             v_mfma_f32_16x16x32_bf16; keys are permuted when K rows are read so that S^T is the operand of
+//             the second product as it stands.
+#include "common.h"
+#include "latent.h"
+#include "mfma_tile.h"
+#include "paged_rows.h"
+
+namespace omnitide {
+namespace {
+
+constexpr int kKT = 32;                  // keys per tile and block
+constexpr int kStep = 2;                 // tiles per step
+constexpr int kRow = 16;                 // vectors per row tile
+constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
+constexpr int kMinShare = 4;             // blocks of a share at least
+constexpr int kOverhead = 6;             // what a sequence costs beside its blocks, in blocks
+
+template <int NS>
+struct Shares {
+  int nb[NS], first[NS], ctx[NS];
+  int per_head, share;
+};
+
+// As in paged decode, with row tiles in place of KV heads.
+template <int NS>
+__device__ inline Shares<NS> plan_shares(const PagedBatch& b, int row_tiles) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int cap = b.max_pages << b.page_shift;
+  Shares<NS> s;
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const int i = n * kWave + lane;
+    s.ctx[n] = i < b.n_seq ? b.ctx_len[i] : -1;
+  }
+  s.per_head = 0;
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    s.nb[n] = s.ctx[n] >= b.n_q && s.ctx[n] <= cap ? (s.ctx[n] + kKT - 1) / kKT : 0;
+    const int work = s.nb[n] > 0 ? kOverhead + s.nb[n] : 0;
+    const int inc = wave_scan_add_i32(work);
+    s.first[n] = s.per_head + inc - work;
+    s.per_head += readlane(inc, kWave - 1);
+  }
+  const int per = max(1, kWGs / row_tiles);
+  s.share = max(kMinShare, (s.per_head + per - 1) / per);
+  return s;
+}
+
+// The swizzle of a key's chunks.  Rows are an odd number of 128 bytes, so a key's bit 0 shifts by half the
+// banks; its bits 1, 3 and 4 do the rest for the 16 keys of a K read (8 i + j, i, j < 4), and bits 1 and 3 move
+// past the two chunks that each of the eight keys of half a transposing read takes.
+__device__ inline int swz(int key) {
+  return ((key >> 1) & 1) << 2 | ((key >> 3) & 1) << 1 | ((key >> 4) & 1);
+}
+
+// RB: row tiles of a workgroup; NS: sequences per lane of the plan.
+template <int RB>
+constexpr int waves_of() { return RB == 2 ? 4 : 8; }
+
+template <int R, int RB, int NS>
+__global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void latent_decode_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ pool, const PagedBatch b, int H,
+    int row_groups, float scale_log2, void* __restrict__ out, bool out_bf16, float* __restrict__ part_o,
+    float2* __restrict__ part_ml, int32_t* __restrict__ status) {
+  constexpr int kWaves = waves_of<RB>(), kThreads = kWaves * kWave;
+  constexpr int D = R + kLatentRope;
+  constexpr int KW = kWaves / RB;          // key groups
+  constexpr int CH = D / 8;                // 16-byte chunks per row
+  constexpr int KS = D / 32;               // K operands of 16 keys
+  constexpr int DT = R / 16;               // 16-dim tiles of the output
+  constexpr int ROWB = D * 2;              // bytes per row
+  constexpr int TILEB = kKT * ROWB;
+  constexpr int LOADS = CH / 8;            // direct loads per 8 keys
+  constexpr int OCTS = 4 * kStep / kWaves; // eights of keys that a wave loads per step
+  constexpr int kHalf = 256;               // dims merged at a time
+  constexpr int kCol = kHalf + 4;          // floats of a row in the merge buffer
+  constexpr int kTilesB = 2 * kStep * TILEB, kMergeB = kWaves * kRow * kCol * 4;
+  constexpr float kSumLimit = 4294967296.f;
+  static_assert(ROWB % 128 == 0 && (ROWB / 128) % 2 == 1, "the swizzle's banks");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kTilesB > kMergeB ? kTilesB : kMergeB];
+  __shared__ float sm[kWaves][kRow], sl[kWaves][kRow];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int rb = wave % RB, kw = wave / RB;
+  const int col = lane & 15, g4 = lane >> 4;
+  const int nq = b.n_q, M = nq * H;
+
+  if (blockIdx.x == 0 && wave == 0) report_batch(b, status);
+  const Shares<NS> sh = plan_shares<NS>(b, row_groups);
+  // idle sequences: zeros
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    uint64_t idle = __ballot(sh.ctx[n] == 0);
+    while (idle != 0) {
+      const int l = __ffsll(static_cast<unsigned long long>(idle)) - 1;
+      idle &= idle - 1;
+      const int s = n * kWave + l;
+      if (s % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x)) {
+        const size_t at = static_cast<size_t>(s) * M * R;
+        for (int i = tid; i < M * R; i += kThreads) {
+          if (out_bf16) static_cast<uint16_t*>(out)[at + i] = 0;
+          else static_cast<float*>(out)[at + i] = 0.f;
+        }
+      }
+    }
+  }
+  const int rg = blockIdx.x % row_groups;
+  const int m0 = rg * RB * kRow;           // the workgroup's first vector
+  const int64_t lo64 = static_cast<int64_t>(blockIdx.x / row_groups) * sh.share;
+  if (lo64 >= sh.per_head) return;
+  const int lo = static_cast<int>(lo64), hi = min(lo + sh.share, sh.per_head);
+
+  // this lane's place in the direct loads of eight keys: chunk c * 64 + lane (row, swizzled chunk)
+  uint32_t off[LOADS];
+#pragma unroll
+  for (int c = 0; c < LOADS; ++c) {
+    const int at = c * kWave + lane, key = at / CH, pc = at % CH;
+    off[c] = key * ROWB + 16u * (pc ^ swz(key));
+  }
+  const uint32_t lds0 = lds_addr(smem);
+  // K rows of S^T tile a: row r = lane % 16 is key 8 (r / 4) + 4 a + r % 4, dims 32 c + 8 g4
+  const int krow = 8 * (col >> 2) + (col & 3);
+  const uint32_t k_lane = ROWB * krow + 16u * (g4 ^ swz(krow));
+  // C^T: keys 8 g4 + col / 4 (+ 4), dims 16 dt + 4 (col % 4)
+  const int vrow = 8 * g4 + (col >> 2);
+  const uint32_t v_lane = ROWB * vrow + 8u * (col & 1), v_unit = 16u * (((col & 3) >> 1) ^ swz(vrow));
+
+  for (int pos = lo; pos < hi;) {
+    // the part of one sequence that starts at pos; its overhead comes before its blocks
+    int seq = 0, u0 = 0, nb = 1, ctx = 1;
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      const uint64_t hit = __ballot(sh.nb[n] > 0 && pos >= sh.first[n] &&
+                                    pos < sh.first[n] + kOverhead + sh.nb[n]);
+      if (hit != 0) {
+        const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+        seq = n * kWave + l;
+        u0 = pos - readlane(sh.first[n], l);
+        nb = readlane(sh.nb[n], l);
+        ctx = readlane(sh.ctx[n], l);
+      }
+    }
+    const int u1 = min(kOverhead + nb, u0 + (hi - pos));
+    const int b0 = max(u0 - kOverhead, 0), b1 = max(u1 - kOverhead, 0);
+    pos += u1 - u0;
+    if (b1 == 0) break;                      // the share ends before the first block
+    const bool whole = b0 == 0 && b1 == nb;
+    // a share holds at most one part that goes on from an earlier share and one that goes on in a later
+    const int slot = 2 * static_cast<int>(blockIdx.x) + (b0 > 0 ? 0 : 1);
+
+    // Q^T operand: column = vector m (token m / H)
+    const int m = m0 + rb * kRow + col;
+    const bool row_ok = m < M;
+    const int lim = ctx - nq + (row_ok ? m / H : 0);           // keys <= lim are visible
+    const uint16_t* qrow = q + (static_cast<size_t>(seq) * M + (row_ok ? m : 0)) * D;
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int c = 0; c < KS; ++c) qf[c] = __builtin_bit_cast(bf16x8, ld16(qrow + 32 * c + 8 * g4));
+
+    // The part ends in front of a bad page: the vectors that see it are spoilt (below), and the others see
+    // no later key either, so nothing is read in its place.
+    const int32_t* table = b.table + static_cast<size_t>(seq) * b.max_pages;
+    int end = min(b1 * kKT, ctx), bad_row = INT32_MAX;         // keys in front of `end` are read
+    {
+      const int p0 = (b0 * kKT) >> b.page_shift, p1 = (end - 1) >> b.page_shift;
+      for (int p = p0; p <= p1; p += kWave) {
+        const int id = p + lane <= p1 ? table[p + lane] : 0;
+        const uint64_t bad = __ballot(id < 0 || id >= b.n_pages);
+        if (bad != 0) {
+          const int first = p + __ffsll(static_cast<unsigned long long>(bad)) - 1;
+          if (lane == 0) set_status(status, OMNITIDE_E_PAGES);
+          end = bad_row = max(first << b.page_shift, b0 * kKT);
+          break;
+        }
+      }
+    }
+    const int steps = (end - b0 * kKT + kStep * kKT - 1) / (kStep * kKT);
+
+    // The first key of this wave's o-th eight of step t, and its page (of the last key's page past it).
+    auto first_key = [&](int t, int o) {
+      return b0 * kKT + t * (kStep * kKT) + 8 * (o * kWaves + wave);
+    };
+    auto page_of = [&](int t, int o) {
+      return __builtin_amdgcn_readfirstlane(table[min(first_key(t, o), end - 1) >> b.page_shift]);
+    };
+    int page[OCTS];                          // of the step that is asked for next
+    // asks for this wave's keys of step t; rows past the last key are clamped to it
+    auto issue = [&](int t) {
+#pragma unroll
+      for (int o = 0; o < OCTS; ++o) {
+        const int oct = o * kWaves + wave;                     // of the step's eights
+        const int ks = min(first_key(t, o), end - 1);
+        const int line = ks & ((1 << b.page_shift) - 1) & ~7;
+        const uint8_t* base = reinterpret_cast<const uint8_t*>(pool) +
+                              ((static_cast<size_t>(page[o]) << b.page_shift) + line) * ROWB;
+        const uint32_t dst = lds0 + static_cast<uint32_t>(((t & 1) * 4 * kStep + oct) * 8 * ROWB);
+        const int last = min(end - 1 - (ks & ~7), 7);          // the last of these eight rows in use
+        const uint32_t flip = 32u * (oct & 1) + 16u * ((oct >> 1) & 1);   // bits 3 and 4 of the keys
+#pragma unroll
+        for (int c = 0; c < LOADS; ++c) {
+          uint32_t from = off[c] ^ flip;
+          if (last < 7) {
+            const int key = (c * kWave + lane) / CH;
+            // (the swizzle is that of the place, not of the row that fills it)
+            from -= static_cast<uint32_t>(max(key - last, 0)) * ROWB;
+          }
+          dma16_once(base, from, dst + static_cast<uint32_t>(c * kWave * 16));
+        }
+      }
+    };
+
+    floatx4 o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
+
+    // the 32 keys from key0 on, in the tile at LDS address `tile`
+    auto work = [&](int key0, uint32_t tile) {
+      floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          const auto* p = reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
+              tile + (k_lane ^ (64u * (c & 1))) + 64u * (c & ~1) + 4u * a * ROWB);
+          s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, *p), qf[c], s[a], 0, 0,
+                                                         0);
+        }
+      float x[8];                            // keys key0 + 8 g4 + i
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3];
+      if (key0 + kKT - 1 > min(ctx - nq, end - 1)) {
+        const int last = min(lim, end - 1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (key0 + 8 * g4 + i > last) x[i] = -INFINITY;
+      }
+      float ex[8], ls = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ex[i] = __builtin_amdgcn_exp2f(fmaf(x[i], scale_log2, -m_run));
+        ls += ex[i];
+      }
+      if (__any(!(ls < kSumLimit))) {
+        // exact maximum of the 32 keys per vector (its four lane groups), move the reference, rescale
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          mx = fmaxf(mx, x[i] == -INFINITY ? -INFINITY : x[i] * scale_log2);
+        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        const float m_new = fmaxf(m_run, mx);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+        m_run = m_new;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          ex[i] = x[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[i], scale_log2, -m_use));
+      }
+      bf16x8 p;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const __bf16 r = static_cast<__bf16>(ex[i]);
+        p[i] = r;
+        l_run += static_cast<float>(r);
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        // (keys 4 on have the same swizzle)
+        auto* at = reinterpret_cast<__attribute__((address_space(3))) shortx4*>(
+            tile + v_lane + (v_unit ^ (32u * (dt & 3))) + 32u * (dt & ~3));
+        const shortx4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
+        const shortx4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 4 * ROWB / 8);
+        const bf16x8 c =
+            __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, p, o[dt], 0, 0, 0);
+      }
+    };
+
+    if (steps > 0) {
+#pragma unroll
+      for (int i = 0; i < OCTS; ++i) page[i] = page_of(0, i);
+      // nothing but the direct loads is counted from here on
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      issue(0);
+#pragma unroll
+      for (int i = 0; i < OCTS; ++i) page[i] = page_of(1, i);
+    }
+    for (int t = 0; t < steps; ++t) {
+      wait_vmcnt<0>();
+      __syncthreads();                       // step t is there, and every wave is done with the one before
+      if (t + 1 < steps) {
+        issue(t + 1);
+#pragma unroll
+        for (int i = 0; i < OCTS; ++i) page[i] = page_of(t + 2, i);
+      }
+      const int key0 = (b0 + t * kStep) * kKT;
+      const uint32_t tile = lds0 + static_cast<uint32_t>((t & 1) * kStep * TILEB);
+      if (m0 + rb * kRow < M) {              // a wave without vectors: its share of the loads
+#pragma unroll
+        for (int i = 0; i < kStep / KW; ++i) {
+          const int at = KW == 1 ? i : kw;
+          if (key0 + at * kKT < end) work(key0 + at * kKT, tile + at * TILEB);
+        }
+      }
+    }
+
+    // Merge the key groups: per vector the reference, the sum, and O^T, 256 dims at a time.  A sum that is no
+    // number (of a bad page, or of keys that are none) spoils the vector to the end: it counts whatever
+    // references there are.
+    float l_tot = l_run + __shfl_xor(l_run, 16, kWave) + __shfl_xor(l_run, 32, kWave) +
+                  __shfl_xor(l_run, 48, kWave);
+    if (lim >= bad_row) l_tot = __builtin_nanf("");
+    if (g4 == 0) {
+      sm[wave][col] = l_tot == l_tot ? m_run : 0.f;
+      sl[wave][col] = l_tot;
+    }
+    float* so = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int half = 0; half < R / kHalf; ++half) {
+      __syncthreads();                       // every wave is done with its tiles, or with the half before
+#pragma unroll
+      for (int dt = 0; dt < kHalf / 16; ++dt)
+        *reinterpret_cast<floatx4*>(so + (wave * kRow + col) * kCol + 16 * dt + 4 * g4) =
+            o[half * (kHalf / 16) + dt];
+      __syncthreads();
+      for (int r = wave; r < RB * kRow && m0 + r < M; r += kWaves) {
+        const int tile = r / kRow, c = r % kRow;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < KW; ++w) mx = fmaxf(mx, sm[w * RB + tile][c]);
+        floatx4 num = {0.f, 0.f, 0.f, 0.f};
+        float den = 0.f;
+        if (mx != -INFINITY) {
+#pragma unroll
+          for (int w = 0; w < KW; ++w) {
+            const int x = w * RB + tile;
+            const float f = sm[x][c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[x][c] - mx);
+            const floatx4 v = *reinterpret_cast<const floatx4*>(so + (x * kRow + c) * kCol + 4 * lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) num[e] = fmaf(f, v[e], num[e]);
+            den = fmaf(f, sl[x][c], den);
+          }
+        }
+        const int d0 = half * kHalf + 4 * lane;
+        if (whole) {
+          const size_t at = (static_cast<size_t>(seq) * M + m0 + r) * R + d0;
+          store_row4(out, at, out_bf16, den == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : num / den);
+        } else {
+          const size_t row = static_cast<size_t>(slot) * (RB * kRow) + r;
+          *reinterpret_cast<floatx4*>(part_o + row * R + d0) = num;
+          if (half == 0 && lane == 0) part_ml[row] = make_float2(mx, den);
+        }
+      }
+    }
+    __syncthreads();                         // the merge buffer becomes the tiles again
+  }
+}
+
+// Merges the parts of one vector that lie in several shares, in share order: a workgroup per vector, R / 4
+// threads, four parts asked for at a time.
+template <int R, int RB, int NS>
+__global__ __launch_bounds__(R / 4) void latent_decode_merge_kernel(
+    const float* __restrict__ part_o, const float2* __restrict__ part_ml, const PagedBatch b, int H,
+    int row_groups, void* __restrict__ out, bool out_bf16) {
+  constexpr int kBatch = 4;
+  const int M = b.n_q * H;
+  const int seq = blockIdx.x / M, m = blockIdx.x % M, rg = m / (RB * kRow), r = m % (RB * kRow);
+  const Shares<NS> sh = plan_shares<NS>(b, row_groups);
+  int first = 0, nb = 0;
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    if (seq / kWave == n) {
+      first = readlane(sh.first[n], seq % kWave);
+      nb = readlane(sh.nb[n], seq % kWave);
+    }
+  }
+  if (nb == 0) return;
+  const int w0 = (first + kOverhead) / sh.share, w1 = (first + kOverhead + nb - 1) / sh.share;
+  if (w0 == w1) return;                      // finished by its workgroup
+  const int d4 = threadIdx.x, n_parts = w1 - w0 + 1;
+  float mx = -INFINITY, den = 0.f;
+  floatx4 num = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < n_parts; p0 += kBatch) {
+    float2 ml[kBatch];
+    floatx4 ov[kBatch];
+#pragma unroll
+    for (int c = 0; c < kBatch; ++c) {
+      const int p = p0 + c;
+      const bool in = p < n_parts;
+      const size_t row =
+          static_cast<size_t>(2 * ((w0 + p) * row_groups + rg) + (p == 0 ? 1 : 0)) * (RB * kRow) + r;
+      ml[c] = in ? part_ml[row] : make_float2(-INFINITY, 0.f);
+      ov[c] = in ? *reinterpret_cast<const floatx4*>(part_o + row * R + 4 * d4)
+                 : floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    float cm = mx;
+#pragma unroll
+    for (int c = 0; c < kBatch; ++c) cm = fmaxf(cm, ml[c].x);
+    if (cm == -INFINITY) continue;
+    const float a = mx == -INFINITY ? 0.f : exp2f(mx - cm);
+    den *= a;
+    num *= a;
+#pragma unroll
+    for (int c = 0; c < kBatch; ++c) {
+      const float w = ml[c].x == -INFINITY ? 0.f : exp2f(ml[c].x - cm);
+      den = fmaf(w, ml[c].y, den);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) num[e] = fmaf(w, ov[c][e], num[e]);
+    }
+    mx = cm;
+  }
+  store_row4(out, static_cast<size_t>(blockIdx.x) * R + 4 * d4, out_bf16,
+             den == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : num / den);
+}
+
+int row_tiles_of(int M) { return M <= 32 ? 2 : M <= 64 ? 4 : 8; }
+
+// Workgroups of a call: a share of every row group each.
+int groups_of(int M) { return (M + kRow * row_tiles_of(M) - 1) / (kRow * row_tiles_of(M)); }
+
+template <int R, int RB, int NS>
+hipError_t launch_t(const LatentDecodeArgs& a, hipStream_t stream) {
+  const PagedBatch& b = a.batch;
+  const int groups = groups_of(b.n_q * a.n_heads);
+  const int wgs = max(1, kWGs / groups) * groups;
+  float2* part_ml = static_cast<float2*>(a.workspace);
+  float* part_o = reinterpret_cast<float*>(part_ml + static_cast<size_t>(2 * wgs) * RB * kRow);
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  hipLaunchKernelGGL((latent_decode_kernel<R, RB, NS>), dim3(wgs), dim3(waves_of<RB>() * kWave), 0, stream,
+                     static_cast<const uint16_t*>(a.q), static_cast<const uint16_t*>(a.pool), b, a.n_heads,
+                     groups, scale_log2, a.out, a.out_bf16, part_o, part_ml, a.d_status);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((latent_decode_merge_kernel<R, RB, NS>), dim3(b.n_tokens * a.n_heads), dim3(R / 4), 0,
+                     stream, part_o, part_ml, b, a.n_heads, groups, a.out, a.out_bf16);
+  return hipGetLastError();
+}
+
+template <int R, int RB>
+hipError_t launch_n(const LatentDecodeArgs& a, hipStream_t stream) {
+  if (a.batch.n_seq <= kWave) return launch_t<R, RB, 1>(a, stream);
+  return launch_t<R, RB, 16>(a, stream);
+}
+
+template <int R>
+hipError_t launch_r(const LatentDecodeArgs& a, hipStream_t stream) {
+  switch (row_tiles_of(a.batch.n_q * a.n_heads)) {
+    case 2: return launch_n<R, 2>(a, stream);
+    case 4: return launch_n<R, 4>(a, stream);
+    default: return launch_n<R, 8>(a, stream);
+  }
+}
+
+}  // namespace
+
+size_t latent_decode_workspace_bytes(int n_q, int n_heads, int latent_dim) {
+  const int M = n_q * n_heads, groups = groups_of(M);
+  const size_t rows = static_cast<size_t>(2 * max(1, kWGs / groups) * groups) * row_tiles_of(M) * kRow;
+  return rows * (static_cast<size_t>(latent_dim) + 2) * sizeof(float);
+}
+
+hipError_t launch_latent_decode(const LatentDecodeArgs& a, hipStream_t stream) {
+  return a.latent_dim == 512 ? launch_r<512>(a, stream) : launch_r<256>(a, stream);
+}
+
+}  // namespace omnitide

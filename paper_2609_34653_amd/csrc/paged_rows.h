@@ -75,4 +75,29 @@ __device__ inline void report_batch(const PagedBatch& b, int32_t* status) {
   }
 }
 
+// Output row t of the sequences' rows in one piece (q_start: their offsets): its sequence and row there, as
+// find_token with rows counted from the sequence's first.
+__device__ inline TokenRow find_row(const PagedBatch& b, int t) {
+  const int lane = threadIdx.x & (kWave - 1);
+  for (int i0 = 0; i0 < b.n_seq; i0 += kWave) {
+    const int i = i0 + lane;
+    int s0 = -1, s1 = -1, c = -1;
+    if (i < b.n_seq) {
+      s0 = b.q_start[i];
+      s1 = b.q_start[i + 1];
+      c = b.ctx_len[i];
+    }
+    const uint64_t hit = __ballot(s0 >= 0 && s0 <= t && t < s1 && s1 <= b.n_tokens);
+    if (hit != 0) {
+      const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+      s0 = readlane(s0, l);
+      s1 = readlane(s1, l);
+      c = readlane(c, l);
+      if (c < s1 - s0 || c > (b.max_pages << b.page_shift)) return {-1, 0};
+      return {i0 + l, t - s0};
+    }
+  }
+  return {-1, 0};
+}
+
 }  // namespace omnitide
