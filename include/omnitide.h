@@ -65,7 +65,8 @@ enum {
   OMNITIDE_E_BUDGET = -16,    /* device: protected (system) tokens exceed the budget */
   OMNITIDE_E_TAGS = -17,      /* device: malformed tags (id or modality out of range, a unit
                                  not one contiguous run, runs out of unit order) */
-  OMNITIDE_E_RANGE = -18,     /* device: a unit score of 2^51 or more (select's ranking key) */
+  OMNITIDE_E_RANGE = -18,     /* device: a unit score of 2^51 or more (select's ranking key), or a
+                                 kept row outside its sequence (omnitide_evict.h) */
   OMNITIDE_E_PAGES = -19      /* device: a page id outside the pool, or token offsets out of order
                                  (omnitide_paged.h) */
 };

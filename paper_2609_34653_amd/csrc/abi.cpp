@@ -787,7 +787,8 @@ const char* omnitide_status_string(int code) {
     case OMNITIDE_E_SCRATCH: return "the call needs more scratch than the library's fixed array";
     case OMNITIDE_E_BUDGET: return "protected tokens exceed the retention budget";
     case OMNITIDE_E_TAGS: return "malformed unit/modality tags";
-    case OMNITIDE_E_RANGE: return "a unit score is outside the range the selection ranks (2^51)";
+    case OMNITIDE_E_RANGE: return "a unit score is outside the range the selection ranks (2^51), or a kept row"
+             " outside its sequence";
     case OMNITIDE_E_PAGES: return "a page id outside the pool, or token offsets out of order";
     default: return "unknown status";
   }

@@ -1,0 +1,552 @@
+// The weight that a call's tokens give to each cached row: attention without its values, summed over queries.
+//
+// Mathematics: with scores x = scale <q, k> in base 2, a first pass over the keys finds each query row's
+// reference m and l = sum_j exp2(x_j - m); a second one recomputes the scores and sums exp2(x_j - m) / l over
+// the rows that see key j, per KV head; a last kernel adds the heads up and the old weight.
+//
+// Bound by the vector units: a score takes 2 d operations of the matrix cores and, twice, an
+// exponential and two or three more vector operations, 1.5 times as long as its products for d = 128.
+// What follows from that:
+//   operands  of each product one side stays in registers (32 query rows per wave in the first pass, 32 keys in
+//             the second), the other streams through LDS tiles filled by direct loads; so the first pass
+//             has a row's statistics and the second a key's sum in the lanes that they belong to.
+//   shares    the first pass has the row tiles and shares of chunk_plan.h.  The second takes items of 256 keys of a
+//             KV head and up to kRowChunk query rows, in turn, whatever the lengths.
+//   sums      no atomics: every item owns its place in a buffer of partial sums, added in a fixed order.
+#include "chunk_plan.h"
+#include "common.h"
+#include "evict.h"
+#include "mfma_tile.h"
+#include "paged_rows.h"
+
+namespace omnitide {
+namespace {
+
+constexpr int kRowChunk = 1024;          // query rows of an item of the second pass
+constexpr int kItemKeys = kWaves * 32;   // its keys
+constexpr int kItemWGs = 512;            // workgroups of the second pass
+constexpr int kSumThreads = 256;
+
+// 64 KB or so of a streamed operand in LDS, in stages of kKeys rows.
+template <int D>
+struct Stage {
+  static constexpr int kKeys = D <= 128 ? 64 : 32;
+  static constexpr int kRing = D == 64 ? 4 : 3;
+  static constexpr int kChunks = D / 8;                    // 16-byte chunks per row
+  static constexpr int kRowB = 2 * D;
+  static constexpr int kBytes = kKeys * kRowB;
+  static constexpr int kOctCalls = kChunks / 8;            // direct loads per eight rows
+  static constexpr int kAllCalls = kKeys / 8 * kOctCalls;  // of the workgroup
+  static constexpr int kCalls = (kAllCalls + kWaves - 1) / kWaves;
+  // Chunks are XOR-swizzled by the row so that the 16 rows that one cycle of an operand read serves lie in
+  // distinct banks: rows of 256 bytes by their number, those of an odd number of 128 bytes by half of it.
+  static __device__ int swz(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+
+  // This wave's direct loads of a stage: the eight rows of load i, and this lane's row among them and byte in it.
+  int oct[kCalls], row[kCalls];
+  uint32_t piece[kCalls];
+  __device__ void make(int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kCalls; ++i) {
+      const int call = wave + kWaves * i, at = call % kOctCalls * kWave + lane;
+      oct[i] = call / kOctCalls;
+      row[i] = at / kChunks;
+      piece[i] = 16u * ((at % kChunks) ^ (swz(8 * oct[i] + row[i]) & (kChunks - 1)));
+      if (D > 128) piece[i] = 16u * ((at % kChunks) ^ swz(8 * oct[i] + row[i]));
+    }
+  }
+  // where load i of the ring's entry e goes
+  static __device__ uint32_t place(uint32_t lds, int wave, int i, int e) {
+    return lds + static_cast<uint32_t>(e * kBytes + (wave + kWaves * i) * kWave * 16);
+  }
+  // waits until all but this wave's loads of the last `later` stages have landed
+  template <int LATER>
+  static __device__ void wait(int wave) {
+    constexpr int lo = kAllCalls / kWaves;
+    if (kAllCalls % kWaves != 0 && wave < kAllCalls % kWaves) wait_vmcnt<LATER * (lo + 1)>();
+    else wait_vmcnt<LATER * lo>();
+  }
+  static __device__ bool mine(int wave, int i) { return wave + kWaves * i < kAllCalls; }
+  // this lane's operand address for chunk 0 of rows [32 sub, 32 sub + 32)
+  static __device__ uint32_t lane_at(int col, int h) {
+    return static_cast<uint32_t>(kRowB * col + 16 * (h ^ (swz(col) & (kChunks - 1))));
+  }
+  static __device__ bf16x8 operand(uint32_t stage, uint32_t lane_at, int c) {
+    // chunk 2 c + h: the low three bits of the chunk (four for 256-byte rows) are flipped
+    constexpr uint32_t flip = D == 128 ? 0xffu : 0x7fu;
+    const uint32_t at = (lane_at ^ (32u * c & flip)) + (32u * c & ~flip);
+    return __builtin_bit_cast(
+        bf16x8, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(stage + at));
+  }
+};
+
+// Tokens of a sequence that has more than max_q count as malformed lengths.
+__device__ inline int weights_ctx(const AttnWeightsArgs& a, int i) {
+  const int n = a.batch.q_start[i + 1] - a.batch.q_start[i];
+  return n > a.max_q ? -1 : a.batch.ctx_len[i];
+}
+
+__device__ inline void report_weights(const AttnWeightsArgs& a) {
+  report_batch(a.batch, a.d_status);
+  bool bad = false;
+  for (int i = threadIdx.x & (kWave - 1); i < a.batch.n_seq; i += kWave) {
+    const int s0 = a.batch.q_start[i], s1 = a.batch.q_start[i + 1];
+    bad |= s0 >= 0 && s1 >= s0 && s1 <= a.batch.n_tokens && s1 - s0 > a.max_q;
+  }
+  if (__any(bad) && (threadIdx.x & (kWave - 1)) == 0) set_status(a.d_status, OMNITIDE_E_CAPACITY);
+}
+
+// What a call's passes hand on.  seqs: every sequence's first token, tokens (0: none, or malformed) and
+// context; stats: per KV head and token, its G heads' (m, 1 / l).
+struct WeightsWork {
+  Joined* joined;
+  int4* seqs;
+  float2* part_ml;
+  float2* stats;
+  float* sums;                           // [row chunk][KV head][sequence][max_ctx]
+  int row_chunks;
+};
+
+// ------------------------------------------------------------------ first pass: the rows' statistics
+
+template <int D, int SEQS>
+__global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(const AttnWeightsArgs a,
+                                                                            const WeightsWork ws,
+                                                                            float scale_log2) {
+  using S = Stage<D>;
+  constexpr int NK = D / 16, kSub = S::kKeys / 32;
+  constexpr float kSumLimit = 4294967296.f;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kRing * S::kBytes];
+  __shared__ PlanMem<SEQS> plan_mem;
+  const PagedBatch& b = a.batch;
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int col = lane & 31, h = lane >> 5;
+  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
+
+  if (blockIdx.x == 0 && wave == 0) report_weights(a);
+  Plan<SEQS> plan;
+  plan.make(plan_mem, b.n_seq, b.n_tokens, b.q_start, b.max_pages << b.page_shift,
+            [&](int i) { return weights_ctx(a, i); }, G, Hkv);
+  const int w = (blockIdx.x % kNumXcd) * (kWGs / kNumXcd) + blockIdx.x / kNumXcd;
+  const int64_t begin = plan.share_begin(w), end = plan.share_begin(w + 1);
+  int64_t cur = begin;
+  if (tid == 0) ws.joined[w].n_parts = 0;
+  if (blockIdx.x == 0)
+    for (int i = tid; i < b.n_seq; i += kThreads) ws.seqs[i] = plan_mem.seq[i];
+  if (begin == end && static_cast<int32_t>(begin) > 0 && tid < kRows)
+    ws.part_ml[static_cast<size_t>(2 * w) * kRows + tid] = make_float2(-INFINITY, 0.f);
+
+  S st;
+  st.make(wave, lane);
+  const uint32_t lds0 = lds_addr(lds);
+  const uint32_t at_lane = S::lane_at(col, h);
+  const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
+
+  for (int round = 0;; ++round) {
+    const bool shared = round >= plan.rounds;
+    if (shared && cur >= end) break;
+    const int i = shared ? static_cast<int>(cur >> 32) : Plan<SEQS>::round_tile(round, w);
+    const int t_begin = shared ? static_cast<int32_t>(cur) : 0;
+    const int g = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(plan.tiles_per_head));
+    const int2 place = plan.find_tile(i - g * plan.tiles_per_head);
+    const int s = uniform(place.x), mt = uniform(place.y);
+    const auto sq = plan.seq(s);
+    const int L = sq.len, ctx = sq.ctx, kept = ctx - L;
+    const int nt = plan.tiles_of(mt, L, ctx);
+    const int t_end = shared && i == static_cast<int>(end >> 32) ? static_cast<int32_t>(end) : nt;
+    const bool whole = t_begin == 0 && t_end == nt;
+    const int slot = 2 * w + (i == static_cast<int>(begin >> 32) ? 0 : 1);
+    const int m0 = mt * kRows;
+    const int full_lim = kept + m0 / G;    // keys <= full_lim are visible to every row
+    if (t_begin > 0 && t_end == nt && wave == 0) {
+      const int w0 = plan.first_share(i, w);
+      const int first_slot = 2 * w0 + (plan.share_begin(w0) == pack_cut(i, 0) ? 0 : 1);
+      if (lane == 0) ws.joined[w] = Joined{w - w0 + 1, first_slot, w, sq.q0, L * G, mt, g, 0};
+    }
+
+    const int m = m0 + wave * 32 + col;    // this lane's row
+    const bool row_ok = m < L * G;
+    const int p = row_ok ? m / G : L - 1;
+    const int lim = kept + p;              // its last visible key
+    const uint16_t* qrow =
+        static_cast<const uint16_t*>(a.q) +
+        (static_cast<size_t>(sq.q0 + p) * Hq + g * G + (row_ok ? m % G : 0)) * D;
+    bf16x8 qf[NK];
+#pragma unroll
+    for (int c = 0; c < NK; ++c) qf[c] = __builtin_bit_cast(bf16x8, ld16(qrow + 16 * c + 8 * h));
+
+    // A bad page spoils every row that sees it (below); the others have its keys masked, and page 0 stands in
+    // its place.
+    const int32_t* table = b.table + static_cast<size_t>(s) * b.max_pages;
+    const int k_end = min(t_end * kKT, ctx);
+    int bad_row = INT32_MAX;
+    for (int p0 = (t_begin * kKT) >> b.page_shift, p1 = (k_end - 1) >> b.page_shift; p0 <= p1; p0 += kWave) {
+      const int id = p0 + lane <= p1 ? table[p0 + lane] : 0;
+      const uint64_t bad = __ballot(id < 0 || id >= b.n_pages);
+      if (bad != 0) {
+        if (lane == 0) set_status(a.d_status, OMNITIDE_E_PAGES);
+        bad_row = (p0 + __ffsll(static_cast<unsigned long long>(bad)) - 1) << b.page_shift;
+        break;
+      }
+    }
+    const uint8_t* k_head = static_cast<const uint8_t*>(a.k) + 2 * g * D;
+    const int u_begin = t_begin * (kKT / S::kKeys), u_end = (k_end + S::kKeys - 1) / S::kKeys;
+    auto issue = [&](int u) {
+      const int e = uniform((u - u_begin) % S::kRing);
+#pragma unroll
+      for (int c = 0; c < S::kCalls; ++c) {
+        if (!S::mine(wave, c)) break;
+        const int first = u * S::kKeys + 8 * st.oct[c], at = min(first, ctx - 1);
+        int page = __builtin_amdgcn_readfirstlane(table[at >> b.page_shift]);
+        if (page < 0 || page >= b.n_pages) page = 0;
+        const int line = at & ((1 << b.page_shift) - 1) & ~7;
+        const uint8_t* base = k_head + ((static_cast<size_t>(page) << b.page_shift) + line) * row_bytes;
+        const int last = ctx - 1 - (at & ~7);
+        dma16(base, static_cast<uint32_t>(min(st.row[c], last)) * row_bytes + st.piece[c],
+              S::place(lds0, wave, c, e));
+      }
+    };
+    float m_run = -INFINITY, l_run = 0.f;
+    __syncthreads();                       // the stages of the part before are done with
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int u = 0; u < S::kRing - 1; ++u)
+      if (u_begin + u < u_end) issue(u_begin + u);
+    for (int u = u_begin; u < u_end; ++u) {
+      if (u + S::kRing - 2 < u_end) S::template wait<S::kRing - 2>(wave);
+      else wait_vmcnt<0>();
+      __syncthreads();
+      if (u + S::kRing - 1 < u_end) issue(u + S::kRing - 1);
+      if (m0 + wave * 32 >= L * G) continue;
+      const uint32_t stage = lds0 + static_cast<uint32_t>(uniform((u - u_begin) % S::kRing) * S::kBytes);
+#pragma unroll
+      for (int sub = 0; sub < kSub; ++sub) {
+        floatx16 x = floatx16{};
+#pragma unroll
+        for (int c = 0; c < NK; ++c)
+          x = mfma(S::operand(stage + 32u * sub * S::kRowB, at_lane, c), qf[c], x);
+        const int key0 = u * S::kKeys + 32 * sub;
+        // accumulator i: key key0 + i % 4 + 8 (i / 4) + 4 h
+        if (key0 + 31 > full_lim) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (key0 + (e & 3) + 8 * (e >> 2) + 4 * h > lim) x[e] = -INFINITY;
+        }
+        float ls[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          ls[e & 1] += __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -m_run));
+        float lsum = ls[0] + ls[1];
+        if (__any(!(lsum < kSumLimit))) {
+          // exact maximum of the 32 keys, move the reference, recompute
+          float mx = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            mx = fmaxf(mx, x[e] == -INFINITY ? -INFINITY : x[e] * scale_log2);
+          mx = max_halves(mx);
+          const float m_new = fmaxf(m_run, mx);
+          const float m_use = m_new == -INFINITY ? 0.f : m_new;
+          l_run *= __builtin_amdgcn_exp2f(m_run - m_use);
+          m_run = m_new;
+          lsum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            lsum += x[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -m_use));
+        }
+        l_run += lsum;
+      }
+    }
+    wait_vmcnt<0>();
+    // A sum that is no number spoils the row to the end, whatever references there are.
+    const float l_tot = lim >= bad_row ? __builtin_nanf("") : sum_halves(l_run);
+    if (row_ok && h == 0) {
+      const float ref = l_tot == l_tot ? m_run : 0.f;
+      if (whole)
+        ws.stats[static_cast<size_t>(g) * b.n_tokens * G + static_cast<size_t>(sq.q0) * G + m] =
+            make_float2(ref, 1.f / l_tot);
+      else
+        ws.part_ml[static_cast<size_t>(slot) * kRows + wave * 32 + col] = make_float2(ref, l_tot);
+    }
+    if (shared) {
+      if (t_end < nt) break;               // it ended inside the row tile
+      cur = pack_cut(i + 1, 0);
+    }
+  }
+}
+
+// Joins the statistics of the row tiles whose parts lie in several shares, in share order.
+__global__ __launch_bounds__(kRows) void weights_join_kernel(const WeightsWork ws, int n_tokens, int G) {
+  const Joined j = ws.joined[blockIdx.x];
+  const int row = threadIdx.x, m = j.mt * kRows + row;
+  if (j.n_parts <= 0 || m >= j.rows) return;
+  auto part = [&](int p) {
+    const int slot = p == 0 ? j.first_slot : 2 * (j.last_share - j.n_parts + 1 + p);
+    return ws.part_ml[static_cast<size_t>(slot) * kRows + row];
+  };
+  float mx = -INFINITY, l = 0.f;
+  for (int p = 0; p < j.n_parts; ++p) mx = fmaxf(mx, part(p).x);
+  for (int p = 0; p < j.n_parts; ++p) {
+    const float2 ml = part(p);
+    if (ml.x != -INFINITY) l = fmaf(exp2f(ml.x - mx), ml.y, l);
+  }
+  ws.stats[static_cast<size_t>(j.g) * n_tokens * G + static_cast<size_t>(j.q0) * G + m] =
+      make_float2(mx, 1.f / l);
+}
+
+// --------------------------------------------------------------------- second pass: sums over the rows
+
+// The first row of a sequence's m = p G + r that sees key j.
+__device__ inline int first_row(int j, int kept, int G) { return max(j - kept, 0) * G; }
+
+template <int D, int SEQS>
+__global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const AttnWeightsArgs a,
+                                                                          const WeightsWork ws,
+                                                                          float scale_log2) {
+  using S = Stage<D>;
+  constexpr int NK = D / 16, kSub = S::kKeys / 32;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kRing * S::kBytes];
+  __shared__ int64_t firsts[SEQS];         // items in front of each sequence
+  __shared__ int64_t chunk_sum[SEQS / kWave];
+  const PagedBatch& b = a.batch;
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int col = lane & 31, h = lane >> 5;
+  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
+  const int max_ctx = b.max_pages << b.page_shift;
+
+  // every sequence's items (key tiles x KV heads x row chunks), and those in front of it
+  const int n_chunks = (b.n_seq + kWave - 1) / kWave;
+  for (int c = wave; c < n_chunks; c += kWaves) {
+    const int i = c * kWave + lane;
+    const int4 q = i < b.n_seq ? ws.seqs[i] : make_int4(0, 0, 0, 0);
+    const int64_t n = q.y == 0 ? 0
+                               : static_cast<int64_t>((q.z + kItemKeys - 1) / kItemKeys) * Hkv *
+                                     ((q.y * G + kRowChunk - 1) / kRowChunk);
+    const int64_t inc = static_cast<int64_t>(wave_scan_add_u64(static_cast<uint64_t>(n)));
+    firsts[i] = inc - n;
+    if (lane == kWave - 1) chunk_sum[c] = inc;
+  }
+  __syncthreads();
+  int64_t total = 0;
+  for (int c = 0; c < n_chunks; ++c) {
+    const int64_t n = chunk_sum[c];
+    if (wave == 0) firsts[c * kWave + lane] += total;
+    total += n;
+  }
+  __syncthreads();
+  total = uniform(total);
+
+  S st;
+  st.make(wave, lane);
+  const uint32_t lds0 = lds_addr(lds);
+  const uint32_t at_lane = S::lane_at(col, h);
+  const uint32_t magic = (0x100000000ull + G - 1) / G;     // x / G for small x (G = 1: 0, see below)
+
+  for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
+    int s = 0;                             // the last sequence that begins at or before the item
+    for (int hi = b.n_seq - 1; s < hi;) {
+      const int mid = (s + hi + 1) / 2;
+      if (firsts[mid] <= item) s = mid;
+      else hi = mid - 1;
+    }
+    s = uniform(s);
+    // (sequences without items begin where the next one does, and the last that begins there has some)
+    const int4 sq = ws.seqs[s];
+    const int q0 = uniform(sq.x), L = uniform(sq.y), ctx = uniform(sq.z);
+    const int kept = ctx - L, rows = L * G;
+    const int tiles = (ctx + kItemKeys - 1) / kItemKeys;
+    const int64_t local = item - uniform(firsts[s]);
+    const int rc = uniform(static_cast<int>(local / (tiles * Hkv)));
+    const int rest = uniform(static_cast<int>(local - static_cast<int64_t>(rc) * tiles * Hkv));
+    const int tile = rest / Hkv, g = rest - tile * Hkv;
+    const int key0 = tile * kItemKeys + wave * 32;         // this wave's keys
+    const int m_begin = max(rc * kRowChunk, first_row(tile * kItemKeys, kept, G));
+    const int m_end = min(rows, (rc + 1) * kRowChunk);
+
+    if (m_begin < m_end) {                 // (otherwise no row of the chunk sees the keys: nothing is added)
+      // this wave's keys, which stay in registers; keys past the context are its last one, and those of a bad
+      // page (whose weights the rows' statistics spoil) come from page 0
+      const int32_t* table = b.table + static_cast<size_t>(s) * b.max_pages;
+      const int kj = min(key0 + col, ctx - 1);
+      int page = table[kj >> b.page_shift];
+      if (page < 0 || page >= b.n_pages) page = 0;
+      const uint16_t* krow =
+          static_cast<const uint16_t*>(a.k) +
+          (((static_cast<size_t>(page) << b.page_shift) + (kj & ((1 << b.page_shift) - 1))) * Hkv + g) * D;
+      bf16x8 kf[NK];
+#pragma unroll
+      for (int c = 0; c < NK; ++c) kf[c] = __builtin_bit_cast(bf16x8, ld16(krow + 16 * c + 8 * h));
+      const float2* stats = ws.stats + static_cast<size_t>(g) * b.n_tokens * G + static_cast<size_t>(q0) * G;
+
+      const int u_begin = m_begin / S::kKeys, u_end = (m_end + S::kKeys - 1) / S::kKeys;
+      const int last_row = rows - 1;
+      // direct loads of query rows [u kKeys, +kKeys): row m is head m % G of token m / G
+      auto issue = [&](int u) {
+        const int e = uniform((u - u_begin) % S::kRing);
+        const int base_m = u * S::kKeys, p0 = base_m / G, r0 = base_m - p0 * G;
+        const uint8_t* base = static_cast<const uint8_t*>(a.q) +
+                              (static_cast<size_t>(q0 + p0) * Hq + static_cast<size_t>(g) * G) * D * 2;
+#pragma unroll
+        for (int c = 0; c < S::kCalls; ++c) {
+          if (!S::mine(wave, c)) break;
+          const int x = r0 + min(8 * st.oct[c] + st.row[c], last_row - base_m);
+          const int pp = G == 1 ? x : static_cast<int>(__umulhi(static_cast<uint32_t>(x), magic));
+          dma16(base, static_cast<uint32_t>(pp * Hq + (x - pp * G)) * (2u * D) + st.piece[c],
+                S::place(lds0, wave, c, e));
+        }
+      };
+      float acc[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+      __syncthreads();                     // the stages of the item before are done with
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int u = 0; u < S::kRing - 1; ++u)
+        if (u_begin + u < u_end) issue(u_begin + u);
+      for (int u = u_begin; u < u_end; ++u) {
+        // the rows' statistics, for this stage (m, and 1 / l: 0 for rows that are none of the item's)
+        float ref[kSub], inv[kSub];
+        int lim[kSub];
+#pragma unroll
+        for (int sub = 0; sub < kSub; ++sub) {
+          const int m = u * S::kKeys + 32 * sub + col, mc = min(m, last_row);
+          const float2 v = stats[mc];
+          ref[sub] = v.x;
+          inv[sub] = m >= m_begin && m < m_end ? v.y : 0.f;
+          lim[sub] = kept + mc / G;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (u + S::kRing - 1 < u_end) issue(u + S::kRing - 1);
+        if (key0 >= ctx) continue;
+        const uint32_t stage = lds0 + static_cast<uint32_t>(uniform((u - u_begin) % S::kRing) * S::kBytes);
+#pragma unroll
+        for (int sub = 0; sub < kSub; ++sub) {
+          floatx16 x = floatx16{};
+#pragma unroll
+          for (int c = 0; c < NK; ++c)
+            x = mfma(kf[c], S::operand(stage + 32u * sub * S::kRowB, at_lane, c), x);
+          // accumulator e: key key0 + e % 4 + 8 (e / 4) + 4 h of this lane's row
+          const bool all = __all(key0 + 31 <= lim[sub]);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float pr = __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -ref[sub]));
+            if (all) {
+              acc[e] = fmaf(pr, inv[sub], acc[e]);
+            } else {
+              const bool seen = key0 + (e & 3) + 8 * (e >> 2) + 4 * h <= lim[sub] && inv[sub] != 0.f;
+              acc[e] = seen ? fmaf(pr, inv[sub], acc[e]) : acc[e];
+            }
+          }
+        }
+      }
+      wait_vmcnt<0>();
+      // over the 32 rows of a half, in a fixed order; lane e of half h then stores key e % 4 + 8 (e / 4) + 4 h
+      float* out = ws.sums + ((static_cast<size_t>(rc) * Hkv + g) * b.n_seq + s) * max_ctx;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float v = acc[e];
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) v += __shfl_xor(v, off, kWave);
+        const int key = key0 + (e & 3) + 8 * (e >> 2) + 4 * h;
+        if (col == e && key < ctx) out[key] = v;
+      }
+    }
+  }
+}
+
+// --------------------------------------------------------------------------------- the new weights
+
+__global__ __launch_bounds__(kSumThreads) void weights_add_kernel(const AttnWeightsArgs a,
+                                                                 const WeightsWork ws) {
+  const PagedBatch& b = a.batch;
+  const int s = blockIdx.y, j = blockIdx.x * kSumThreads + threadIdx.x;
+  const int4 q = ws.seqs[s];
+  if (q.y == 0 || j >= q.z) return;
+  const int G = a.n_q_heads / a.n_kv_heads, kept = q.z - q.y, rows = q.y * G;
+  const int max_ctx = b.max_pages << b.page_shift;
+  const int tile = j / kItemKeys;
+  const int rc0 = first_row(tile * kItemKeys, kept, G) / kRowChunk, rc1 = (rows - 1) / kRowChunk;
+  float sum = 0.f;
+  for (int rc = rc0; rc <= rc1; ++rc)
+    for (int g = 0; g < a.n_kv_heads; ++g)
+      sum += ws.sums[((static_cast<size_t>(rc) * a.n_kv_heads + g) * b.n_seq + s) * max_ctx + j];
+  const size_t at = static_cast<size_t>(s) * a.weight_stride + j;
+  if (a.weight_in != nullptr) {
+    const int seen = a.seen_len != nullptr ? a.seen_len[s] : kept;
+    if (j < seen) sum = fmaf(a.decay, a.weight_in[at], sum);
+  }
+  a.weight_out[at] = sum;
+}
+
+size_t align16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
+
+struct Layout {
+  size_t seqs, part_ml, stats, sums, bytes;
+  int row_chunks;
+};
+Layout layout(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, int n_kv_heads) {
+  Layout l;
+  const int64_t rows = static_cast<int64_t>(max_q < n_tokens ? max_q : n_tokens) * (n_q_heads / n_kv_heads);
+  l.row_chunks = static_cast<int>((rows + kRowChunk - 1) / kRowChunk);
+  l.seqs = align16(kWGs * sizeof(Joined));
+  l.part_ml = l.seqs + n_seq * sizeof(int4);
+  l.stats = l.part_ml + static_cast<size_t>(2 * kWGs) * kRows * sizeof(float2);
+  l.sums = align16(l.stats + static_cast<size_t>(n_tokens) * n_q_heads * sizeof(float2));
+  l.bytes = l.sums + static_cast<size_t>(l.row_chunks) * n_kv_heads * n_seq * max_ctx * sizeof(float);
+  return l;
+}
+
+template <int D, int SEQS>
+hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
+  const PagedBatch& b = a.batch;
+  const int max_ctx = b.max_pages << b.page_shift;
+  const Layout l = layout(b.n_tokens, b.n_seq, max_ctx, a.max_q, a.n_q_heads, a.n_kv_heads);
+  uint8_t* base = static_cast<uint8_t*>(a.workspace);
+  const WeightsWork ws{reinterpret_cast<Joined*>(base), reinterpret_cast<int4*>(base + l.seqs),
+                       reinterpret_cast<float2*>(base + l.part_ml),
+                       reinterpret_cast<float2*>(base + l.stats), reinterpret_cast<float*>(base + l.sums),
+                       l.row_chunks};
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  hipLaunchKernelGGL((weights_stats_kernel<D, SEQS>), dim3(kWGs), dim3(kThreads), 0, stream, a, ws,
+                     scale_log2);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(weights_join_kernel, dim3(kWGs), dim3(kRows), 0, stream, ws, b.n_tokens,
+                     a.n_q_heads / a.n_kv_heads);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((weights_sum_kernel<D, SEQS>), dim3(kItemWGs), dim3(kThreads), 0, stream, a, ws,
+                     scale_log2);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(weights_add_kernel, dim3((max_ctx + kSumThreads - 1) / kSumThreads, b.n_seq),
+                     dim3(kSumThreads), 0, stream, a, ws);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_d(const AttnWeightsArgs& a, hipStream_t stream) {
+  return a.batch.n_seq <= 256 ? launch_t<D, 256>(a, stream) : launch_t<D, 1024>(a, stream);
+}
+
+}  // namespace
+
+size_t attn_weights_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads,
+                                    int n_kv_heads, int) {
+  return layout(n_tokens, n_seq, max_ctx, max_q, n_q_heads, n_kv_heads).bytes;
+}
+
+hipError_t launch_attn_weights(const AttnWeightsArgs& a, hipStream_t stream) {
+  switch (a.head_dim) {
+    case 64: return launch_d<64>(a, stream);
+    case 128: return launch_d<128>(a, stream);
+    case 320: return launch_d<320>(a, stream);
+    default: return launch_d<576>(a, stream);
+  }
+}
+
+}  // namespace omnitide
