@@ -382,13 +382,16 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
   }
 }
 
-// Merges the parts of one vector that lie in several shares, in share order: a workgroup per vector, R / 4
-// threads, four parts asked for at a time.
-template <int R, int RB, int NS>
-__global__ __launch_bounds__(R / 4) void latent_decode_merge_kernel(
+// Merges the parts of one vector that lie in several shares, in share order: a workgroup per vector and DIMS of
+// its dims, four of them per thread, 1024 / DIMS parts side by side and four of each asked for at a time.
+constexpr int kMergeThreads = 256;
+template <int R, int RB, int NS, int DIMS>
+__global__ __launch_bounds__(kMergeThreads) void latent_decode_merge_kernel(
     const float* __restrict__ part_o, const float2* __restrict__ part_ml, const PagedBatch b, int H,
     int row_groups, void* __restrict__ out, bool out_bf16) {
-  constexpr int kBatch = 4;
+  constexpr int kBatch = 4, TPR = DIMS / 4, TS = kMergeThreads / TPR;
+  __shared__ floatx4 sn[TS][TPR];
+  __shared__ float2 sml[TS];
   const int M = b.n_q * H;
   const int seq = blockIdx.x / M, m = blockIdx.x % M, rg = m / (RB * kRow), r = m % (RB * kRow);
   const Shares<NS> sh = plan_shares<NS>(b, row_groups);
@@ -403,41 +406,46 @@ __global__ __launch_bounds__(R / 4) void latent_decode_merge_kernel(
   if (nb == 0) return;
   const int w0 = (first + kOverhead) / sh.share, w1 = (first + kOverhead + nb - 1) / sh.share;
   if (w0 == w1) return;                      // finished by its workgroup
-  const int d4 = threadIdx.x, n_parts = w1 - w0 + 1;
+  const int ts = threadIdx.x / TPR, t = threadIdx.x % TPR, d = blockIdx.y * DIMS + 4 * t;
+  const int n_parts = w1 - w0 + 1;
   float mx = -INFINITY, den = 0.f;
   floatx4 num = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = 0; p0 < n_parts; p0 += kBatch) {
+  auto add = [&](float pm, float pl, floatx4 po) {
+    if (pm == -INFINITY) return;
+    const float m_new = fmaxf(mx, pm), u = mx == -INFINITY ? 0.f : exp2f(mx - m_new), v = exp2f(pm - m_new);
+    den = fmaf(den, u, v * pl);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) num[e] = fmaf(num[e], u, v * po[e]);
+    mx = m_new;
+  };
+  for (int p0 = ts; p0 < n_parts; p0 += TS * kBatch) {
     float2 ml[kBatch];
     floatx4 ov[kBatch];
 #pragma unroll
     for (int c = 0; c < kBatch; ++c) {
-      const int p = p0 + c;
+      const int p = p0 + c * TS;
       const bool in = p < n_parts;
       const size_t row =
           static_cast<size_t>(2 * ((w0 + p) * row_groups + rg) + (p == 0 ? 1 : 0)) * (RB * kRow) + r;
       ml[c] = in ? part_ml[row] : make_float2(-INFINITY, 0.f);
-      ov[c] = in ? *reinterpret_cast<const floatx4*>(part_o + row * R + 4 * d4)
-                 : floatx4{0.f, 0.f, 0.f, 0.f};
+      ov[c] = in ? *reinterpret_cast<const floatx4*>(part_o + row * R + d) : floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    float cm = mx;
 #pragma unroll
-    for (int c = 0; c < kBatch; ++c) cm = fmaxf(cm, ml[c].x);
-    if (cm == -INFINITY) continue;
-    const float a = mx == -INFINITY ? 0.f : exp2f(mx - cm);
-    den *= a;
-    num *= a;
-#pragma unroll
-    for (int c = 0; c < kBatch; ++c) {
-      const float w = ml[c].x == -INFINITY ? 0.f : exp2f(ml[c].x - cm);
-      den = fmaf(w, ml[c].y, den);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) num[e] = fmaf(w, ov[c][e], num[e]);
-    }
-    mx = cm;
+    for (int c = 0; c < kBatch; ++c) add(ml[c].x, ml[c].y, ov[c]);
   }
-  store_row4(out, static_cast<size_t>(blockIdx.x) * R + 4 * d4, out_bf16,
+  sn[ts][t] = num;
+  if (t == 0) sml[ts] = make_float2(mx, den);
+  __syncthreads();
+  if (ts != 0) return;
+#pragma unroll
+  for (int c = 1; c < TS; ++c) add(sml[c].x, sml[c].y, sn[c][t]);
+  store_row4(out, static_cast<size_t>(blockIdx.x) * R + d, out_bf16,
              den == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : num / den);
 }
+
+// Vectors from which on a merge workgroup takes all dims of one: there are enough of them, of few parts each (24
+// x 128 vectors: 24 us by quarters, 16 whole), and few have many (16 of 134 parts: 7 and 23).
+constexpr int kWideVecs = 512;
 
 int row_tiles_of(int M) { return M <= 32 ? 2 : M <= 64 ? 4 : 8; }
 
@@ -457,8 +465,13 @@ hipError_t launch_t(const LatentDecodeArgs& a, hipStream_t stream) {
                      groups, scale_log2, a.out, a.out_bf16, part_o, part_ml, a.d_status);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((latent_decode_merge_kernel<R, RB, NS>), dim3(b.n_tokens * a.n_heads), dim3(R / 4), 0,
-                     stream, part_o, part_ml, b, a.n_heads, groups, a.out, a.out_bf16);
+  const int vecs = b.n_tokens * a.n_heads;
+  if (vecs < kWideVecs)
+    hipLaunchKernelGGL((latent_decode_merge_kernel<R, RB, NS, 128>), dim3(vecs, R / 128), dim3(kMergeThreads), 0,
+                       stream, part_o, part_ml, b, a.n_heads, groups, a.out, a.out_bf16);
+  else
+    hipLaunchKernelGGL((latent_decode_merge_kernel<R, RB, NS, R>), dim3(vecs), dim3(kMergeThreads), 0, stream,
+                       part_o, part_ml, b, a.n_heads, groups, a.out, a.out_bf16);
   return hipGetLastError();
 }
 
