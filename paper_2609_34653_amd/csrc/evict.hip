@@ -2,11 +2,14 @@
 //
 // The plan of a sequence of n > high rows: its first `sink`, its last `recent`, and of the m between the k =
 // budget - sink - recent of the largest weight.  Weights are ranked as 32-bit integers that order like them;
-// the k-th largest is found digit by digit (8 bits: counts of each value among the rows that agree in the
-// digits before), then one pass in order of the rows gives each kept one its place: the larger ones in
-// front of it plus the equal ones, as many of those as there is room for.  A workgroup per sequence.
+// the k-th largest is found digit by digit (11, 11 and 10 bits: counts of each value among the rows that agree
+// in the digits before), then every row's place follows from the kept ones in front of it: the larger ones
+// plus the equal ones, as many of those as there is room for.  Bound by latency: 4 bytes a row, and a
+// dependent pass over them per digit.  So a workgroup holds up to 16,384 rows in registers, 16 a thread, and
+// reads them once; longer sequences are cut into such slices in four launches: a slice's counts of the first
+// digit; the rows of that digit, put aside; the last two digits among those; the places.
 //
-// The move is a copy, bound by memory: each kept row is read and written once.  A wave takes kMoveRows rows; their
+// The move is a copy, bound by memory: each kept row is read and written once.  A wave takes up to kMoveRows rows; their
 // pages and angles are worked out a row per lane and a pair per lane, the copy goes by items of eight
 // values, keys as two runs of four so that both members of a rotated pair sit in one lane.
 #include "common.h"
@@ -18,8 +21,11 @@ namespace omnitide {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kPlanPer = 4;              // rows of a thread per pass
-constexpr int kDigits = 256;
+constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kPlanPer = 16;             // rows of a thread
+constexpr int kSlice = kPlanThreads * kPlanPer;
+constexpr int kDigits = 2 * kPlanThreads;
+constexpr int kMaxSlices = 1024;         // of 2^24 rows
 
 // Orders like the weight: NaN lowest, -0 as 0.
 __device__ inline uint32_t weight_key(float w) {
@@ -28,109 +34,319 @@ __device__ inline uint32_t weight_key(float w) {
   return (u & 0x80000000u) != 0 ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(const EvictPlanArgs a) {
-  __shared__ uint32_t hist[kDigits];
-  __shared__ uint32_t found[2];          // the digit, what is left of k
-  __shared__ uint64_t scratch[kPlanThreads / kWave + 1];
-  const int s = blockIdx.x, tid = threadIdx.x;
-  const float* w = a.weight + s * a.weight_stride;
+constexpr int digit_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
+constexpr uint32_t digit_bits(int d) { return d == 2 ? 1023u : 2047u; }
+
+// A sequence as the plan sees it; n < 0: malformed.
+struct PlanSeq {
+  const float* w;
+  int n, k;                              // rows; rows to choose (where n > high)
+};
+__device__ inline PlanSeq plan_seq(const EvictPlanArgs& a, int s) {
+  const int n = a.ctx_len[s];
+  return {a.weight + s * a.weight_stride, n <= a.max_ctx ? n : -1, a.budget - a.sink - a.recent};
+}
+
+// A workgroup's slice of a sequence: row(i) = first + 64 i, 16 of each lane, so that a wave's rows are 1,024 in a
+// row.
+struct Slice {
+  int first, n, mid0, mid1;              // rows [mid0, mid1) are chosen from
+  float x[kPlanPer];
+  __device__ void load(const EvictPlanArgs& a, const PlanSeq& q, int slice) {
+    first = slice * kSlice + static_cast<int>(threadIdx.x / kWave) * (kPlanPer * kWave) +
+            static_cast<int>(threadIdx.x % kWave);
+    n = q.n;
+    mid0 = a.sink;
+    mid1 = q.n - a.recent;
+#pragma unroll
+    for (int i = 0; i < kPlanPer; ++i) x[i] = row(i) < n ? q.w[row(i)] : 0.f;
+  }
+  __device__ int row(int i) const { return first + i * kWave; }
+  __device__ bool middle(int i) const { return row(i) >= mid0 && row(i) < mid1; }
+};
+
+struct PlanMem {
+  uint32_t hist[kDigits];
+  uint32_t found[2];                     // the digit, what is left of k
+  uint32_t count;
+  uint32_t scratch[kPlanWaves + 1];
+  uint2 counts[kPlanWaves];
+};
+
+__device__ inline void clear_counts(PlanMem& m) {
+  __syncthreads();
+  m.hist[threadIdx.x] = 0;
+  m.hist[threadIdx.x + kPlanThreads] = 0;
+  if (threadIdx.x == 0) m.count = 0;
+  __syncthreads();
+}
+
+// The digit of the left-th largest (left > 0), from its counts c1 and c0 of digits 2047 - 2 t and one less for
+// thread t; left becomes what is left of it within the digit.
+__device__ inline uint32_t find_digit(PlanMem& m, uint32_t c1, uint32_t c0, uint32_t& left) {
+  const uint32_t d1 = kDigits - 1 - 2 * threadIdx.x;
+  uint32_t total;
+  const uint32_t before = block_exclusive_scan(c1 + c0, m.scratch, &total);
+  if (before < left && left <= before + c1) {
+    m.found[0] = d1;
+    m.found[1] = left - before;
+  } else if (before + c1 < left && left <= before + c1 + c0) {
+    m.found[0] = d1 - 1;
+    m.found[1] = left - before - c1;
+  }
+  __syncthreads();
+  left = m.found[1];
+  return m.found[0];
+}
+__device__ inline uint32_t find_digit(PlanMem& m, uint32_t& left) {
+  __syncthreads();
+  const uint32_t d1 = kDigits - 1 - 2 * threadIdx.x;
+  return find_digit(m, m.hist[d1], m.hist[d1 - 1], left);
+}
+
+// The kept rows of a slice to their places: those above the key `last` and the first `left` of those that equal
+// it; above0 and equal0 are in the slices in front.
+__device__ inline void place_rows(const EvictPlanArgs& a, int s, const Slice& sl, uint32_t last, uint32_t left,
+                                  uint32_t above0, uint32_t equal0, PlanMem& m) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   int32_t* src = a.src_row + s * a.src_stride;
   float* wo = a.weight_out != nullptr ? a.weight_out + s * a.weight_out_stride : nullptr;
-  const int n = a.ctx_len[s];
-  if (n < 0 || n > a.max_ctx) {
-    if (tid == 0) {
+  auto keep = [&](int i, int to) {
+    src[to] = sl.row(i);
+    if (wo != nullptr) wo[to] = sl.x[i];
+  };
+  if (sl.n <= a.high) {
+#pragma unroll
+    for (int i = 0; i < kPlanPer; ++i)
+      if (sl.row(i) < sl.n) keep(i, sl.row(i));
+    return;
+  }
+  uint64_t above[kPlanPer], equal[kPlanPer];
+  uint32_t na = 0, ne = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanPer; ++i) {
+    const uint32_t key = weight_key(sl.x[i]);
+    above[i] = __ballot(sl.middle(i) && key > last);
+    equal[i] = __ballot(sl.middle(i) && key == last);
+    na += __popcll(above[i]);
+    ne += __popcll(equal[i]);
+  }
+  if (lane == 0) m.counts[wave] = make_uint2(na, ne);
+  __syncthreads();
+  uint32_t pa = above0, pe = equal0;     // in front of this wave
+#pragma unroll
+  for (int v = 0; v < kPlanWaves; ++v) {
+    const uint2 c = m.counts[v];
+    pa += v < wave ? c.x : 0;
+    pe += v < wave ? c.y : 0;
+  }
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < kPlanPer; ++i) {
+    const uint32_t fa = pa + __popcll(above[i] & below), fe = pe + __popcll(equal[i] & below);
+    const bool ab = (above[i] >> lane) & 1, eq = (equal[i] >> lane) & 1;
+    const int row = sl.row(i);
+    if (row < sl.mid0 || (row >= sl.mid1 && row < sl.n)) {
+      keep(i, row < sl.mid0 ? row : a.budget - (sl.n - row));
+    } else if (ab || (eq && fe < left)) {
+      keep(i, sl.mid0 + static_cast<int>(fa + min(fe, left)));
+    }
+    pa += __popcll(above[i]);
+    pe += __popcll(equal[i]);
+  }
+}
+
+// Sequences of one slice at most.
+__global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(const EvictPlanArgs a) {
+  __shared__ PlanMem m;
+  const int s = blockIdx.x;
+  const PlanSeq q = plan_seq(a, s);
+  if (q.n < 0) {
+    if (threadIdx.x == 0) {
       a.new_len[s] = 0;
       set_status(a.d_status, OMNITIDE_E_CAPACITY);
     }
     return;
   }
-  auto keep = [&](int row, int to) {
-    src[to] = row;
-    if (wo != nullptr) wo[to] = w[row];
-  };
-  if (n <= a.high) {
-    if (tid == 0) a.new_len[s] = n;
-    for (int r = tid; r < n; r += kPlanThreads) keep(r, r);
-    return;
+  Slice sl;
+  sl.load(a, q, 0);
+  if (threadIdx.x == 0) a.new_len[s] = q.n <= a.high ? q.n : a.budget;
+  uint32_t last = 0xffffffffu, left = static_cast<uint32_t>(q.k);   // (no key is that large)
+  if (q.n > a.high && q.k > 0) {
+    uint32_t prefix = 0, mask = 0;
+#pragma unroll
+    for (int d = 0; d < 3; ++d) {
+      clear_counts(m);
+#pragma unroll
+      for (int i = 0; i < kPlanPer; ++i) {
+        const uint32_t key = weight_key(sl.x[i]);
+        if (sl.middle(i) && (key & mask) == prefix)
+          atomicAdd(&m.hist[(key >> digit_shift(d)) & digit_bits(d)], 1u);
+      }
+      prefix |= find_digit(m, left) << digit_shift(d);
+      mask |= digit_bits(d) << digit_shift(d);
+    }
+    last = prefix;
   }
-  if (tid == 0) a.new_len[s] = a.budget;
-  for (int r = tid; r < a.sink; r += kPlanThreads) keep(r, r);
-  for (int r = tid; r < a.recent; r += kPlanThreads)
-    keep(n - a.recent + r, a.budget - a.recent + r);
-  const int lo = a.sink, m = n - a.sink - a.recent, k = a.budget - a.sink - a.recent;
-  if (k == 0) return;
+  place_rows(a, s, sl, last, left, 0, 0, m);
+}
 
-  uint32_t prefix = 0, mask = 0, left = static_cast<uint32_t>(k);
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    __syncthreads();
-    if (tid < kDigits) hist[tid] = 0;
-    __syncthreads();
-    for (int r = tid; r < m; r += kPlanThreads) {
-      const uint32_t key = weight_key(w[lo + r]);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (kDigits - 1)], 1u);
-    }
-    __syncthreads();
-    if (tid < kWave) {
-      // four digits a lane, from the largest down
-      uint32_t c[4], sum = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        c[e] = hist[kDigits - 1 - (4 * tid + e)];
-        sum += c[e];
-      }
-      uint32_t before = static_cast<uint32_t>(wave_scan_add_i32(static_cast<int>(sum))) - sum;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (before < left && left <= before + c[e]) {
-          found[0] = kDigits - 1 - (4 * tid + e);
-          found[1] = left - before;
-        }
-        before += c[e];
-      }
-    }
-    __syncthreads();
-    prefix |= found[0] << shift;
-    mask |= (kDigits - 1u) << shift;
-    left = found[1];
+// ---- longer ones, in slices.  Per sequence: the slices' counts, what they put aside and how much, the last key
+// kept and how many of those that equal it.
+struct PlanWork {
+  uint32_t* hist;                        // [sequence][slice][kDigits]
+  uint32_t* keys;                        // [sequence][slice][kSlice]: keys of the digit that is cut
+  uint4* sums;                           // [sequence][slice]: above that digit, keys put aside; then: above the
+                                         //   last key kept and equal to it, in the slices in front
+  uint4* cut;                            // [sequence]: the first digit, what is left of k; then last key, left
+  int slices;
+};
+
+__global__ __launch_bounds__(kPlanThreads) void evict_count_kernel(const EvictPlanArgs a, const PlanWork ws) {
+  __shared__ PlanMem m;
+  const int s = blockIdx.y, slice = blockIdx.x;
+  const PlanSeq q = plan_seq(a, s);
+  if (slice == 0 && threadIdx.x == 0) {
+    a.new_len[s] = q.n < 0 ? 0 : q.n <= a.high ? q.n : a.budget;
+    if (q.n < 0) set_status(a.d_status, OMNITIDE_E_CAPACITY);
   }
-  // the rows above the key `prefix`, and the first `left` of those that equal it
-  uint64_t before = 0;                   // above (high half) and equal (low half) in the passes before
-  for (int r0 = 0; r0 < m; r0 += kPlanThreads * kPlanPer) {
-    uint64_t c = 0;
-    uint32_t above = 0, equal = 0;
+  if (q.n <= a.high || q.k == 0 || slice * kSlice >= q.n) return;
+  Slice sl;
+  sl.load(a, q, slice);
+  clear_counts(m);
 #pragma unroll
-    for (int e = 0; e < kPlanPer; ++e) {
-      const int r = r0 + tid * kPlanPer + e;
-      if (r >= m) break;
-      const uint32_t key = weight_key(w[lo + r]);
-      above |= (key > prefix ? 1u : 0u) << e;
-      equal |= (key == prefix ? 1u : 0u) << e;
-    }
-    c = (static_cast<uint64_t>(__popc(above)) << 32) | static_cast<uint32_t>(__popc(equal));
-    uint64_t total;
-    const uint64_t at = before + block_exclusive_scan(c, scratch, &total);
-    uint32_t na = static_cast<uint32_t>(at >> 32), ne = static_cast<uint32_t>(at);
+  for (int i = 0; i < kPlanPer; ++i)
+    if (sl.middle(i)) atomicAdd(&m.hist[weight_key(sl.x[i]) >> digit_shift(0)], 1u);
+  __syncthreads();
+  uint32_t* h = ws.hist + (static_cast<size_t>(s) * ws.slices + slice) * kDigits;
+  h[threadIdx.x] = m.hist[threadIdx.x];
+  h[threadIdx.x + kPlanThreads] = m.hist[threadIdx.x + kPlanThreads];
+}
+
+__global__ __launch_bounds__(kPlanThreads) void evict_aside_kernel(const EvictPlanArgs a, const PlanWork ws) {
+  constexpr int kFlight = 8;
+  __shared__ PlanMem m;
+  const int s = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x;
+  const PlanSeq q = plan_seq(a, s);
+  if (q.n <= a.high || q.k == 0 || slice * kSlice >= q.n) return;
+  Slice sl;
+  sl.load(a, q, slice);
+  // every slice adds the counts of all up and finds the digit
+  const int slices = (q.n + kSlice - 1) / kSlice;
+  const uint2* h = reinterpret_cast<const uint2*>(ws.hist + static_cast<size_t>(s) * ws.slices * kDigits) +
+                   (kPlanThreads - 1 - tid);
+  uint2 c = make_uint2(0, 0);
+  for (int v0 = 0; v0 < slices; v0 += kFlight) {
+    uint2 t[kFlight];
 #pragma unroll
-    for (int e = 0; e < kPlanPer; ++e) {
-      const bool ab = (above >> e) & 1, eq = (equal >> e) & 1;
-      if (ab || (eq && ne < left))
-        keep(lo + r0 + tid * kPlanPer + e, lo + static_cast<int>(na + min(ne, left)));
-      na += ab ? 1 : 0;
-      ne += eq ? 1 : 0;
+    for (int v = 0; v < kFlight; ++v)
+      t[v] = v0 + v < slices ? h[static_cast<size_t>(v0 + v) * (kDigits / 2)] : make_uint2(0, 0);
+#pragma unroll
+    for (int v = 0; v < kFlight; ++v) {
+      c.x += t[v].x;
+      c.y += t[v].y;
     }
-    before += total;
   }
+  if (tid == 0) m.count = 0;
+  uint32_t left = static_cast<uint32_t>(q.k);
+  const uint32_t digit = find_digit(m, c.y, c.x, left);
+  uint32_t* keys = ws.keys + (static_cast<size_t>(s) * ws.slices + slice) * kSlice;
+  uint32_t above = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanPer; ++i) {
+    const uint32_t key = weight_key(sl.x[i]), d = key >> digit_shift(0);
+    if (!sl.middle(i)) continue;
+    above += d > digit ? 1 : 0;
+    if (d == digit) keys[atomicAdd(&m.count, 1u)] = key;
+  }
+  above = block_sum(above, m.scratch);
+  if (tid == 0) {
+    ws.sums[static_cast<size_t>(s) * ws.slices + slice] = make_uint4(above, m.count, 0, 0);
+    if (slice == 0) ws.cut[s] = make_uint4(digit, left, 0, 0);
+  }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void evict_cut_kernel(const EvictPlanArgs a, const PlanWork ws) {
+  __shared__ PlanMem m;
+  __shared__ uint4 sums[kMaxSlices];
+  const int s = blockIdx.x, tid = threadIdx.x;
+  const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const PlanSeq q = plan_seq(a, s);
+  if (q.n <= a.high || q.k == 0) return;
+  const int slices = (q.n + kSlice - 1) / kSlice;
+  const uint4 cut = ws.cut[s];
+  uint4* mine = ws.sums + static_cast<size_t>(s) * ws.slices;
+  const uint32_t* keys = ws.keys + static_cast<size_t>(s) * ws.slices * kSlice;
+  if (tid < slices) sums[tid] = mine[tid];
+  uint32_t prefix = cut.x << digit_shift(0), mask = digit_bits(0) << digit_shift(0), left = cut.y;
+#pragma unroll
+  for (int d = 1; d < 3; ++d) {
+    clear_counts(m);
+    for (int v = 0; v < slices; ++v)
+      for (uint32_t i = tid; i < sums[v].y; i += kPlanThreads) {
+        const uint32_t key = keys[static_cast<size_t>(v) * kSlice + i];
+        if ((key & mask) == prefix) atomicAdd(&m.hist[(key >> digit_shift(d)) & digit_bits(d)], 1u);
+      }
+    prefix |= find_digit(m, left) << digit_shift(d);
+    mask |= digit_bits(d) << digit_shift(d);
+  }
+  // a wave counts a slice's keys above the last one and equal to it
+  for (int v = wave; v < slices; v += kPlanWaves) {
+    uint32_t na = 0, ne = 0;
+    const uint32_t n = sums[v].y;
+    for (uint32_t i = 0; i < n; i += kWave) {
+      const uint32_t key = i + lane < n ? keys[static_cast<size_t>(v) * kSlice + i + lane] : 0;
+      na += __popcll(__ballot(i + lane < n && key > prefix));
+      ne += __popcll(__ballot(i + lane < n && key == prefix));
+    }
+    if (lane == 0) {
+      sums[v].z = sums[v].x + na;
+      sums[v].w = ne;
+    }
+  }
+  __syncthreads();
+  const uint64_t c = tid < slices ? static_cast<uint64_t>(sums[tid].z) << 32 | sums[tid].w : 0;
+  __shared__ uint64_t scratch[kPlanWaves + 1];
+  uint64_t total;
+  const uint64_t before = block_exclusive_scan(c, scratch, &total);
+  if (tid < slices)
+    mine[tid] = make_uint4(static_cast<uint32_t>(before >> 32), static_cast<uint32_t>(before), 0, 0);
+  if (tid == 0) ws.cut[s] = make_uint4(prefix, left, 0, 0);
+}
+
+__global__ __launch_bounds__(kPlanThreads) void evict_place_kernel(const EvictPlanArgs a, const PlanWork ws) {
+  __shared__ PlanMem m;
+  const int s = blockIdx.y, slice = blockIdx.x;
+  const PlanSeq q = plan_seq(a, s);
+  if (q.n < 0 || slice * kSlice >= q.n) return;
+  Slice sl;
+  sl.load(a, q, slice);
+  uint4 cut = make_uint4(0xffffffffu, 0, 0, 0), front = make_uint4(0, 0, 0, 0);
+  if (q.n > a.high && q.k > 0) {
+    cut = ws.cut[s];
+    front = ws.sums[static_cast<size_t>(s) * ws.slices + slice];
+  }
+  place_rows(a, s, sl, cut.x, cut.y, front.x, front.y, m);
 }
 
 // ---------------------------------------------------------------------------------------------
 
 constexpr int kMoveWaves = 4;
 constexpr int kMoveThreads = kMoveWaves * kWave;
-constexpr int kMoveRows = 4;             // rows of a wave
+constexpr int kMoveRows = 8;             // rows of a wave at most
 constexpr int kMoveFlight = 4;           // items of a lane on their way at once
 
+// How a wave's items are numbered: `rows` rows of `per` items, `per_head` of each head; quotients of numbers below
+// 512 by multiplication (x * magic >> 20: exact, as 512 x 512 < 2^20).
+struct MoveItems {
+  int rows, per, per_head;
+  uint32_t by_per, by_head;
+};
+
 template <bool HALF, bool TURN>
-__global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const PagedCompactArgs a) {
+__global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const PagedCompactArgs a,
+                                                                   const MoveItems items) {
   __shared__ __attribute__((aligned(16))) float2 cs[kMoveWaves][kMoveRows][kMaxRopePairs];
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -142,19 +358,19 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
     if (blockIdx.x == 0 && threadIdx.x == 0) set_status(a.d_status, OMNITIDE_E_CAPACITY);
     return;
   }
-  const int i0 = (blockIdx.x * kMoveWaves + wave) * kMoveRows;
+  const int i0 = (blockIdx.x * kMoveWaves + wave) * items.rows;
   if (i0 >= kept) return;
 
-  // lane r < kMoveRows: row i0 + r's slots and shift (from < 0: not moved)
+  // lane r < items.rows: row i0 + r's slots and shift (from < 0: not moved)
   int64_t from = -1, to = -1;
   int shift = 0;
-  if (lane < kMoveRows && i0 + lane < kept) {
+  if (lane < items.rows && i0 + lane < kept) {
     const int i = i0 + lane, j = a.src_row[s * a.src_stride + i];
+    const int p1 = a.dst_table[static_cast<int64_t>(s) * a.dst_max_pages + (i >> b.page_shift)];
     if (j < 0 || j >= n) {
       set_status(a.d_status, OMNITIDE_E_RANGE);
     } else {
       const int p0 = b.table[static_cast<int64_t>(s) * b.max_pages + (j >> b.page_shift)];
-      const int p1 = a.dst_table[static_cast<int64_t>(s) * a.dst_max_pages + (i >> b.page_shift)];
       if (p0 < 0 || p0 >= b.n_pages || p1 < 0 || p1 >= b.n_pages) {
         set_status(a.d_status, OMNITIDE_E_PAGES);
       } else {
@@ -167,41 +383,29 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
     }
   }
   if (__ballot(from >= 0) == 0) return;
-  if constexpr (TURN) {
-#pragma unroll
-    for (int r = 0; r < kMoveRows; ++r) {
-      const int d = readlane(shift, r);
-      if (d != 0 && lane < a.rope_dims / 2) {
-        const double rev = static_cast<double>(d) * a.turns[lane];
-        float sn, cn;
-        sincospif(2.f * static_cast<float>(rev - rint(rev)), &sn, &cn);
-        cs[wave][r][lane] = make_float2(cn, sn);
-      }
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the wave reads what it wrote
-  }
-  const int per = a.row_elems / 8, all = kMoveRows * per, per_head = a.head_dim / 8;
-  const int R = TURN ? a.rope_dims : 0;
+  const int all = items.rows * items.per, R = TURN ? a.rope_dims : 0;
   const size_t row_bytes = static_cast<size_t>(a.row_elems) * 2;
-  for (int it0 = 0; it0 < all; it0 += kMoveFlight * kWave) {
-    u32x4 ka[kMoveFlight], kb[kMoveFlight], v[kMoveFlight];
-    int row[kMoveFlight], da[kMoveFlight], db[kMoveFlight], pair[kMoveFlight];
-    int64_t dst[kMoveFlight];
+
+  u32x2 ka[kMoveFlight], kb[kMoveFlight];
+  u32x4 v[kMoveFlight];
+  int row[kMoveFlight], piece[kMoveFlight], da[kMoveFlight], db[kMoveFlight], pair[kMoveFlight];
+  bool on[kMoveFlight];
+  auto load = [&](int it0) {
 #pragma unroll
     for (int f = 0; f < kMoveFlight; ++f) {
       const int it = it0 + f * kWave + lane;
       const bool in = it < all;
-      row[f] = in ? it / per : 0;
-      const int piece = in ? it - row[f] * per : 0;
-      int64_t at = __shfl(static_cast<long long>(from), row[f], kWave);
-      dst[f] = __shfl(static_cast<long long>(to), row[f], kWave);
-      if (!in) at = -1;
+      row[f] = in ? static_cast<int>((static_cast<uint32_t>(it) * items.by_per) >> 20) : 0;
+      piece[f] = in ? it - row[f] * items.per : 0;
+      const int64_t at = __shfl(static_cast<long long>(from), row[f], kWave);
+      on[f] = in && at >= 0;
       pair[f] = -1;
-      da[f] = 8 * piece;
-      db[f] = 8 * piece + 4;
+      da[f] = 8 * piece[f];
+      db[f] = 8 * piece[f] + 4;
       if constexpr (TURN) {
         // of each head first the rotated items, then the other dimensions
-        const int head = piece / per_head, x = piece - head * per_head;
+        const int head = static_cast<int>((static_cast<uint32_t>(piece[f]) * items.by_head) >> 20);
+        const int x = piece[f] - head * items.per_head;
         if (8 * x < R) {
           pair[f] = 4 * x;
           da[f] = a.rope_offset + (HALF ? 4 * x : 8 * x);
@@ -214,23 +418,39 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
         da[f] += head * a.head_dim;
         db[f] += head * a.head_dim;
       }
-      if (at >= 0) {
+      if (on[f]) {
         const uint8_t* k = static_cast<const uint8_t*>(a.k) + at * row_bytes;
-        ka[f] = load_quad<false>(k, da[f]);
-        kb[f] = load_quad<false>(k, db[f]);
+        ka[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * da[f]));
+        kb[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * db[f]));
         if (a.v != nullptr)
-          v[f] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.v) + at * row_bytes +
-                                                 16 * piece);
-      } else {
-        dst[f] = -1;
+          v[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
+              static_cast<const uint8_t*>(a.v) + at * row_bytes + 16 * piece[f]));
       }
     }
+  };
+  load(0);
+  if constexpr (TURN) {                  // the angles, while the first rows are on their way
+    for (int r = 0; r < items.rows; ++r) {
+      const int d = readlane(shift, r);
+      if (d != 0 && lane < a.rope_dims / 2) {
+        const double rev = static_cast<double>(d) * a.turns[lane];
+        float sn, cn;
+        sincospif(2.f * static_cast<float>(rev - rint(rev)), &sn, &cn);
+        cs[wave][r][lane] = make_float2(cn, sn);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the wave reads what it wrote
+  }
+  for (int it0 = 0; it0 < all; it0 += kMoveFlight * kWave) {
+    if (it0 > 0) load(it0);
 #pragma unroll
     for (int f = 0; f < kMoveFlight; ++f) {
+      const int64_t at = __shfl(static_cast<long long>(to), row[f], kWave);
       if constexpr (TURN) {
         const int d = __shfl(shift, row[f], kWave);
-        if (dst[f] >= 0 && pair[f] >= 0 && d != 0) {
-          floatx4 x = unpack_quad<false>(ka[f]), y = unpack_quad<false>(kb[f]), c, sn;
+        if (on[f] && pair[f] >= 0 && d != 0) {
+          floatx4 x = unpack_quad<false>(u32x4{ka[f][0], ka[f][1], 0, 0});
+          floatx4 y = unpack_quad<false>(u32x4{kb[f][0], kb[f][1], 0, 0}), c, sn;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float2 t = cs[wave][row[f]][pair[f] + e];
@@ -238,42 +458,81 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
             sn[e] = t.y;
           }
           turn_quads<HALF>(x, y, c, sn);
-          ka[f] = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), 0, 0};
-          kb[f] = u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), 0, 0};
+          ka[f] = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+          kb[f] = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
         }
       }
-      if (dst[f] < 0) continue;
-      uint8_t* k = static_cast<uint8_t*>(a.k) + dst[f] * row_bytes;
-      *reinterpret_cast<u32x2*>(k + 2 * da[f]) = u32x2{ka[f][0], ka[f][1]};
-      *reinterpret_cast<u32x2*>(k + 2 * db[f]) = u32x2{kb[f][0], kb[f][1]};
-      if (a.v != nullptr) {
-        const int piece = it0 + f * kWave + lane - row[f] * per;
-        *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.v) + dst[f] * row_bytes + 16 * piece) = v[f];
-      }
+      if (!on[f]) continue;
+      uint8_t* k = static_cast<uint8_t*>(a.k) + at * row_bytes;
+      *reinterpret_cast<u32x2*>(k + 2 * da[f]) = ka[f];
+      *reinterpret_cast<u32x2*>(k + 2 * db[f]) = kb[f];
+      if (a.v != nullptr)
+        *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.v) + at * row_bytes + 16 * piece[f]) = v[f];
     }
   }
 }
 
+struct PlanLayout {
+  size_t keys, sums, cut, bytes;
+  int slices;
+};
+PlanLayout plan_layout(int n_seq, int max_ctx) {
+  PlanLayout l{};
+  l.slices = (max_ctx + kSlice - 1) / kSlice;
+  if (l.slices == 1) return l;
+  const size_t n = static_cast<size_t>(n_seq) * l.slices;
+  l.keys = n * kDigits * sizeof(uint32_t);
+  l.sums = l.keys + n * kSlice * sizeof(uint32_t);
+  l.cut = l.sums + n * sizeof(uint4);
+  l.bytes = l.cut + n_seq * sizeof(uint4);
+  return l;
+}
+
 }  // namespace
 
-size_t evict_plan_workspace_bytes(int, int) { return 0; }
+size_t evict_plan_workspace_bytes(int n_seq, int max_ctx) { return plan_layout(n_seq, max_ctx).bytes; }
 
 hipError_t launch_evict_plan(const EvictPlanArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(evict_plan_kernel, dim3(a.n_seq), dim3(kPlanThreads), 0, stream, a);
+  const PlanLayout l = plan_layout(a.n_seq, a.max_ctx);
+  if (l.slices == 1) {
+    hipLaunchKernelGGL(evict_plan_kernel, dim3(a.n_seq), dim3(kPlanThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  uint8_t* base = static_cast<uint8_t*>(a.workspace);
+  const PlanWork ws{reinterpret_cast<uint32_t*>(base), reinterpret_cast<uint32_t*>(base + l.keys),
+                    reinterpret_cast<uint4*>(base + l.sums), reinterpret_cast<uint4*>(base + l.cut), l.slices};
+  const dim3 grid(l.slices, a.n_seq), block(kPlanThreads);
+  hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, stream, a, ws);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(evict_aside_kernel, grid, block, 0, stream, a, ws);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(evict_cut_kernel, dim3(a.n_seq), block, 0, stream, a, ws);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(evict_place_kernel, grid, block, 0, stream, a, ws);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream) {
   const int64_t cap = static_cast<int64_t>(a.dst_max_pages) << a.batch.page_shift;
   const int64_t rows = a.src_stride < cap ? a.src_stride : cap;
-  const int per = kMoveWaves * kMoveRows;
+  // as many rows per wave as its lanes have items on their way for
+  MoveItems items;
+  items.per = a.row_elems / 8;
+  items.rows = max(1, min(kMoveRows, kMoveFlight * kWave / items.per));
+  items.per_head = max(1, a.head_dim / 8);
+  items.by_per = ((1u << 20) + items.per - 1) / items.per;
+  items.by_head = ((1u << 20) + items.per_head - 1) / items.per_head;
+  const int per = kMoveWaves * items.rows;
   const dim3 grid(static_cast<unsigned>((rows + per - 1) / per), static_cast<unsigned>(a.batch.n_seq));
   if (a.rope_dims == 0)
-    hipLaunchKernelGGL((paged_compact_kernel<false, false>), grid, dim3(kMoveThreads), 0, stream, a);
+    hipLaunchKernelGGL((paged_compact_kernel<false, false>), grid, dim3(kMoveThreads), 0, stream, a, items);
   else if (a.rope_half)
-    hipLaunchKernelGGL((paged_compact_kernel<true, true>), grid, dim3(kMoveThreads), 0, stream, a);
+    hipLaunchKernelGGL((paged_compact_kernel<true, true>), grid, dim3(kMoveThreads), 0, stream, a, items);
   else
-    hipLaunchKernelGGL((paged_compact_kernel<false, true>), grid, dim3(kMoveThreads), 0, stream, a);
+    hipLaunchKernelGGL((paged_compact_kernel<false, true>), grid, dim3(kMoveThreads), 0, stream, a, items);
   return hipGetLastError();
 }
 
