@@ -1,0 +1,452 @@
+// The weight that few tokens of each sequence give to each cached row (up to 16 query vectors per KV head): the
+// keys are read once.
+//
+// Mathematics: as attn_weights.hip.  Bound by memory: 2 d bytes of a key serve 16 vectors at most.  So the scores
+// of the one pass over the keys are kept (4 bytes per query head and key, a twelfth to a half of the keys),
+// beside each vector's running reference and sum per share; a second kernel joins the sums of the shares, a
+// third sums exp2(x - m) / l over the vectors, a key per thread.
+//   shares    as in paged decode: the 16-key blocks of all sequences with tokens, one after the other, cut into
+//             equal shares, one per workgroup and KV head, a fixed cost counted for each sequence.
+//   waves     each takes every fourth block of its workgroup's part and owns a ring of LDS buffers filled by
+//             direct loads marked as read once; no barrier until the waves merge.
+//   products  S^T (16 keys x 16 vectors) = K Q^T with v_mfma_f32_16x16x32_bf16: a lane holds four
+//             consecutive keys of a vector, stored as 16 bytes.
+#include "common.h"
+#include "evict.h"
+#include "mfma_tile.h"
+#include "paged_rows.h"
+
+namespace omnitide {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kKB = 16;                  // keys per block
+constexpr int kCols = 16;                // query vectors of a sequence and KV head at most
+constexpr int kMaxWGs = 512;
+constexpr int kMinShare = 8;             // blocks of a share at least
+constexpr int kOverhead = 12;            // what a sequence costs beside its blocks, in blocks
+constexpr size_t kScoreBytes = size_t{1} << 30;   // scores that are kept at most
+constexpr int kSumThreads = 256;
+
+template <int D>
+constexpr int wgs_of() { return D <= 128 ? kMaxWGs : kMaxWGs / 2; }
+
+// sequence i = 64 n + lane holds nb[n] blocks, work for kOverhead + nb[n] (none without blocks); first[n] is its KV
+// head's work before it, per_head all of it, `share` that of a workgroup.
+template <int NS>
+struct FewShares {
+  int nb[NS], first[NS], ctx[NS], q0[NS], len[NS];
+  int per_head, share;
+};
+
+// A sequence that starts in front of an earlier offset has no tokens, nor has one with more than max_q.
+template <int NS>
+__device__ inline FewShares<NS> plan_few(const AttnWeightsArgs& a, int wgs) {
+  const PagedBatch& b = a.batch;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int cap = b.max_pages << b.page_shift;
+  FewShares<NS> s;
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const int i = n * kWave + lane;
+    s.q0[n] = i < b.n_seq ? b.q_start[i] : 0;
+    s.len[n] = i < b.n_seq ? b.q_start[i + 1] : 0;
+    s.ctx[n] = i < b.n_seq ? b.ctx_len[i] : -1;
+  }
+  s.per_head = 0;
+  int front = 0;
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const int q0 = s.q0[n], q1 = s.len[n];
+    const int before = max(front, wave_exclusive_max_i32(q0, 0));
+    front = max(front, wave_max_i32(q0));
+    const bool ok = q0 >= before && q1 > q0 && q1 <= b.n_tokens && q1 - q0 <= a.max_q &&
+                    s.ctx[n] >= q1 - q0 && s.ctx[n] <= cap;
+    s.len[n] = ok ? q1 - q0 : 0;
+    s.nb[n] = ok ? (s.ctx[n] + kKB - 1) / kKB : 0;
+    const int work = ok ? kOverhead + s.nb[n] : 0;
+    const int inc = wave_scan_add_i32(work);
+    s.first[n] = s.per_head + inc - work;
+    s.per_head += readlane(inc, kWave - 1);
+  }
+  const int per = max(1, wgs / a.n_kv_heads);
+  s.share = max(kMinShare, (s.per_head + per - 1) / per);
+  return s;
+}
+
+// What the kernels hand on.
+struct FewWork {
+  int4* seqs;                            // first token, tokens (0: none), context
+  float2* part_ml;                       // [2 x workgroup][kCols]
+  float2* stats;                         // (m, 1 / l) [token][query head]
+  float* scores;                         // [token][query head][max_ctx]
+};
+
+template <int D, int NS>
+__global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kernel(
+    const AttnWeightsArgs a, const FewWork ws, float scale_log2) {
+  constexpr int KC = D / 32;               // 32-dim slices of a key
+  constexpr int CH = D / 8;                // 16-byte chunks per row
+  constexpr int LOADS = CH / 8;            // direct loads per eight keys
+  constexpr int BLOCKB = kKB * 2 * D;
+  constexpr int RING = D == 64 ? 8 : D == 128 ? 4 : D == 320 ? 3 : 2;
+  constexpr int CALLS = 2 * LOADS;         // direct loads of a block
+  constexpr float kSumLimit = 4294967296.f;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kWaves * RING * BLOCKB];
+  __shared__ float sm[kWaves][kCols], sl[kWaves][kCols];
+  const PagedBatch& b = a.batch;
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int c16 = lane & 15, g4 = lane >> 4;
+  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
+  const int max_ctx = b.max_pages << b.page_shift;
+
+  const FewShares<NS> sh = plan_few<NS>(a, gridDim.x);
+  if (blockIdx.x == 0 && wave == 0) {
+    report_batch(b, a.d_status);
+    bool many = false;
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      const int i = n * kWave + lane;
+      if (i >= b.n_seq) continue;
+      ws.seqs[i] = make_int4(sh.q0[n], sh.len[n], sh.ctx[n], 0);
+      const int s0 = b.q_start[i], s1 = b.q_start[i + 1];
+      many |= s0 >= 0 && s1 >= s0 && s1 <= b.n_tokens && s1 - s0 > a.max_q;
+    }
+    if (__any(many) && lane == 0) set_status(a.d_status, OMNITIDE_E_CAPACITY);
+  }
+  const int g = blockIdx.x % Hkv;
+  const int64_t lo64 = static_cast<int64_t>(blockIdx.x / Hkv) * sh.share;
+  if (lo64 >= sh.per_head) return;
+  const int lo = static_cast<int>(lo64), hi = min(lo + sh.share, sh.per_head);
+
+  // The swizzle: 16 keys' equal chunks lie in distinct banks (rows of 256 bytes by their number, those of an odd
+  // number of 128 bytes by half of it).
+  auto swz = [](int key) { return D == 128 ? key & 15 : (key >> 1) & 7; };
+  const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
+  // direct load c of a block: chunk c * 64 + lane of its 16 rows
+  uint32_t off[CALLS];
+  int row[CALLS];
+#pragma unroll
+  for (int c = 0; c < CALLS; ++c) {
+    const int at = c * kWave + lane;
+    row[c] = at / CH;
+    off[c] = 16u * ((at % CH) ^ swz(row[c]));
+  }
+  const uint32_t ring = lds_addr(smem) + static_cast<uint32_t>(wave * RING * BLOCKB);
+  constexpr uint32_t kFlip = D == 128 ? 0xffu : 0x7fu;
+  const uint32_t k_lane = 2u * D * c16 + 16u * (g4 ^ swz(c16));
+
+  for (int pos = lo; pos < hi;) {
+    // the part of one sequence that starts at pos; its overhead comes before its blocks
+    int seq = 0, u0 = 0, nb = 1, ctx = 1, q0 = 0, len = 1;
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      const uint64_t hit = __ballot(sh.nb[n] > 0 && pos >= sh.first[n] &&
+                                    pos < sh.first[n] + kOverhead + sh.nb[n]);
+      if (hit != 0) {
+        const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+        seq = n * kWave + l;
+        u0 = pos - readlane(sh.first[n], l);
+        nb = readlane(sh.nb[n], l);
+        ctx = readlane(sh.ctx[n], l);
+        q0 = readlane(sh.q0[n], l);
+        len = readlane(sh.len[n], l);
+      }
+    }
+    const int u1 = min(kOverhead + nb, u0 + (hi - pos));
+    const int b0 = max(u0 - kOverhead, 0), b1 = max(u1 - kOverhead, 0);
+    pos += u1 - u0;
+    if (b1 == 0) break;                      // the share ends before the first block
+    const bool whole = b0 == 0 && b1 == nb;
+    // a share holds at most one part that goes on from an earlier share and one that goes on in a later
+    const int slot = 2 * static_cast<int>(blockIdx.x) + (b0 > 0 ? 0 : 1);
+
+    // Q^T operand: column c16 = query vector (token c16 / G, head g*G + c16 % G)
+    const bool col_ok = c16 < len * G;
+    const int tok = col_ok ? c16 / G : 0;
+    const int lim = ctx - len + tok;         // keys <= lim are visible
+    const size_t vec = static_cast<size_t>(q0 + tok) * Hq + g * G + (col_ok ? c16 % G : 0);
+    const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + vec * D;
+    float* scores = ws.scores + vec * max_ctx;
+    bf16x8 qf[KC];
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+      qf[kc] = __builtin_bit_cast(bf16x8, ld16(qrow + 32 * kc + 8 * g4));
+
+    int n_it = (b1 - b0 - wave + kWaves - 1) / kWaves;          // this wave's blocks
+    int bad_row = INT32_MAX;                 // the first row of this wave's first block of a bad page
+    const int32_t* table = b.table + static_cast<size_t>(seq) * b.max_pages;
+    int pages = 0;                           // page of block it, in lane it % 64
+    auto block_of = [&](int it) { return b0 + wave + kWaves * it; };
+    // A block of a bad page is the wave's end: the vectors that see it are spoilt (below), and the others see
+    // no later one either.
+    auto load_pages = [&](int it) {
+      const int i = it + lane;
+      const bool in = i < n_it;
+      const int p = in ? table[(block_of(i) * kKB) >> b.page_shift] : 0;
+      const uint64_t bad = __ballot(in && (p < 0 || p >= b.n_pages));
+      if (bad != 0) {
+        if (lane == 0) set_status(a.d_status, OMNITIDE_E_PAGES);
+        n_it = it + __ffsll(static_cast<unsigned long long>(bad)) - 1;
+        bad_row = block_of(n_it) * kKB;
+      }
+      pages = p;
+    };
+    auto issue = [&](int it, int e) {
+      const int key0 = block_of(it) * kKB;
+      const int page = readlane(pages, it & (kWave - 1));
+      const uint8_t* base = static_cast<const uint8_t*>(a.k) + 2 * g * D +
+                            ((static_cast<size_t>(page) << b.page_shift) +
+                             (key0 & ((1 << b.page_shift) - 1))) * row_bytes;
+      const int last = ctx - 1 - key0;       // rows past it are clamped to it
+#pragma unroll
+      for (int c = 0; c < CALLS; ++c)
+        dma16_once(base, static_cast<uint32_t>(min(row[c], last)) * row_bytes + off[c],
+                   ring + static_cast<uint32_t>(e * BLOCKB + c * kWave * 16));
+    };
+    float m_run = -INFINITY, l_run = 0.f;
+    load_pages(0);
+    // nothing but the direct loads and the stores of scores is counted from here on
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
+#pragma unroll
+    for (int e = 0; e < RING; ++e)
+      if (e < n_it) issue(e, e);
+    for (int it0 = 0; it0 < n_it; it0 += RING) {
+#pragma unroll
+      for (int e = 0; e < RING; ++e) {
+        const int it = it0 + e;
+        if (it >= n_it) break;
+        // This block has landed: what was asked for after it are the loads of the blocks behind and the
+        // stores of the blocks in front, RING - 1 of each at most (fewer at both ends, where all are waited
+        // for).  Loads and stores come back in their order.
+        if (it >= RING && it + RING - 1 < n_it) wait_vmcnt<(RING - 1) * (CALLS + 1)>();
+        else wait_vmcnt<0>();
+        const uint32_t kb = ring + static_cast<uint32_t>(e * BLOCKB);
+        floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) {
+          const uint32_t at = (k_lane ^ (64u * kc & kFlip)) + (64u * kc & ~kFlip);
+          const u32x4 w = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(kb + at);
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), qf[kc], s, 0, 0, 0);
+        }
+        const int key0 = block_of(it) * kKB;
+        // the next block into this entry, whose reads have returned
+        if (it + RING < n_it) {
+          if (((it + RING) & (kWave - 1)) == 0) {
+            load_pages(it + RING);
+            asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(s) : : "memory");
+          if (it + RING < n_it) issue(it + RING, e);
+        }
+        if (col_ok) __builtin_nontemporal_store(s, reinterpret_cast<floatx4*>(scores + key0 + 4 * g4));
+        if (key0 + kKB - 1 > ctx - len) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (key0 + 4 * g4 + i > lim) s[i] = -INFINITY;
+        }
+        float ls = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ls += __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -m_run));
+        if (__any(!(ls < kSumLimit))) {
+          // exact block maximum per column (its four lane groups), move the reference, recompute
+          float mx = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[i] == -INFINITY ? -INFINITY : s[i] * scale_log2);
+          mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+          const float m_new = fmaxf(m_run, mx);
+          const float m_use = m_new == -INFINITY ? 0.f : m_new;
+          l_run *= __builtin_amdgcn_exp2f(m_run - m_use);
+          m_run = m_new;
+          ls = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            ls += s[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -m_use));
+        }
+        l_run += ls;
+      }
+    }
+    // merge the waves; a sum that is no number spoils the column to the end, whatever references there are
+    if (lim >= bad_row) l_run = __builtin_nanf("");
+    const float l_col = l_run + __shfl_xor(l_run, 16, kWave) + __shfl_xor(l_run, 32, kWave) +
+                        __shfl_xor(l_run, 48, kWave);
+    __syncthreads();                         // the part before has been merged
+    if (g4 == 0) {
+      sm[wave][c16] = l_col == l_col ? m_run : 0.f;
+      sl[wave][c16] = l_col;
+    }
+    __syncthreads();
+    if (tid < kCols) {
+      float M = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm[w][tid]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        if (sm[w][tid] != -INFINITY) l = fmaf(__builtin_amdgcn_exp2f(sm[w][tid] - M), sl[w][tid], l);
+      if (!whole) ws.part_ml[static_cast<size_t>(slot) * kCols + tid] = make_float2(M, l);
+      else if (col_ok) ws.stats[vec] = make_float2(M, 1.f / l);        // (c16 = tid here)
+    }
+  }
+}
+
+// Joins a vector's statistics over the shares that its sequence lies in: a wave per vector, a part per lane.
+template <int NS>
+__global__ __launch_bounds__(kThreads) void weights_few_join_kernel(const AttnWeightsArgs a, const FewWork ws,
+                                                                  int wgs) {
+  const PagedBatch& b = a.batch;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
+  const int64_t vec = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
+  if (vec >= static_cast<int64_t>(b.n_tokens) * Hq) return;
+  const int t = static_cast<int>(vec / Hq), head = static_cast<int>(vec - static_cast<int64_t>(t) * Hq);
+  const int g = head / G;
+  const FewShares<NS> sh = plan_few<NS>(a, wgs);
+  int first = 0, nb = 0, tok = 0;
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const uint64_t hit = __ballot(sh.nb[n] > 0 && t >= sh.q0[n] && t < sh.q0[n] + sh.len[n]);
+    if (hit != 0) {
+      const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+      first = readlane(sh.first[n], l);
+      nb = readlane(sh.nb[n], l);
+      tok = t - readlane(sh.q0[n], l);
+    }
+  }
+  if (nb == 0) return;
+  const int w0 = (first + kOverhead) / sh.share, w1 = (first + kOverhead + nb - 1) / sh.share;
+  if (w0 == w1) return;                    // finished by its workgroup
+  const int col = tok * G + head % G;
+  float mx = -INFINITY, l = 0.f;
+  for (int p = lane; p <= w1 - w0; p += kWave) {
+    const float2 v =
+        ws.part_ml[static_cast<size_t>(2 * ((w0 + p) * Hkv + g) + (p == 0 ? 1 : 0)) * kCols + col];
+    const float m = fmaxf(mx, v.x);
+    if (m != -INFINITY) {
+      l = (mx == -INFINITY ? 0.f : l * exp2f(mx - m)) + (v.x == -INFINITY ? 0.f : v.y * exp2f(v.x - m));
+      mx = m;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const float m2 = __shfl_xor(mx, o, kWave), l2 = __shfl_xor(l, o, kWave), m = fmaxf(mx, m2);
+    if (m != -INFINITY) {
+      // (the lower lane's part first, in both lanes)
+      const float u = mx == -INFINITY ? 0.f : l * exp2f(mx - m);
+      const float v = m2 == -INFINITY ? 0.f : l2 * exp2f(m2 - m);
+      l = u + v;
+      mx = m;
+    }
+  }
+  if (lane == 0) ws.stats[vec] = make_float2(mx, 1.f / l);
+}
+
+// The new weights: a key per thread, over the tokens and heads.
+__global__ __launch_bounds__(kSumThreads) void weights_few_add_kernel(const AttnWeightsArgs a,
+                                                                    const FewWork ws, float scale_log2) {
+  constexpr int kFlight = 8;
+  const PagedBatch& b = a.batch;
+  const int s = blockIdx.y, j = blockIdx.x * kSumThreads + threadIdx.x;
+  const int4 q = ws.seqs[s];
+  if (q.y == 0 || static_cast<int>(blockIdx.x) * kSumThreads >= q.z) return;
+  const int max_ctx = b.max_pages << b.page_shift, kept = q.z - q.y;
+  const bool in = j < q.z;
+  const int n = q.y * a.n_q_heads;         // the sequence's vectors, token by token
+  const size_t vec0 = static_cast<size_t>(q.x) * a.n_q_heads;
+  const float* scores = ws.scores + vec0 * max_ctx + (in ? j : 0);
+  const float2* stats = ws.stats + vec0;
+  // vectors of tokens that see row j: those from token j - kept on
+  const int v_from = max(j - kept, 0) * a.n_q_heads;
+  float sum = 0.f;
+  for (int v0 = 0; v0 < n; v0 += kFlight) {
+    float x[kFlight];
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i)
+      x[i] = __builtin_nontemporal_load(scores + static_cast<size_t>(min(v0 + i, n - 1)) * max_ctx);
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      const float2 ml = stats[min(v0 + i, n - 1)];
+      const float p = __builtin_amdgcn_exp2f(fmaf(x[i], scale_log2, -ml.x));
+      sum = v0 + i < n && v0 + i >= v_from ? fmaf(p, ml.y, sum) : sum;
+    }
+  }
+  if (!in) return;
+  const size_t at = static_cast<size_t>(s) * a.weight_stride + j;
+  if (a.weight_in != nullptr) {
+    const int seen = a.seen_len != nullptr ? a.seen_len[s] : kept;
+    if (j < seen) sum = fmaf(a.decay, a.weight_in[at], sum);
+  }
+  a.weight_out[at] = sum;
+}
+
+struct Layout {
+  size_t part_ml, stats, scores, bytes;
+};
+Layout layout(int n_tokens, int n_seq, int max_ctx, int n_q_heads) {
+  Layout l;
+  const size_t vecs = static_cast<size_t>(n_tokens) * n_q_heads;
+  l.part_ml = n_seq * sizeof(int4);
+  l.stats = l.part_ml + 2 * kMaxWGs * kCols * sizeof(float2);
+  l.scores = (l.stats + vecs * sizeof(float2) + 15) & ~static_cast<size_t>(15);
+  l.bytes = l.scores + vecs * max_ctx * sizeof(float);
+  return l;
+}
+
+template <int D, int NS>
+hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
+  const PagedBatch& b = a.batch;
+  const int max_ctx = b.max_pages << b.page_shift;
+  const Layout l = layout(b.n_tokens, b.n_seq, max_ctx, a.n_q_heads);
+  uint8_t* base = static_cast<uint8_t*>(a.workspace);
+  const FewWork ws{reinterpret_cast<int4*>(base), reinterpret_cast<float2*>(base + l.part_ml),
+                   reinterpret_cast<float2*>(base + l.stats), reinterpret_cast<float*>(base + l.scores)};
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  // a workgroup per KV head and share
+  const int wgs = max(1, wgs_of<D>() / a.n_kv_heads) * a.n_kv_heads;
+  hipLaunchKernelGGL((weights_score_kernel<D, NS>), dim3(wgs), dim3(kThreads), 0, stream, a, ws, scale_log2);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t vecs = static_cast<int64_t>(b.n_tokens) * a.n_q_heads;
+  hipLaunchKernelGGL(weights_few_join_kernel<NS>, dim3(static_cast<unsigned>((vecs + kWaves - 1) / kWaves)),
+                     dim3(kThreads), 0, stream, a, ws, wgs);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(weights_few_add_kernel, dim3((max_ctx + kSumThreads - 1) / kSumThreads, b.n_seq),
+                     dim3(kSumThreads), 0, stream, a, ws, scale_log2);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_d(const AttnWeightsArgs& a, hipStream_t stream) {
+  return a.batch.n_seq <= kWave ? launch_t<D, 1>(a, stream) : launch_t<D, 16>(a, stream);
+}
+
+}  // namespace
+
+bool attn_weights_few(int n_tokens, int max_ctx, int max_q, int n_q_heads, int n_kv_heads) {
+  return static_cast<int64_t>(max_q) * (n_q_heads / n_kv_heads) <= kCols && n_kv_heads <= 64 &&
+         static_cast<size_t>(n_tokens) * n_q_heads * max_ctx <= kScoreBytes / sizeof(float);
+}
+
+size_t attn_weights_few_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int n_q_heads) {
+  const size_t vecs = static_cast<size_t>(n_tokens) * n_q_heads;
+  const Layout l = layout(n_tokens, n_seq, max_ctx, n_q_heads);
+  // (of a call whose scores are too many to be kept: as many as are)
+  return l.scores + (vecs * max_ctx <= kScoreBytes / sizeof(float) ? vecs * max_ctx * sizeof(float)
+                                                                  : kScoreBytes);
+}
+
+hipError_t launch_attn_weights_few(const AttnWeightsArgs& a, hipStream_t stream) {
+  switch (a.head_dim) {
+    case 64: return launch_d<64>(a, stream);
+    case 128: return launch_d<128>(a, stream);
+    case 320: return launch_d<320>(a, stream);
+    default: return launch_d<576>(a, stream);
+  }
+}
+
+}  // namespace omnitide

@@ -68,7 +68,7 @@ int omnitide_paged_attn_weights(const void* q, const void* k_pool, int n_pages, 
   a.k = k_pool;
   a.batch = omnitide::PagedBatch{page_table, q_start,   ctx_len, n_seq,  n_tokens,
                                  0,          max_pages, shift,   n_pages};
-  a.max_q = max_q < n_tokens ? max_q : n_tokens;
+  a.max_q = max_q;
   a.n_q_heads = n_q_heads;
   a.n_kv_heads = n_kv_heads;
   a.head_dim = head_dim;
