@@ -60,9 +60,10 @@ struct Stage {
     return lds + static_cast<uint32_t>(e * kBytes + (wave + kWaves * i) * kWave * 16);
   }
   // waits until all but this wave's loads of the last `later` stages have landed
-  template <int LATER>
+  // (each with MORE loads beside)
+  template <int LATER, int MORE = 0>
   static __device__ void wait(int wave) {
-    constexpr int lo = kAllCalls / kWaves;
+    constexpr int lo = kAllCalls / kWaves + MORE;
     if (kAllCalls % kWaves != 0 && wave < kAllCalls % kWaves) wait_vmcnt<LATER * (lo + 1)>();
     else wait_vmcnt<LATER * lo>();
   }
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
       for (int c = 0; c < S::kCalls; ++c) {
         if (!S::mine(wave, c)) break;
         const int first = u * S::kKeys + 8 * st.oct[c], at = min(first, ctx - 1);
-        int page = __builtin_amdgcn_readfirstlane(table[at >> b.page_shift]);
+        int page = scalar_entry(table, at >> b.page_shift);
         if (page < 0 || page >= b.n_pages) page = 0;
         const int line = at & ((1 << b.page_shift) - 1) & ~7;
         const uint8_t* base = k_head + ((static_cast<size_t>(page) << b.page_shift) + line) * row_bytes;
@@ -209,6 +210,9 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
       }
     };
     float m_run = -INFINITY, l_run = 0.f;
+    // nothing but the direct loads is counted from here on: the queries are there (and known to be)
+#pragma unroll
+    for (int c = 0; c < NK; ++c) asm volatile("" : "+v"(qf[c]));
     __syncthreads();                       // the stages of the part before are done with
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
@@ -306,7 +310,9 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
                                                                           float scale_log2) {
   using S = Stage<D>;
   constexpr int NK = D / 16, kSub = S::kKeys / 32;
+  constexpr int kStatCalls = 2 * S::kKeys / kWave;         // direct loads of a stage's statistics
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kRing * S::kBytes];
+  __shared__ float2 lds_stats[S::kRing][S::kKeys];         // (m, 1 / l) of a stage's rows
   __shared__ int64_t firsts[SEQS];         // items in front of each sequence
   __shared__ int64_t chunk_sum[SEQS / kWave];
   const PagedBatch& b = a.batch;
@@ -383,9 +389,14 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
 
       const int u_begin = m_begin / S::kKeys, u_end = (m_end + S::kKeys - 1) / S::kKeys;
       const int last_row = rows - 1;
-      // direct loads of query rows [u kKeys, +kKeys): row m is head m % G of token m / G
+      // direct loads of query rows [u kKeys, +kKeys) (row m is head m % G of token m / G) and their statistics
       auto issue = [&](int u) {
         const int e = uniform((u - u_begin) % S::kRing);
+        if (wave < kStatCalls) {
+          const int x = wave * kWave + lane;               // of the stage's floats
+          dma4(stats, 8u * static_cast<uint32_t>(min(u * S::kKeys + (x >> 1), last_row)) + 4u * (x & 1),
+               lds_addr(&lds_stats[e][0]) + static_cast<uint32_t>(wave * kWave * 4));
+        }
         const int base_m = u * S::kKeys, p0 = base_m / G, r0 = base_m - p0 * G;
         const uint8_t* base = static_cast<const uint8_t*>(a.q) +
                               (static_cast<size_t>(q0 + p0) * Hq + static_cast<size_t>(g) * G) * D * 2;
@@ -401,44 +412,46 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
       float acc[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NK; ++c) asm volatile("" : "+v"(kf[c]));         // (there, and known to be)
       __syncthreads();                     // the stages of the item before are done with
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
       for (int u = 0; u < S::kRing - 1; ++u)
         if (u_begin + u < u_end) issue(u_begin + u);
       for (int u = u_begin; u < u_end; ++u) {
-        // the rows' statistics, for this stage (m, and 1 / l: 0 for rows that are none of the item's)
-        float ref[kSub], inv[kSub];
-        int lim[kSub];
-#pragma unroll
-        for (int sub = 0; sub < kSub; ++sub) {
-          const int m = u * S::kKeys + 32 * sub + col, mc = min(m, last_row);
-          const float2 v = stats[mc];
-          ref[sub] = v.x;
-          inv[sub] = m >= m_begin && m < m_end ? v.y : 0.f;
-          lim[sub] = kept + mc / G;
+        // this stage has landed; the later ones may be in flight
+        if (u + S::kRing - 2 < u_end) {
+          if (wave < kStatCalls) S::template wait<S::kRing - 2, 1>(wave);
+          else S::template wait<S::kRing - 2, 0>(wave);
+        } else {
+          wait_vmcnt<0>();
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (u + S::kRing - 1 < u_end) issue(u + S::kRing - 1);
         if (key0 >= ctx) continue;
         const uint32_t stage = lds0 + static_cast<uint32_t>(uniform((u - u_begin) % S::kRing) * S::kBytes);
 #pragma unroll
         for (int sub = 0; sub < kSub; ++sub) {
+          // this lane's row, its statistics (1 / l: 0 where the row is none of the item's) and last visible key
+          const int m = u * S::kKeys + 32 * sub + col;
+          const float2 ml = lds_stats[uniform((u - u_begin) % S::kRing)][32 * sub + col];
+          const float inv = m >= m_begin && m < m_end ? ml.y : 0.f;
           floatx16 x = floatx16{};
 #pragma unroll
           for (int c = 0; c < NK; ++c)
             x = mfma(kf[c], S::operand(stage + 32u * sub * S::kRowB, at_lane, c), x);
           // accumulator e: key key0 + e % 4 + 8 (e / 4) + 4 h of this lane's row
-          const bool all = __all(key0 + 31 <= lim[sub]);
+          if (key0 + 31 <= kept + (u * S::kKeys + 32 * sub) / G) {         // every row sees every key
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float pr = __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -ref[sub]));
-            if (all) {
-              acc[e] = fmaf(pr, inv[sub], acc[e]);
-            } else {
-              const bool seen = key0 + (e & 3) + 8 * (e >> 2) + 4 * h <= lim[sub] && inv[sub] != 0.f;
-              acc[e] = seen ? fmaf(pr, inv[sub], acc[e]) : acc[e];
+            for (int e = 0; e < 16; ++e)
+              acc[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -ml.x)), inv, acc[e]);
+          } else {
+            const int lim = inv != 0.f ? kept + min(m, last_row) / G : -1;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float p = __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -ml.x));
+              acc[e] = key0 + (e & 3) + 8 * (e >> 2) + 4 * h <= lim ? fmaf(p, inv, acc[e]) : acc[e];
             }
           }
         }

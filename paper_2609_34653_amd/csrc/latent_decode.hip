@@ -32,6 +32,7 @@ constexpr int kKT = 32;                  // keys per tile and block
 constexpr int kStep = 2;                 // tiles per step
 constexpr int kRow = 16;                 // vectors per row tile
 constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
+constexpr int kNumXcd = 8;
 constexpr int kMinShare = 4;             // blocks of a share at least
 constexpr int kOverhead = 6;             // what a sequence costs beside its blocks, in blocks
 
@@ -61,7 +62,7 @@ __device__ inline Shares<NS> plan_shares(const PagedBatch& b, int row_tiles) {
     s.first[n] = s.per_head + inc - work;
     s.per_head += readlane(inc, kWave - 1);
   }
-  const int per = max(1, kWGs / row_tiles);
+  const int per = kWGs / kNumXcd / row_tiles * kNumXcd;
   s.share = max(kMinShare, (s.per_head + per - 1) / per);
   return s;
 }
@@ -99,6 +100,8 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
   static_assert(ROWB % 128 == 0 && (ROWB / 128) % 2 == 1, "the swizzle's banks");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kTilesB > kMergeB ? kTilesB : kMergeB];
   __shared__ float sm[kWaves][kRow], sl[kWaves][kRow];
+  __shared__ int slim[kWaves][kRow];
+  __shared__ int3 seqs[NS * kWave];        // work in front of it, blocks, context
 
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
@@ -109,36 +112,31 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
 
   if (blockIdx.x == 0 && wave == 0) report_batch(b, status);
   const Shares<NS> sh = plan_shares<NS>(b, row_groups);
-  // idle sequences: zeros
+  // what the parts are found from, out of registers
+  const int per_head = sh.per_head, share = sh.share;
+  if (wave == 0) {
 #pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    uint64_t idle = __ballot(sh.ctx[n] == 0);
-    while (idle != 0) {
-      const int l = __ffsll(static_cast<unsigned long long>(idle)) - 1;
-      idle &= idle - 1;
-      const int s = n * kWave + l;
-      if (s % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x)) {
-        const size_t at = static_cast<size_t>(s) * M * R;
-        for (int i = tid; i < M * R; i += kThreads) {
-          if (out_bf16) static_cast<uint16_t*>(out)[at + i] = 0;
-          else static_cast<float*>(out)[at + i] = 0.f;
-        }
-      }
+    for (int n = 0; n < NS; ++n)
+      seqs[n * kWave + lane] = make_int3(sh.first[n], sh.nb[n], sh.ctx[n]);
+  }
+  __syncthreads();
+  // idle sequences: zeros
+  for (int s = blockIdx.x; s < b.n_seq; s += gridDim.x) {
+    if (seqs[s].z != 0) continue;
+    const size_t at = static_cast<size_t>(s) * M * R;
+    for (int i = tid; i < M * R; i += kThreads) {
+      if (out_bf16) static_cast<uint16_t*>(out)[at + i] = 0;
+      else static_cast<float*>(out)[at + i] = 0.f;
     }
   }
-  const int rg = blockIdx.x % row_groups;
+  // the row groups of a share (the same keys) on one XCD: workgroups are dealt round-robin over 8
+  const int on_xcd = blockIdx.x / kNumXcd, rg = on_xcd % row_groups;
+  const int wg = on_xcd / row_groups * kNumXcd + blockIdx.x % kNumXcd;       // its share
   const int m0 = rg * RB * kRow;           // the workgroup's first vector
-  const int64_t lo64 = static_cast<int64_t>(blockIdx.x / row_groups) * sh.share;
-  if (lo64 >= sh.per_head) return;
-  const int lo = static_cast<int>(lo64), hi = min(lo + sh.share, sh.per_head);
+  const int64_t lo64 = static_cast<int64_t>(wg) * share;
+  if (lo64 >= per_head) return;
+  const int lo = static_cast<int>(lo64), hi = min(lo + share, per_head);
 
-  // this lane's place in the direct loads of eight keys: chunk c * 64 + lane (row, swizzled chunk)
-  uint32_t off[LOADS];
-#pragma unroll
-  for (int c = 0; c < LOADS; ++c) {
-    const int at = c * kWave + lane, key = at / CH, pc = at % CH;
-    off[c] = key * ROWB + 16u * (pc ^ swz(key));
-  }
   const uint32_t lds0 = lds_addr(smem);
   // K rows of S^T tile a: row r = lane % 16 is key 8 (r / 4) + 4 a + r % 4, dims 32 c + 8 g4
   const int krow = 8 * (col >> 2) + (col & 3);
@@ -150,16 +148,16 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
   for (int pos = lo; pos < hi;) {
     // the part of one sequence that starts at pos; its overhead comes before its blocks
     int seq = 0, u0 = 0, nb = 1, ctx = 1;
-#pragma unroll
     for (int n = 0; n < NS; ++n) {
-      const uint64_t hit = __ballot(sh.nb[n] > 0 && pos >= sh.first[n] &&
-                                    pos < sh.first[n] + kOverhead + sh.nb[n]);
+      const int3 q = seqs[n * kWave + lane];
+      const uint64_t hit = __ballot(q.y > 0 && pos >= q.x && pos < q.x + kOverhead + q.y);
       if (hit != 0) {
         const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
         seq = n * kWave + l;
-        u0 = pos - readlane(sh.first[n], l);
-        nb = readlane(sh.nb[n], l);
-        ctx = readlane(sh.ctx[n], l);
+        u0 = pos - readlane(q.x, l);
+        nb = readlane(q.y, l);
+        ctx = readlane(q.z, l);
+        break;
       }
     }
     const int u1 = min(kOverhead + nb, u0 + (hi - pos));
@@ -168,12 +166,12 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
     if (b1 == 0) break;                      // the share ends before the first block
     const bool whole = b0 == 0 && b1 == nb;
     // a share holds at most one part that goes on from an earlier share and one that goes on in a later
-    const int slot = 2 * static_cast<int>(blockIdx.x) + (b0 > 0 ? 0 : 1);
+    const int slot = 2 * (wg * row_groups + rg) + (b0 > 0 ? 0 : 1);
 
     // Q^T operand: column = vector m (token m / H)
     const int m = m0 + rb * kRow + col;
     const bool row_ok = m < M;
-    const int lim = ctx - nq + (row_ok ? m / H : 0);           // keys <= lim are visible
+    if (g4 == 0) slim[wave][col] = ctx - nq + (row_ok ? m / H : 0);   // the last visible key
     const uint16_t* qrow = q + (static_cast<size_t>(seq) * M + (row_ok ? m : 0)) * D;
     bf16x8 qf[KS];
 #pragma unroll
@@ -203,7 +201,7 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
       return b0 * kKT + t * (kStep * kKT) + 8 * (o * kWaves + wave);
     };
     auto page_of = [&](int t, int o) {
-      return __builtin_amdgcn_readfirstlane(table[min(first_key(t, o), end - 1) >> b.page_shift]);
+      return scalar_entry(table, min(first_key(t, o), end - 1) >> b.page_shift);
     };
     int page[OCTS];                          // of the step that is asked for next
     // asks for this wave's keys of step t; rows past the last key are clamped to it
@@ -217,16 +215,17 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
                               ((static_cast<size_t>(page[o]) << b.page_shift) + line) * ROWB;
         const uint32_t dst = lds0 + static_cast<uint32_t>(((t & 1) * 4 * kStep + oct) * 8 * ROWB);
         const int last = min(end - 1 - (ks & ~7), 7);          // the last of these eight rows in use
-        const uint32_t flip = 32u * (oct & 1) + 16u * ((oct >> 1) & 1);   // bits 3 and 4 of the keys
+        const uint32_t flip = 2u * (oct & 1) + ((oct >> 1) & 1);   // of bits 3 and 4 of the keys
+        // this lane's place in load c: chunk c * 64 + lane of the eight rows (worked out anew: kept, the
+        // offsets of all loads would be spilt, and their reloads wait for the loads in flight)
+        const int ln = lane_now();
 #pragma unroll
         for (int c = 0; c < LOADS; ++c) {
-          uint32_t from = off[c] ^ flip;
-          if (last < 7) {
-            const int key = (c * kWave + lane) / CH;
-            // (the swizzle is that of the place, not of the row that fills it)
-            from -= static_cast<uint32_t>(max(key - last, 0)) * ROWB;
-          }
+          const int at = c * kWave + ln, key = at / CH, pc = at - key * CH;
+          // (the swizzle is that of the place, not of the row that fills it)
+          const uint32_t from = static_cast<uint32_t>(min(key, last)) * ROWB + 16u * (pc ^ swz(key) ^ flip);
           dma16_once(base, from, dst + static_cast<uint32_t>(c * kWave * 16));
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     };
@@ -236,39 +235,71 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
     for (int dt = 0; dt < DT; ++dt) o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, l_run = 0.f;
 
-    // the 32 keys from key0 on, in the tile at LDS address `tile`
-    auto work = [&](int key0, uint32_t tile) {
-      floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+    // The 32 keys from key0 on, in the tile at LDS address `tile`.  Operands are read kAhead products ahead,
+    // the first ones of the values while the softmax is worked out.
+    constexpr int kAhead = 3, kOps = 4;
+    auto work = [&](int key0, uint32_t tile) __attribute__((always_inline)) {
+      // this lane's places, as they are (the compiler would make a sum of its own for each operand)
+      uint32_t kat[2], vat[4];
 #pragma unroll
-      for (int c = 0; c < KS; ++c)
+      for (int j = 0; j < 2; ++j) {
+        kat[j] = tile + (k_lane ^ (64u * j));
+        asm volatile("" : "+v"(kat[j]));
+      }
+      // K operand i: dims 32 (i / 2), keys of S^T tile i % 2
+      auto kop = [&](int i) __attribute__((always_inline)) {
+        const int c = i >> 1, a = i & 1;
+        return __builtin_bit_cast(
+            bf16x8, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
+                        kat[c & 1] + (64u * (c & ~1) + 4u * a * ROWB)));
+      };
+      // C^T operand of 16 dims dt (keys 4 on have the same swizzle)
+      auto vop = [&](int dt) __attribute__((always_inline)) {
+        auto* at = reinterpret_cast<__attribute__((address_space(3))) shortx4*>(
+            vat[dt & 3] + 32u * (dt & ~3));
+        const shortx4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
+        const shortx4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 4 * ROWB / 8);
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      bf16x8 op[kOps];
+      floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};   // keys key0 + 8 g4 + 4 a + i
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const auto* p = reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
-              tile + (k_lane ^ (64u * (c & 1))) + 64u * (c & ~1) + 4u * a * ROWB);
-          s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, *p), qf[c], s[a], 0, 0,
-                                                         0);
-        }
-      float x[8];                            // keys key0 + 8 g4 + i
+      for (int i = 0; i < kAhead; ++i) op[i] = kop(i);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3];
+      for (int i = 0; i < 2 * KS; ++i) {
+        if (i + kAhead < 2 * KS) op[(i + kAhead) % kOps] = kop(i + kAhead);
+        s[i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[i % kOps], qf[i >> 1], s[i & 1], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        vat[j] = tile + v_lane + (v_unit ^ (32u * j));
+        asm volatile("" : "+v"(vat[j]));
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) op[i] = vop(i);
+      __builtin_amdgcn_sched_barrier(0);
       if (key0 + kKT - 1 > min(ctx - nq, end - 1)) {
-        const int last = min(lim, end - 1);
+        const int last = min(slim[wave][lane_now() & 15], end - 1);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (key0 + 8 * g4 + i > last) x[i] = -INFINITY;
+          if (key0 + 8 * (lane_now() >> 4) + i > last) s[i >> 2][i & 3] = -INFINITY;
       }
-      float ex[8], ls = 0.f;
+      bf16x8 p;
+      float ls = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        ex[i] = __builtin_amdgcn_exp2f(fmaf(x[i], scale_log2, -m_run));
-        ls += ex[i];
+        const __bf16 e = static_cast<__bf16>(
+            __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale_log2, -m_run)));
+        p[i] = e;
+        ls += static_cast<float>(e);
       }
       if (__any(!(ls < kSumLimit))) {
         // exact maximum of the 32 keys per vector (its four lane groups), move the reference, rescale
         float mx = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          mx = fmaxf(mx, x[i] == -INFINITY ? -INFINITY : x[i] * scale_log2);
+          mx = fmaxf(mx, s[i >> 2][i & 3] == -INFINITY ? -INFINITY : s[i >> 2][i & 3] * scale_log2);
         mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
         const float m_new = fmaxf(m_run, mx);
@@ -278,35 +309,32 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
         m_run = m_new;
+        ls = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          ex[i] = x[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[i], scale_log2, -m_use));
+        for (int i = 0; i < 8; ++i) {
+          const float x = s[i >> 2][i & 3];
+          const __bf16 e = static_cast<__bf16>(
+              x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x, scale_log2, -m_use)));
+          p[i] = e;
+          ls += static_cast<float>(e);
+        }
       }
-      bf16x8 p;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const __bf16 r = static_cast<__bf16>(ex[i]);
-        p[i] = r;
-        l_run += static_cast<float>(r);
-      }
+      l_run += ls;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        // (keys 4 on have the same swizzle)
-        auto* at = reinterpret_cast<__attribute__((address_space(3))) shortx4*>(
-            tile + v_lane + (v_unit ^ (32u * (dt & 3))) + 32u * (dt & ~3));
-        const shortx4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
-        const shortx4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 4 * ROWB / 8);
-        const bf16x8 c =
-            __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
-        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, p, o[dt], 0, 0, 0);
+        if (dt + kAhead < DT) op[(dt + kAhead) % kOps] = vop(dt + kAhead);
+        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[dt % kOps], p, o[dt], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
 
+    // Nothing but the direct loads is counted from here on: the queries are there (and known to be).
+#pragma unroll
+    for (int c = 0; c < KS; ++c) asm volatile("" : "+v"(qf[c]));
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (steps > 0) {
 #pragma unroll
       for (int i = 0; i < OCTS; ++i) page[i] = page_of(0, i);
-      // nothing but the direct loads is counted from here on
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       issue(0);
 #pragma unroll
       for (int i = 0; i < OCTS; ++i) page[i] = page_of(1, i);
@@ -322,7 +350,7 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
       const int key0 = (b0 + t * kStep) * kKT;
       const uint32_t tile = lds0 + static_cast<uint32_t>((t & 1) * kStep * TILEB);
       if (m0 + rb * kRow < M) {              // a wave without vectors: its share of the loads
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < kStep / KW; ++i) {
           const int at = KW == 1 ? i : kw;
           if (key0 + at * kKT < end) work(key0 + at * kKT, tile + at * TILEB);
@@ -335,7 +363,7 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
     // references there are.
     float l_tot = l_run + __shfl_xor(l_run, 16, kWave) + __shfl_xor(l_run, 32, kWave) +
                   __shfl_xor(l_run, 48, kWave);
-    if (lim >= bad_row) l_tot = __builtin_nanf("");
+    if (slim[wave][col] >= bad_row) l_tot = __builtin_nanf("");
     if (g4 == 0) {
       sm[wave][col] = l_tot == l_tot ? m_run : 0.f;
       sl[wave][col] = l_tot;
@@ -447,16 +475,19 @@ __global__ __launch_bounds__(kMergeThreads) void latent_decode_merge_kernel(
 // x 128 vectors: 24 us by quarters, 16 whole), and few have many (16 of 134 parts: 7 and 23).
 constexpr int kWideVecs = 512;
 
-int row_tiles_of(int M) { return M <= 32 ? 2 : M <= 64 ? 4 : 8; }
+int row_tiles_of(int M) { return M <= 32 ? 2 : 4; }
 
 // Workgroups of a call: a share of every row group each.
 int groups_of(int M) { return (M + kRow * row_tiles_of(M) - 1) / (kRow * row_tiles_of(M)); }
+
+// Shares of a row group: whole rounds over the XCDs.
+int shares_of(int groups) { return kWGs / kNumXcd / groups * kNumXcd; }
 
 template <int R, int RB, int NS>
 hipError_t launch_t(const LatentDecodeArgs& a, hipStream_t stream) {
   const PagedBatch& b = a.batch;
   const int groups = groups_of(b.n_q * a.n_heads);
-  const int wgs = max(1, kWGs / groups) * groups;
+  const int wgs = shares_of(groups) * groups;
   float2* part_ml = static_cast<float2*>(a.workspace);
   float* part_o = reinterpret_cast<float*>(part_ml + static_cast<size_t>(2 * wgs) * RB * kRow);
   const float scale_log2 = a.scale * 1.4426950408889634f;
@@ -485,8 +516,7 @@ template <int R>
 hipError_t launch_r(const LatentDecodeArgs& a, hipStream_t stream) {
   switch (row_tiles_of(a.batch.n_q * a.n_heads)) {
     case 2: return launch_n<R, 2>(a, stream);
-    case 4: return launch_n<R, 4>(a, stream);
-    default: return launch_n<R, 8>(a, stream);
+    default: return launch_n<R, 4>(a, stream);
   }
 }
 
@@ -494,7 +524,7 @@ hipError_t launch_r(const LatentDecodeArgs& a, hipStream_t stream) {
 
 size_t latent_decode_workspace_bytes(int n_q, int n_heads, int latent_dim) {
   const int M = n_q * n_heads, groups = groups_of(M);
-  const size_t rows = static_cast<size_t>(2 * max(1, kWGs / groups) * groups) * row_tiles_of(M) * kRow;
+  const size_t rows = static_cast<size_t>(2 * shares_of(groups) * groups) * row_tiles_of(M) * kRow;
   return rows * (static_cast<size_t>(latent_dim) + 2) * sizeof(float);
 }
 

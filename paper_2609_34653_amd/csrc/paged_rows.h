@@ -23,6 +23,13 @@ __device__ inline void wait_vmcnt() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
+// table[i] for a wave-uniform i, by a scalar load: a vector load would have the compiler wait for it with
+// every direct load that is on its way.  (The table is not written while the kernel runs.)
+__device__ inline int scalar_entry(const int32_t* table, int i) {
+  typedef const __attribute__((address_space(4))) int32_t* const_i32;
+  return reinterpret_cast<const_i32>(reinterpret_cast<uintptr_t>(table))[__builtin_amdgcn_readfirstlane(i)];
+}
+
 // Sequence and row of a token.
 struct TokenRow {
   int seq, row;                          // seq < 0: the token belongs to no (valid) sequence
