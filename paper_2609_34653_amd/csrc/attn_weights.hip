@@ -10,10 +10,12 @@
 //   operands  of each product one side stays in registers (32 query rows per wave in the first pass, 32 keys in
 //             the second), the other streams through LDS tiles filled by direct loads; so the first pass
 //             has a row's statistics and the second a key's sum in the lanes that they belong to.
-//   shares    the first pass has the row tiles and shares of chunk_plan.h.  The second takes items of 256 keys of a
-//             KV head and up to kRowChunk query rows, in turn, whatever the lengths.
+//   items     the first pass is dealt out as 256 query rows of a KV head (tokens times its query heads) and a
+//             chunk of the keys, the second as 256 keys of a KV head and up to kRowChunk query rows; 512 workgroups
+//             take them in turn, two on a CU, so that one's vector work hides what the other waits for.
 //   sums      no atomics: every item owns its place in a buffer of partial sums, added in a fixed order.
-#include "chunk_plan.h"
+#include <type_traits>
+
 #include "common.h"
 #include "evict.h"
 #include "mfma_tile.h"
@@ -22,9 +24,15 @@
 namespace omnitide {
 namespace {
 
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kRows = kWaves * 32;       // query rows of an item of the first pass
+constexpr int kMinKeys = 1024;           // its keys at least
+constexpr int kMaxChunks = 16;           // chunks of the keys at most
 constexpr int kRowChunk = 1024;          // query rows of an item of the second pass
 constexpr int kItemKeys = kWaves * 32;   // its keys
-constexpr int kItemWGs = 512;            // workgroups of the second pass
+constexpr int kItemWGs = 512;            // workgroups of a pass
+constexpr int kNumXcd = 8;
 constexpr int kSumThreads = 256;
 
 // 64 KB or so of a streamed operand in LDS, in stages of kKeys rows.
@@ -81,12 +89,6 @@ struct Stage {
   }
 };
 
-// Tokens of a sequence that has more than max_q count as malformed lengths.
-__device__ inline int weights_ctx(const AttnWeightsArgs& a, int i) {
-  const int n = a.batch.q_start[i + 1] - a.batch.q_start[i];
-  return n > a.max_q ? -1 : a.batch.ctx_len[i];
-}
-
 __device__ inline void report_weights(const AttnWeightsArgs& a) {
   report_batch(a.batch, a.d_status);
   bool bad = false;
@@ -98,27 +100,111 @@ __device__ inline void report_weights(const AttnWeightsArgs& a) {
 }
 
 // What a call's passes hand on.  seqs: every sequence's first token, tokens (0: none, or malformed) and
-// context; stats: per KV head and token, its G heads' (m, 1 / l).
+// context; part: (m, l) of each key chunk, KV head and query row; stats: (m, 1 / l) of each KV head and query
+// row (a sequence's rows are token by token the KV head's G query heads).
 struct WeightsWork {
-  Joined* joined;
   int4* seqs;
-  float2* part_ml;
+  float2* part;
   float2* stats;
   float* sums;                           // [row chunk][KV head][sequence][max_ctx]
-  int row_chunks;
+  int chunk_keys;
 };
+
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+  const uint64_t u = static_cast<uint64_t>(x);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
+  return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
+// The items of a call, sequence by sequence, in LDS: how many are in front of each.
+template <int SEQS>
+struct Items {
+  int64_t first[SEQS];
+  int64_t chunk_sum[SEQS / kWave];
+  // by the whole workgroup; n(i): of sequence i
+  template <class N>
+  __device__ int64_t make(int n_seq, N n) {
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(static_cast<int>(threadIdx.x / kWave));
+    const int chunks = (n_seq + kWave - 1) / kWave;
+    for (int c = wave; c < chunks; c += kWaves) {
+      const int i = c * kWave + lane;
+      const int64_t mine = i < n_seq ? n(i) : 0;
+      const int64_t inc = static_cast<int64_t>(wave_scan_add_u64(static_cast<uint64_t>(mine)));
+      first[i] = inc - mine;
+      if (lane == kWave - 1) chunk_sum[c] = inc;
+    }
+    __syncthreads();
+    int64_t total = 0;
+    for (int c = 0; c < chunks; ++c) {
+      const int64_t sum = chunk_sum[c];
+      if (wave == 0) first[c * kWave + lane] += total;
+      total += sum;
+    }
+    __syncthreads();
+    return uniform(total);
+  }
+  // the sequence of an item (those without items begin where the next one does, and the last that begins
+  // there has some)
+  __device__ int find(int n_seq, int64_t item) const {
+    int s = 0;
+    for (int hi = n_seq - 1; s < hi;) {
+      const int mid = (s + hi + 1) / 2;
+      if (first[mid] <= item) s = mid;
+      else hi = mid - 1;
+    }
+    return uniform(s);
+  }
+};
+
+// The first item of a workgroup: those of one XCD (workgroups are dealt round-robin over them) are next to each
+// other, so that they read the same keys, or rows, together.
+__device__ inline int first_item() {
+  return blockIdx.x % kNumXcd * (kItemWGs / kNumXcd) + blockIdx.x / kNumXcd;
+}
+
+// Every sequence into LDS, by the whole workgroup: one that starts in front of an earlier offset has no tokens, nor
+// has one with more than max_q, or with fewer rows than tokens.
+template <int SEQS>
+__device__ inline void read_seqs(const AttnWeightsArgs& a, int4 (&seqs)[SEQS]) {
+  const PagedBatch& b = a.batch;
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(static_cast<int>(threadIdx.x / kWave));
+  const int cap = b.max_pages << b.page_shift, chunks = (b.n_seq + kWave - 1) / kWave;
+  for (int c = wave; c < chunks; c += kWaves) {
+    const int i = c * kWave + lane;
+    int s0 = 0, s1 = 0, n = 0;
+    if (i < b.n_seq) {
+      s0 = b.q_start[i];
+      s1 = b.q_start[i + 1];
+      n = b.ctx_len[i];
+    }
+    int front = wave_exclusive_max_i32(s0, 0), before = 0;
+    for (int j = lane; j < c * kWave; j += kWave) before = max(before, b.q_start[j]);
+    front = max(front, wave_max_i32(before));
+    const bool ok = s0 >= front && s1 > s0 && s1 <= b.n_tokens && s1 - s0 <= a.max_q && n >= s1 - s0 && n <= cap;
+    seqs[i] = make_int4(s0, ok ? s1 - s0 : 0, n, 0);
+  }
+  __syncthreads();
+}
+
+// Keys that a row tile's last row sees, and so the chunks of its sequence that it has.
+__device__ inline int tile_keys(int rt, int G, int len, int ctx) {
+  const int last = static_cast<int>(static_cast<uint32_t>((rt + 1) * kRows - 1) / static_cast<uint32_t>(G));
+  return ctx - len + min(len - 1, last) + 1;
+}
 
 // ------------------------------------------------------------------ first pass: the rows' statistics
 
 template <int D, int SEQS>
-__global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(const AttnWeightsArgs a,
-                                                                            const WeightsWork ws,
-                                                                            float scale_log2) {
+__global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void weights_stats_kernel(
+    const AttnWeightsArgs a, const WeightsWork ws, float scale_log2) {
   using S = Stage<D>;
   constexpr int NK = D / 16, kSub = S::kKeys / 32;
   constexpr float kSumLimit = 4294967296.f;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kRing * S::kBytes];
-  __shared__ PlanMem<SEQS> plan_mem;
+  __shared__ int4 seqs[SEQS];
+  __shared__ Items<SEQS> items;
   const PagedBatch& b = a.batch;
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
@@ -127,17 +213,15 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
   const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
 
   if (blockIdx.x == 0 && wave == 0) report_weights(a);
-  Plan<SEQS> plan;
-  plan.make(plan_mem, b.n_seq, b.n_tokens, b.q_start, b.max_pages << b.page_shift,
-            [&](int i) { return weights_ctx(a, i); }, G, Hkv);
-  const int w = (blockIdx.x % kNumXcd) * (kWGs / kNumXcd) + blockIdx.x / kNumXcd;
-  const int64_t begin = plan.share_begin(w), end = plan.share_begin(w + 1);
-  int64_t cur = begin;
-  if (tid == 0) ws.joined[w].n_parts = 0;
+  read_seqs(a, seqs);
   if (blockIdx.x == 0)
-    for (int i = tid; i < b.n_seq; i += kThreads) ws.seqs[i] = plan_mem.seq[i];
-  if (begin == end && static_cast<int32_t>(begin) > 0 && tid < kRows)
-    ws.part_ml[static_cast<size_t>(2 * w) * kRows + tid] = make_float2(-INFINITY, 0.f);
+    for (int i = tid; i < b.n_seq; i += kThreads) ws.seqs[i] = seqs[i];
+  const int64_t total = items.make(b.n_seq, [&](int i) {
+    const int4 q = seqs[i];
+    if (q.y == 0) return int64_t{0};
+    return static_cast<int64_t>((q.y * G + kRows - 1) / kRows) * Hkv *
+           ((q.z + ws.chunk_keys - 1) / ws.chunk_keys);
+  });
 
   S st;
   st.make(wave, lane);
@@ -145,27 +229,20 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
   const uint32_t at_lane = S::lane_at(col, h);
   const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
 
-  for (int round = 0;; ++round) {
-    const bool shared = round >= plan.rounds;
-    if (shared && cur >= end) break;
-    const int i = shared ? static_cast<int>(cur >> 32) : Plan<SEQS>::round_tile(round, w);
-    const int t_begin = shared ? static_cast<int32_t>(cur) : 0;
-    const int g = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(plan.tiles_per_head));
-    const int2 place = plan.find_tile(i - g * plan.tiles_per_head);
-    const int s = uniform(place.x), mt = uniform(place.y);
-    const auto sq = plan.seq(s);
-    const int L = sq.len, ctx = sq.ctx, kept = ctx - L;
-    const int nt = plan.tiles_of(mt, L, ctx);
-    const int t_end = shared && i == static_cast<int>(end >> 32) ? static_cast<int32_t>(end) : nt;
-    const bool whole = t_begin == 0 && t_end == nt;
-    const int slot = 2 * w + (i == static_cast<int>(begin >> 32) ? 0 : 1);
-    const int m0 = mt * kRows;
+  for (int64_t item = first_item(); item < total; item += kItemWGs) {
+    const int s = items.find(b.n_seq, item);
+    const int q0 = uniform(seqs[s].x), L = uniform(seqs[s].y), ctx = uniform(seqs[s].z);
+    const int kept = ctx - L, tiles = (L * G + kRows - 1) / kRows;
+    // chunk of the keys, KV head, row tile
+    const int64_t local = item - uniform(items.first[s]);
+    const int kc = uniform(static_cast<int>(local / (static_cast<int64_t>(tiles) * Hkv)));
+    const int rest = uniform(static_cast<int>(local - static_cast<int64_t>(kc) * tiles * Hkv));
+    const int g = rest / tiles, rt = rest - g * tiles;
+    const int k_begin = kc * ws.chunk_keys;
+    const int k_end = min(k_begin + ws.chunk_keys, tile_keys(rt, G, L, ctx));
+    if (k_begin >= k_end) continue;        // no row of the tile sees the chunk
+    const int m0 = rt * kRows;
     const int full_lim = kept + m0 / G;    // keys <= full_lim are visible to every row
-    if (t_begin > 0 && t_end == nt && wave == 0) {
-      const int w0 = plan.first_share(i, w);
-      const int first_slot = 2 * w0 + (plan.share_begin(w0) == pack_cut(i, 0) ? 0 : 1);
-      if (lane == 0) ws.joined[w] = Joined{w - w0 + 1, first_slot, w, sq.q0, L * G, mt, g, 0};
-    }
 
     const int m = m0 + wave * 32 + col;    // this lane's row
     const bool row_ok = m < L * G;
@@ -173,7 +250,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
     const int lim = kept + p;              // its last visible key
     const uint16_t* qrow =
         static_cast<const uint16_t*>(a.q) +
-        (static_cast<size_t>(sq.q0 + p) * Hq + g * G + (row_ok ? m % G : 0)) * D;
+        (static_cast<size_t>(q0 + p) * Hq + g * G + (row_ok ? m % G : 0)) * D;
     bf16x8 qf[NK];
 #pragma unroll
     for (int c = 0; c < NK; ++c) qf[c] = __builtin_bit_cast(bf16x8, ld16(qrow + 16 * c + 8 * h));
@@ -181,9 +258,8 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
     // A bad page spoils every row that sees it (below); the others have its keys masked, and page 0 stands in
     // its place.
     const int32_t* table = b.table + static_cast<size_t>(s) * b.max_pages;
-    const int k_end = min(t_end * kKT, ctx);
     int bad_row = INT32_MAX;
-    for (int p0 = (t_begin * kKT) >> b.page_shift, p1 = (k_end - 1) >> b.page_shift; p0 <= p1; p0 += kWave) {
+    for (int p0 = k_begin >> b.page_shift, p1 = (k_end - 1) >> b.page_shift; p0 <= p1; p0 += kWave) {
       const int id = p0 + lane <= p1 ? table[p0 + lane] : 0;
       const uint64_t bad = __ballot(id < 0 || id >= b.n_pages);
       if (bad != 0) {
@@ -193,9 +269,8 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
       }
     }
     const uint8_t* k_head = static_cast<const uint8_t*>(a.k) + 2 * g * D;
-    const int u_begin = t_begin * (kKT / S::kKeys), u_end = (k_end + S::kKeys - 1) / S::kKeys;
-    auto issue = [&](int u) {
-      const int e = uniform((u - u_begin) % S::kRing);
+    const int u_begin = k_begin / S::kKeys, u_end = (k_end + S::kKeys - 1) / S::kKeys;
+    auto issue = [&](int u, int e) {
 #pragma unroll
       for (int c = 0; c < S::kCalls; ++c) {
         if (!S::mine(wave, c)) break;
@@ -213,35 +288,63 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
     // nothing but the direct loads is counted from here on: the queries are there (and known to be)
 #pragma unroll
     for (int c = 0; c < NK; ++c) asm volatile("" : "+v"(qf[c]));
-    __syncthreads();                       // the stages of the part before are done with
+    __syncthreads();                       // the stages of the item before are done with
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int u = 0; u < S::kRing - 1; ++u)
-      if (u_begin + u < u_end) issue(u_begin + u);
-    for (int u = u_begin; u < u_end; ++u) {
+    for (int u = 0; u < S::kRing; ++u)
+      if (u_begin + u < u_end) issue(u_begin + u, u);
+    // this stage has landed, the later ones may be in flight
+    auto landed = [&](int u) {
       if (u + S::kRing - 2 < u_end) S::template wait<S::kRing - 2>(wave);
       else wait_vmcnt<0>();
       __syncthreads();
-      if (u + S::kRing - 1 < u_end) issue(u + S::kRing - 1);
-      if (m0 + wave * 32 >= L * G) continue;
-      const uint32_t stage = lds0 + static_cast<uint32_t>(uniform((u - u_begin) % S::kRing) * S::kBytes);
+    };
+    if (u_begin + S::kRing - 1 < u_end) S::template wait<S::kRing - 1>(wave);
+    else wait_vmcnt<0>();
+    __syncthreads();
+    const bool idle = m0 + wave * 32 >= L * G;             // a wave without rows: its share of the loads
+    floatx16 x = floatx16{};               // scores of the 32 keys at hand
+    if (!idle) {
+#pragma unroll
+      for (int c = 0; c < NK; ++c) x = mfma(S::operand(lds0, at_lane, c), qf[c], x);
+    }
+    int entry = 0;                         // (u - u_begin) % kRing
+    for (int u = u_begin; u < u_end; ++u) {
+      const int after = entry < S::kRing - 1 ? entry + 1 : 0;
 #pragma unroll
       for (int sub = 0; sub < kSub; ++sub) {
-        floatx16 x = floatx16{};
-#pragma unroll
-        for (int c = 0; c < NK; ++c)
-          x = mfma(S::operand(stage + 32u * sub * S::kRowB, at_lane, c), qf[c], x);
+        if (sub == kSub - 1 && u + 1 < u_end) {
+          // the next stage; this one's last scores are there, and its entry is free
+          landed(u + 1);
+          if (u + S::kRing < u_end) issue(u + S::kRing, entry);
+        }
+        if (idle) continue;
         const int key0 = u * S::kKeys + 32 * sub;
-        // accumulator i: key key0 + i % 4 + 8 (i / 4) + 4 h
+        // accumulator i: key key0 + i % 4 + 8 (i / 4) + 4 h (those past the item's are past the rows' limits)
         if (key0 + 31 > full_lim) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (key0 + (e & 3) + 8 * (e >> 2) + 4 * h > lim) x[e] = -INFINITY;
         }
+        // The next 32 keys' products between these keys' exponentials, since a wave issues in order.  (After the
+        // last ones: of whatever lies there, not used.)
+        const uint32_t next = lds0 + static_cast<uint32_t>(sub < kSub - 1 ? entry * S::kBytes + 32 * (sub + 1) * S::kRowB
+                                                                          : after * S::kBytes);
+        constexpr int kAhead = 3, kOps = 4;
+        bf16x8 op[kOps];
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) op[c] = S::operand(next, at_lane, c);
+        floatx16 y = floatx16{};
         float ls[2] = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          ls[e & 1] += __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -m_run));
+        for (int c = 0; c < NK; ++c) {
+          y = mfma(op[c % kOps], qf[c], y);
+          if (c + kAhead < NK) op[(c + kAhead) % kOps] = S::operand(next, at_lane, c + kAhead);
+#pragma unroll
+          for (int e = c * 16 / NK; e < (c + 1) * 16 / NK; ++e)
+            ls[e & 1] += __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -m_run));
+          __builtin_amdgcn_sched_barrier(0);
+        }
         float lsum = ls[0] + ls[1];
         if (__any(!(lsum < kSumLimit))) {
           // exact maximum of the 32 keys, move the reference, recompute
@@ -260,43 +363,40 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_stats_kernel(con
             lsum += x[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -m_use));
         }
         l_run += lsum;
+        x = y;
       }
+      entry = after;
     }
     wait_vmcnt<0>();
     // A sum that is no number spoils the row to the end, whatever references there are.
     const float l_tot = lim >= bad_row ? __builtin_nanf("") : sum_halves(l_run);
-    if (row_ok && h == 0) {
-      const float ref = l_tot == l_tot ? m_run : 0.f;
-      if (whole)
-        ws.stats[static_cast<size_t>(g) * b.n_tokens * G + static_cast<size_t>(sq.q0) * G + m] =
-            make_float2(ref, 1.f / l_tot);
-      else
-        ws.part_ml[static_cast<size_t>(slot) * kRows + wave * 32 + col] = make_float2(ref, l_tot);
-    }
-    if (shared) {
-      if (t_end < nt) break;               // it ended inside the row tile
-      cur = pack_cut(i + 1, 0);
-    }
+    if (row_ok && h == 0)
+      ws.part[(static_cast<size_t>(kc) * Hkv + g) * b.n_tokens * G + static_cast<size_t>(q0) * G + m] =
+          make_float2(l_tot == l_tot ? m_run : 0.f, l_tot);
   }
 }
 
-// Joins the statistics of the row tiles whose parts lie in several shares, in share order.
-__global__ __launch_bounds__(kRows) void weights_join_kernel(const WeightsWork ws, int n_tokens, int G) {
-  const Joined j = ws.joined[blockIdx.x];
-  const int row = threadIdx.x, m = j.mt * kRows + row;
-  if (j.n_parts <= 0 || m >= j.rows) return;
-  auto part = [&](int p) {
-    const int slot = p == 0 ? j.first_slot : 2 * (j.last_share - j.n_parts + 1 + p);
-    return ws.part_ml[static_cast<size_t>(slot) * kRows + row];
-  };
+// Joins a query row's statistics over the key chunks, in their order.
+__global__ __launch_bounds__(kRows) void weights_join_kernel(const AttnWeightsArgs a, const WeightsWork ws) {
+  const PagedBatch& b = a.batch;
+  const int rt = blockIdx.x, g = blockIdx.y, s = blockIdx.z, m = rt * kRows + static_cast<int>(threadIdx.x);
+  const int G = a.n_q_heads / a.n_kv_heads;
+  const int4 q = ws.seqs[s];
+  if (m >= q.y * G) return;
+  const int chunks = (tile_keys(rt, G, q.y, q.z) + ws.chunk_keys - 1) / ws.chunk_keys;
+  const size_t rows = static_cast<size_t>(b.n_tokens) * G, row = static_cast<size_t>(q.x) * G + m;
+  float2 v[kMaxChunks];
   float mx = -INFINITY, l = 0.f;
-  for (int p = 0; p < j.n_parts; ++p) mx = fmaxf(mx, part(p).x);
-  for (int p = 0; p < j.n_parts; ++p) {
-    const float2 ml = part(p);
-    if (ml.x != -INFINITY) l = fmaf(exp2f(ml.x - mx), ml.y, l);
+#pragma unroll
+  for (int c = 0; c < kMaxChunks; ++c) {
+    v[c] = c < chunks ? ws.part[(static_cast<size_t>(c) * a.n_kv_heads + g) * rows + row]
+                      : make_float2(-INFINITY, 0.f);
+    mx = fmaxf(mx, v[c].x);
   }
-  ws.stats[static_cast<size_t>(j.g) * n_tokens * G + static_cast<size_t>(j.q0) * G + m] =
-      make_float2(mx, 1.f / l);
+#pragma unroll
+  for (int c = 0; c < kMaxChunks; ++c)
+    if (v[c].x != -INFINITY) l = fmaf(exp2f(v[c].x - mx), v[c].y, l);
+  ws.stats[g * rows + row] = make_float2(mx, 1.f / l);
 }
 
 // --------------------------------------------------------------------- second pass: sums over the rows
@@ -305,7 +405,7 @@ __global__ __launch_bounds__(kRows) void weights_join_kernel(const WeightsWork w
 __device__ inline int first_row(int j, int kept, int G) { return max(j - kept, 0) * G; }
 
 template <int D, int SEQS>
-__global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const AttnWeightsArgs a,
+__global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void weights_sum_kernel(const AttnWeightsArgs a,
                                                                           const WeightsWork ws,
                                                                           float scale_log2) {
   using S = Stage<D>;
@@ -313,8 +413,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
   constexpr int kStatCalls = 2 * S::kKeys / kWave;         // direct loads of a stage's statistics
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kRing * S::kBytes];
   __shared__ float2 lds_stats[S::kRing][S::kKeys];         // (m, 1 / l) of a stage's rows
-  __shared__ int64_t firsts[SEQS];         // items in front of each sequence
-  __shared__ int64_t chunk_sum[SEQS / kWave];
+  __shared__ Items<SEQS> items;
   const PagedBatch& b = a.batch;
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
@@ -323,27 +422,12 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
   const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
   const int max_ctx = b.max_pages << b.page_shift;
 
-  // every sequence's items (key tiles x KV heads x row chunks), and those in front of it
-  const int n_chunks = (b.n_seq + kWave - 1) / kWave;
-  for (int c = wave; c < n_chunks; c += kWaves) {
-    const int i = c * kWave + lane;
-    const int4 q = i < b.n_seq ? ws.seqs[i] : make_int4(0, 0, 0, 0);
-    const int64_t n = q.y == 0 ? 0
-                               : static_cast<int64_t>((q.z + kItemKeys - 1) / kItemKeys) * Hkv *
-                                     ((q.y * G + kRowChunk - 1) / kRowChunk);
-    const int64_t inc = static_cast<int64_t>(wave_scan_add_u64(static_cast<uint64_t>(n)));
-    firsts[i] = inc - n;
-    if (lane == kWave - 1) chunk_sum[c] = inc;
-  }
-  __syncthreads();
-  int64_t total = 0;
-  for (int c = 0; c < n_chunks; ++c) {
-    const int64_t n = chunk_sum[c];
-    if (wave == 0) firsts[c * kWave + lane] += total;
-    total += n;
-  }
-  __syncthreads();
-  total = uniform(total);
+  const int64_t total = items.make(b.n_seq, [&](int i) {
+    const int4 q = ws.seqs[i];
+    if (q.y == 0) return int64_t{0};
+    return static_cast<int64_t>((q.z + kItemKeys - 1) / kItemKeys) * Hkv *
+           ((q.y * G + kRowChunk - 1) / kRowChunk);
+  });
 
   S st;
   st.make(wave, lane);
@@ -351,20 +435,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
   const uint32_t at_lane = S::lane_at(col, h);
   const uint32_t magic = (0x100000000ull + G - 1) / G;     // x / G for small x (G = 1: 0, see below)
 
-  for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
-    int s = 0;                             // the last sequence that begins at or before the item
-    for (int hi = b.n_seq - 1; s < hi;) {
-      const int mid = (s + hi + 1) / 2;
-      if (firsts[mid] <= item) s = mid;
-      else hi = mid - 1;
-    }
-    s = uniform(s);
-    // (sequences without items begin where the next one does, and the last that begins there has some)
+  for (int64_t item = blockIdx.x; item < total; item += kItemWGs) {
+    const int s = items.find(b.n_seq, item);
     const int4 sq = ws.seqs[s];
     const int q0 = uniform(sq.x), L = uniform(sq.y), ctx = uniform(sq.z);
     const int kept = ctx - L, rows = L * G;
     const int tiles = (ctx + kItemKeys - 1) / kItemKeys;
-    const int64_t local = item - uniform(firsts[s]);
+    const int64_t local = item - uniform(items.first[s]);
     const int rc = uniform(static_cast<int>(local / (tiles * Hkv)));
     const int rest = uniform(static_cast<int>(local - static_cast<int64_t>(rc) * tiles * Hkv));
     const int tile = rest / Hkv, g = rest - tile * Hkv;
@@ -390,8 +467,7 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
       const int u_begin = m_begin / S::kKeys, u_end = (m_end + S::kKeys - 1) / S::kKeys;
       const int last_row = rows - 1;
       // direct loads of query rows [u kKeys, +kKeys) (row m is head m % G of token m / G) and their statistics
-      auto issue = [&](int u) {
-        const int e = uniform((u - u_begin) % S::kRing);
+      auto issue = [&](int u, int e) {
         if (wave < kStatCalls) {
           const int x = wave * kWave + lane;               // of the stage's floats
           dma4(stats, 8u * static_cast<uint32_t>(min(u * S::kKeys + (x >> 1), last_row)) + 4u * (x & 1),
@@ -418,7 +494,10 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
       for (int u = 0; u < S::kRing - 1; ++u)
-        if (u_begin + u < u_end) issue(u_begin + u);
+        if (u_begin + u < u_end) issue(u_begin + u, u);
+      // rows m >= m_full see all of this wave's keys; row m sees key key0 + e if m >= m_key0 + e G
+      const int m_full = first_row(key0 + 31, kept, G), m_key0 = max(key0 - kept, -32) * G;
+      int entry = 0;                       // (u - u_begin) % kRing
       for (int u = u_begin; u < u_end; ++u) {
         // this stage has landed; the later ones may be in flight
         if (u + S::kRing - 2 < u_end) {
@@ -428,30 +507,32 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void weights_sum_kernel(const
           wait_vmcnt<0>();
         }
         __syncthreads();
-        if (u + S::kRing - 1 < u_end) issue(u + S::kRing - 1);
+        if (u + S::kRing - 1 < u_end) issue(u + S::kRing - 1, entry > 0 ? entry - 1 : S::kRing - 1);
+        const int here = entry;
+        entry = entry < S::kRing - 1 ? entry + 1 : 0;
         if (key0 >= ctx) continue;
-        const uint32_t stage = lds0 + static_cast<uint32_t>(uniform((u - u_begin) % S::kRing) * S::kBytes);
+        const uint32_t stage = lds0 + static_cast<uint32_t>(here * S::kBytes);
 #pragma unroll
         for (int sub = 0; sub < kSub; ++sub) {
-          // this lane's row, its statistics (1 / l: 0 where the row is none of the item's) and last visible key
-          const int m = u * S::kKeys + 32 * sub + col;
-          const float2 ml = lds_stats[uniform((u - u_begin) % S::kRing)][32 * sub + col];
+          // this lane's row and its statistics (1 / l: 0 where the row is none of the item's)
+          const int base_m = u * S::kKeys + 32 * sub, m = base_m + (lane_now() & 31);
+          const float2 ml = lds_stats[here][32 * sub + (m - base_m)];
           const float inv = m >= m_begin && m < m_end ? ml.y : 0.f;
           floatx16 x = floatx16{};
 #pragma unroll
           for (int c = 0; c < NK; ++c)
             x = mfma(kf[c], S::operand(stage + 32u * sub * S::kRowB, at_lane, c), x);
           // accumulator e: key key0 + e % 4 + 8 (e / 4) + 4 h of this lane's row
-          if (key0 + 31 <= kept + (u * S::kKeys + 32 * sub) / G) {         // every row sees every key
+          if (base_m >= m_full) {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
               acc[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -ml.x)), inv, acc[e]);
           } else {
-            const int lim = inv != 0.f ? kept + min(m, last_row) / G : -1;
+            const int rel = inv != 0.f ? m - m_key0 : INT32_MIN;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const float p = __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, -ml.x));
-              acc[e] = key0 + (e & 3) + 8 * (e >> 2) + 4 * h <= lim ? fmaf(p, inv, acc[e]) : acc[e];
+              acc[e] = rel >= ((e & 3) + 8 * (e >> 2) + 4 * h) * G ? fmaf(p, inv, acc[e]) : acc[e];
             }
           }
         }
@@ -498,17 +579,22 @@ __global__ __launch_bounds__(kSumThreads) void weights_add_kernel(const AttnWeig
 size_t align16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
 
 struct Layout {
-  size_t seqs, part_ml, stats, sums, bytes;
-  int row_chunks;
+  size_t part, stats, sums, bytes;
+  int chunk_keys, row_chunks;
 };
 Layout layout(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, int n_kv_heads) {
   Layout l;
+  // (the chunk grows in whole stages; chunks are as many as a longer call's at most)
+  const int keys = (max_ctx + kMaxChunks - 1) / kMaxChunks;
+  l.chunk_keys = keys <= kMinKeys ? kMinKeys : (keys + 63) / 64 * 64;
   const int64_t rows = static_cast<int64_t>(max_q < n_tokens ? max_q : n_tokens) * (n_q_heads / n_kv_heads);
   l.row_chunks = static_cast<int>((rows + kRowChunk - 1) / kRowChunk);
-  l.seqs = align16(kWGs * sizeof(Joined));
-  l.part_ml = l.seqs + n_seq * sizeof(int4);
-  l.stats = l.part_ml + static_cast<size_t>(2 * kWGs) * kRows * sizeof(float2);
-  l.sums = align16(l.stats + static_cast<size_t>(n_tokens) * n_q_heads * sizeof(float2));
+  const size_t vecs = static_cast<size_t>(n_tokens) * n_q_heads * sizeof(float2);
+  const int chunks = (max_ctx + kMinKeys - 1) / kMinKeys < kMaxChunks ? (max_ctx + kMinKeys - 1) / kMinKeys
+                                                                      : kMaxChunks;
+  l.part = n_seq * sizeof(int4);
+  l.stats = l.part + chunks * vecs;
+  l.sums = align16(l.stats + vecs);
   l.bytes = l.sums + static_cast<size_t>(l.row_chunks) * n_kv_heads * n_seq * max_ctx * sizeof(float);
   return l;
 }
@@ -519,17 +605,19 @@ hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
   const int max_ctx = b.max_pages << b.page_shift;
   const Layout l = layout(b.n_tokens, b.n_seq, max_ctx, a.max_q, a.n_q_heads, a.n_kv_heads);
   uint8_t* base = static_cast<uint8_t*>(a.workspace);
-  const WeightsWork ws{reinterpret_cast<Joined*>(base), reinterpret_cast<int4*>(base + l.seqs),
-                       reinterpret_cast<float2*>(base + l.part_ml),
+  const WeightsWork ws{reinterpret_cast<int4*>(base), reinterpret_cast<float2*>(base + l.part),
                        reinterpret_cast<float2*>(base + l.stats), reinterpret_cast<float*>(base + l.sums),
-                       l.row_chunks};
+                       l.chunk_keys};
   const float scale_log2 = a.scale * 1.4426950408889634f;
-  hipLaunchKernelGGL((weights_stats_kernel<D, SEQS>), dim3(kWGs), dim3(kThreads), 0, stream, a, ws,
+  hipLaunchKernelGGL((weights_stats_kernel<D, SEQS>), dim3(kItemWGs), dim3(kThreads), 0, stream, a, ws,
                      scale_log2);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(weights_join_kernel, dim3(kWGs), dim3(kRows), 0, stream, ws, b.n_tokens,
-                     a.n_q_heads / a.n_kv_heads);
+  const int64_t rows =
+      static_cast<int64_t>(a.max_q < b.n_tokens ? a.max_q : b.n_tokens) * (a.n_q_heads / a.n_kv_heads);
+  hipLaunchKernelGGL(weights_join_kernel,
+                     dim3(static_cast<unsigned>((rows + kRows - 1) / kRows), a.n_kv_heads, b.n_seq), dim3(kRows),
+                     0, stream, a, ws);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((weights_sum_kernel<D, SEQS>), dim3(kItemWGs), dim3(kThreads), 0, stream, a, ws,
