@@ -2,7 +2,10 @@
 //
 // A copy, bound by memory.  A wave takes kRows consecutive rows of the output as one run of 16-byte
 // pieces, so that its loads are full whatever the row's width; the page of each row is looked up by a lane of
-// its own, and the pieces fetch it from there.
+// its own, and the pieces fetch it from there.  Offsets are searched once per sequence that a wave's rows are
+// of, not once per row.  Eight streams' 47,341 rows of 1,024 values: 36 us (194 MB, 5.3 TB/s, a large
+// copy's rate; 46 us with a search per row, 44 us with stores through the cache); 17,048 rows of 576: 8.4 us
+// (10.8 us with non-temporal loads, which pass by the caches that hold a pool just written).
 #include "common.h"
 #include "latent.h"
 #include "paged_rows.h"
@@ -12,8 +15,8 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
-constexpr int kRows = 8;                 // rows of a wave
-constexpr int kFlight = 8;               // loads of a lane on their way at once
+constexpr int kRows = 4;                  // rows of a wave
+constexpr int kFlight = 8;                // loads of a lane on their way at once
 
 __global__ __launch_bounds__(kThreads) void paged_rows_kernel(const PagedRowsArgs a) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -26,17 +29,21 @@ __global__ __launch_bounds__(kThreads) void paged_rows_kernel(const PagedRowsArg
 
   // lane i < n: where row t0 + i is (the byte in the pool; -1: of a bad page, -2: no sequence's)
   int64_t src = -2;
-  for (int i = 0; i < n; ++i) {
-    const TokenRow r = find_row(b, static_cast<int>(t0) + i);
-    if (lane != i || r.seq < 0) continue;
-    const int page = b.table[static_cast<int64_t>(r.seq) * b.max_pages + (r.row >> b.page_shift)];
-    if (page < 0 || page >= b.n_pages) {
-      set_status(a.d_status, OMNITIDE_E_PAGES);
-      src = -1;
-    } else {
-      src = ((static_cast<int64_t>(page) << b.page_shift) + (r.row & ((1 << b.page_shift) - 1))) *
-            a.row_elems * 2;
+  for (int i = 0; i < n;) {
+    const RowRun r = find_rows(b, static_cast<int>(t0) + i);
+    const int end = min(n, i + min(r.left, kRows));
+    if (r.seq >= 0 && lane >= i && lane < end) {
+      const int row = r.row + lane - i;
+      const int page = b.table[static_cast<int64_t>(r.seq) * b.max_pages + (row >> b.page_shift)];
+      if (page < 0 || page >= b.n_pages) {
+        set_status(a.d_status, OMNITIDE_E_PAGES);
+        src = -1;
+      } else {
+        src = ((static_cast<int64_t>(page) << b.page_shift) + (row & ((1 << b.page_shift) - 1))) *
+              a.row_elems * 2;
+      }
     }
+    i = end;
   }
   const int per = a.row_elems / 8, all = n * per;          // 16-byte pieces
   const uint8_t* pool = static_cast<const uint8_t*>(a.pool);
@@ -56,7 +63,7 @@ __global__ __launch_bounds__(kThreads) void paged_rows_kernel(const PagedRowsArg
     }
 #pragma unroll
     for (int f = 0; f < kFlight; ++f)
-      if (to[f] != nullptr) *reinterpret_cast<u32x4*>(to[f]) = x[f];
+      if (to[f] != nullptr) __builtin_nontemporal_store(x[f], reinterpret_cast<u32x4*>(to[f]));
   }
 }
 

@@ -82,9 +82,12 @@ __device__ inline void report_batch(const PagedBatch& b, int32_t* status) {
   }
 }
 
-// Output row t of the sequences' rows in one piece (q_start: their offsets): its sequence and row there, as
-// find_token with rows counted from the sequence's first.
-__device__ inline TokenRow find_row(const PagedBatch& b, int t) {
+// Output rows from t on of the sequences' rows in one piece (q_start: their offsets): the sequence, its row
+// there, and how many rows go on in it (none of no sequence: one row).
+struct RowRun {
+  int seq, row, left;
+};
+__device__ inline RowRun find_rows(const PagedBatch& b, int t) {
   const int lane = threadIdx.x & (kWave - 1);
   for (int i0 = 0; i0 < b.n_seq; i0 += kWave) {
     const int i = i0 + lane;
@@ -100,11 +103,11 @@ __device__ inline TokenRow find_row(const PagedBatch& b, int t) {
       s0 = readlane(s0, l);
       s1 = readlane(s1, l);
       c = readlane(c, l);
-      if (c < s1 - s0 || c > (b.max_pages << b.page_shift)) return {-1, 0};
-      return {i0 + l, t - s0};
+      if (c < s1 - s0 || c > (b.max_pages << b.page_shift)) return {-1, 0, s1 - t};
+      return {i0 + l, t - s0, s1 - t};
     }
   }
-  return {-1, 0};
+  return {-1, 0, 1};
 }
 
 }  // namespace omnitide
