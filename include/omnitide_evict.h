@@ -86,9 +86,10 @@ size_t omnitide_evict_plan_workspace_bytes(int n_seq, int max_ctx);
  *   page_table, ctx_len  where the rows are: 0 <= src_row[s][i] < ctx_len[s] (OMNITIDE_E_RANGE: the row is
  *               not written)
  *   dst_table   int32 [n_seq][dst_max_pages]: pages of the sequences after the move.  None is a page that
- *               the call reads rows from, with one exception: dst_table[s][p] may be page_table[s][p] where
- *               every row of page p stays (src_row[s][i] == i); nothing is moved there.  (Copies between
- *               pages that break this are made in no particular order.)
+ *               the call reads rows from, with one exception: a page whose kept rows all keep their slots in
+ *               it, because none in front goes or only whole pages of them.  Nothing moves there; keys whose
+ *               row has changed turn where they are (then no other sequence has the page).  (Copies
+ *               between pages that break this are made in no particular order.)
  *   new_len     int32 [n_seq], at most src_stride and dst_max_pages * page_size (OMNITIDE_E_CAPACITY:
  *               nothing of the sequence is moved, nor for a ctx_len outside [0, max_pages * page_size])
  *   theta       HOST double [rope_dims / 2], or NULL: keys are copied bit for bit (values always are, and

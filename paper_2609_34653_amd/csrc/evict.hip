@@ -9,9 +9,13 @@
 // reads them once; longer sequences are cut into such slices in four launches: a slice's counts of the first
 // digit; the rows of that digit, put aside; the last two digits among those; the places.
 //
-// The move is a copy, bound by memory: each kept row is read and written once.  A wave takes up to kMoveRows rows; their
-// pages and angles are worked out a row per lane and a pair per lane, the copy goes by items of eight
-// values, keys as two runs of four so that both members of a rotated pair sit in one lane.
+// The move is a copy: each kept row is read and written once, behind a chain of four loads (length, row, page,
+// values).  So a workgroup takes only as many rows as its threads hold in two items of eight values each, and
+// many of them run at once: 4 (key, value) rows of 1,024 or 7 latent rows of 576.  16,384 of the former: 29 us (134
+// MB, 4.6 TB/s; 35 us with waves of their own of four items a lane, 29 us with one item, which costs the latent
+// rows, of 72 items, 44 us in place of 34: 129 MB, 3.8 TB/s).  Pages and angles are worked
+// out a row per lane and a pair per lane; keys go as two runs of four so that both members of a rotated pair sit in
+// one lane.
 #include "common.h"
 #include "evict.h"
 #include "paged_rows.h"
@@ -332,13 +336,13 @@ __global__ __launch_bounds__(kPlanThreads) void evict_place_kernel(const EvictPl
 
 // ---------------------------------------------------------------------------------------------
 
-constexpr int kMoveWaves = 4;
-constexpr int kMoveThreads = kMoveWaves * kWave;
-constexpr int kMoveRows = 8;             // rows of a wave at most
-constexpr int kMoveFlight = 4;           // items of a lane on their way at once
+constexpr int kMoveThreads = 256;
+constexpr int kMoveFlight = 2;           // items of a thread on their way at once
+constexpr int kMoveRows = 16;            // rows of a workgroup at most
+constexpr int kMoveGrid = 1 << 20;       // workgroups along x at most (2^32 threads are not launched)
 
-// How a wave's items are numbered: `rows` rows of `per` items, `per_head` of each head; quotients of numbers below
-// 512 by multiplication (x * magic >> 20: exact, as 512 x 512 < 2^20).
+// How a workgroup's items are numbered: `rows` rows of `per` items, `per_head` of each head; quotients of numbers
+// below 1,024 by multiplication (x * magic >> 20: exact, as 1,024 x 1,024 = 2^20).
 struct MoveItems {
   int rows, per, per_head;
   uint32_t by_per, by_head;
@@ -347,25 +351,24 @@ struct MoveItems {
 template <bool HALF, bool TURN>
 __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const PagedCompactArgs a,
                                                                    const MoveItems items) {
-  __shared__ __attribute__((aligned(16))) float2 cs[kMoveWaves][kMoveRows][kMaxRopePairs];
-  const int lane = threadIdx.x & (kWave - 1);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  __shared__ __attribute__((aligned(16))) float2 cs[kMoveRows][kMaxRopePairs];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const PagedBatch& b = a.batch;
   const int s = blockIdx.y;
   const int n = b.ctx_len[s], kept = a.new_len[s];
   if (kept < 0 || kept > a.src_stride || kept > (static_cast<int64_t>(a.dst_max_pages) << b.page_shift) ||
       n < 0 || n > (b.max_pages << b.page_shift)) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) set_status(a.d_status, OMNITIDE_E_CAPACITY);
+    if (blockIdx.x == 0 && blockIdx.z == 0 && tid == 0) set_status(a.d_status, OMNITIDE_E_CAPACITY);
     return;
   }
-  const int i0 = (blockIdx.x * kMoveWaves + wave) * items.rows;
+  const int64_t i0 = (static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x) * items.rows;
   if (i0 >= kept) return;
 
-  // lane r < items.rows: row i0 + r's slots and shift (from < 0: not moved)
+  // lane r < items.rows of every wave: row i0 + r's slots and shift (from < 0: not moved)
   int64_t from = -1, to = -1;
   int shift = 0;
   if (lane < items.rows && i0 + lane < kept) {
-    const int i = i0 + lane, j = a.src_row[s * a.src_stride + i];
+    const int i = static_cast<int>(i0) + lane, j = a.src_row[s * a.src_stride + i];
     const int p1 = a.dst_table[static_cast<int64_t>(s) * a.dst_max_pages + (i >> b.page_shift)];
     if (j < 0 || j >= n) {
       set_status(a.d_status, OMNITIDE_E_RANGE);
@@ -377,12 +380,12 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
         const int line = (1 << b.page_shift) - 1;
         from = (static_cast<int64_t>(p0) << b.page_shift) + (j & line);
         to = (static_cast<int64_t>(p1) << b.page_shift) + (i & line);
-        if (from == to) from = -1;       // stays where it is
         shift = i - j;
+        if (from == to && (!TURN || shift == 0)) from = -1;    // stays as it is
       }
     }
   }
-  if (__ballot(from >= 0) == 0) return;
+  if (__ballot(from >= 0) == 0) return;  // (the same in every wave)
   const int all = items.rows * items.per, R = TURN ? a.rope_dims : 0;
   const size_t row_bytes = static_cast<size_t>(a.row_elems) * 2;
 
@@ -393,7 +396,7 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
   auto load = [&](int it0) {
 #pragma unroll
     for (int f = 0; f < kMoveFlight; ++f) {
-      const int it = it0 + f * kWave + lane;
+      const int it = it0 + f * kMoveThreads + tid;
       const bool in = it < all;
       row[f] = in ? static_cast<int>((static_cast<uint32_t>(it) * items.by_per) >> 20) : 0;
       piece[f] = in ? it - row[f] * items.per : 0;
@@ -430,18 +433,19 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
   };
   load(0);
   if constexpr (TURN) {                  // the angles, while the first rows are on their way
-    for (int r = 0; r < items.rows; ++r) {
-      const int d = readlane(shift, r);
-      if (d != 0 && lane < a.rope_dims / 2) {
-        const double rev = static_cast<double>(d) * a.turns[lane];
+    for (int x = tid; x < kMoveRows * kMaxRopePairs; x += kMoveThreads) {
+      const int r = x / kMaxRopePairs, p = x % kMaxRopePairs;
+      const int d = __shfl(shift, r, kWave);
+      if (d != 0 && r < items.rows && p < a.rope_dims / 2) {
+        const double rev = static_cast<double>(d) * a.turns[p];
         float sn, cn;
         sincospif(2.f * static_cast<float>(rev - rint(rev)), &sn, &cn);
-        cs[wave][r][lane] = make_float2(cn, sn);
+        cs[r][p] = make_float2(cn, sn);
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the wave reads what it wrote
+    __syncthreads();
   }
-  for (int it0 = 0; it0 < all; it0 += kMoveFlight * kWave) {
+  for (int it0 = 0; it0 < all; it0 += kMoveFlight * kMoveThreads) {
     if (it0 > 0) load(it0);
 #pragma unroll
     for (int f = 0; f < kMoveFlight; ++f) {
@@ -453,7 +457,7 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
           floatx4 y = unpack_quad<false>(u32x4{kb[f][0], kb[f][1], 0, 0}), c, sn;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float2 t = cs[wave][row[f]][pair[f] + e];
+            const float2 t = cs[row[f]][pair[f] + e];
             c[e] = t.x;
             sn[e] = t.y;
           }
@@ -518,15 +522,17 @@ hipError_t launch_evict_plan(const EvictPlanArgs& a, hipStream_t stream) {
 hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream) {
   const int64_t cap = static_cast<int64_t>(a.dst_max_pages) << a.batch.page_shift;
   const int64_t rows = a.src_stride < cap ? a.src_stride : cap;
-  // as many rows per wave as its lanes have items on their way for
+  // as many rows of a workgroup as its threads have items on their way for
   MoveItems items;
   items.per = a.row_elems / 8;
-  items.rows = max(1, min(kMoveRows, kMoveFlight * kWave / items.per));
+  items.rows = max(1, min(kMoveRows, kMoveFlight * kMoveThreads / items.per));
   items.per_head = max(1, a.head_dim / 8);
   items.by_per = ((1u << 20) + items.per - 1) / items.per;
   items.by_head = ((1u << 20) + items.per_head - 1) / items.per_head;
-  const int per = kMoveWaves * items.rows;
-  const dim3 grid(static_cast<unsigned>((rows + per - 1) / per), static_cast<unsigned>(a.batch.n_seq));
+  const int64_t blocks = (rows + items.rows - 1) / items.rows;
+  const int64_t gx = min(blocks, static_cast<int64_t>(kMoveGrid));
+  const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>(a.batch.n_seq),
+                  static_cast<unsigned>((blocks + gx - 1) / gx));
   if (a.rope_dims == 0)
     hipLaunchKernelGGL((paged_compact_kernel<false, false>), grid, dim3(kMoveThreads), 0, stream, a, items);
   else if (a.rope_half)

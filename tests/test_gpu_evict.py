@@ -406,6 +406,48 @@ def test_compact_pages_that_stay():
     assert torch.equal(gk.cpu()[src_t[0, :2]], k[src_t[0, :2]])
 
 
+def test_compact_pages_turned_in_place():
+    """Whole pages go: the rows behind them keep their slots, their keys turn where they are."""
+    from paper_2609_34653_amd import evict as ev, paged as pg
+    n, P, H, d = 107, 16, 2, 64
+    src_t, _, n_pages = tables([n], [1], P, 1)
+    keep = np.concatenate([np.arange(32), np.arange(64, n)])
+    dst_t = src_t[:, [0, 1, 4, 5, 6]]
+    k, v = rand(1, n_pages, P, H, d).to(BF), rand(2, n_pages, P, H, d).to(BF)
+    gk, gv = k.cuda(), v.cuda()
+    th = pg.omnitide_rope_thetas(1.0e4, d)
+    ev.omnitide_paged_compact(gk, gv, i32(src_t), i32([n]), i32(dst_t), i32(keep[None]), i32([len(keep)]),
+                              theta=th)
+    torch.cuda.synchronize()
+    assert torch.equal(gv.cpu(), v)
+    i = np.arange(32, len(keep))
+    at = src_t[0, (i + 32) // P], i % P
+    want = op.norm_rope(f64(k[at]), None, 0.0, th, np.full(len(i), -32), "half")
+    assert_close(gk.cpu()[at], want, f64(k[at]), d, "half", BF)
+    same = k.clone()
+    same[at] = gk.cpu()[at]
+    assert torch.equal(gk.cpu(), same)
+
+
+def test_compact_long_src_row():
+    """Room for 2^28 rows of 4096 values, a workgroup each: more threads than one launch's first dimension holds."""
+    from paper_2609_34653_amd import evict as ev
+    P, n = 256, 20
+    k = rand(1, 4, P, 4096).to(BF).view(4, P, 1, 4096)
+    gk = k.cuda()
+    src = torch.zeros(1, 1 << 28, dtype=torch.int32, device="cuda")
+    src[0, :n] = torch.arange(3, 3 + n)
+    dst = torch.zeros(1, 1 << 20, dtype=torch.int32, device="cuda")
+    dst[0, 0] = 2
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ev.omnitide_paged_compact(gk, None, i32([[1]]), i32([40]), dst, src, i32([n]), d_status=st)
+    torch.cuda.synchronize()
+    want = k.clone()
+    want[2, :n] = k[1, 3:3 + n]
+    assert int(st.item()) == 0
+    assert torch.equal(gk.cpu(), want)
+
+
 @pytest.mark.parametrize("what", ["src", "row", "dst", "kept", "long"])
 def test_compact_refused_on_the_device(what):
     from paper_2609_34653_amd import evict as ev, omnitide as ot, paged as pg
