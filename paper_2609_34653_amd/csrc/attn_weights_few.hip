@@ -3,12 +3,15 @@
 //
 // Mathematics: as attn_weights.hip.  Bound by memory: 2 d bytes of a key serve 16 vectors at most.  So the scores
 // of the one pass over the keys are kept (4 bytes per query head and key, a twelfth to a half of the keys),
-// beside each vector's running reference and sum per share; a second kernel joins the sums of the shares, a
-// third sums exp2(x - m) / l over the vectors, a key per thread.
+// beside each vector's running reference and sum per share; a second kernel joins the sums of the shares and
+// sums exp2(x - m) / l over the vectors, a key per thread.
 //   shares    as in paged decode: the 16-key blocks of all sequences with tokens, one after the other, cut into
 //             equal shares, one per workgroup and KV head, a fixed cost counted for each sequence.
 //   waves     each takes every fourth block of its workgroup's part and owns a ring of LDS buffers filled by
 //             direct loads marked as read once; no barrier until the waves merge.
+//   measured  24 tokens of 32 heads over 119,095 keys of 8 x 128 in all: 50 us for the scores (244 MB read and 15
+//             written, 5.2 TB/s, a copy's rate; without the stores 42 us; with non-temporal ones 54 us) and
+//             9 us for the sum (7 us and a kernel of 4.6 us for the join, when that was one).
 //   products  S^T (16 keys x 16 vectors) = K Q^T with v_mfma_f32_16x16x32_bf16: a lane holds four
 //             consecutive keys of a vector, stored as 16 bytes.
 #include "common.h"
@@ -24,6 +27,7 @@ constexpr int kThreads = kWaves * kWave;
 constexpr int kKB = 16;                  // keys per block
 constexpr int kCols = 16;                // query vectors of a sequence and KV head at most
 constexpr int kMaxWGs = 512;
+constexpr int kMaxKvHeads = 64;
 constexpr int kMinShare = 8;             // blocks of a share at least
 constexpr int kOverhead = 12;            // what a sequence costs beside its blocks, in blocks
 constexpr size_t kScoreBytes = size_t{1} << 30;   // scores that are kept at most
@@ -75,11 +79,24 @@ __device__ inline FewShares<NS> plan_few(const AttnWeightsArgs& a, int wgs) {
   return s;
 }
 
-// What the kernels hand on.
+// Waits until at most the LOADS loads of each of `ahead` <= AHEAD blocks and `stores` <= STORES stores are on their
+// way.
+template <int LOADS, int AHEAD, int STORES>
+__device__ inline void wait_landed(int ahead, int stores) {
+  if constexpr (STORES > 0) {
+    if (stores < STORES) return wait_landed<LOADS, AHEAD, STORES - 1>(ahead, stores);
+  }
+  if constexpr (AHEAD > 0) {
+    if (ahead < AHEAD) return wait_landed<LOADS, AHEAD - 1, STORES>(ahead, STORES);
+  }
+  wait_vmcnt<LOADS * AHEAD + STORES>();
+}
+
+// What the first kernel hands on.
 struct FewWork {
-  int4* seqs;                            // first token, tokens (0: none), context
+  int4* seqs;                            // first token, tokens (0: none), context, its shares: first | count << 16
   float2* part_ml;                       // [2 x workgroup][kCols]
-  float2* stats;                         // (m, 1 / l) [token][query head]
+  float2* stats;                         // (m, 1 / l) [token][query head], of sequences in one share
   float* scores;                         // [token][query head][max_ctx]
 };
 
@@ -111,7 +128,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
     for (int n = 0; n < NS; ++n) {
       const int i = n * kWave + lane;
       if (i >= b.n_seq) continue;
-      ws.seqs[i] = make_int4(sh.q0[n], sh.len[n], sh.ctx[n], 0);
+      const int w0 = (sh.first[n] + kOverhead) / sh.share;
+      const int w1 = (sh.first[n] + kOverhead + max(sh.nb[n], 1) - 1) / sh.share;
+      ws.seqs[i] = make_int4(sh.q0[n], sh.len[n], sh.ctx[n], w0 | (w1 - w0 + 1) << 16);
       const int s0 = b.q_start[i], s1 = b.q_start[i + 1];
       many |= s0 >= 0 && s1 >= s0 && s1 <= b.n_tokens && s1 - s0 > a.max_q;
     }
@@ -219,11 +238,11 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
       for (int e = 0; e < RING; ++e) {
         const int it = it0 + e;
         if (it >= n_it) break;
-        // This block has landed: what was asked for after it are the loads of the blocks behind and the
-        // stores of the blocks in front, RING - 1 of each at most (fewer at both ends, where all are waited
-        // for).  Loads and stores come back in their order.
-        if (it >= RING && it + RING - 1 < n_it) wait_vmcnt<(RING - 1) * (CALLS + 1)>();
-        else wait_vmcnt<0>();
+        // This block has landed: behind its loads come those of the blocks ahead of it, RING - 1 at most, and
+        // the stores of the RING blocks in front (loads and stores come back in their order).
+        const int ahead = min(n_it - 1 - it, RING - 1);
+        if (it0 > 0) wait_landed<CALLS, RING - 1, RING>(ahead, RING);
+        else wait_landed<CALLS, RING - 1, RING>(ahead, e);
         const uint32_t kb = ring + static_cast<uint32_t>(e * BLOCKB);
         floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -242,7 +261,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
           asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(s) : : "memory");
           if (it + RING < n_it) issue(it + RING, e);
         }
-        if (col_ok) __builtin_nontemporal_store(s, reinterpret_cast<floatx4*>(scores + key0 + 4 * g4));
+        if (col_ok) *reinterpret_cast<floatx4*>(scores + key0 + 4 * g4) = s;
         if (key0 + kKB - 1 > ctx - len) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -293,80 +312,73 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
   }
 }
 
-// Joins a vector's statistics over the shares that its sequence lies in: a wave per vector, a part per lane.
-template <int NS>
-__global__ __launch_bounds__(kThreads) void weights_few_join_kernel(const AttnWeightsArgs a, const FewWork ws,
-                                                                  int wgs) {
-  const PagedBatch& b = a.batch;
-  const int lane = threadIdx.x & (kWave - 1);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
-  const int64_t vec = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
-  if (vec >= static_cast<int64_t>(b.n_tokens) * Hq) return;
-  const int t = static_cast<int>(vec / Hq), head = static_cast<int>(vec - static_cast<int64_t>(t) * Hq);
-  const int g = head / G;
-  const FewShares<NS> sh = plan_few<NS>(a, wgs);
-  int first = 0, nb = 0, tok = 0;
-#pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    const uint64_t hit = __ballot(sh.nb[n] > 0 && t >= sh.q0[n] && t < sh.q0[n] + sh.len[n]);
-    if (hit != 0) {
-      const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
-      first = readlane(sh.first[n], l);
-      nb = readlane(sh.nb[n], l);
-      tok = t - readlane(sh.q0[n], l);
-    }
-  }
-  if (nb == 0) return;
-  const int w0 = (first + kOverhead) / sh.share, w1 = (first + kOverhead + nb - 1) / sh.share;
-  if (w0 == w1) return;                    // finished by its workgroup
-  const int col = tok * G + head % G;
-  float mx = -INFINITY, l = 0.f;
-  for (int p = lane; p <= w1 - w0; p += kWave) {
-    const float2 v =
-        ws.part_ml[static_cast<size_t>(2 * ((w0 + p) * Hkv + g) + (p == 0 ? 1 : 0)) * kCols + col];
-    const float m = fmaxf(mx, v.x);
-    if (m != -INFINITY) {
-      l = (mx == -INFINITY ? 0.f : l * exp2f(mx - m)) + (v.x == -INFINITY ? 0.f : v.y * exp2f(v.x - m));
-      mx = m;
-    }
-  }
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const float m2 = __shfl_xor(mx, o, kWave), l2 = __shfl_xor(l, o, kWave), m = fmaxf(mx, m2);
-    if (m != -INFINITY) {
-      // (the lower lane's part first, in both lanes)
-      const float u = mx == -INFINITY ? 0.f : l * exp2f(mx - m);
-      const float v = m2 == -INFINITY ? 0.f : l2 * exp2f(m2 - m);
-      l = u + v;
-      mx = m;
-    }
-  }
-  if (lane == 0) ws.stats[vec] = make_float2(mx, 1.f / l);
-}
-
-// The new weights: a key per thread, over the tokens and heads.
+// The new weights: a key per thread, over the tokens and heads.  Each workgroup first joins the statistics of its
+// sequence's vectors over the shares that the sequence lies in, `width` lanes a vector and a part per lane, while
+// its first scores are on their way.
 __global__ __launch_bounds__(kSumThreads) void weights_few_add_kernel(const AttnWeightsArgs a,
                                                                     const FewWork ws, float scale_log2) {
   constexpr int kFlight = 8;
+  __shared__ float2 stats[kCols * kMaxKvHeads];
   const PagedBatch& b = a.batch;
-  const int s = blockIdx.y, j = blockIdx.x * kSumThreads + threadIdx.x;
+  const int tid = threadIdx.x, s = blockIdx.y, j = blockIdx.x * kSumThreads + tid;
   const int4 q = ws.seqs[s];
   if (q.y == 0 || static_cast<int>(blockIdx.x) * kSumThreads >= q.z) return;
   const int max_ctx = b.max_pages << b.page_shift, kept = q.z - q.y;
   const bool in = j < q.z;
-  const int n = q.y * a.n_q_heads;         // the sequence's vectors, token by token
-  const size_t vec0 = static_cast<size_t>(q.x) * a.n_q_heads;
+  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
+  const int n = q.y * Hq;                  // the sequence's vectors, token by token
+  const size_t vec0 = static_cast<size_t>(q.x) * Hq;
   const float* scores = ws.scores + vec0 * max_ctx + (in ? j : 0);
-  const float2* stats = ws.stats + vec0;
+  float x[kFlight];
+  auto load = [&](int v0) {
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) x[i] = scores[static_cast<size_t>(min(v0 + i, n - 1)) * max_ctx];
+  };
+  load(0);
+
+  const int w0 = q.w & 0xffff, parts = q.w >> 16;
+  int width = 1;
+  while (width < min(parts, kWave)) width <<= 1;
+  const int sub = tid & (width - 1), step = kSumThreads / width;
+  for (int u = tid / width; u < (n + step - 1) / step * step; u += step) {
+    const int v = min(u, n - 1);
+    const int tok = v / Hq, head = v - tok * Hq, g = head / G, col = tok * G + head - g * G;
+    float mx = -INFINITY, l = 0.f;
+    if (parts == 1) {
+      const float2 ml = ws.stats[vec0 + v];
+      mx = ml.x;
+      l = ml.y;
+    } else {
+      for (int p = sub; p < parts; p += width) {
+        const float2 ml =
+            ws.part_ml[static_cast<size_t>(2 * ((w0 + p) * Hkv + g) + (p == 0 ? 1 : 0)) * kCols + col];
+        const float m = fmaxf(mx, ml.x);
+        if (m != -INFINITY) {
+          l = (mx == -INFINITY ? 0.f : l * exp2f(mx - m)) +
+              (ml.x == -INFINITY ? 0.f : ml.y * exp2f(ml.x - m));
+          mx = m;
+        }
+      }
+      for (int o = 1; o < width; o <<= 1) {
+        const float m2 = __shfl_xor(mx, o, kWave), l2 = __shfl_xor(l, o, kWave), m = fmaxf(mx, m2);
+        if (m != -INFINITY) {
+          const float y = mx == -INFINITY ? 0.f : l * exp2f(mx - m);
+          const float z = m2 == -INFINITY ? 0.f : l2 * exp2f(m2 - m);
+          l = y + z;
+          mx = m;
+        }
+      }
+      l = 1.f / l;
+    }
+    if (sub == 0 && u < n) stats[u] = make_float2(mx, l);
+  }
+  __syncthreads();
+
   // vectors of tokens that see row j: those from token j - kept on
-  const int v_from = max(j - kept, 0) * a.n_q_heads;
+  const int v_from = max(j - kept, 0) * Hq;
   float sum = 0.f;
   for (int v0 = 0; v0 < n; v0 += kFlight) {
-    float x[kFlight];
-#pragma unroll
-    for (int i = 0; i < kFlight; ++i)
-      x[i] = __builtin_nontemporal_load(scores + static_cast<size_t>(min(v0 + i, n - 1)) * max_ctx);
+    if (v0 > 0) load(v0);
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
       const float2 ml = stats[min(v0 + i, n - 1)];
@@ -410,11 +422,6 @@ hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((weights_score_kernel<D, NS>), dim3(wgs), dim3(kThreads), 0, stream, a, ws, scale_log2);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t vecs = static_cast<int64_t>(b.n_tokens) * a.n_q_heads;
-  hipLaunchKernelGGL(weights_few_join_kernel<NS>, dim3(static_cast<unsigned>((vecs + kWaves - 1) / kWaves)),
-                     dim3(kThreads), 0, stream, a, ws, wgs);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
   hipLaunchKernelGGL(weights_few_add_kernel, dim3((max_ctx + kSumThreads - 1) / kSumThreads, b.n_seq),
                      dim3(kSumThreads), 0, stream, a, ws, scale_log2);
   return hipGetLastError();
@@ -428,7 +435,7 @@ hipError_t launch_d(const AttnWeightsArgs& a, hipStream_t stream) {
 }  // namespace
 
 bool attn_weights_few(int n_tokens, int max_ctx, int max_q, int n_q_heads, int n_kv_heads) {
-  return static_cast<int64_t>(max_q) * (n_q_heads / n_kv_heads) <= kCols && n_kv_heads <= 64 &&
+  return static_cast<int64_t>(max_q) * (n_q_heads / n_kv_heads) <= kCols && n_kv_heads <= kMaxKvHeads &&
          static_cast<size_t>(n_tokens) * n_q_heads * max_ctx <= kScoreBytes / sizeof(float);
 }
 
