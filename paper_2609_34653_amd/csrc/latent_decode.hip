@@ -20,52 +20,18 @@
 //   products  S^T (16 keys x 16 vectors, twice) = K Q^T and O^T (16 dims x 16 vectors) = C^T P^T with
 //             v_mfma_f32_16x16x32_bf16; keys are permuted when K rows are read so that S^T is the operand of
 //             the second product as it stands.
-#include "common.h"
-#include "latent.h"
-#include "mfma_tile.h"
-#include "paged_rows.h"
+#include "latent_decode.h"
 
 namespace omnitide {
 namespace {
 
-constexpr int kKT = 32;                  // keys per tile and block
-constexpr int kStep = 2;                 // tiles per step
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
 constexpr int kRow = 16;                 // vectors per row tile
-constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
-constexpr int kNumXcd = 8;
-constexpr int kMinShare = 4;             // blocks of a share at least
+constexpr int RB = 2;                    // row tiles of a workgroup
+constexpr int KW = kWaves / RB;          // key groups
+constexpr int kGroup = RB * kRow;        // its vectors
 constexpr int kOverhead = 6;             // what a sequence costs beside its blocks, in blocks
-
-template <int NS>
-struct Shares {
-  int nb[NS], first[NS], ctx[NS];
-  int per_head, share;
-};
-
-// As in paged decode, with row tiles in place of KV heads.
-template <int NS>
-__device__ inline Shares<NS> plan_shares(const PagedBatch& b, int row_tiles) {
-  const int lane = threadIdx.x & (kWave - 1);
-  const int cap = b.max_pages << b.page_shift;
-  Shares<NS> s;
-#pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    const int i = n * kWave + lane;
-    s.ctx[n] = i < b.n_seq ? b.ctx_len[i] : -1;
-  }
-  s.per_head = 0;
-#pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    s.nb[n] = s.ctx[n] >= b.n_q && s.ctx[n] <= cap ? (s.ctx[n] + kKT - 1) / kKT : 0;
-    const int work = s.nb[n] > 0 ? kOverhead + s.nb[n] : 0;
-    const int inc = wave_scan_add_i32(work);
-    s.first[n] = s.per_head + inc - work;
-    s.per_head += readlane(inc, kWave - 1);
-  }
-  const int per = kWGs / kNumXcd / row_tiles * kNumXcd;
-  s.share = max(kMinShare, (s.per_head + per - 1) / per);
-  return s;
-}
 
 // The swizzle of a key's chunks.  Rows are an odd number of 128 bytes, so a key's bit 0 shifts by half the
 // banks; its bits 1, 3 and 4 do the rest for the 16 keys of a K read (8 i + j, i, j < 4), and bits 1 and 3 move
@@ -74,18 +40,13 @@ __device__ inline int swz(int key) {
   return ((key >> 1) & 1) << 2 | ((key >> 3) & 1) << 1 | ((key >> 4) & 1);
 }
 
-// RB: row tiles of a workgroup; NS: sequences per lane of the plan.
-template <int RB>
-constexpr int waves_of() { return RB == 2 ? 4 : 8; }
-
-template <int R, int RB, int NS>
-__global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void latent_decode_kernel(
+// NS: sequences per lane of the plan.
+template <int R, int NS>
+__global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ pool, const PagedBatch b, int H,
-    int row_groups, float scale_log2, void* __restrict__ out, bool out_bf16, float* __restrict__ part_o,
+    float scale_log2, void* __restrict__ out, bool out_bf16, float* __restrict__ part_o,
     float2* __restrict__ part_ml, int32_t* __restrict__ status) {
-  constexpr int kWaves = waves_of<RB>(), kThreads = kWaves * kWave;
   constexpr int D = R + kLatentRope;
-  constexpr int KW = kWaves / RB;          // key groups
   constexpr int CH = D / 8;                // 16-byte chunks per row
   constexpr int KS = D / 32;               // K operands of 16 keys
   constexpr int DT = R / 16;               // 16-dim tiles of the output
@@ -111,7 +72,7 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
   const int nq = b.n_q, M = nq * H;
 
   if (blockIdx.x == 0 && wave == 0) report_batch(b, status);
-  const Shares<NS> sh = plan_shares<NS>(b, row_groups);
+  const Shares<NS> sh = plan_shares<NS>(b, 1, kOverhead);
   // what the parts are found from, out of registers
   const int per_head = sh.per_head, share = sh.share;
   if (wave == 0) {
@@ -129,10 +90,7 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
       else static_cast<float*>(out)[at + i] = 0.f;
     }
   }
-  // the row groups of a share (the same keys) on one XCD: workgroups are dealt round-robin over 8
-  const int on_xcd = blockIdx.x / kNumXcd, rg = on_xcd % row_groups;
-  const int wg = on_xcd / row_groups * kNumXcd + blockIdx.x % kNumXcd;       // its share
-  const int m0 = rg * RB * kRow;           // the workgroup's first vector
+  const int wg = blockIdx.x;               // its share
   const int64_t lo64 = static_cast<int64_t>(wg) * share;
   if (lo64 >= per_head) return;
   const int lo = static_cast<int>(lo64), hi = min(lo + share, per_head);
@@ -144,6 +102,19 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
   // C^T: keys 8 g4 + col / 4 (+ 4), dims 16 dt + 4 (col % 4)
   const int vrow = 8 * g4 + (col >> 2);
   const uint32_t v_lane = ROWB * vrow + 8u * (col & 1), v_unit = 16u * (((col & 3) >> 1) ^ swz(vrow));
+
+  // Direct load c of eight rows: chunk c * 64 + lane of them, at `from` this byte of them (bits 3 and 4 of a wave's
+  // keys are those of its number).  The swizzle is that of the place, not of the row that fills it.
+  auto load_from = [&](int c, int ln, int last) {
+    const int at = c * kWave + ln, key = at / CH, pc = at - key * CH;
+    return static_cast<uint32_t>(min(key, last)) * ROWB + 16u * (pc ^ swz(key + 8 * wave));
+  };
+  uint32_t from[LOADS];
+#pragma unroll
+  for (int c = 0; c < LOADS; ++c) {
+    from[c] = load_from(c, lane, 7);
+    asm volatile("" : "+v"(from[c]));        // kept
+  }
 
   for (int pos = lo; pos < hi;) {
     // the part of one sequence that starts at pos; its overhead comes before its blocks
@@ -166,25 +137,23 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
     if (b1 == 0) break;                      // the share ends before the first block
     const bool whole = b0 == 0 && b1 == nb;
     // a share holds at most one part that goes on from an earlier share and one that goes on in a later
-    const int slot = 2 * (wg * row_groups + rg) + (b0 > 0 ? 0 : 1);
+    const int slot = 2 * wg + (b0 > 0 ? 0 : 1);
 
     // Q^T operand: column = vector m (token m / H)
-    const int m = m0 + rb * kRow + col;
+    const int m = rb * kRow + col;
     const bool row_ok = m < M;
     if (g4 == 0) slim[wave][col] = ctx - nq + (row_ok ? m / H : 0);   // the last visible key
-    const uint16_t* qrow = q + (static_cast<size_t>(seq) * M + (row_ok ? m : 0)) * D;
-    bf16x8 qf[KS];
-#pragma unroll
-    for (int c = 0; c < KS; ++c) qf[c] = __builtin_bit_cast(bf16x8, ld16(qrow + 32 * c + 8 * g4));
-
     // The part ends in front of a bad page: the vectors that see it are spoilt (below), and the others see
     // no later key either, so nothing is read in its place.
     const int32_t* table = b.table + static_cast<size_t>(seq) * b.max_pages;
     int end = min(b1 * kKT, ctx), bad_row = INT32_MAX;         // keys in front of `end` are read
+    int ids = 0;                             // page p0 + lane
+    const int p0 = (b0 * kKT) >> b.page_shift;
     {
-      const int p0 = (b0 * kKT) >> b.page_shift, p1 = (end - 1) >> b.page_shift;
+      const int p1 = (end - 1) >> b.page_shift;
       for (int p = p0; p <= p1; p += kWave) {
         const int id = p + lane <= p1 ? table[p + lane] : 0;
+        if (p == p0) ids = id;
         const uint64_t bad = __ballot(id < 0 || id >= b.n_pages);
         if (bad != 0) {
           const int first = p + __ffsll(static_cast<unsigned long long>(bad)) - 1;
@@ -214,21 +183,55 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
         const uint8_t* base = reinterpret_cast<const uint8_t*>(pool) +
                               ((static_cast<size_t>(page[o]) << b.page_shift) + line) * ROWB;
         const uint32_t dst = lds0 + static_cast<uint32_t>(((t & 1) * 4 * kStep + oct) * 8 * ROWB);
-        const int last = min(end - 1 - (ks & ~7), 7);          // the last of these eight rows in use
-        const uint32_t flip = 2u * (oct & 1) + ((oct >> 1) & 1);   // of bits 3 and 4 of the keys
-        // this lane's place in load c: chunk c * 64 + lane of the eight rows (worked out anew: kept, the
-        // offsets of all loads would be spilt, and their reloads wait for the loads in flight)
-        const int ln = lane_now();
+        const int last = end - 1 - (ks & ~7);                  // the last of these eight rows in use
+        if (last >= 7) {
 #pragma unroll
-        for (int c = 0; c < LOADS; ++c) {
-          const int at = c * kWave + ln, key = at / CH, pc = at - key * CH;
-          // (the swizzle is that of the place, not of the row that fills it)
-          const uint32_t from = static_cast<uint32_t>(min(key, last)) * ROWB + 16u * (pc ^ swz(key) ^ flip);
-          dma16_once(base, from, dst + static_cast<uint32_t>(c * kWave * 16));
-          __builtin_amdgcn_sched_barrier(0);
+          for (int c = 0; c < LOADS; ++c) {
+            dma16_once(base, from[c], dst + static_cast<uint32_t>(c * kWave * 16));
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          continue;
         }
+        const int ln = lane_now();
+#pragma unroll 1
+        for (int c = 0; c < LOADS; ++c)
+          dma16_once(base, load_from(c, ln, last), dst + static_cast<uint32_t>(c * kWave * 16));
       }
     };
+
+    // The first step's keys are asked for, then the queries; nothing but direct loads is counted.
+    if (steps > 0) {
+      auto first_page = [&](int t, int o) {
+        return readlane(ids, (min(first_key(t, o), end - 1) >> b.page_shift) - p0);
+      };
+#pragma unroll
+      for (int i = 0; i < OCTS; ++i) page[i] = first_page(0, i);
+      issue(0);
+#pragma unroll
+      for (int i = 0; i < OCTS; ++i) page[i] = first_page(1, i);
+    }
+    // (a wave's eight vectors, as if they were keys of the next step)
+    const uint32_t queries = lds0 + kStep * TILEB;
+    {
+      const int ln = lane_now(), v0 = min(8 * wave, M - 1), last = min(M - 1 - v0, 7);
+      const uint16_t* at = q + (static_cast<size_t>(seq) * M + v0) * D;
+#pragma unroll 1
+      for (int c = 0; c < LOADS; ++c)
+        dma16(at, load_from(c, ln, last), queries + static_cast<uint32_t>(wave * 8 * ROWB + c * kWave * 16));
+    }
+    wait_vmcnt<0>();
+    __syncthreads();
+    bf16x8 qf[KS];
+    {
+      const int r = rb * kRow + col;
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+        qf[c] = __builtin_bit_cast(
+            bf16x8, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
+                        queries + ROWB * r + (16u * (g4 ^ swz(r)) ^ 64u * (c & 1)) + 128u * (c >> 1)));
+#pragma unroll
+      for (int c = 0; c < KS; ++c) asm volatile("" : "+v"(qf[c]));
+    }
 
     floatx4 o[DT];
 #pragma unroll
@@ -328,17 +331,6 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
       }
     };
 
-    // Nothing but the direct loads is counted from here on: the queries are there (and known to be).
-#pragma unroll
-    for (int c = 0; c < KS; ++c) asm volatile("" : "+v"(qf[c]));
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (steps > 0) {
-#pragma unroll
-      for (int i = 0; i < OCTS; ++i) page[i] = page_of(0, i);
-      issue(0);
-#pragma unroll
-      for (int i = 0; i < OCTS; ++i) page[i] = page_of(1, i);
-    }
     for (int t = 0; t < steps; ++t) {
       wait_vmcnt<0>();
       __syncthreads();                       // step t is there, and every wave is done with the one before
@@ -349,7 +341,7 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
       }
       const int key0 = (b0 + t * kStep) * kKT;
       const uint32_t tile = lds0 + static_cast<uint32_t>((t & 1) * kStep * TILEB);
-      if (m0 + rb * kRow < M) {              // a wave without vectors: its share of the loads
+      if (rb * kRow < M) {                   // a wave without vectors: its share of the loads
 #pragma unroll 1
         for (int i = 0; i < kStep / KW; ++i) {
           const int at = KW == 1 ? i : kw;
@@ -377,7 +369,7 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
         *reinterpret_cast<floatx4*>(so + (wave * kRow + col) * kCol + 16 * dt + 4 * g4) =
             o[half * (kHalf / 16) + dt];
       __syncthreads();
-      for (int r = wave; r < RB * kRow && m0 + r < M; r += kWaves) {
+      for (int r = wave; r < M; r += kWaves) {
         const int tile = r / kRow, c = r % kRow;
         float mx = -INFINITY;
 #pragma unroll
@@ -397,10 +389,10 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
         }
         const int d0 = half * kHalf + 4 * lane;
         if (whole) {
-          const size_t at = (static_cast<size_t>(seq) * M + m0 + r) * R + d0;
+          const size_t at = (static_cast<size_t>(seq) * M + r) * R + d0;
           store_row4(out, at, out_bf16, den == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : num / den);
         } else {
-          const size_t row = static_cast<size_t>(slot) * (RB * kRow) + r;
+          const size_t row = static_cast<size_t>(slot) * kGroup + r;
           *reinterpret_cast<floatx4*>(part_o + row * R + d0) = num;
           if (half == 0 && lane == 0) part_ml[row] = make_float2(mx, den);
         }
@@ -410,125 +402,36 @@ __global__ __launch_bounds__(waves_of<RB>() * kWave, waves_of<RB>() / 4) void la
   }
 }
 
-// Merges the parts of one vector that lie in several shares, in share order: a workgroup per vector and DIMS of
-// its dims, four of them per thread, 1024 / DIMS parts side by side and four of each asked for at a time.
-constexpr int kMergeThreads = 256;
-template <int R, int RB, int NS, int DIMS>
-__global__ __launch_bounds__(kMergeThreads) void latent_decode_merge_kernel(
-    const float* __restrict__ part_o, const float2* __restrict__ part_ml, const PagedBatch b, int H,
-    int row_groups, void* __restrict__ out, bool out_bf16) {
-  constexpr int kBatch = 4, TPR = DIMS / 4, TS = kMergeThreads / TPR;
-  __shared__ floatx4 sn[TS][TPR];
-  __shared__ float2 sml[TS];
-  const int M = b.n_q * H;
-  const int seq = blockIdx.x / M, m = blockIdx.x % M, rg = m / (RB * kRow), r = m % (RB * kRow);
-  const Shares<NS> sh = plan_shares<NS>(b, row_groups);
-  int first = 0, nb = 0;
-#pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    if (seq / kWave == n) {
-      first = readlane(sh.first[n], seq % kWave);
-      nb = readlane(sh.nb[n], seq % kWave);
-    }
-  }
-  if (nb == 0) return;
-  const int w0 = (first + kOverhead) / sh.share, w1 = (first + kOverhead + nb - 1) / sh.share;
-  if (w0 == w1) return;                      // finished by its workgroup
-  const int ts = threadIdx.x / TPR, t = threadIdx.x % TPR, d = blockIdx.y * DIMS + 4 * t;
-  const int n_parts = w1 - w0 + 1;
-  float mx = -INFINITY, den = 0.f;
-  floatx4 num = {0.f, 0.f, 0.f, 0.f};
-  auto add = [&](float pm, float pl, floatx4 po) {
-    if (pm == -INFINITY) return;
-    const float m_new = fmaxf(mx, pm), u = mx == -INFINITY ? 0.f : exp2f(mx - m_new), v = exp2f(pm - m_new);
-    den = fmaf(den, u, v * pl);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) num[e] = fmaf(num[e], u, v * po[e]);
-    mx = m_new;
-  };
-  for (int p0 = ts; p0 < n_parts; p0 += TS * kBatch) {
-    float2 ml[kBatch];
-    floatx4 ov[kBatch];
-#pragma unroll
-    for (int c = 0; c < kBatch; ++c) {
-      const int p = p0 + c * TS;
-      const bool in = p < n_parts;
-      const size_t row =
-          static_cast<size_t>(2 * ((w0 + p) * row_groups + rg) + (p == 0 ? 1 : 0)) * (RB * kRow) + r;
-      ml[c] = in ? part_ml[row] : make_float2(-INFINITY, 0.f);
-      ov[c] = in ? *reinterpret_cast<const floatx4*>(part_o + row * R + d) : floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-#pragma unroll
-    for (int c = 0; c < kBatch; ++c) add(ml[c].x, ml[c].y, ov[c]);
-  }
-  sn[ts][t] = num;
-  if (t == 0) sml[ts] = make_float2(mx, den);
-  __syncthreads();
-  if (ts != 0) return;
-#pragma unroll
-  for (int c = 1; c < TS; ++c) add(sml[c].x, sml[c].y, sn[c][t]);
-  store_row4(out, static_cast<size_t>(blockIdx.x) * R + d, out_bf16,
-             den == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : num / den);
-}
-
-// Vectors from which on a merge workgroup takes all dims of one: there are enough of them, of few parts each (24
-// x 128 vectors: 24 us by quarters, 16 whole), and few have many (16 of 134 parts: 7 and 23).
-constexpr int kWideVecs = 512;
-
-int row_tiles_of(int M) { return M <= 32 ? 2 : 4; }
-
-// Workgroups of a call: a share of every row group each.
-int groups_of(int M) { return (M + kRow * row_tiles_of(M) - 1) / (kRow * row_tiles_of(M)); }
-
-// Shares of a row group: whole rounds over the XCDs.
-int shares_of(int groups) { return kWGs / kNumXcd / groups * kNumXcd; }
-
-template <int R, int RB, int NS>
+template <int R, int NS>
 hipError_t launch_t(const LatentDecodeArgs& a, hipStream_t stream) {
   const PagedBatch& b = a.batch;
-  const int groups = groups_of(b.n_q * a.n_heads);
-  const int wgs = shares_of(groups) * groups;
+  constexpr int wgs = kWGs;
   float2* part_ml = static_cast<float2*>(a.workspace);
-  float* part_o = reinterpret_cast<float*>(part_ml + static_cast<size_t>(2 * wgs) * RB * kRow);
+  float* part_o = reinterpret_cast<float*>(part_ml + static_cast<size_t>(2 * wgs) * kGroup);
   const float scale_log2 = a.scale * 1.4426950408889634f;
-  hipLaunchKernelGGL((latent_decode_kernel<R, RB, NS>), dim3(wgs), dim3(waves_of<RB>() * kWave), 0, stream,
+  hipLaunchKernelGGL((latent_decode_kernel<R, NS>), dim3(wgs), dim3(kThreads), 0, stream,
                      static_cast<const uint16_t*>(a.q), static_cast<const uint16_t*>(a.pool), b, a.n_heads,
-                     groups, scale_log2, a.out, a.out_bf16, part_o, part_ml, a.d_status);
+                     scale_log2, a.out, a.out_bf16, part_o, part_ml, a.d_status);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int vecs = b.n_tokens * a.n_heads;
-  if (vecs < kWideVecs)
-    hipLaunchKernelGGL((latent_decode_merge_kernel<R, RB, NS, 128>), dim3(vecs, R / 128), dim3(kMergeThreads), 0,
-                       stream, part_o, part_ml, b, a.n_heads, groups, a.out, a.out_bf16);
-  else
-    hipLaunchKernelGGL((latent_decode_merge_kernel<R, RB, NS, R>), dim3(vecs), dim3(kMergeThreads), 0, stream,
-                       part_o, part_ml, b, a.n_heads, groups, a.out, a.out_bf16);
-  return hipGetLastError();
-}
-
-template <int R, int RB>
-hipError_t launch_n(const LatentDecodeArgs& a, hipStream_t stream) {
-  if (a.batch.n_seq <= kWave) return launch_t<R, RB, 1>(a, stream);
-  return launch_t<R, RB, 16>(a, stream);
+  return launch_merge<R, kGroup, NS>(a, 1, kOverhead, part_o, part_ml, stream);
 }
 
 template <int R>
 hipError_t launch_r(const LatentDecodeArgs& a, hipStream_t stream) {
-  switch (row_tiles_of(a.batch.n_q * a.n_heads)) {
-    case 2: return launch_n<R, 2>(a, stream);
-    default: return launch_n<R, 4>(a, stream);
-  }
+  return a.batch.n_seq <= kWave ? launch_t<R, 1>(a, stream) : launch_t<R, 16>(a, stream);
 }
 
 }  // namespace
 
 size_t latent_decode_workspace_bytes(int n_q, int n_heads, int latent_dim) {
-  const int M = n_q * n_heads, groups = groups_of(M);
-  const size_t rows = static_cast<size_t>(2 * shares_of(groups) * groups) * row_tiles_of(M) * kRow;
+  const int M = n_q * n_heads;
+  const size_t rows = M > kGroup ? latent_decode_wide_rows(M) : static_cast<size_t>(2 * kWGs) * kGroup;
   return rows * (static_cast<size_t>(latent_dim) + 2) * sizeof(float);
 }
 
 hipError_t launch_latent_decode(const LatentDecodeArgs& a, hipStream_t stream) {
+  if (a.batch.n_q * a.n_heads > kGroup) return launch_latent_decode_wide(a, stream);
   return a.latent_dim == 512 ? launch_r<512>(a, stream) : launch_r<256>(a, stream);
 }
 
