@@ -24,8 +24,7 @@ ARCH = "gfx950"
 SOURCES = ["abi.cpp", "score.hip", "select.hip", "spans.hip", "compact.hip", "native.hip",
            "attention.hip", "decode.hip", "paged_abi.cpp", "norm_rope.hip",
            "paged_chunk.hip", "paged_decode.hip", "latent_abi.cpp", "latent_append.hip",
-           "latent_rows.hip", "latent_decode.hip", "latent_decode_wide.hip", "latent_chunk.hip",
-           "evict_abi.cpp",
+           "latent_rows.hip", "latent_decode.hip", "latent_chunk.hip", "evict_abi.cpp",
            "attn_weights.hip", "attn_weights_few.hip", "evict.hip"]
 
 # Packed fp32 instructions are kept out of the device code (-packed-fp32-ops).

@@ -50,9 +50,6 @@ struct LatentDecodeArgs {
 };
 size_t latent_decode_workspace_bytes(int n_q, int n_heads, int latent_dim);
 hipError_t launch_latent_decode(const LatentDecodeArgs& a, hipStream_t stream);
-// The same for more vectors of a sequence than latent_decode.hip takes; rows of its partial results.
-size_t latent_decode_wide_rows(int vecs);
-hipError_t launch_latent_decode_wide(const LatentDecodeArgs& a, hipStream_t stream);
 
 struct LatentChunkArgs {
   const void* q;
