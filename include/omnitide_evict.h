@@ -66,7 +66,8 @@ size_t omnitide_paged_attn_weights_workspace_bytes(int n_tokens, int n_seq, int 
  *   new_len     int32 [n_seq]: rows kept
  *   weight_out  float [n_seq][weight_out_stride], weight_out_stride >= high: the kept rows' weights, bit
  *               for bit, or NULL.  Not weight itself.
- *   workspace   device scratch of omnitide_evict_plan_workspace_bytes() bytes (may be 0, then NULL)
+ *   workspace   device scratch of omnitide_evict_plan_workspace_bytes() bytes (may be 0, then NULL), whose
+ *               number never falls as n_seq or max_ctx grows
  * 0 <= sink, 0 <= recent, sink + recent <= budget <= high, 1 <= budget, high <= 2^24, max_ctx <= 2^24,
  * n_seq <= 65535.
  */

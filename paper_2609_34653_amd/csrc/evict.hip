@@ -16,6 +16,8 @@
 // rows, of 72 items, 44 us in place of 34: 129 MB, 3.8 TB/s).  Pages and angles are worked
 // out a row per lane and a pair per lane; keys go as two runs of four so that both members of a rotated pair sit in
 // one lane.
+#include <algorithm>
+
 #include "common.h"
 #include "evict.h"
 #include "paged_rows.h"
@@ -26,10 +28,10 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
-constexpr int kPlanPer = 16;             // rows of a thread
-constexpr int kSlice = kPlanThreads * kPlanPer;
+constexpr int kMaxPer = 16;              // rows of a thread at most; a slice is kPlanThreads * PER rows
 constexpr int kDigits = 2 * kPlanThreads;
-constexpr int kMaxSlices = 1024;         // of 2^24 rows
+constexpr int kMaxSlices = 1024;         // of 2^24 rows, 16 a thread
+constexpr int kFewSlices = 32;           // slices of a sequence that fewer rows a thread are taken for
 
 // Orders like the weight: NaN lowest, -0 as 0.
 __device__ inline uint32_t weight_key(float w) {
@@ -51,19 +53,20 @@ __device__ inline PlanSeq plan_seq(const EvictPlanArgs& a, int s) {
   return {a.weight + s * a.weight_stride, n <= a.max_ctx ? n : -1, a.budget - a.sink - a.recent};
 }
 
-// A workgroup's slice of a sequence: row(i) = first + 64 i, 16 of each lane, so that a wave's rows are 1,024 in a
-// row.
+// A workgroup's slice of a sequence: row(i) = first + 64 i, PER of each lane, so that a wave's rows are next to each
+// other.
+template <int PER>
 struct Slice {
   int first, n, mid0, mid1;              // rows [mid0, mid1) are chosen from
-  float x[kPlanPer];
+  float x[PER];
   __device__ void load(const EvictPlanArgs& a, const PlanSeq& q, int slice) {
-    first = slice * kSlice + static_cast<int>(threadIdx.x / kWave) * (kPlanPer * kWave) +
+    first = (slice * kPlanThreads + static_cast<int>(threadIdx.x / kWave) * kWave) * PER +
             static_cast<int>(threadIdx.x % kWave);
     n = q.n;
     mid0 = a.sink;
     mid1 = q.n - a.recent;
 #pragma unroll
-    for (int i = 0; i < kPlanPer; ++i) x[i] = row(i) < n ? q.w[row(i)] : 0.f;
+    for (int i = 0; i < PER; ++i) x[i] = row(i) < n ? q.w[row(i)] : 0.f;
   }
   __device__ int row(int i) const { return first + i * kWave; }
   __device__ bool middle(int i) const { return row(i) >= mid0 && row(i) < mid1; }
@@ -110,7 +113,8 @@ __device__ inline uint32_t find_digit(PlanMem& m, uint32_t& left) {
 
 // The kept rows of a slice to their places: those above the key `last` and the first `left` of those that equal
 // it; above0 and equal0 are in the slices in front.
-__device__ inline void place_rows(const EvictPlanArgs& a, int s, const Slice& sl, uint32_t last, uint32_t left,
+template <int PER>
+__device__ inline void place_rows(const EvictPlanArgs& a, int s, const Slice<PER>& sl, uint32_t last, uint32_t left,
                                   uint32_t above0, uint32_t equal0, PlanMem& m) {
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -122,14 +126,14 @@ __device__ inline void place_rows(const EvictPlanArgs& a, int s, const Slice& sl
   };
   if (sl.n <= a.high) {
 #pragma unroll
-    for (int i = 0; i < kPlanPer; ++i)
+    for (int i = 0; i < PER; ++i)
       if (sl.row(i) < sl.n) keep(i, sl.row(i));
     return;
   }
-  uint64_t above[kPlanPer], equal[kPlanPer];
+  uint64_t above[PER], equal[PER];
   uint32_t na = 0, ne = 0;
 #pragma unroll
-  for (int i = 0; i < kPlanPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const uint32_t key = weight_key(sl.x[i]);
     above[i] = __ballot(sl.middle(i) && key > last);
     equal[i] = __ballot(sl.middle(i) && key == last);
@@ -147,7 +151,7 @@ __device__ inline void place_rows(const EvictPlanArgs& a, int s, const Slice& sl
   }
   const uint64_t below = (1ull << lane) - 1;
 #pragma unroll
-  for (int i = 0; i < kPlanPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const uint32_t fa = pa + __popcll(above[i] & below), fe = pe + __popcll(equal[i] & below);
     const bool ab = (above[i] >> lane) & 1, eq = (equal[i] >> lane) & 1;
     const int row = sl.row(i);
@@ -162,6 +166,7 @@ __device__ inline void place_rows(const EvictPlanArgs& a, int s, const Slice& sl
 }
 
 // Sequences of one slice at most.
+template <int PER>
 __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(const EvictPlanArgs a) {
   __shared__ PlanMem m;
   const int s = blockIdx.x;
@@ -173,7 +178,7 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(const EvictPla
     }
     return;
   }
-  Slice sl;
+  Slice<PER> sl;
   sl.load(a, q, 0);
   if (threadIdx.x == 0) a.new_len[s] = q.n <= a.high ? q.n : a.budget;
   uint32_t last = 0xffffffffu, left = static_cast<uint32_t>(q.k);   // (no key is that large)
@@ -183,7 +188,7 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(const EvictPla
     for (int d = 0; d < 3; ++d) {
       clear_counts(m);
 #pragma unroll
-      for (int i = 0; i < kPlanPer; ++i) {
+      for (int i = 0; i < PER; ++i) {
         const uint32_t key = weight_key(sl.x[i]);
         if (sl.middle(i) && (key & mask) == prefix)
           atomicAdd(&m.hist[(key >> digit_shift(d)) & digit_bits(d)], 1u);
@@ -200,13 +205,14 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(const EvictPla
 // kept and how many of those that equal it.
 struct PlanWork {
   uint32_t* hist;                        // [sequence][slice][kDigits]
-  uint32_t* keys;                        // [sequence][slice][kSlice]: keys of the digit that is cut
+  uint32_t* keys;                        // [sequence][slice][rows of a slice]: keys of the digit that is cut
   uint4* sums;                           // [sequence][slice]: above that digit, keys put aside; then: above the
                                          //   last key kept and equal to it, in the slices in front
   uint4* cut;                            // [sequence]: the first digit, what is left of k; then last key, left
-  int slices;
+  int slices, slice;                     // of a sequence at most; rows of one
 };
 
+template <int PER>
 __global__ __launch_bounds__(kPlanThreads) void evict_count_kernel(const EvictPlanArgs a, const PlanWork ws) {
   __shared__ PlanMem m;
   const int s = blockIdx.y, slice = blockIdx.x;
@@ -215,12 +221,12 @@ __global__ __launch_bounds__(kPlanThreads) void evict_count_kernel(const EvictPl
     a.new_len[s] = q.n < 0 ? 0 : q.n <= a.high ? q.n : a.budget;
     if (q.n < 0) set_status(a.d_status, OMNITIDE_E_CAPACITY);
   }
-  if (q.n <= a.high || q.k == 0 || slice * kSlice >= q.n) return;
-  Slice sl;
+  if (q.n <= a.high || q.k == 0 || slice * (kPlanThreads * PER) >= q.n) return;
+  Slice<PER> sl;
   sl.load(a, q, slice);
   clear_counts(m);
 #pragma unroll
-  for (int i = 0; i < kPlanPer; ++i)
+  for (int i = 0; i < PER; ++i)
     if (sl.middle(i)) atomicAdd(&m.hist[weight_key(sl.x[i]) >> digit_shift(0)], 1u);
   __syncthreads();
   uint32_t* h = ws.hist + (static_cast<size_t>(s) * ws.slices + slice) * kDigits;
@@ -228,16 +234,17 @@ __global__ __launch_bounds__(kPlanThreads) void evict_count_kernel(const EvictPl
   h[threadIdx.x + kPlanThreads] = m.hist[threadIdx.x + kPlanThreads];
 }
 
+template <int PER>
 __global__ __launch_bounds__(kPlanThreads) void evict_aside_kernel(const EvictPlanArgs a, const PlanWork ws) {
   constexpr int kFlight = 8;
   __shared__ PlanMem m;
   const int s = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x;
   const PlanSeq q = plan_seq(a, s);
-  if (q.n <= a.high || q.k == 0 || slice * kSlice >= q.n) return;
-  Slice sl;
+  if (q.n <= a.high || q.k == 0 || slice * (kPlanThreads * PER) >= q.n) return;
+  Slice<PER> sl;
   sl.load(a, q, slice);
   // every slice adds the counts of all up and finds the digit
-  const int slices = (q.n + kSlice - 1) / kSlice;
+  const int slices = (q.n + ws.slice - 1) / ws.slice;
   const uint2* h = reinterpret_cast<const uint2*>(ws.hist + static_cast<size_t>(s) * ws.slices * kDigits) +
                    (kPlanThreads - 1 - tid);
   uint2 c = make_uint2(0, 0);
@@ -255,10 +262,10 @@ __global__ __launch_bounds__(kPlanThreads) void evict_aside_kernel(const EvictPl
   if (tid == 0) m.count = 0;
   uint32_t left = static_cast<uint32_t>(q.k);
   const uint32_t digit = find_digit(m, c.y, c.x, left);
-  uint32_t* keys = ws.keys + (static_cast<size_t>(s) * ws.slices + slice) * kSlice;
+  uint32_t* keys = ws.keys + (static_cast<size_t>(s) * ws.slices + slice) * ws.slice;
   uint32_t above = 0;
 #pragma unroll
-  for (int i = 0; i < kPlanPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const uint32_t key = weight_key(sl.x[i]), d = key >> digit_shift(0);
     if (!sl.middle(i)) continue;
     above += d > digit ? 1 : 0;
@@ -278,31 +285,47 @@ __global__ __launch_bounds__(kPlanThreads) void evict_cut_kernel(const EvictPlan
   const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const PlanSeq q = plan_seq(a, s);
   if (q.n <= a.high || q.k == 0) return;
-  const int slices = (q.n + kSlice - 1) / kSlice;
+  const int slices = (q.n + ws.slice - 1) / ws.slice;
   const uint4 cut = ws.cut[s];
   uint4* mine = ws.sums + static_cast<size_t>(s) * ws.slices;
-  const uint32_t* keys = ws.keys + static_cast<size_t>(s) * ws.slices * kSlice;
+  const uint32_t* keys = ws.keys + static_cast<size_t>(s) * ws.slices * ws.slice;
   if (tid < slices) sums[tid] = mine[tid];
   uint32_t prefix = cut.x << digit_shift(0), mask = digit_bits(0) << digit_shift(0), left = cut.y;
+  // a wave takes every 16th slice, eight loads of a lane on their way at once; f(key) for each key put aside
+  auto each = [&](int v, auto f) __attribute__((always_inline)) {
+    constexpr int kFlight = 8;
+    const uint32_t n = sums[v].y;
+    for (uint32_t i0 = lane; i0 < n; i0 += kFlight * kWave) {
+      uint32_t key[kFlight];
+#pragma unroll
+      for (int i = 0; i < kFlight; ++i)
+        key[i] = keys[static_cast<size_t>(v) * ws.slice + min(i0 + i * kWave, n - 1)];
+#pragma unroll
+      for (int i = 0; i < kFlight; ++i)
+        if (i0 + i * kWave < n) f(key[i]);
+    }
+  };
 #pragma unroll
   for (int d = 1; d < 3; ++d) {
     clear_counts(m);
-    for (int v = 0; v < slices; ++v)
-      for (uint32_t i = tid; i < sums[v].y; i += kPlanThreads) {
-        const uint32_t key = keys[static_cast<size_t>(v) * kSlice + i];
+    for (int v = wave; v < slices; v += kPlanWaves)
+      each(v, [&](uint32_t key) {
         if ((key & mask) == prefix) atomicAdd(&m.hist[(key >> digit_shift(d)) & digit_bits(d)], 1u);
-      }
+      });
     prefix |= find_digit(m, left) << digit_shift(d);
     mask |= digit_bits(d) << digit_shift(d);
   }
   // a wave counts a slice's keys above the last one and equal to it
   for (int v = wave; v < slices; v += kPlanWaves) {
     uint32_t na = 0, ne = 0;
-    const uint32_t n = sums[v].y;
-    for (uint32_t i = 0; i < n; i += kWave) {
-      const uint32_t key = i + lane < n ? keys[static_cast<size_t>(v) * kSlice + i + lane] : 0;
-      na += __popcll(__ballot(i + lane < n && key > prefix));
-      ne += __popcll(__ballot(i + lane < n && key == prefix));
+    each(v, [&](uint32_t key) {
+      na += key > prefix ? 1 : 0;
+      ne += key == prefix ? 1 : 0;
+    });
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      na += __shfl_xor(na, o, kWave);
+      ne += __shfl_xor(ne, o, kWave);
     }
     if (lane == 0) {
       sums[v].z = sums[v].x + na;
@@ -319,12 +342,13 @@ __global__ __launch_bounds__(kPlanThreads) void evict_cut_kernel(const EvictPlan
   if (tid == 0) ws.cut[s] = make_uint4(prefix, left, 0, 0);
 }
 
+template <int PER>
 __global__ __launch_bounds__(kPlanThreads) void evict_place_kernel(const EvictPlanArgs a, const PlanWork ws) {
   __shared__ PlanMem m;
   const int s = blockIdx.y, slice = blockIdx.x;
   const PlanSeq q = plan_seq(a, s);
-  if (q.n < 0 || slice * kSlice >= q.n) return;
-  Slice sl;
+  if (q.n < 0 || slice * (kPlanThreads * PER) >= q.n) return;
+  Slice<PER> sl;
   sl.load(a, q, slice);
   uint4 cut = make_uint4(0xffffffffu, 0, 0, 0), front = make_uint4(0, 0, 0, 0);
   if (q.n > a.high && q.k > 0) {
@@ -478,45 +502,71 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
 
 struct PlanLayout {
   size_t keys, sums, cut, bytes;
-  int slices;
+  int per, slices;
 };
 PlanLayout plan_layout(int n_seq, int max_ctx) {
   PlanLayout l{};
-  l.slices = (max_ctx + kSlice - 1) / kSlice;
+  // one workgroup for a sequence if it holds it, with as few rows a thread as do (8,192 rows: 9.5 us, 14.4 us with
+  // 16 a thread); otherwise few rows a thread while the slices are few (81,920 rows: 4.5 us for the places of
+  // 20 slices, 10 us of 5), as every one of them adds up the counts of all
+  l.per = 4;
+  while (l.per < kMaxPer && max_ctx > kPlanThreads * l.per * (max_ctx > kPlanThreads * kMaxPer ? kFewSlices : 1))
+    l.per *= 2;
+  const int rows = kPlanThreads * l.per;
+  l.slices = (max_ctx + rows - 1) / rows;
   if (l.slices == 1) return l;
   const size_t n = static_cast<size_t>(n_seq) * l.slices;
   l.keys = n * kDigits * sizeof(uint32_t);
-  l.sums = l.keys + n * kSlice * sizeof(uint32_t);
+  l.sums = l.keys + n * rows * sizeof(uint32_t);
   l.cut = l.sums + n * sizeof(uint4);
   l.bytes = l.cut + n_seq * sizeof(uint4);
   return l;
 }
 
-}  // namespace
-
-size_t evict_plan_workspace_bytes(int n_seq, int max_ctx) { return plan_layout(n_seq, max_ctx).bytes; }
-
-hipError_t launch_evict_plan(const EvictPlanArgs& a, hipStream_t stream) {
-  const PlanLayout l = plan_layout(a.n_seq, a.max_ctx);
+template <int PER>
+hipError_t launch_plan(const EvictPlanArgs& a, const PlanLayout& l, hipStream_t stream) {
   if (l.slices == 1) {
-    hipLaunchKernelGGL(evict_plan_kernel, dim3(a.n_seq), dim3(kPlanThreads), 0, stream, a);
+    hipLaunchKernelGGL(evict_plan_kernel<PER>, dim3(a.n_seq), dim3(kPlanThreads), 0, stream, a);
     return hipGetLastError();
   }
   uint8_t* base = static_cast<uint8_t*>(a.workspace);
-  const PlanWork ws{reinterpret_cast<uint32_t*>(base), reinterpret_cast<uint32_t*>(base + l.keys),
-                    reinterpret_cast<uint4*>(base + l.sums), reinterpret_cast<uint4*>(base + l.cut), l.slices};
+  const PlanWork ws{reinterpret_cast<uint32_t*>(base),
+                    reinterpret_cast<uint32_t*>(base + l.keys),
+                    reinterpret_cast<uint4*>(base + l.sums),
+                    reinterpret_cast<uint4*>(base + l.cut),
+                    l.slices,
+                    kPlanThreads * PER};
   const dim3 grid(l.slices, a.n_seq), block(kPlanThreads);
-  hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, stream, a, ws);
+  hipLaunchKernelGGL(evict_count_kernel<PER>, grid, block, 0, stream, a, ws);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(evict_aside_kernel, grid, block, 0, stream, a, ws);
+  hipLaunchKernelGGL(evict_aside_kernel<PER>, grid, block, 0, stream, a, ws);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(evict_cut_kernel, dim3(a.n_seq), block, 0, stream, a, ws);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(evict_place_kernel, grid, block, 0, stream, a, ws);
+  hipLaunchKernelGGL(evict_place_kernel<PER>, grid, block, 0, stream, a, ws);
   return hipGetLastError();
+}
+
+}  // namespace
+
+// (of no shorter sequences more)
+size_t evict_plan_workspace_bytes(int n_seq, int max_ctx) {
+  size_t bytes = plan_layout(n_seq, max_ctx).bytes;
+  for (int per = 4; per < kMaxPer; per *= 2)
+    bytes = std::max(bytes, plan_layout(n_seq, std::min(max_ctx, kPlanThreads * per * kFewSlices)).bytes);
+  return bytes;
+}
+
+hipError_t launch_evict_plan(const EvictPlanArgs& a, hipStream_t stream) {
+  const PlanLayout l = plan_layout(a.n_seq, a.max_ctx);
+  switch (l.per) {
+    case 4: return launch_plan<4>(a, l, stream);
+    case 8: return launch_plan<8>(a, l, stream);
+    default: return launch_plan<kMaxPer>(a, l, stream);
+  }
 }
 
 hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream) {
@@ -530,7 +580,7 @@ hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream) {
   items.by_per = ((1u << 20) + items.per - 1) / items.per;
   items.by_head = ((1u << 20) + items.per_head - 1) / items.per_head;
   const int64_t blocks = (rows + items.rows - 1) / items.rows;
-  const int64_t gx = min(blocks, static_cast<int64_t>(kMoveGrid));
+  const int64_t gx = std::min(blocks, static_cast<int64_t>(kMoveGrid));
   const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>(a.batch.n_seq),
                   static_cast<unsigned>((blocks + gx - 1) / gx));
   if (a.rope_dims == 0)

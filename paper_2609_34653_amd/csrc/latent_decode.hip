@@ -85,6 +85,9 @@ __device__ inline int swz(int key) {
   return ((key >> 1) & 1) << 2 | ((key >> 4) & 1) << 1 | ((key >> 2) & 1);
 }
 
+// Rows of a part, of a call of M vectors per sequence.
+__host__ __device__ inline int part_rows(int M) { return M <= kRow ? kRow : kGroup; }
+
 // NS: sequences per lane of the plan.
 template <int R, int NS>
 __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(
@@ -470,7 +473,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(
     float den = hf == 0 ? l_half + sx[wave ^ 1][col] : sx[wave ^ 1][col] + l_half;
     if (slim[vt * kRow + col] >= bad_row) den = __builtin_nanf("");
     const float by = den == 0.f ? 0.f : 1.f / den;
-    const size_t row = static_cast<size_t>(slot) * kGroup + vt * kRow + col;
+    const size_t row = static_cast<size_t>(slot) * part_rows(M) + vt * kRow + col;
     const size_t at = (static_cast<size_t>(seq) * M + m) * R;
     if (row_ok) {
       if (!whole && hf == 0 && h == 0) part_ml[row] = make_float2(den == den ? m_run : 0.f, den);
@@ -532,7 +535,7 @@ __global__ __launch_bounds__(kMergeThreads) void latent_decode_merge_kernel(
       const int p = p0 + c * TS;
       const bool in = p < n_parts;
       const size_t row =
-          static_cast<size_t>(2 * ((w0 + p) * row_groups + rg) + (p == 0 ? 1 : 0)) * kGroup + r;
+          static_cast<size_t>(2 * ((w0 + p) * row_groups + rg) + (p == 0 ? 1 : 0)) * part_rows(M) + r;
       ml[c] = in ? part_ml[row] : make_float2(-INFINITY, 0.f);
       ov[c] = in ? *reinterpret_cast<const floatx4*>(part_o + row * R + d) : floatx4{0.f, 0.f, 0.f, 0.f};
     }
@@ -563,7 +566,8 @@ hipError_t launch_t(const LatentDecodeArgs& a, hipStream_t stream) {
   const PagedBatch& b = a.batch;
   const int groups = groups_of(b.n_q * a.n_heads), wgs = shares_of(groups) * groups;
   float2* part_ml = static_cast<float2*>(a.workspace);
-  float* part_o = reinterpret_cast<float*>(part_ml + static_cast<size_t>(2 * wgs) * kGroup);
+  float* part_o =
+      reinterpret_cast<float*>(part_ml + static_cast<size_t>(2 * wgs) * part_rows(b.n_q * a.n_heads));
   const float scale_log2 = a.scale * 1.4426950408889634f;
   hipLaunchKernelGGL((latent_decode_kernel<R, NS>), dim3(wgs), dim3(kThreads), 0, stream,
                      static_cast<const uint16_t*>(a.q), static_cast<const uint16_t*>(a.pool), b, a.n_heads,
@@ -589,7 +593,7 @@ hipError_t launch_r(const LatentDecodeArgs& a, hipStream_t stream) {
 
 size_t latent_decode_workspace_bytes(int n_q, int n_heads, int latent_dim) {
   const int groups = groups_of(n_q * n_heads);
-  const size_t rows = static_cast<size_t>(2 * shares_of(groups) * groups) * kGroup;
+  const size_t rows = static_cast<size_t>(2 * shares_of(groups) * groups) * part_rows(n_q * n_heads);
   return rows * (static_cast<size_t>(latent_dim) + 2) * sizeof(float);
 }
 

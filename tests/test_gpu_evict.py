@@ -304,6 +304,22 @@ def test_plan(case, kind):
         assert (wo[s, len(keep):] == -9.0).all()
 
 
+@pytest.mark.parametrize("kind", ["exp", "equal", "near"])
+@pytest.mark.parametrize("cap", [4096, 4097, 8192, 8193, 16384, 16385, 131072, 131073, 262145, 700000])
+def test_plan_at_the_ends_of_slices(cap, kind):
+    """Lengths around those that change how a sequence is cut: to the last row, one less, and a short one."""
+    ctx, budget = [cap, cap - 1, 100], cap // 3
+    w = some_weights(kind, len(ctx), cap, cap)
+    src, new, wo, st = run_plan(w.cuda(), ctx, budget + 9, budget, 5, 70)
+    assert st == 0 and list(new) == [budget, budget, 100]
+    host = w.numpy()
+    for s, n in enumerate(ctx):
+        keep = oe.plan(host[s, :n].tolist(), budget + 9, budget, 5, 70)
+        assert np.array_equal(src[s, :len(keep)], keep)
+        assert np.array_equal(wo[s, :len(keep)].view(np.int32), host[s, keep].view(np.int32))
+        assert (src[s, len(keep):] == -9).all() and (wo[s, len(keep):] == -9.0).all()
+
+
 def test_plan_lengths_refused_on_the_device():
     from paper_2609_34653_amd import omnitide as ot
     w = rand(1, 4, 100).exp().cuda()

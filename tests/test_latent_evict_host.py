@@ -214,6 +214,16 @@ def move(L, **kw):
     return L.omnitide_paged_compact(*a.values(), None)
 
 
+def test_plan_workspace_never_falls():
+    from paper_2609_34653_amd import evict as ev
+    sizes = [1, 100, 4096, 4097, 8192, 16384, 16385, 70000, 131072, 131073, 140000, 262144, 262145, 300000,
+             1 << 20, 1 << 24]
+    for n_seq in (1, 3, 200):
+        got = [ev.omnitide_evict_plan_workspace_bytes(n_seq, n) for n in sizes]
+        assert got == sorted(got) and got[5] == 0 and got[6] > 0
+        assert got[-1] <= ev.omnitide_evict_plan_workspace_bytes(n_seq + 1, sizes[-1])
+
+
 def test_compact_refusals(L):
     for k in ("k", "tab", "ctx", "dst", "src", "new", "th"):
         assert move(L, **{k: None}) == ot.E_NULL, k
