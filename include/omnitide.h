@@ -13,7 +13,8 @@
  * attention of the last few tokens over the compacted pool); omnitide_evict_native,
  * omnitide_pack_suffix, omnitide_place_chunk and omnitide_span_attn keep the native (logical-only)
  * layout with holes instead.  omnitide_paged.h declares the calls over a paged cache that streams
- * of different lengths share.
+ * of different lengths share, omnitide_latent.h those over a latent cache on such pages, and
+ * omnitide_evict.h eviction from both by attention weight.
  *
  * Conventions shared by every entry point
  *   - Array arguments are DEVICE pointers into memory the caller allocated (hipMalloc or a

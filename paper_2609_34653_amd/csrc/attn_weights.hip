@@ -14,6 +14,11 @@
 //             chunk of the keys, the second as 256 keys of a KV head and up to kRowChunk query rows; 512 workgroups
 //             take them in turn, two on a CU, so that one's vector work hides what the other waits for.
 //   sums      no atomics: every item owns its place in a buffer of partial sums, added in a fixed order.
+//   measured  665 tokens of 32 heads over 17,048 keys of 8 x 128: 139 us and 143 us for the passes (91 GFLOP each), 5
+//             and 9 us for the other two kernels.  Matrix cores busy 0.41 and 0.36, vector units 0.64 and 0.61: what
+//             one waits for, the other does, most of the time.  In the first pass the products of the next keys
+//             stand between the exponentials of these (whole row tiles in turn, without: 170 us); in the second
+//             that takes the registers that a second workgroup of the CU needs (191 us and more).
 #include <type_traits>
 
 #include "common.h"

@@ -5,9 +5,10 @@
 // the k-th largest is found digit by digit (11, 11 and 10 bits: counts of each value among the rows that agree
 // in the digits before), then every row's place follows from the kept ones in front of it: the larger ones
 // plus the equal ones, as many of those as there is room for.  Bound by latency: 4 bytes a row, and a
-// dependent pass over them per digit.  So a workgroup holds up to 16,384 rows in registers, 16 a thread, and
+// dependent pass over them per digit.  So a workgroup holds up to 16,384 rows in registers, 4 to 16 a thread, and
 // reads them once; longer sequences are cut into such slices in four launches: a slice's counts of the first
-// digit; the rows of that digit, put aside; the last two digits among those; the places.
+// digit; the rows of that digit, put aside; the last two digits among those; the places.  24 sequences of up to
+// 8,192 rows: 9.6 us; one of 81,920: 4 + 7 + 8 + 5 us.
 //
 // The move is a copy: each kept row is read and written once, behind a chain of four loads (length, row, page,
 // values).  So a workgroup takes only as many rows as its threads hold in two items of eight values each, and

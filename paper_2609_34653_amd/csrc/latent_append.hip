@@ -8,7 +8,9 @@
 // Bound by memory (each value read and written once).  A token's work is dealt to waves: one norms the
 // latent (4 values per lane at a time, coalesced), the others turn the parts, eight heads of eight
 // lanes each per group (the key part is the first head), both members of a pair in one lane.  A lane's place in
-// its head is the same in every group, so it reads the four (cos, sin) it needs once.
+// its head is the same in every group, so it reads the four (cos, sin) it needs once.  33,083 float32 tokens with 32
+// heads: 106 us (521 MB, 4.9 TB/s; a large copy reaches 5.3); one token of each of 24 streams: 4.4 us, a launch and
+// three dependent loads.
 #include "common.h"
 #include "latent.h"
 #include "paged_rows.h"
@@ -186,7 +188,8 @@ hipError_t launch_i(const LatentAppendArgs& a, int groups, hipStream_t stream) {
 template <int R, bool IN32>
 hipError_t launch_t(const LatentAppendArgs& a, hipStream_t stream) {
   const int groups = (1 + a.n_heads + HPW - 1) / HPW;
-  // one group per wave while every wave finds a slot of the chip at once, four beyond, as in norm_rope.hip
+  // one group per wave while every wave finds a slot of the chip at once (24 tokens of 16 heads: 4.4 us, 4.8 with four
+  // groups), four beyond (33,083 tokens of 32: 106 us, 114 with one)
   if (static_cast<int64_t>(a.batch.n_tokens) * (1 + groups) <= kWaveSlots)
     return launch_i<R, IN32, 1>(a, groups, stream);
   return launch_i<R, IN32, 4>(a, groups, stream);

@@ -9,7 +9,9 @@
 // the next and the value products of the last).  What differs: a key's scores take (d + 64) / 16 products of
 // 32 keys, its values d / 16, so a step has slots with one product and slots with two; rows are contiguous in
 // the caller's tensors, at strides of their own; the wider keys leave LDS for rings of three tiles (K 24 KB,
-// V 16 KB for d = 128), asked for one tile ahead.
+// V 16 KB for d = 128), asked for one tile ahead.  665 tokens over 17,048 keys, 16 heads of 128: 128 us and 8 us for
+// the merge (114 GFLOP, 0.89 PFLOP/s; matrix cores busy 0.49, as in paged_chunk.hip, at the clock that power
+// allows); 89 over 601, 4 heads of 64: 9.2 and 3 us, latency.
 #include <type_traits>
 
 #include "chunk_plan.h"

@@ -27,7 +27,11 @@
 //             as if they were the step behind the first.
 //   products  S^T (32 keys x 32 vectors) = K Q^T and O^T (32 dims x 32 vectors) = C^T P^T with
 //             v_mfma_f32_32x32x16_bf16; keys are permuted when K rows are read so that S^T is the operand of
-//             the second product as it stands.
+//             the second product as it stands.  Probabilities are rounded to bf16 for it, and summed as rounded.
+//   measured  24 x 128 vectors over 119,095 rows of 576 in all: 53 us and 10 us for the merge (33 GFLOP, matrix cores
+//             busy 0.33; 2.5 us for a step of 64 keys, of which the products take 1.1; the start of a part takes 5
+//             us and its end 4, which writes 37 MB).  16 vectors per wave, with all of the dimensions, took 71 us.
+//             16 vectors over 16,948 rows: 14.5 and 7 us, all of it latency (pages, first keys, two steps, parts).
 #include "common.h"
 #include "latent.h"
 #include "mfma_tile.h"
@@ -40,7 +44,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kRow = 32;                 // vectors of a tile
 constexpr int kGroup = 2 * kRow;         // of a workgroup
-constexpr int kOverhead = 10;            // what a sequence costs beside its blocks, in blocks
+constexpr int kOverhead = 10;            // what a sequence costs beside its blocks, in blocks (24 x 128 vectors: 59 us
+                                         //   with 4, 55 with 6, 52 to 53 with 9 to 12, 54 with 16)
 constexpr int kKT = 32;                  // keys per tile and block
 constexpr int kStep = 2;                 // tiles per step
 constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
@@ -553,7 +558,8 @@ __global__ __launch_bounds__(kMergeThreads) void latent_decode_merge_kernel(
 }
 
 // Vectors from which on a merge workgroup takes all dims of one: there are enough of them, of few parts each (24
-// x 128 vectors: 24 us by quarters, 16 whole), and few have many (16 of 134 parts: 7 and 23).
+// x 128 vectors: 18.8 us by quarters, 10.1 whole; 24 x 32: 8.5 and 7.2), and few have many (16 of 134 parts: 7.0
+// and 16.1; 24 x 16 of 6: 5.9 and 6.5).
 constexpr int kWideVecs = 512;
 
 // Shares of a row group: whole rounds over the XCDs.
