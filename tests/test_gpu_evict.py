@@ -501,6 +501,30 @@ def test_compact_refused_on_the_device(what):
     assert torch.equal(gk.cpu(), want)
 
 
+@pytest.mark.parametrize("m", [2, 60])
+def test_pages_beyond_four_gib(m):
+    """Weights and move on the last pages of a large pool: the bits of a small one."""
+    from paper_2609_34653_amd import evict as ev, paged as pg
+    ctx, kept, P, H, d = [200, 90], [150, 90], 32, 4, 128
+    src_t, dst_t, n_pages = tables(ctx, kept, P, 3)
+    small = torch.nan_to_num(key_pool(ctx, src_t, n_pages, P, H, d, 1), posinf=1.0).cuda()
+    n = (7 << 30) // (P * H * d * 2)
+    large = torch.zeros(n, P, H, d, dtype=BF, device="cuda")
+    large[n - n_pages:] = small
+    q = rand(2, 2 * m, 8, d).to(BF).cuda()
+    src = np.stack([np.arange(150) + 50 * (np.arange(150) > 80), np.arange(150)])
+    th = pg.omnitide_rope_thetas(1.0e4, d)
+    got = []
+    for pool, up in ((small, 0), (large, n - n_pages)):
+        w, st = weights(q, pool, src_t + up, [0, m, 2 * m], ctx, m, 0.09)
+        assert st == 0
+        ev.omnitide_paged_compact(pool, pool.clone(), i32(src_t + up), i32(ctx), i32(dst_t + up), i32(src),
+                                  i32(kept), theta=th)
+        torch.cuda.synchronize()
+        got.append((w, pool[up:].clone()))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
 # --------------------------------------------------------------------------------- together
 
 def evict_step(pool, v_pool, table, dst, ctx, w, high, budget, sink, recent, th, offset, style=0):

@@ -334,6 +334,67 @@ def test_decode_large_and_equal_scores(H, rise):
     near(got[0], want, spread, 2.0 ** -10, F32)
 
 
+@pytest.mark.parametrize("H", [3, 16, 33, 64, 80])
+def test_decode_reference_moves_in_any_step(H):
+    """Parts of several steps whose scores rise and fall by 30 per 32 keys, the other way for every other head: all
+    sums are exact (multiples of 2^-5 below 2^11), rows of one score differ in pairs of dimensions."""
+    S, n, R, P = 40, 1500, 256, 32
+    ctx = [n - 7 * s for s in range(S)]
+    table, n_pages = layout(ctx, P, 1)
+    pool = pool_of(ctx, table, n_pages, P, R + E, 3)
+    rng = np.random.default_rng(5)
+    q = torch.full((S, 1, H, R + E), 0.5, dtype=BF)
+    q[:, :, 1::2] = -0.5
+    for s in range(S):
+        r = np.arange(ctx[s])
+        level = rng.permutation(47)[r // 32] if s % 2 else r // 32
+        x = np.repeat((level * 3 / 16)[:, None], R + E, 1)
+        sign = rng.integers(-1, 2, ctx[s])[:, None] / 16
+        x[:, ::2] += sign
+        x[:, 1::2] -= sign
+        pool[table[s, r // P], r % P] = torch.from_numpy(x).to(BF)
+    got, st = decode(q.cuda(), pool.cuda(), table, ctx, 1.0, F32)
+    assert st == 0
+    for s in range(S):
+        r = np.arange(ctx[s])
+        rows = pool[table[s, r // P], r % P].double().numpy()
+        want, spread = ol.absorbed_attention(f64(q[s]), rows, R, 1.0)
+        near(got[s], want, spread, 2.0 ** -10, F32)
+
+
+def far_pool(table, small, used):
+    """A pool of 7 GiB with the pages of `small` that `table` names at its end: the pool and its table."""
+    P, W = small.shape[1:3]
+    n = (7 << 30) // (P * small[0, 0].numel() * 2)
+    pool = torch.empty((n, *small.shape[1:]), dtype=BF, device="cuda")
+    shift = n - small.shape[0]
+    pool[shift:] = small
+    return pool, np.where(table >= 0, table + shift, table)
+
+
+def test_pages_beyond_four_gib():
+    """Each call on the last pages of a large pool gives the bits that it gives on a small one."""
+    from paper_2609_34653_amd import latent as la, paged as pg
+    ctx, new, P, R, H = [300, 77], [40, 1], 16, 512, 40
+    table, n_pages = layout(ctx, P, 3)
+    small = pool_of(ctx, table, n_pages, P, R + E, 1).cuda()
+    large, far = far_pool(table, small, ctx)
+    assert large.numel() * 2 > 7 * 10 ** 9
+    T, th = sum(new), pg.omnitide_rope_thetas(1.0e4, E)
+    c, e, q = rand(1, T, R).to(BF).cuda(), rand(2, T, E).to(BF).cuda(), queries(3, 2, 1, H, R).cuda()
+    got = []
+    for pool, tab in ((small, table), (large, far)):
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        la.omnitide_latent_append(c, e, pool, i32(tab), i32([0, 40, 41]), i32(ctx), theta=th, d_status=st)
+        out = torch.zeros(sum(ctx), R + E, dtype=BF, device="cuda")
+        la.omnitide_paged_rows(pool, i32(tab), i32([0, 300, 377]), i32(ctx), out, d_status=st)
+        dec, code = decode(q, pool, tab, ctx, SCALE, F32)
+        assert code == 0 and int(st.item()) == 0
+        got.append((out, dec))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert torch.isfinite(got[0][1]).all()
+
+
 @pytest.mark.parametrize("scale", [-0.05, 0.0])
 def test_decode_scales(scale):
     ctx, P, R = [300, 40], 16, 512
@@ -458,6 +519,22 @@ def test_chunk_tensors_of_their_own():
     b, st2 = chunk(q.cuda(), None, kr.cuda(), [0, m], [0, n], 0.1, F32,
                    split=(wide[..., 8:8 + d], kv[..., d:].contiguous().cuda()))
     assert st == 0 and st2 == 0 and torch.equal(a, b) and torch.isfinite(a).all()
+
+
+def test_chunk_rows_far_apart():
+    """The largest strides, 2^24 elements, so rows beyond 4 GiB: the bits of contiguous tensors."""
+    n, T, H, d = 150, 70, 2, 64
+    wide = torch.empty(n, 1 << 24, dtype=BF, device="cuda")
+    kv, kr = rand(1, n, H, 2 * d).to(BF).cuda(), rand(2, n, E).to(BF).cuda()
+    wide[:, :H * 2 * d] = kv.view(n, -1)
+    wide[:, -E:] = kr
+    q = rand(3, T, H, d + E).to(BF).cuda()
+    got = []
+    for x, r in ((kv, kr), (wide[:, :H * 2 * d].unflatten(1, (H, 2 * d)), wide[:, -E:])):
+        out, st = chunk(q, x, r, [0, T], [0, n], SCALE, F32)
+        assert st == 0
+        got.append(out)
+    assert torch.equal(got[0], got[1]) and torch.isfinite(got[0]).all()
 
 
 @pytest.mark.parametrize("rise", [True, False])
