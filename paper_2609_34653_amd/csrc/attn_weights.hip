@@ -569,10 +569,20 @@ __global__ __launch_bounds__(kSumThreads) void weights_add_kernel(const AttnWeig
   const int max_ctx = b.max_pages << b.page_shift;
   const int tile = j / kItemKeys;
   const int rc0 = first_row(tile * kItemKeys, kept, G) / kRowChunk, rc1 = (rows - 1) / kRowChunk;
+  // [row chunk][KV head], eight of them on their way at once
+  constexpr int kFlight = 8;
+  const int64_t first = static_cast<int64_t>(rc0) * a.n_kv_heads;
+  const int64_t last = (static_cast<int64_t>(rc1) + 1) * a.n_kv_heads - 1;
+  const size_t step = static_cast<size_t>(b.n_seq) * max_ctx;
+  const float* sums = ws.sums + static_cast<size_t>(s) * max_ctx + j;
   float sum = 0.f;
-  for (int rc = rc0; rc <= rc1; ++rc)
-    for (int g = 0; g < a.n_kv_heads; ++g)
-      sum += ws.sums[((static_cast<size_t>(rc) * a.n_kv_heads + g) * b.n_seq + s) * max_ctx + j];
+  for (int64_t i0 = first; i0 <= last; i0 += kFlight) {
+    float x[kFlight];
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) x[i] = sums[static_cast<size_t>(min(i0 + i, last)) * step];
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) sum += i0 + i <= last ? x[i] : 0.f;
+  }
   const size_t at = static_cast<size_t>(s) * a.weight_stride + j;
   if (a.weight_in != nullptr) {
     const int seen = a.seen_len != nullptr ? a.seen_len[s] : kept;
