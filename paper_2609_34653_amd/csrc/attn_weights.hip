@@ -11,11 +11,11 @@
 //             the second), the other streams through LDS tiles filled by direct loads; so the first pass
 //             has a row's statistics and the second a key's sum in the lanes that they belong to.
 //   items     the first pass is dealt out as 256 query rows of a KV head (tokens times its query heads) and a
-//             chunk of the keys, the second as 256 keys of a KV head and up to kRowChunk query rows; 512 workgroups
+//             chunk of the keys, the second as 256 keys of a KV head and up to 1,024 query rows; 512 workgroups
 //             take them in turn, two on a CU, so that one's vector work hides what the other waits for.
 //   sums      no atomics: every item owns its place in a buffer of partial sums, added in a fixed order.
 //   measured  665 tokens of 32 heads over 17,048 keys of 8 x 128: 139 us and 143 us for the passes (91 GFLOP each), 5
-//             and 9 us for the other two kernels.  Matrix cores busy 0.41 and 0.36, vector units 0.64 and 0.61: what
+//             us for each of the other two kernels.  Matrix cores busy 0.41 and 0.36, vector units 0.64 and 0.61: what
 //             one waits for, the other does, most of the time.  In the first pass the products of the next keys
 //             stand between the exponentials of these (whole row tiles in turn, without: 170 us); in the second
 //             that takes the registers that a second workgroup of the CU needs (191 us and more).
@@ -32,9 +32,11 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kRows = kWaves * 32;       // query rows of an item of the first pass
-constexpr int kMinKeys = 1024;           // its keys at least
+constexpr int kMinKeys = 256;            // its keys at least
+constexpr int kManyKeys = 1024;          // and at least where there are items enough
 constexpr int kMaxChunks = 16;           // chunks of the keys at most
-constexpr int kRowChunk = 1024;          // query rows of an item of the second pass
+constexpr int kRowChunk = 1024;          // query rows of an item of the second pass at most
+constexpr int kMinRowChunk = 128;        // and at least
 constexpr int kItemKeys = kWaves * 32;   // its keys
 constexpr int kItemWGs = 512;            // workgroups of a pass
 constexpr int kNumXcd = 8;
@@ -112,7 +114,7 @@ struct WeightsWork {
   float2* part;
   float2* stats;
   float* sums;                           // [row chunk][KV head][sequence][max_ctx]
-  int chunk_keys;
+  int chunk_keys, row_chunk;             // keys of an item of the first pass, query rows of one of the second
 };
 
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -431,7 +433,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void 
     const int4 q = ws.seqs[i];
     if (q.y == 0) return int64_t{0};
     return static_cast<int64_t>((q.z + kItemKeys - 1) / kItemKeys) * Hkv *
-           ((q.y * G + kRowChunk - 1) / kRowChunk);
+           ((q.y * G + ws.row_chunk - 1) / ws.row_chunk);
   });
 
   S st;
@@ -451,8 +453,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void 
     const int rest = uniform(static_cast<int>(local - static_cast<int64_t>(rc) * tiles * Hkv));
     const int tile = rest / Hkv, g = rest - tile * Hkv;
     const int key0 = tile * kItemKeys + wave * 32;         // this wave's keys
-    const int m_begin = max(rc * kRowChunk, first_row(tile * kItemKeys, kept, G));
-    const int m_end = min(rows, (rc + 1) * kRowChunk);
+    const int m_begin = max(rc * ws.row_chunk, first_row(tile * kItemKeys, kept, G));
+    const int m_end = min(rows, (rc + 1) * ws.row_chunk);
 
     if (m_begin < m_end) {                 // (otherwise no row of the chunk sees the keys: nothing is added)
       // this wave's keys, which stay in registers; keys past the context are its last one, and those of a bad
@@ -568,7 +570,7 @@ __global__ __launch_bounds__(kSumThreads) void weights_add_kernel(const AttnWeig
   const int G = a.n_q_heads / a.n_kv_heads, kept = q.z - q.y, rows = q.y * G;
   const int max_ctx = b.max_pages << b.page_shift;
   const int tile = j / kItemKeys;
-  const int rc0 = first_row(tile * kItemKeys, kept, G) / kRowChunk, rc1 = (rows - 1) / kRowChunk;
+  const int rc0 = first_row(tile * kItemKeys, kept, G) / ws.row_chunk, rc1 = (rows - 1) / ws.row_chunk;
   // [row chunk][KV head], eight of them on their way at once
   constexpr int kFlight = 8;
   const int64_t first = static_cast<int64_t>(rc0) * a.n_kv_heads;
@@ -595,22 +597,37 @@ size_t align16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
 
 struct Layout {
   size_t part, stats, sums, bytes;
-  int chunk_keys, row_chunks;
+  int chunk_keys, row_chunk;
 };
+// Items of both passes: large ones where there are many, smaller ones while all of them find a workgroup at once (300
+// tokens over 6,000 keys: 29 us for the first pass in chunks of 512 keys, 47 in chunks of 1,024 and 41 in chunks of
+// 384, which are more than 512; 100 over 3,000: 19 us with 256, 40 with 1,024).  What is worked out from max_ctx and
+// n_tokens is an upper bound, so short sequences in long tables have large items.
 Layout layout(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, int n_kv_heads) {
   Layout l;
-  // (the chunk grows in whole stages; chunks are as many as a longer call's at most)
-  const int keys = (max_ctx + kMaxChunks - 1) / kMaxChunks;
-  l.chunk_keys = keys <= kMinKeys ? kMinKeys : (keys + 63) / 64 * 64;
-  const int64_t rows = static_cast<int64_t>(max_q < n_tokens ? max_q : n_tokens) * (n_q_heads / n_kv_heads);
-  l.row_chunks = static_cast<int>((rows + kRowChunk - 1) / kRowChunk);
+  const int64_t G = n_q_heads / n_kv_heads;
+  const int64_t tiles = (n_tokens * G + kRows - 1) / kRows + (n_seq < n_tokens ? n_seq : n_tokens) - 1;
+  const int most = (max_ctx + kMinKeys - 1) / kMinKeys < kMaxChunks ? (max_ctx + kMinKeys - 1) / kMinKeys
+                                                                    : kMaxChunks;
+  int64_t chunks = kItemWGs / (tiles * n_kv_heads);
+  const int least = (max_ctx + kManyKeys - 1) / kManyKeys;
+  chunks = chunks < least ? least : chunks;
+  chunks = chunks > most ? most : chunks;
+  // (whole stages)
+  l.chunk_keys = static_cast<int>(((max_ctx + chunks - 1) / chunks + 63) / 64 * 64);
+  const int64_t rows = (max_q < n_tokens ? max_q : n_tokens) * G;
+  const int64_t key_items = static_cast<int64_t>((max_ctx + kItemKeys - 1) / kItemKeys) * n_kv_heads * n_seq;
+  auto row_chunks = [&](int64_t chunk) { return (rows + chunk - 1) / chunk; };
+  l.row_chunk = kRowChunk;
+  while (l.row_chunk > kMinRowChunk && key_items * row_chunks(l.row_chunk / 2) <= kItemWGs) l.row_chunk /= 2;
   const size_t vecs = static_cast<size_t>(n_tokens) * n_q_heads * sizeof(float2);
-  const int chunks = (max_ctx + kMinKeys - 1) / kMinKeys < kMaxChunks ? (max_ctx + kMinKeys - 1) / kMinKeys
-                                                                      : kMaxChunks;
   l.part = n_seq * sizeof(int4);
-  l.stats = l.part + chunks * vecs;
+  l.stats = l.part + most * vecs;
   l.sums = align16(l.stats + vecs);
-  l.bytes = l.sums + static_cast<size_t>(l.row_chunks) * n_kv_heads * n_seq * max_ctx * sizeof(float);
+  // (with smaller chunks there are kItemWGs items of kItemKeys sums at most)
+  const size_t sums = static_cast<size_t>(row_chunks(kRowChunk)) * n_kv_heads * n_seq * max_ctx;
+  constexpr size_t few = static_cast<size_t>(kItemWGs) * kItemKeys;
+  l.bytes = l.sums + (sums > few ? sums : few) * sizeof(float);
   return l;
 }
 
@@ -622,7 +639,7 @@ hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
   uint8_t* base = static_cast<uint8_t*>(a.workspace);
   const WeightsWork ws{reinterpret_cast<int4*>(base), reinterpret_cast<float2*>(base + l.part),
                        reinterpret_cast<float2*>(base + l.stats), reinterpret_cast<float*>(base + l.sums),
-                       l.chunk_keys};
+                       l.chunk_keys, l.row_chunk};
   const float scale_log2 = a.scale * 1.4426950408889634f;
   hipLaunchKernelGGL((weights_stats_kernel<D, SEQS>), dim3(kItemWGs), dim3(kThreads), 0, stream, a, ws,
                      scale_log2);
