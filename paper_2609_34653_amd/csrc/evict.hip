@@ -13,10 +13,10 @@
 // The move is a copy: each kept row is read and written once, behind a chain of four loads (length, row, page,
 // values).  So a workgroup takes only as many rows as its threads hold in two items of eight values each, and
 // many of them run at once: 4 (key, value) rows of 1,024 or 7 latent rows of 576.  16,384 of the former: 29 us (134
-// MB, 4.6 TB/s; 35 us with waves of their own of four items a lane, 29 us with one item, which costs the latent
-// rows, of 72 items, 44 us in place of 34: 129 MB, 3.8 TB/s).  Pages and angles are worked
-// out a row per lane and a pair per lane; keys go as two runs of four so that both members of a rotated pair sit in
-// one lane.
+// MB, 4.7 TB/s; 35 us with waves of their own of four items a lane), 55,939 of the latter: 29 us (129 MB, 4.4 TB/s; 44
+// us with one item a thread, 34 with all items in two halves).  Pages and angles are worked out a row per
+// lane and a pair per lane.  An item is 16 bytes next to each other, but of the rotated dimensions in the style that
+// pairs the halves, twice four values, so that both members of a pair sit in one lane.
 #include <algorithm>
 
 #include "common.h"
@@ -448,8 +448,14 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
       }
       if (on[f]) {
         const uint8_t* k = static_cast<const uint8_t*>(a.k) + at * row_bytes;
-        ka[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * da[f]));
-        kb[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * db[f]));
+        if (!HALF || pair[f] < 0) {        // next to each other
+          const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + 2 * da[f]));
+          ka[f] = u32x2{x[0], x[1]};
+          kb[f] = u32x2{x[2], x[3]};
+        } else {
+          ka[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * da[f]));
+          kb[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * db[f]));
+        }
         if (a.v != nullptr)
           v[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
               static_cast<const uint8_t*>(a.v) + at * row_bytes + 16 * piece[f]));
@@ -493,8 +499,12 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
       }
       if (!on[f]) continue;
       uint8_t* k = static_cast<uint8_t*>(a.k) + at * row_bytes;
-      *reinterpret_cast<u32x2*>(k + 2 * da[f]) = ka[f];
-      *reinterpret_cast<u32x2*>(k + 2 * db[f]) = kb[f];
+      if (!HALF || pair[f] < 0) {
+        *reinterpret_cast<u32x4*>(k + 2 * da[f]) = u32x4{ka[f][0], ka[f][1], kb[f][0], kb[f][1]};
+      } else {
+        *reinterpret_cast<u32x2*>(k + 2 * da[f]) = ka[f];
+        *reinterpret_cast<u32x2*>(k + 2 * db[f]) = kb[f];
+      }
       if (a.v != nullptr)
         *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.v) + at * row_bytes + 16 * piece[f]) = v[f];
     }
