@@ -14,6 +14,8 @@
 //             9 us for the sum (7 us and a kernel of 4.6 us for the join, when that was one).
 //   products  S^T (16 keys x 16 vectors) = K Q^T with v_mfma_f32_16x16x32_bf16: a lane holds four
 //             consecutive keys of a vector, stored as 16 bytes.
+#include <type_traits>
+
 #include "common.h"
 #include "evict.h"
 #include "mfma_tile.h"
@@ -31,7 +33,8 @@ constexpr int kMaxKvHeads = 64;
 constexpr int kMinShare = 8;             // blocks of a share at least
 constexpr int kOverhead = 12;            // what a sequence costs beside its blocks, in blocks
 constexpr size_t kScoreBytes = size_t{1} << 30;   // scores that are kept at most
-constexpr int kSumThreads = 256;
+constexpr int kSumThreads = 256;          // of the second kernel, and keys of one of its workgroups
+constexpr int kSumWaves = kSumThreads / kWave;
 
 template <int D>
 constexpr int wgs_of() { return D <= 128 ? kMaxWGs : kMaxWGs / 2; }
@@ -312,81 +315,121 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
   }
 }
 
-// The new weights: a key per thread, over the tokens and heads.  Each workgroup first joins the statistics of its
-// sequence's vectors over the shares that the sequence lies in, `width` lanes a vector and a part per lane, while
-// its first scores are on their way.
+// The new weights: four keys per lane and a quarter of the sequence's vectors per wave, whose sums are added in
+// order.  Each workgroup first joins the statistics of the vectors over the shares that the sequence lies in,
+// `width` lanes a vector and a part per lane, while its first scores are on their way.
 __global__ __launch_bounds__(kSumThreads) void weights_few_add_kernel(const AttnWeightsArgs a,
                                                                     const FewWork ws, float scale_log2) {
-  constexpr int kFlight = 8;
+  constexpr int kFlight = 4;
   __shared__ float2 stats[kCols * kMaxKvHeads];
+  __shared__ __attribute__((aligned(16))) float part[kSumWaves][kSumThreads];
   const PagedBatch& b = a.batch;
   const int tid = threadIdx.x, s = blockIdx.y, j = blockIdx.x * kSumThreads + tid;
+  const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int4 q = ws.seqs[s];
   if (q.y == 0 || static_cast<int>(blockIdx.x) * kSumThreads >= q.z) return;
   const int max_ctx = b.max_pages << b.page_shift, kept = q.z - q.y;
-  const bool in = j < q.z;
   const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
   const int n = q.y * Hq;                  // the sequence's vectors, token by token
   const size_t vec0 = static_cast<size_t>(q.x) * Hq;
-  const float* scores = ws.scores + vec0 * max_ctx + (in ? j : 0);
-  float x[kFlight];
-  auto load = [&](int v0) {
+  const int j4 = blockIdx.x * kSumThreads + 4 * lane;      // this lane's keys
+  const int quarter = (n + kSumWaves - 1) / kSumWaves, v0 = wave * quarter, v1 = min(n, v0 + quarter);
+  const float* scores = ws.scores + vec0 * max_ctx + min(j4, max_ctx - 4);
+  floatx4 x[kFlight];
+  auto load = [&](int v) {
 #pragma unroll
-    for (int i = 0; i < kFlight; ++i) x[i] = scores[static_cast<size_t>(min(v0 + i, n - 1)) * max_ctx];
+    for (int i = 0; i < kFlight; ++i)
+      x[i] = *reinterpret_cast<const floatx4*>(scores + static_cast<size_t>(min(v + i, n - 1)) * max_ctx);
   };
-  load(0);
+  load(v0);
 
   const int w0 = q.w & 0xffff, parts = q.w >> 16;
   int width = 1;
   while (width < min(parts, kWave)) width <<= 1;
   const int sub = tid & (width - 1), step = kSumThreads / width;
-  for (int u = tid / width; u < (n + step - 1) / step * step; u += step) {
-    const int v = min(u, n - 1);
-    const int tok = v / Hq, head = v - tok * Hq, g = head / G, col = tok * G + head - g * G;
-    float mx = -INFINITY, l = 0.f;
-    if (parts == 1) {
-      const float2 ml = ws.stats[vec0 + v];
-      mx = ml.x;
-      l = ml.y;
-    } else {
-      for (int p = sub; p < parts; p += width) {
-        const float2 ml =
-            ws.part_ml[static_cast<size_t>(2 * ((w0 + p) * Hkv + g) + (p == 0 ? 1 : 0)) * kCols + col];
-        const float m = fmaxf(mx, ml.x);
-        if (m != -INFINITY) {
-          l = (mx == -INFINITY ? 0.f : l * exp2f(mx - m)) +
-              (ml.x == -INFINITY ? 0.f : ml.y * exp2f(ml.x - m));
-          mx = m;
+  // J vectors at a time: one where a pass has room for all of them, else four, whose loads are under way together (128
+  // vectors: 19.3 us for the kernel, 22.6 one by one; 32, in one pass: 9.0 us, 9.9 with four)
+  auto join = [&](auto many) __attribute__((always_inline)) {
+    constexpr int J = many;
+    for (int u0 = tid / width; u0 < (n + step - 1) / step * step; u0 += J * step) {
+      float mx[J], l[J];               // of vectors u0 + c step
+      int at[J];                           // their places among a share's
+#pragma unroll
+      for (int c = 0; c < J; ++c) {
+        const int v = min(u0 + c * step, n - 1), tok = v / Hq, head = v - tok * Hq, g = head / G;
+        at[c] = g * 2 * kCols + tok * G + head - g * G;
+        mx[c] = -INFINITY;
+        l[c] = 0.f;
+        if (parts == 1) {
+          const float2 ml = ws.stats[vec0 + v];
+          mx[c] = ml.x;
+          l[c] = ml.y;
         }
       }
-      for (int o = 1; o < width; o <<= 1) {
-        const float m2 = __shfl_xor(mx, o, kWave), l2 = __shfl_xor(l, o, kWave), m = fmaxf(mx, m2);
-        if (m != -INFINITY) {
-          const float y = mx == -INFINITY ? 0.f : l * exp2f(mx - m);
-          const float z = m2 == -INFINITY ? 0.f : l2 * exp2f(m2 - m);
-          l = y + z;
-          mx = m;
+      if (parts > 1) {
+        for (int p = sub; p < parts; p += width) {
+          const float2* mine = ws.part_ml + (static_cast<size_t>(2 * (w0 + p) * Hkv) + (p == 0 ? 1 : 0)) * kCols;
+          float2 ml[J];
+#pragma unroll
+          for (int c = 0; c < J; ++c) ml[c] = mine[at[c]];
+#pragma unroll
+          for (int c = 0; c < J; ++c) {
+            const float m = fmaxf(mx[c], ml[c].x);
+            if (m != -INFINITY) {
+              l[c] = (mx[c] == -INFINITY ? 0.f : l[c] * exp2f(mx[c] - m)) +
+                     (ml[c].x == -INFINITY ? 0.f : ml[c].y * exp2f(ml[c].x - m));
+              mx[c] = m;
+            }
+          }
         }
+        for (int o = 1; o < width; o <<= 1) {
+#pragma unroll
+          for (int c = 0; c < J; ++c) {
+            const float m2 = __shfl_xor(mx[c], o, kWave), l2 = __shfl_xor(l[c], o, kWave);
+            const float m = fmaxf(mx[c], m2);
+            if (m != -INFINITY) {
+              const float y = mx[c] == -INFINITY ? 0.f : l[c] * exp2f(mx[c] - m);
+              const float z = m2 == -INFINITY ? 0.f : l2 * exp2f(m2 - m);
+              l[c] = y + z;
+              mx[c] = m;
+            }
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < J; ++c) l[c] = 1.f / l[c];
       }
-      l = 1.f / l;
+#pragma unroll
+      for (int c = 0; c < J; ++c)
+        if (sub == 0 && u0 + c * step < n) stats[u0 + c * step] = make_float2(mx[c], l[c]);
     }
-    if (sub == 0 && u < n) stats[u] = make_float2(mx, l);
-  }
+  };
+  if (n <= step) join(std::integral_constant<int, 1>{});
+  else join(std::integral_constant<int, 4>{});
   __syncthreads();
 
-  // vectors of tokens that see row j: those from token j - kept on
-  const int v_from = max(j - kept, 0) * Hq;
-  float sum = 0.f;
-  for (int v0 = 0; v0 < n; v0 += kFlight) {
-    if (v0 > 0) load(v0);
+  // vectors of tokens that see row j4 + e: those from token j4 + e - kept on
+  int from[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) from[e] = max(j4 + e - kept, 0) * Hq;
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int v = v0; v < v1; v += kFlight) {
+    if (v > v0) load(v);
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
-      const float2 ml = stats[min(v0 + i, n - 1)];
-      const float p = __builtin_amdgcn_exp2f(fmaf(x[i], scale_log2, -ml.x));
-      sum = v0 + i < n && v0 + i >= v_from ? fmaf(p, ml.y, sum) : sum;
+      const float2 ml = stats[min(v + i, n - 1)];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(x[i][e], scale_log2, -ml.x));
+        acc[e] = v + i < v1 && v + i >= from[e] ? fmaf(p, ml.y, acc[e]) : acc[e];
+      }
     }
   }
-  if (!in) return;
+  *reinterpret_cast<floatx4*>(&part[wave][4 * lane]) = acc;
+  __syncthreads();
+  if (j >= q.z) return;
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kSumWaves; ++w) sum += part[w][tid];
   const size_t at = static_cast<size_t>(s) * a.weight_stride + j;
   if (a.weight_in != nullptr) {
     const int seen = a.seen_len != nullptr ? a.seen_len[s] : kept;
