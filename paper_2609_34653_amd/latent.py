@@ -75,6 +75,10 @@ def _strided(t, name: str, dtype, dev: int, dims: int):
 
 def _mat(t, name: str, dtype, dev: int):
     """(address, rows, width, row stride) of a matrix with contiguous rows."""
+    if type(t) is _T and t.dtype is dtype and t.get_device() == dev:
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 2 and stride[1] == 1:
+            return t.data_ptr(), shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1]
     at = _strided(t, name, dtype, dev, 2)
     n, w = t.shape
     return at, n, w, t.stride(0) if n > 1 else w
@@ -82,6 +86,10 @@ def _mat(t, name: str, dtype, dev: int):
 
 def _heads(t, name: str, dtype, dev: int):
     """(address, rows, heads, width, row stride, head stride) of [rows, heads, width]."""
+    if type(t) is _T and t.dtype is dtype and t.get_device() == dev:
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 3 and stride[2] == 1 and shape[0] > 1 and shape[1] > 1:
+            return t.data_ptr(), *shape, stride[0], stride[1]
     at = _strided(t, name, dtype, dev, 3)
     n, h, w = t.shape
     hs = t.stride(1) if h > 1 else w
@@ -90,6 +98,10 @@ def _heads(t, name: str, dtype, dev: int):
 
 def _pool(pool, name: str, dev: int):
     """(address, n_pages, page_size, row elements) of a pool [n_pages, page_size, ...]."""
+    if type(pool) is _T and pool.dtype is _BF16 and pool.get_device() == dev and pool.is_contiguous():
+        shape = pool.shape
+        if len(shape) == 3:
+            return pool.data_ptr(), *shape
     if not (isinstance(pool, _T) and pool.dim() >= 3):
         raise ValueError(f"{name} must be [n_pages, page_size, ...]")
     at = _dev(pool, name, _BF16, pool.numel(), dev)
