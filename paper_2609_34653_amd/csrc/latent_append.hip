@@ -9,7 +9,7 @@
 // latent (4 values per lane at a time, coalesced), the others turn the parts, eight heads of eight
 // lanes each per group (the key part is the first head), both members of a pair in one lane.  A lane's place in
 // its head is the same in every group, so it reads the four (cos, sin) it needs once.  33,083 float32 tokens with 32
-// heads: 106 us (521 MB, 4.9 TB/s; a large copy reaches 5.3); one token of each of 24 streams: 4.4 us, a launch and
+// heads: 106 us (521 MB, 4.9 TB/s; a large copy reaches 5.3); one token of each of 24 streams: 4.0 us, a launch and
 // three dependent loads.
 #include "common.h"
 #include "latent.h"
@@ -22,6 +22,7 @@ namespace {
 constexpr int kRowWaves = 4;
 constexpr int kRowThreads = kRowWaves * kWave;
 constexpr int kWaveSlots = 8192;         // waves that the chip holds at once (32 on each CU)
+constexpr int64_t kMaxGrid = 1 << 20;    // workgroups along x at most
 constexpr int E = kLatentRope;
 constexpr int LPH = E / 8;               // lanes per head
 constexpr int HPW = kWave / LPH;         // heads per group
@@ -42,11 +43,13 @@ __global__ __launch_bounds__(kRowThreads) void latent_append_kernel(const Latent
 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  if (blockIdx.x == 0 && wave == 0) report_batch(a.batch, a.d_status);
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * kRowWaves + wave;
-  const int t = static_cast<int>(w / waves_per_token);
-  const int part = static_cast<int>(w % waves_per_token);   // 0: the latent
-  if (t >= a.batch.n_tokens) return;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) report_batch(a.batch, a.d_status);
+  // (2^24 tokens of 4,096 heads are 2^31 waves)
+  const uint32_t w = (blockIdx.y * gridDim.x + blockIdx.x) * kRowWaves + wave;
+  const uint32_t token = w / static_cast<uint32_t>(waves_per_token);
+  const int part = static_cast<int>(w - token * waves_per_token);          // 0: the latent
+  if (token >= static_cast<uint32_t>(a.batch.n_tokens)) return;
+  const int t = static_cast<int>(token);
 
   const int c = lane % LPH, hl = lane / LPH, g0 = (part - 1) * kIters;
   const int da = HALF ? 4 * c : 8 * c, db = HALF ? E / 2 + 4 * c : 8 * c + 4;
@@ -175,7 +178,10 @@ template <int R, bool IN32, int kIters>
 hipError_t launch_i(const LatentAppendArgs& a, int groups, hipStream_t stream) {
   const int wpt = 1 + (groups + kIters - 1) / kIters;
   const int64_t waves = static_cast<int64_t>(a.batch.n_tokens) * wpt;
-  const dim3 grid(static_cast<unsigned>((waves + kRowWaves - 1) / kRowWaves));
+  // (2^32 threads along one dimension are not launched)
+  const int64_t blocks = (waves + kRowWaves - 1) / kRowWaves;
+  const int64_t gx = blocks < kMaxGrid ? blocks : kMaxGrid;
+  const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>((blocks + gx - 1) / gx));
   if (a.rope_half)
     hipLaunchKernelGGL((latent_append_kernel<R, IN32, true, kIters>), grid, dim3(kRowThreads), 0, stream, a,
                        wpt);
@@ -188,7 +194,7 @@ hipError_t launch_i(const LatentAppendArgs& a, int groups, hipStream_t stream) {
 template <int R, bool IN32>
 hipError_t launch_t(const LatentAppendArgs& a, hipStream_t stream) {
   const int groups = (1 + a.n_heads + HPW - 1) / HPW;
-  // one group per wave while every wave finds a slot of the chip at once (24 tokens of 16 heads: 4.4 us, 4.8 with four
+  // one group per wave while every wave finds a slot of the chip at once (24 tokens of 16 heads: 4.0 us, 0.4 more with four
   // groups), four beyond (33,083 tokens of 32: 106 us, 114 with one)
   if (static_cast<int64_t>(a.batch.n_tokens) * (1 + groups) <= kWaveSlots)
     return launch_i<R, IN32, 1>(a, groups, stream);

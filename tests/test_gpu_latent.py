@@ -126,6 +126,23 @@ def test_append(case):
         assert (f64(out[other]) == 7.0).all() and (f64(out[..., :R]) == 7.0).all()
 
 
+def test_append_of_millions():
+    """More workgroups than one dimension of a launch has: every row is there, bit for bit."""
+    from paper_2609_34653_amd import latent as la
+    n, P, R = (1 << 22) + 5, 256, 256
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn(n, R + E, generator=g, device="cuda", dtype=BF)
+    pool = torch.zeros(-(-n // P) + 1, P, R + E, dtype=BF, device="cuda")
+    pages = torch.randperm(pool.shape[0] - 1, generator=g, device="cuda").to(torch.int32)
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    la.omnitide_latent_append(x[:, :R], x[:, R:], pool, pages[None], i32([0, n]), i32([n]), d_status=st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    assert torch.equal(pool[pages.long()].view(-1, R + E)[:n], x)
+    assert not pool[-1].any()
+
+
 def test_append_queries_in_place():
     from paper_2609_34653_amd import latent as la, paged as pg
     T, H, R, P = 21, 5, 256, 16
