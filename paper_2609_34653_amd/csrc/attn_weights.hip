@@ -11,8 +11,9 @@
 //             the second), the other streams through LDS tiles filled by direct loads; so the first pass
 //             has a row's statistics and the second a key's sum in the lanes that they belong to.
 //   items     the first pass is dealt out as 256 query rows of a KV head (tokens times its query heads) and a
-//             chunk of the keys, the second as 256 keys of a KV head and up to 1,024 query rows; 512 workgroups
-//             take them in turn, two on a CU, so that one's vector work hides what the other waits for.
+//             chunk of the keys, the second as 256 keys of a KV head and up to 1,024 query rows; as many
+//             workgroups as the chip holds take them in turn, two on a CU for d <= 128, so that one's vector work
+//             hides what the other waits for.
 //   sums      no atomics: every item owns its place in a buffer of partial sums, added in a fixed order.
 //   measured  665 tokens of 32 heads over 17,048 keys of 8 x 128: 139 us and 143 us for the passes (91 GFLOP each), 5
 //             us for each of the other two kernels.  Matrix cores busy 0.41 and 0.36, vector units 0.64 and 0.61: what
@@ -38,7 +39,8 @@ constexpr int kMaxChunks = 16;           // chunks of the keys at most
 constexpr int kRowChunk = 1024;          // query rows of an item of the second pass at most
 constexpr int kMinRowChunk = 128;        // and at least
 constexpr int kItemKeys = kWaves * 32;   // its keys
-constexpr int kItemWGs = 512;            // workgroups of a pass
+// Workgroups of a pass: two on a CU, of keys whose operands leave registers for that.
+constexpr int wgs_of(int head_dim) { return head_dim <= 128 ? 512 : 256; }
 constexpr int kNumXcd = 8;
 constexpr int kSumThreads = 256;
 
@@ -168,7 +170,7 @@ struct Items {
 // The first item of a workgroup: those of one XCD (workgroups are dealt round-robin over them) are next to each
 // other, so that they read the same keys, or rows, together.
 __device__ inline int first_item() {
-  return blockIdx.x % kNumXcd * (kItemWGs / kNumXcd) + blockIdx.x / kNumXcd;
+  return blockIdx.x % kNumXcd * (gridDim.x / kNumXcd) + blockIdx.x / kNumXcd;
 }
 
 // Every sequence into LDS, by the whole workgroup: one that starts in front of an earlier offset has no tokens, nor
@@ -236,7 +238,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void 
   const uint32_t at_lane = S::lane_at(col, h);
   const uint32_t row_bytes = 2u * static_cast<uint32_t>(Hkv * D);
 
-  for (int64_t item = first_item(); item < total; item += kItemWGs) {
+  for (int64_t item = first_item(); item < total; item += wgs_of(D)) {
     const int s = items.find(b.n_seq, item);
     const int q0 = uniform(seqs[s].x), L = uniform(seqs[s].y), ctx = uniform(seqs[s].z);
     const int kept = ctx - L, tiles = (L * G + kRows - 1) / kRows;
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void 
   const uint32_t at_lane = S::lane_at(col, h);
   const uint32_t magic = (0x100000000ull + G - 1) / G;     // x / G for small x (G = 1: 0, see below)
 
-  for (int64_t item = blockIdx.x; item < total; item += kItemWGs) {
+  for (int64_t item = blockIdx.x; item < total; item += wgs_of(D)) {
     const int s = items.find(b.n_seq, item);
     const int4 sq = ws.seqs[s];
     const int q0 = uniform(sq.x), L = uniform(sq.y), ctx = uniform(sq.z);
@@ -603,13 +605,14 @@ struct Layout {
 // tokens over 6,000 keys: 29 us for the first pass in chunks of 512 keys, 47 in chunks of 1,024 and 41 in chunks of
 // 384, which are more than 512; 100 over 3,000: 19 us with 256, 40 with 1,024).  What is worked out from max_ctx and
 // n_tokens is an upper bound, so short sequences in long tables have large items.
-Layout layout(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, int n_kv_heads) {
+Layout layout(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, int n_kv_heads, int head_dim) {
   Layout l;
   const int64_t G = n_q_heads / n_kv_heads;
   const int64_t tiles = (n_tokens * G + kRows - 1) / kRows + (n_seq < n_tokens ? n_seq : n_tokens) - 1;
   const int most = (max_ctx + kMinKeys - 1) / kMinKeys < kMaxChunks ? (max_ctx + kMinKeys - 1) / kMinKeys
                                                                     : kMaxChunks;
-  int64_t chunks = kItemWGs / (tiles * n_kv_heads);
+  const int wgs = wgs_of(head_dim);
+  int64_t chunks = wgs / (tiles * n_kv_heads);
   const int least = (max_ctx + kManyKeys - 1) / kManyKeys;
   chunks = chunks < least ? least : chunks;
   chunks = chunks > most ? most : chunks;
@@ -619,14 +622,17 @@ Layout layout(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, in
   const int64_t key_items = static_cast<int64_t>((max_ctx + kItemKeys - 1) / kItemKeys) * n_kv_heads * n_seq;
   auto row_chunks = [&](int64_t chunk) { return (rows + chunk - 1) / chunk; };
   l.row_chunk = kRowChunk;
-  while (l.row_chunk > kMinRowChunk && key_items * row_chunks(l.row_chunk / 2) <= kItemWGs) l.row_chunk /= 2;
+  if (key_items <= wgs) {
+    const int64_t n = wgs / key_items, chunk = ((rows + n - 1) / n + 63) / 64 * 64;
+    l.row_chunk = static_cast<int>(chunk < kMinRowChunk ? kMinRowChunk : chunk < kRowChunk ? chunk : kRowChunk);
+  }
   const size_t vecs = static_cast<size_t>(n_tokens) * n_q_heads * sizeof(float2);
   l.part = n_seq * sizeof(int4);
   l.stats = l.part + most * vecs;
   l.sums = align16(l.stats + vecs);
-  // (with smaller chunks there are kItemWGs items of kItemKeys sums at most)
+  // (with smaller chunks there are as many items of kItemKeys sums as workgroups at most)
   const size_t sums = static_cast<size_t>(row_chunks(kRowChunk)) * n_kv_heads * n_seq * max_ctx;
-  constexpr size_t few = static_cast<size_t>(kItemWGs) * kItemKeys;
+  const size_t few = static_cast<size_t>(wgs) * kItemKeys;
   l.bytes = l.sums + (sums > few ? sums : few) * sizeof(float);
   return l;
 }
@@ -635,13 +641,13 @@ template <int D, int SEQS>
 hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
   const PagedBatch& b = a.batch;
   const int max_ctx = b.max_pages << b.page_shift;
-  const Layout l = layout(b.n_tokens, b.n_seq, max_ctx, a.max_q, a.n_q_heads, a.n_kv_heads);
+  const Layout l = layout(b.n_tokens, b.n_seq, max_ctx, a.max_q, a.n_q_heads, a.n_kv_heads, D);
   uint8_t* base = static_cast<uint8_t*>(a.workspace);
   const WeightsWork ws{reinterpret_cast<int4*>(base), reinterpret_cast<float2*>(base + l.part),
                        reinterpret_cast<float2*>(base + l.stats), reinterpret_cast<float*>(base + l.sums),
                        l.chunk_keys, l.row_chunk};
   const float scale_log2 = a.scale * 1.4426950408889634f;
-  hipLaunchKernelGGL((weights_stats_kernel<D, SEQS>), dim3(kItemWGs), dim3(kThreads), 0, stream, a, ws,
+  hipLaunchKernelGGL((weights_stats_kernel<D, SEQS>), dim3(wgs_of(D)), dim3(kThreads), 0, stream, a, ws,
                      scale_log2);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -652,7 +658,7 @@ hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
                      0, stream, a, ws);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((weights_sum_kernel<D, SEQS>), dim3(kItemWGs), dim3(kThreads), 0, stream, a, ws,
+  hipLaunchKernelGGL((weights_sum_kernel<D, SEQS>), dim3(wgs_of(D)), dim3(kThreads), 0, stream, a, ws,
                      scale_log2);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -669,8 +675,8 @@ hipError_t launch_d(const AttnWeightsArgs& a, hipStream_t stream) {
 }  // namespace
 
 size_t attn_weights_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads,
-                                    int n_kv_heads, int) {
-  const size_t n = layout(n_tokens, n_seq, max_ctx, max_q, n_q_heads, n_kv_heads).bytes;
+                                    int n_kv_heads, int head_dim) {
+  const size_t n = layout(n_tokens, n_seq, max_ctx, max_q, n_q_heads, n_kv_heads, head_dim).bytes;
   // (the larger of both ways where either may be taken, so that a larger call's serves a smaller one)
   if (!attn_weights_few(1, 1, max_q, n_q_heads, n_kv_heads)) return n;
   const size_t few = attn_weights_few_workspace_bytes(n_tokens, n_seq, max_ctx, n_q_heads);
