@@ -102,6 +102,8 @@ def _pool(pool, name: str, dev: int):
         shape = pool.shape
         if len(shape) == 3:
             return pool.data_ptr(), *shape
+        if len(shape) == 4:
+            return pool.data_ptr(), shape[0], shape[1], shape[2] * shape[3]
     if not (isinstance(pool, _T) and pool.dim() >= 3):
         raise ValueError(f"{name} must be [n_pages, page_size, ...]")
     at = _dev(pool, name, _BF16, pool.numel(), dev)
