@@ -27,7 +27,8 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKB = 16;                  // keys per block
-constexpr int kCols = 16;                // query vectors of a sequence and KV head at most
+constexpr int kTile = 16;                // query vectors of a product
+constexpr int kCols = 32;                // of a sequence and KV head at most
 constexpr int kMaxWGs = 512;
 constexpr int kMaxKvHeads = 64;
 constexpr int kMinShare = 8;             // blocks of a share at least
@@ -103,7 +104,8 @@ struct FewWork {
   float* scores;                         // [token][query head][max_ctx]
 };
 
-template <int D, int NS>
+// NC: tiles of query vectors.
+template <int D, int NS, int NC>
 __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kernel(
     const AttnWeightsArgs a, const FewWork ws, float scale_log2) {
   constexpr int KC = D / 32;               // 32-dim slices of a key
@@ -114,7 +116,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
   constexpr int CALLS = 2 * LOADS;         // direct loads of a block
   constexpr float kSumLimit = 4294967296.f;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kWaves * RING * BLOCKB];
-  __shared__ float sm[kWaves][kCols], sl[kWaves][kCols];
+  __shared__ float sm[kWaves][NC * kTile], sl[kWaves][NC * kTile];
   const PagedBatch& b = a.batch;
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
@@ -186,17 +188,28 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
     // a share holds at most one part that goes on from an earlier share and one that goes on in a later
     const int slot = 2 * static_cast<int>(blockIdx.x) + (b0 > 0 ? 0 : 1);
 
-    // Q^T operand: column c16 = query vector (token c16 / G, head g*G + c16 % G)
-    const bool col_ok = c16 < len * G;
-    const int tok = col_ok ? c16 / G : 0;
-    const int lim = ctx - len + tok;         // keys <= lim are visible
-    const size_t vec = static_cast<size_t>(q0 + tok) * Hq + g * G + (col_ok ? c16 % G : 0);
-    const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + vec * D;
-    float* scores = ws.scores + vec * max_ctx;
-    bf16x8 qf[KC];
+    // Q^T operand: column c = 16 ct + c16 = query vector (token c / G, head g*G + c % G)
+    const int cols = len * G;
+    auto vec_of = [&](int c) {               // of a column in use
+      return static_cast<size_t>(q0 + c / G) * Hq + g * G + c % G;
+    };
+    bool col_ok[NC];
+    int lim[NC];                             // keys <= lim are visible
+    float* scores[NC];
+    bf16x8 qf[NC][KC];
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc)
-      qf[kc] = __builtin_bit_cast(bf16x8, ld16(qrow + 32 * kc + 8 * g4));
+    for (int ct = 0; ct < NC; ++ct) {
+      const int c = kTile * ct + c16;
+      col_ok[ct] = c < cols;
+      lim[ct] = ctx - len + (col_ok[ct] ? c / G : 0);
+      const size_t vec = vec_of(col_ok[ct] ? c : 0);
+      scores[ct] = ws.scores + vec * max_ctx + 4 * g4;
+      const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + vec * D;
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc)
+        qf[ct][kc] = __builtin_bit_cast(bf16x8, ld16(qrow + 32 * kc + 8 * g4));
+    }
+    const bool both = NC == 2 && cols > kTile;             // (a tile of no vectors stores nothing)
 
     int n_it = (b1 - b0 - wave + kWaves - 1) / kWaves;          // this wave's blocks
     int bad_row = INT32_MAX;                 // the first row of this wave's first block of a bad page
@@ -229,7 +242,12 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
         dma16_once(base, static_cast<uint32_t>(min(row[c], last)) * row_bytes + off[c],
                    ring + static_cast<uint32_t>(e * BLOCKB + c * kWave * 16));
     };
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run[NC], l_run[NC];
+#pragma unroll
+    for (int ct = 0; ct < NC; ++ct) {
+      m_run[ct] = -INFINITY;
+      l_run[ct] = 0.f;
+    }
     load_pages(0);
     // nothing but the direct loads and the stores of scores is counted from here on
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
@@ -242,17 +260,28 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
         const int it = it0 + e;
         if (it >= n_it) break;
         // This block has landed: behind its loads come those of the blocks ahead of it, RING - 1 at most, and
-        // the stores of the RING blocks in front (loads and stores come back in their order).
+        // the stores of the RING blocks in front, one for each tile with vectors (loads and stores come back in
+        // their order).
         const int ahead = min(n_it - 1 - it, RING - 1);
-        if (it0 > 0) wait_landed<CALLS, RING - 1, RING>(ahead, RING);
-        else wait_landed<CALLS, RING - 1, RING>(ahead, e);
+        if (both) {
+          if (it0 > 0) wait_landed<CALLS, RING - 1, NC * RING>(ahead, NC * RING);
+          else wait_landed<CALLS, RING - 1, NC * RING>(ahead, NC * e);
+        } else {
+          if (it0 > 0) wait_landed<CALLS, RING - 1, RING>(ahead, RING);
+          else wait_landed<CALLS, RING - 1, RING>(ahead, e);
+        }
         const uint32_t kb = ring + static_cast<uint32_t>(e * BLOCKB);
-        floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
+        floatx4 s[NC];
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct) s[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kc = 0; kc < KC; ++kc) {
           const uint32_t at = (k_lane ^ (64u * kc & kFlip)) + (64u * kc & ~kFlip);
           const u32x4 w = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(kb + at);
-          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), qf[kc], s, 0, 0, 0);
+#pragma unroll
+          for (int ct = 0; ct < NC; ++ct)
+            s[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), qf[ct][kc], s[ct], 0,
+                                                            0, 0);
         }
         const int key0 = block_of(it) * kKB;
         // the next block into this entry, whose reads have returned
@@ -261,48 +290,58 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
             load_pages(it + RING);
             asm volatile("s_waitcnt vmcnt(0)" : "+v"(pages) : : "memory");
           }
-          asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(s) : : "memory");
+#pragma unroll
+          for (int ct = 0; ct < NC; ++ct) asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(s[ct]) : : "memory");
           if (it + RING < n_it) issue(it + RING, e);
         }
-        if (col_ok) *reinterpret_cast<floatx4*>(scores + key0 + 4 * g4) = s;
-        if (key0 + kKB - 1 > ctx - len) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (key0 + 4 * g4 + i > lim) s[i] = -INFINITY;
+        for (int ct = 0; ct < NC; ++ct)
+          if (col_ok[ct]) *reinterpret_cast<floatx4*>(scores[ct] + key0) = s[ct];
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct) {
+          floatx4& x = s[ct];
+          if (key0 + kKB - 1 > ctx - len) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (key0 + 4 * g4 + i > lim[ct]) x[i] = -INFINITY;
+          }
+          float ls = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ls += __builtin_amdgcn_exp2f(fmaf(x[i], scale_log2, -m_run[ct]));
+          if (__any(!(ls < kSumLimit))) {
+            // exact block maximum per column (its four lane groups), move the reference, recompute
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[i] == -INFINITY ? -INFINITY : x[i] * scale_log2);
+            mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+            const float m_new = fmaxf(m_run[ct], mx);
+            const float m_use = m_new == -INFINITY ? 0.f : m_new;
+            l_run[ct] *= __builtin_amdgcn_exp2f(m_run[ct] - m_use);
+            m_run[ct] = m_new;
+            ls = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              ls += x[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[i], scale_log2, -m_use));
+          }
+          l_run[ct] += ls;
         }
-        float ls = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ls += __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -m_run));
-        if (__any(!(ls < kSumLimit))) {
-          // exact block maximum per column (its four lane groups), move the reference, recompute
-          float mx = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[i] == -INFINITY ? -INFINITY : s[i] * scale_log2);
-          mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-          const float m_new = fmaxf(m_run, mx);
-          const float m_use = m_new == -INFINITY ? 0.f : m_new;
-          l_run *= __builtin_amdgcn_exp2f(m_run - m_use);
-          m_run = m_new;
-          ls = 0.f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            ls += s[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -m_use));
-        }
-        l_run += ls;
       }
     }
     // merge the waves; a sum that is no number spoils the column to the end, whatever references there are
-    if (lim >= bad_row) l_run = __builtin_nanf("");
-    const float l_col = l_run + __shfl_xor(l_run, 16, kWave) + __shfl_xor(l_run, 32, kWave) +
-                        __shfl_xor(l_run, 48, kWave);
     __syncthreads();                         // the part before has been merged
-    if (g4 == 0) {
-      sm[wave][c16] = l_col == l_col ? m_run : 0.f;
-      sl[wave][c16] = l_col;
+#pragma unroll
+    for (int ct = 0; ct < NC; ++ct) {
+      if (lim[ct] >= bad_row) l_run[ct] = __builtin_nanf("");
+      const float l_col = l_run[ct] + __shfl_xor(l_run[ct], 16, kWave) + __shfl_xor(l_run[ct], 32, kWave) +
+                          __shfl_xor(l_run[ct], 48, kWave);
+      if (g4 == 0) {
+        sm[wave][kTile * ct + c16] = l_col == l_col ? m_run[ct] : 0.f;
+        sl[wave][kTile * ct + c16] = l_col;
+      }
     }
     __syncthreads();
-    if (tid < kCols) {
+    if (tid < NC * kTile) {
       float M = -INFINITY, l = 0.f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm[w][tid]);
@@ -310,7 +349,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
       for (int w = 0; w < kWaves; ++w)
         if (sm[w][tid] != -INFINITY) l = fmaf(__builtin_amdgcn_exp2f(sm[w][tid] - M), sl[w][tid], l);
       if (!whole) ws.part_ml[static_cast<size_t>(slot) * kCols + tid] = make_float2(M, l);
-      else if (col_ok) ws.stats[vec] = make_float2(M, 1.f / l);        // (c16 = tid here)
+      else if (tid < cols) ws.stats[vec_of(tid)] = make_float2(M, 1.f / l);
     }
   }
 }
@@ -451,7 +490,7 @@ Layout layout(int n_tokens, int n_seq, int max_ctx, int n_q_heads) {
   return l;
 }
 
-template <int D, int NS>
+template <int D, int NS, int NC>
 hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
   const PagedBatch& b = a.batch;
   const int max_ctx = b.max_pages << b.page_shift;
@@ -462,7 +501,7 @@ hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
   const float scale_log2 = a.scale * 1.4426950408889634f;
   // a workgroup per KV head and share
   const int wgs = max(1, wgs_of<D>() / a.n_kv_heads) * a.n_kv_heads;
-  hipLaunchKernelGGL((weights_score_kernel<D, NS>), dim3(wgs), dim3(kThreads), 0, stream, a, ws, scale_log2);
+  hipLaunchKernelGGL((weights_score_kernel<D, NS, NC>), dim3(wgs), dim3(kThreads), 0, stream, a, ws, scale_log2);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(weights_few_add_kernel, dim3((max_ctx + kSumThreads - 1) / kSumThreads, b.n_seq),
@@ -470,9 +509,15 @@ hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int D, int NC>
+hipError_t launch_n(const AttnWeightsArgs& a, hipStream_t stream) {
+  return a.batch.n_seq <= kWave ? launch_t<D, 1, NC>(a, stream) : launch_t<D, 16, NC>(a, stream);
+}
+
 template <int D>
 hipError_t launch_d(const AttnWeightsArgs& a, hipStream_t stream) {
-  return a.batch.n_seq <= kWave ? launch_t<D, 1>(a, stream) : launch_t<D, 16>(a, stream);
+  const int64_t cols = static_cast<int64_t>(a.max_q) * (a.n_q_heads / a.n_kv_heads);
+  return cols <= kTile ? launch_n<D, 1>(a, stream) : launch_n<D, 2>(a, stream);
 }
 
 }  // namespace

@@ -89,6 +89,12 @@ WEIGHTS = [
     ([20 + 3 * i for i in range(1024)], [i % 2 for i in range(1024)], 16, 3, 3, 64),
     ([30000], [1], 64, 8, 2, 128),
     ([30000], [4], 16, 8, 1, 64),
+    ([700, 33, 5000], [2, 1, 2], 16, 16, 1, 576),            # 32 vectors of a KV head, 16 in between
+    ([900, 64, 20], [1, 1, 1], 32, 32, 1, 320),
+    ([3000, 100], [3, 2], 64, 28, 4, 128),                   # 21 and 14
+    ([40 + i for i in range(70)], [1 + i % 4 for i in range(70)], 16, 14, 2, 64),
+    ([20000], [4], 16, 32, 4, 128),
+    ([300 + i for i in range(80)], [1 + i % 2 for i in range(80)], 16, 16, 1, 576),
 ]
 
 
