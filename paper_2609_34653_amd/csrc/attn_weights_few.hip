@@ -1,8 +1,8 @@
-// The weight that few tokens of each sequence give to each cached row (up to 16 query vectors per KV head): the
-// keys are read once.
+// The weight that few tokens of each sequence give to each cached row (up to 32 query vectors per KV head, of
+// latents up to 64): the keys are read once.
 //
-// Mathematics: as attn_weights.hip.  Bound by memory: 2 d bytes of a key serve 16 vectors at most.  So the scores
-// of the one pass over the keys are kept (4 bytes per query head and key, a twelfth to a half of the keys),
+// Mathematics: as attn_weights.hip.  Bound by memory: 2 d bytes of a key serve that many vectors.  So the scores
+// of the one pass over the keys are kept (4 bytes per query head and key, at most half of the keys' bytes for d >= 128),
 // beside each vector's running reference and sum per share; a second kernel joins the sums of the shares and
 // sums exp2(x - m) / l over the vectors, a key per thread.
 //   shares    as in paged decode: the 16-key blocks of all sequences with tokens, one after the other, cut into
@@ -12,8 +12,11 @@
 //   measured  24 tokens of 32 heads over 119,095 keys of 8 x 128 in all: 50 us for the scores (244 MB read and 15
 //             written, 5.2 TB/s, a copy's rate; without the stores 42 us; with non-temporal ones 54 us) and
 //             9 us for the sum (7 us and a kernel of 4.6 us for the join, when that was one).
-//   products  S^T (16 keys x 16 vectors) = K Q^T with v_mfma_f32_16x16x32_bf16: a lane holds four
-//             consecutive keys of a vector, stored as 16 bytes.
+//   products  S^T (16 keys x 16 vectors) = K Q^T with v_mfma_f32_16x16x32_bf16, for one, two or four tiles of
+//             vectors: a lane holds four consecutive keys of a vector, stored as 16 bytes.
+//   vectors   against the two passes: 24 x 8 tokens of 32 / 8 heads (32 vectors) 117 us, 137 there; 24 streams of
+//             latents with 32 heads 49 us, 97 there; with 64 heads 70 us, 105 there.  (More of them than that,
+//             and the scores outweigh the keys, or the queries the registers.)
 #include <type_traits>
 
 #include "common.h"
@@ -28,7 +31,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKB = 16;                  // keys per block
 constexpr int kTile = 16;                // query vectors of a product
-constexpr int kCols = 32;                // of a sequence and KV head at most
+constexpr int kCols = 64;                // of a sequence and KV head at most: of latents,
+constexpr int kColsHeads = 32;           // and of keys of heads
 constexpr int kMaxWGs = 512;
 constexpr int kMaxKvHeads = 64;
 constexpr int kMinShare = 8;             // blocks of a share at least
@@ -209,7 +213,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
       for (int kc = 0; kc < KC; ++kc)
         qf[ct][kc] = __builtin_bit_cast(bf16x8, ld16(qrow + 32 * kc + 8 * g4));
     }
-    const bool both = NC == 2 && cols > kTile;             // (a tile of no vectors stores nothing)
+    const int tiles = min((cols + kTile - 1) / kTile, NC); // (a tile of no vectors stores nothing)
 
     int n_it = (b1 - b0 - wave + kWaves - 1) / kWaves;          // this wave's blocks
     int bad_row = INT32_MAX;                 // the first row of this wave's first block of a bad page
@@ -263,13 +267,12 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
         // the stores of the RING blocks in front, one for each tile with vectors (loads and stores come back in
         // their order).
         const int ahead = min(n_it - 1 - it, RING - 1);
-        if (both) {
-          if (it0 > 0) wait_landed<CALLS, RING - 1, NC * RING>(ahead, NC * RING);
-          else wait_landed<CALLS, RING - 1, NC * RING>(ahead, NC * e);
-        } else {
-          if (it0 > 0) wait_landed<CALLS, RING - 1, RING>(ahead, RING);
-          else wait_landed<CALLS, RING - 1, RING>(ahead, e);
-        }
+#pragma unroll
+        for (int n = 1; n <= NC; ++n)
+          if (tiles == n) {
+            if (it0 > 0) wait_landed<CALLS, RING - 1, NC * RING>(ahead, n * RING);
+            else wait_landed<CALLS, RING - 1, NC * RING>(ahead, n * e);
+          }
         const uint32_t kb = ring + static_cast<uint32_t>(e * BLOCKB);
         floatx4 s[NC];
 #pragma unroll
@@ -360,7 +363,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
 __global__ __launch_bounds__(kSumThreads) void weights_few_add_kernel(const AttnWeightsArgs a,
                                                                     const FewWork ws, float scale_log2) {
   constexpr int kFlight = 4;
-  __shared__ float2 stats[kCols * kMaxKvHeads];
+  __shared__ float2 stats[kColsHeads * kMaxKvHeads];       // (latents have one KV head)
   __shared__ __attribute__((aligned(16))) float part[kSumWaves][kSumThreads];
   const PagedBatch& b = a.batch;
   const int tid = threadIdx.x, s = blockIdx.y, j = blockIdx.x * kSumThreads + tid;
@@ -517,13 +520,18 @@ hipError_t launch_n(const AttnWeightsArgs& a, hipStream_t stream) {
 template <int D>
 hipError_t launch_d(const AttnWeightsArgs& a, hipStream_t stream) {
   const int64_t cols = static_cast<int64_t>(a.max_q) * (a.n_q_heads / a.n_kv_heads);
-  return cols <= kTile ? launch_n<D, 1>(a, stream) : launch_n<D, 2>(a, stream);
+  if (cols <= kTile) return launch_n<D, 1>(a, stream);
+  if constexpr (D > 128) {
+    if (cols > 2 * kTile) return launch_n<D, 4>(a, stream);
+  }
+  return launch_n<D, 2>(a, stream);
 }
 
 }  // namespace
 
-bool attn_weights_few(int n_tokens, int max_ctx, int max_q, int n_q_heads, int n_kv_heads) {
-  return static_cast<int64_t>(max_q) * (n_q_heads / n_kv_heads) <= kCols && n_kv_heads <= kMaxKvHeads &&
+bool attn_weights_few(int n_tokens, int max_ctx, int max_q, int n_q_heads, int n_kv_heads, int head_dim) {
+  return static_cast<int64_t>(max_q) * (n_q_heads / n_kv_heads) <= (head_dim > 128 ? kCols : kColsHeads) &&
+         n_kv_heads <= kMaxKvHeads &&
          static_cast<size_t>(n_tokens) * n_q_heads * max_ctx <= kScoreBytes / sizeof(float);
 }
 

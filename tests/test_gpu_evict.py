@@ -95,6 +95,10 @@ WEIGHTS = [
     ([40 + i for i in range(70)], [1 + i % 4 for i in range(70)], 16, 14, 2, 64),
     ([20000], [4], 16, 32, 4, 128),
     ([300 + i for i in range(80)], [1 + i % 2 for i in range(80)], 16, 16, 1, 576),
+    ([2500, 900, 64], [3, 2, 1], 32, 16, 1, 576),            # 48, 32 and 16 of 64 vectors
+    ([900, 31], [1, 1], 16, 64, 1, 320),
+    ([100 + 5 * i for i in range(90)], [1 + i % 4 for i in range(90)], 16, 16, 1, 576),
+    ([700, 90], [1, 1], 16, 65, 1, 576),
 ]
 
 
