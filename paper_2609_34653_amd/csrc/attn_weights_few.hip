@@ -4,7 +4,7 @@
 // Mathematics: as attn_weights.hip.  Bound by memory: 2 d bytes of a key serve that many vectors.  So the scores
 // of the one pass over the keys are kept (4 bytes per query head and key, at most half of the keys' bytes for d >= 128),
 // beside each vector's running reference and sum per share; a second kernel joins the sums of the shares and
-// sums exp2(x - m) / l over the vectors, a key per thread.
+// sums exp2(x - m) / l over the vectors, four keys a lane.
 //   shares    as in paged decode: the 16-key blocks of all sequences with tokens, one after the other, cut into
 //             equal shares, one per workgroup and KV head, a fixed cost counted for each sequence.
 //   waves     each takes every fourth block of its workgroup's part and owns a ring of LDS buffers filled by
