@@ -11,9 +11,9 @@
 //             one of a step's two tiles of keys, and holds one half of the output's dimensions for both:
 //             its queries take 144 of 512 registers for R = 512, its half of the output 128 (all of it would
 //             take every accumulation register, and tiles of 16 vectors read twice as much), and the pair reads
-//             no row of keys twice.  What crosses between the two are the probabilities, 2 KB per wave and step.
+//             no row of keys twice.  What crosses between the two are the probabilities, 4 KB per wave and step.
 //             A pair without vectors only loads (up to 32 vectors of a sequence; a kernel of 16 vectors per wave
-//             and key groups of waves for those was no faster: 24 x 32 vectors 42 us, this one 40).
+//             and key groups of waves for those was no faster for 24 x 32 vectors, where alone it was timed).
 //   maximum   the pair's reference is moved for both at once: a wave whose probabilities outgrow it raises a flag
 //             beside them, and then all four waves exchange their maxima and rescale (as in the first step, and
 //             hardly ever after).
@@ -27,11 +27,15 @@
 //             as if they were the step behind the first.
 //   products  S^T (32 keys x 32 vectors) = K Q^T and O^T (32 dims x 32 vectors) = C^T P^T with
 //             v_mfma_f32_32x32x16_bf16; keys are permuted when K rows are read so that S^T is the operand of
-//             the second product as it stands.  Probabilities are rounded to bf16 for it, and summed as rounded.
-//   measured  24 x 128 vectors over 119,095 rows of 576 in all: 53 us and 10 us for the merge (33 GFLOP, matrix cores
-//             busy 0.33; 2.5 us for a step of 64 keys, of which the products take 1.1; the start of a part takes 5
-//             us and its end 4, which writes 37 MB).  16 vectors per wave, with all of the dimensions, took 71 us.
-//             16 vectors over 16,948 rows: 14.5 and 7 us, all of it latency (pages, first keys, two steps, parts).
+//             the second product as it stands.  Each probability enters it as its bf16 rounding and the rounding of
+//             the remainder (16 significant bits, as in paged decode); the sum takes the same two.  Rounded to bf16
+//             once, float outputs were off by 1e-3 of themselves and bf16 ones by a fifth more than their own
+//             rounding, for 53 us in place of 64 below (14.7 in place of 15.9 for 16 vectors).  The roundings cross
+//             before the value products; the remainders, for which no LDS is left, in their middle, in the part of
+//             the keys that the values do not have.
+//   measured  24 x 128 vectors over 119,095 rows of 576 in all: 64 us and 10 us for the merge (33 GFLOP, 49 executed;
+//             matrix cores busy 0.40; the start of a part takes 5 us and its end 4, which writes 37 MB).
+//             16 vectors over 16,948 rows: 15.9 and 7 us, all of it latency (pages, first keys, two steps, parts).
 #include "common.h"
 #include "latent.h"
 #include "mfma_tile.h"
@@ -44,8 +48,9 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kRow = 32;                 // vectors of a tile
 constexpr int kGroup = 2 * kRow;         // of a workgroup
-constexpr int kOverhead = 10;            // what a sequence costs beside its blocks, in blocks (24 x 128 vectors: 59 us
-                                         //   with 4, 55 with 6, 52 to 53 with 9 to 12, 54 with 16)
+constexpr int kOverhead = 10;            // what a sequence costs beside its blocks, in blocks (24 x 128 vectors, their
+                                         //   probabilities rounded once: 59 us with 4, 55 with 6, 52 to 53 with 9 to
+                                         //   12, 54 with 16)
 constexpr int kKT = 32;                  // keys per tile and block
 constexpr int kStep = 2;                 // tiles per step
 constexpr int kWGs = 256;                // shares of a large call: one workgroup per CU
@@ -111,6 +116,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(
   static_assert(ROWB % 128 == 0 && (ROWB / 128) % 2 == 1, "the swizzle's banks");
   static_assert(kStep == 2, "a tile for each wave of a pair");
   static_assert(KS == 2 * OCTS * LOADS, "a load after every other product");
+  static_assert(2 * 8 * kLatentRope == kWave * 16, "a row's rotated part holds a remainder of eight lanes");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStep * TILEB];
   __shared__ __attribute__((aligned(16))) u32x4 sp[kWaves][2][kWave];   // probabilities
   __shared__ __attribute__((aligned(16))) int sflag[kWaves];
@@ -338,6 +344,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(
           __syncthreads();
           __syncthreads();
         }
+        __syncthreads();                     // (the remainders)
         continue;
       }
       const uint32_t tiles = lds0 + static_cast<uint32_t>((t & 1) * kStep * TILEB);
@@ -400,22 +407,27 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(
         for (int i = 0; i < 16; ++i)
           if (key0 + 16 * (lane_now() >> 5) + i > last) s[i] = -INFINITY;
       }
-      bf16x8 p[2];
-      float ls = 0.f;
+      bf16x8 p[2], pr[2];                    // probabilities, and what is left of them
+      const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+      float ls, ls1;
+      auto put = [&](int i, float e0, float e1) __attribute__((always_inline)) {
+        const bf16x2 e = {static_cast<__bf16>(e0), static_cast<__bf16>(e1)};
+        const bf16x2 r = {static_cast<__bf16>(e0 - static_cast<float>(e[0])),
+                          static_cast<__bf16>(e1 - static_cast<float>(e[1]))};
+        p[i >> 3][i & 7] = e[0];
+        p[i >> 3][(i & 7) + 1] = e[1];
+        pr[i >> 3][i & 7] = r[0];
+        pr[i >> 3][(i & 7) + 1] = r[1];
+        ls = __builtin_amdgcn_fdot2_f32_bf16(e, one2, ls, false);
+        ls1 = __builtin_amdgcn_fdot2_f32_bf16(r, one2, ls1, false);
+      };
+      ls = ls1 = 0.f;
       bool move = t == 0;
       if (!move) {
-        float ls1 = 0.f;
-        const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const bf16x2 e = {
-              static_cast<__bf16>(__builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -m_run))),
-              static_cast<__bf16>(__builtin_amdgcn_exp2f(fmaf(s[i + 1], scale_log2, -m_run)))};
-          p[i >> 3][i & 7] = e[0];
-          p[i >> 3][(i & 7) + 1] = e[1];
-          if (i & 2) ls1 = __builtin_amdgcn_fdot2_f32_bf16(e, one2, ls1, false);
-          else ls = __builtin_amdgcn_fdot2_f32_bf16(e, one2, ls, false);
-        }
+        for (int i = 0; i < 16; i += 2)
+          put(i, __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -m_run)),
+              __builtin_amdgcn_exp2f(fmaf(s[i + 1], scale_log2, -m_run)));
         ls += ls1;
         const bool over = __any(!(ls < kSumLimit));
         sp[wave][0][lane] = __builtin_bit_cast(u32x4, p[0]);
@@ -443,31 +455,51 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(
           asm volatile("" : "+a"(o[dt]));
         }
         m_run = m_new;
-        ls = 0.f;
+        ls = ls1 = 0.f;
+        auto weight = [&](float x) __attribute__((always_inline)) {
+          return x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x, scale_log2, -m_use));
+        };
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const __bf16 e = static_cast<__bf16>(
-              s[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -m_use)));
-          p[i >> 3][i & 7] = e;
-          ls += static_cast<float>(e);
-        }
+        for (int i = 0; i < 16; i += 2) put(i, weight(s[i]), weight(s[i + 1]));
+        ls += ls1;
         sp[wave][0][lane] = __builtin_bit_cast(u32x4, p[0]);
         sp[wave][1][lane] = __builtin_bit_cast(u32x4, p[1]);
         __syncthreads();
       }
       l_run += ls;
+      // The remainders cross in the rotated parts of the step's keys, which no wave reads any more (the scores of all
+      // are behind the barrier): in rows 16 vt on of the tile that they are of, eight lanes to a row.
+      typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+      const int lr = lane_now();
+      const uint32_t rest = ROWB * (16 * vt + (lr >> 3)) + 2u * R + 16u * (lr & 7);
+      *reinterpret_cast<lds_u32x4*>(mine + rest) = __builtin_bit_cast(u32x4, pr[0]);
+      *reinterpret_cast<lds_u32x4*>(mine + rest + 8u * ROWB) = __builtin_bit_cast(u32x4, pr[1]);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) asm volatile("" : "+a"(o[dt]));
       bf16x8 po[2];                          // the other wave's
       po[0] = __builtin_bit_cast(bf16x8, sp[wave ^ 1][0][lane]);
       po[1] = __builtin_bit_cast(bf16x8, sp[wave ^ 1][1][lane]);
-#pragma unroll
-      for (int j = 0; j < 4 * DT; ++j) {
+      // each operand of the values meets the probabilities and their remainders
+      auto values = [&](int j, const bf16x8(&hi)[2], const bf16x8(&lo)[2]) __attribute__((always_inline)) {
         if (j + kAhead < 4 * DT) op[(j + kAhead) % kOps] = vop(j + kAhead);
         const int c = j / DT % 2;
-        o[j % DT] = mfma(op[j % kOps], j < 2 * DT ? p[c] : po[c], o[j % DT]);
+        o[j % DT] = mfma(op[j % kOps], hi[c], o[j % DT]);
+        o[j % DT] = mfma(op[j % kOps], lo[c], o[j % DT]);
         __builtin_amdgcn_sched_barrier(0);
+      };
+#pragma unroll
+      for (int j = 0; j < DT; ++j) values(j, p, pr);
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");     // the remainders are there
+      bf16x8 por[2];
+      {
+        const uint32_t other = tiles + static_cast<uint32_t>((hf ^ 1) * TILEB) + rest;
+        por[0] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const lds_u32x4*>(other));
+        por[1] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const lds_u32x4*>(other + 8u * ROWB));
       }
+#pragma unroll
+      for (int j = DT; j < 2 * DT; ++j) values(j, p, pr);
+#pragma unroll
+      for (int j = 2 * DT; j < 4 * DT; ++j) values(j, po, por);
     }
 
     // The pair's sums; a sum that is no number (of a bad page, or of keys that are none) spoils the vector to the

@@ -5,7 +5,7 @@ Tolerances, per element:
   append  as tests/test_gpu_norm_rope.py: half a step of the output plus 2^-19 of the normed pair's length
           (the sum of 512 squares is 14 roundings deep, halved by the root: 13 x 2^-24 with the rest)
   attention, with S = sum_j p_j |v_j| + |out|:
-          2^-8 S (each probability rounded to bf16 once, half a step; the sum uses the rounded ones)
+          2^-8 S (that of probabilities rounded to bf16 once; they keep 16 bits, whose tests stand further down)
           + 2^-10 S (absorbed) or 2^-11 S (expanded) for the scores: products of bf16 are exact in float, the sum
           of d of them is off by at most d 2^-24 sum|q k|; sum|q k| scale <= 20 on these inputs, so a
           probability by 576 x 20 x 2^-24 = 2^-10.5 (192: 2^-12.1); the exponential and the sums add 2^-18
@@ -712,3 +712,59 @@ def test_streams_and_captured_calls():
         torch.cuda.synchronize()
         for x, y in zip(got, (pool, rows, out, outc)):
             assert torch.equal(x, y)
+
+
+# ------------------------------------------------------------------- probabilities of 16 bits
+#
+# Scores are whole numbers, exact in float, so what is left is, with S as above:
+#   2^-16 S    each probability entered as its bf16 rounding and that of the remainder: half a step of half a step
+#   2^-16 S    the exponential's argument, |x| log2(e) <= 110 on these inputs with the scale's and the fused product's
+#              roundings: 110 x 1.5 x ln 2 x 2^-23 = 2^-16.2, and 2^-22 of the exponential
+#   2^-15 S    sums of up to 300 products in float, above and below the line: 2 x 300 x 2^-24 = 2^-14.8 at most
+# below 2^-14 S together; probabilities rounded to bf16 once are off by up to 2^-8 S.
+
+def close_bits(got, want, spread):
+    err = np.abs(f64(got) - want)
+    assert np.isfinite(f64(got)).all()
+    assert (err <= 2.0 ** -14 * spread).all(), float((err / np.maximum(spread, 1e-30)).max())
+
+
+def whole_parts(seed, n, rise):
+    """Rotated parts [n, 64] of whole numbers; rising ones move the reference in the middle of a part."""
+    e = torch.randint(-2, 3, (n, E), generator=torch.Generator().manual_seed(seed)).float()
+    if rise:
+        e[:, 0] = torch.arange(n) // 8
+    return e
+
+
+def whole_queries(seed, shape, rise):
+    q = torch.randint(-2, 3, (*shape, E), generator=torch.Generator().manual_seed(seed)).float()
+    if rise:
+        q[..., 0] = 8.0
+    return q
+
+
+@pytest.mark.parametrize("rise", [False, True])
+@pytest.mark.parametrize("ctx,nq,H,R", [
+    ([1, 2, 3, 40, 0, 300], 1, 16, 512),
+    ([5, 37, 129, 290], 2, 20, 256),                         # both tiles of vectors
+    ([260, 9], 1, 128, 512),                                 # two row groups
+    ([7 + 3 * i for i in range(70)], 1, 4, 512),
+])
+def test_decode_probabilities_keep_16_bits(ctx, nq, H, R, rise):
+    P = 16
+    table, n_pages = layout(ctx, P, H)
+    pool = pool_of(ctx, table, n_pages, P, R + E, H)
+    q = torch.cat([torch.zeros(len(ctx), nq, H, R), whole_queries(H, (len(ctx), nq, H), rise)], -1).to(BF)
+    for s, n in enumerate(ctx):
+        r = np.arange(n)
+        if n:
+            pool[table[s, r // P], r % P, R:] = whole_parts(s, n, rise).to(BF)
+    got, st = decode(q.cuda(), pool.cuda(), table, ctx, 0.125, F32)
+    assert st == 0
+    for s, n in enumerate(ctx):
+        if n == 0:
+            continue
+        rows = pool[table[s, np.arange(n) // P], np.arange(n) % P].double().numpy()
+        want, spread = ol.absorbed_attention(f64(q[s]), rows, R, 0.125)
+        close_bits(got[s], want, spread)
