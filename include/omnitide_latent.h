@@ -115,7 +115,8 @@ size_t omnitide_latent_decode_workspace_bytes(int n_seq, int n_q, int max_ctx, i
  *               omnitide_paged_chunk_attn
  * Device checks: OMNITIDE_E_PAGES for offsets of either kind that are out of order,
  * OMNITIDE_E_CAPACITY for a sequence with fewer rows than tokens (its outputs are then not written).
- * Tokens of no sequence: as in a padded batch.  Numerics as omnitide_paged_chunk_attn.  head_dim is 64 or
+ * Tokens of no sequence: as in a padded batch.  Numerics as omnitide_latent_decode_attn (probabilities with
+ * 16 significant bits, whichever out_dtype: omnitide_paged_chunk_attn has 8).  head_dim is 64 or
  * 128 (keys and values alike); n_heads <= 4096, n_seq <= 1024, n_rows <= 2^27, n_rows * n_heads <= 2^34,
  * n_tokens * n_heads <= 2^28; strides are multiples of 8, at least the widths of what they step over and at
  * most 2^24; |scale| <= 1e30.

@@ -7,11 +7,17 @@
 // Bound by the matrix cores, as paged_chunk.hip, whose form it has (row tiles of 256 query rows of a head, the
 // shares of chunk_plan.h, steps of 32 keys with the softmax of this step between the score products of
 // the next and the value products of the last).  What differs: a key's scores take (d + 64) / 16 products of
-// 32 keys, its values d / 16, so a step has slots with one product and slots with two; rows are contiguous in
-// the caller's tensors, at strides of their own; the wider keys leave LDS for rings of three tiles (K 24 KB,
-// V 16 KB for d = 128), asked for one tile ahead.  665 tokens over 17,048 keys, 16 heads of 128: 128 us and 8 us for
-// the merge (114 GFLOP, 0.89 PFLOP/s; matrix cores busy 0.49, as in paged_chunk.hip, at the clock that power
-// allows); 89 over 601, 4 heads of 64: 9.2 and 3 us, latency.
+// 32 keys, its values two for each of d / 16 operands, so a step has slots with one product and slots with three; rows
+// are contiguous in the caller's tensors, at strides of their own; the wider keys leave LDS for rings of three tiles
+// (K 24 KB, V 16 KB for d = 128), asked for one tile ahead.
+//
+// Each probability enters the value products as its bf16 rounding and the rounding of the remainder (16 significant
+// bits, as in paged decode and the absorbed form, so that both forms of one cache agree); the sum takes the same two.
+// Rounded once, as paged_chunk.hip does, a float output was off by 1.5e-3 of itself and a bf16 one by a third more
+// than its own rounding, for 131 us a call in place of 171 (665 tokens over 17,048 keys, 16 heads of 128).
+//
+// Those 171 us, 8 of them the merge: 114 GFLOP, 159 executed (0.67 and 0.93 PFLOP/s; matrix cores busy 0.51, as in
+// paged_chunk.hip, at the clock that power allows); 89 tokens over 601, 4 heads of 64: 13.5 us, latency.
 #include <type_traits>
 
 #include "chunk_plan.h"
@@ -55,6 +61,25 @@ struct Tile {
   static constexpr int kChunks = D / 8;                             // 16-byte chunks per row
   static constexpr int kCalls = kElems / 8 / kWave / kWaves;        // direct loads per wave
   static constexpr int kCallKeys = kWave / kChunks;                 // keys of one load
+};
+
+// A lane's probabilities of 32 keys, 16 of them, as the value products take them: each rounded to bf16, and what that
+// leaves of it rounded likewise (16 bits together).
+struct Probs {
+  bf16x8 hi[2], lo[2];
+  // numbers i and i + 1, and their part of the sum: of what the products take
+  __device__ inline void put(int i, float e0, float e1, float (&sum)[2]) {
+    const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+    const bf16x2 e = {static_cast<__bf16>(e0), static_cast<__bf16>(e1)};
+    const bf16x2 r = {static_cast<__bf16>(e0 - static_cast<float>(e[0])),
+                      static_cast<__bf16>(e1 - static_cast<float>(e[1]))};
+    hi[i >> 3][i & 7] = e[0];
+    hi[i >> 3][(i & 7) + 1] = e[1];
+    lo[i >> 3][i & 7] = r[0];
+    lo[i >> 3][(i & 7) + 1] = r[1];
+    sum[0] = __builtin_amdgcn_fdot2_f32_bf16(e, one2, sum[0], false);
+    sum[1] = __builtin_amdgcn_fdot2_f32_bf16(r, one2, sum[1], false);
+  }
 };
 
 // SEQS: sequences at most.
@@ -198,11 +223,11 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void latent_chunk_kernel(
 
     floatx16 o[D / 32];
     floatx16 sA = floatx16{}, sB;          // scores of 32 keys, current and next in turn
-    bf16x8 pA[2], pB[2];                   // probabilities of 32 keys: the operand of the products
+    Probs pA, pB;                          // probabilities of 32 keys: the operands of the products
     float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) o[dt] = floatx16{};
-    pB[0] = pB[1] = bf16x8{};
+    pB.hi[0] = pB.hi[1] = pB.lo[0] = pB.lo[1] = bf16x8{};
     // A step has a slot per K operand; NV of them multiply a V operand too.
     constexpr int NS = NK;
     // Operands read ahead, and their registers.  The next step's first ones are read after the ring
@@ -261,11 +286,9 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void latent_chunk_kernel(
       // second step the first halves of the next tile's keys and this one's values: dk and dv bytes
       // from the tiles before.  `middle` is called half-way.  (The first step's p_prev are zeros; the
       // last one's next scores are of stale keys and not used.)
-      const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
       bf16x8 ka[kOps], va[kOps];
-      auto step = [&](auto second, floatx16& s_cur, floatx16& s_nxt, bf16x8(&p_prev)[2],
-                      bf16x8(&p_cur)[2], uint32_t dk, uint32_t dv, int key0,
-                      auto middle) __attribute__((always_inline)) {
+      auto step = [&](auto second, floatx16& s_cur, floatx16& s_nxt, Probs& p_prev, Probs& p_cur, uint32_t dk,
+                      uint32_t dv, int key0, auto middle) __attribute__((always_inline)) {
         // operand j of this step and, from NS (NV) on, of the next one
         auto next_k = [&](int j) __attribute__((always_inline)) {
           const bool on = decltype(second)::value == (j < NS);     // of a new tile
@@ -292,7 +315,8 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void latent_chunk_kernel(
           if (has_v(i)) {
             const int j = v_index(i);
             const bf16x8 vc = va[j % kOps];
-            o[j % (D / 32)] = mfma(vc, p_prev[j / (D / 32)], o[j % (D / 32)]);
+            o[j % (D / 32)] = mfma(vc, p_prev.hi[j / (D / 32)], o[j % (D / 32)]);
+            o[j % (D / 32)] = mfma(vc, p_prev.lo[j / (D / 32)], o[j % (D / 32)]);
             va[(j + kAhead) % kOps] = next_v(j + kAhead);
           }
           __builtin_amdgcn_sched_barrier(0);
@@ -301,19 +325,14 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void latent_chunk_kernel(
             constexpr int EPS = 16 / NV;
 #pragma unroll
             for (int at = v_index(i) * EPS; at < (v_index(i) + 1) * EPS; at += 2) {
-              const float e0 = __builtin_amdgcn_exp2f(fmaf(s_cur[at], scale_log2, -m_run));
-              const float e1 = __builtin_amdgcn_exp2f(fmaf(s_cur[at + 1], scale_log2, -m_run));
-              const bf16x2 pr = {static_cast<__bf16>(e0), static_cast<__bf16>(e1)};
-              p_cur[at >> 3][at & 7] = pr[0];
-              p_cur[at >> 3][(at & 7) + 1] = pr[1];
-              ls[(at >> 1) & 1] =
-                  __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ls[(at >> 1) & 1], false);
+              p_cur.put(at, __builtin_amdgcn_exp2f(fmaf(s_cur[at], scale_log2, -m_run)),
+                        __builtin_amdgcn_exp2f(fmaf(s_cur[at + 1], scale_log2, -m_run)), ls);
             }
           }
           __builtin_amdgcn_sched_barrier(0);
           if (i == NS / 2 - 1) {
             // (the first half's softmax is not to be put off to behind the branches in there)
-            asm volatile("" : "+v"(p_cur[0]), "+v"(ls[0]), "+v"(ls[1]));
+            asm volatile("" : "+v"(p_cur.hi[0]), "+v"(p_cur.lo[0]), "+v"(ls[0]), "+v"(ls[1]));
             middle();
           }
         }
@@ -332,15 +351,13 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void latent_chunk_kernel(
 #pragma unroll
           for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
           m_run = m_new;
-          lsum = 0.f;
+          ls[0] = ls[1] = 0.f;
+          auto weight = [&](float sx) __attribute__((always_inline)) {
+            return sx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(sx, scale_log2, -m_use));
+          };
 #pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            const float sx = s_cur[x];
-            const __bf16 p = static_cast<__bf16>(
-                sx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(sx, scale_log2, -m_use)));
-            p_cur[x >> 3][x & 7] = p;
-            lsum += static_cast<float>(p);
-          }
+          for (int x = 0; x < 16; x += 2) p_cur.put(x, weight(s_cur[x]), weight(s_cur[x + 1]), ls);
+          lsum = ls[0] + ls[1];
         }
         l_run += lsum;
       };
@@ -385,7 +402,8 @@ __global__ __launch_bounds__(kThreads, kWaves / 4) void latent_chunk_kernel(
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const bf16x8 vc = vop(j, 1);
-        o[j % (D / 32)] = mfma(vc, pB[j / (D / 32)], o[j % (D / 32)]);
+        o[j % (D / 32)] = mfma(vc, pB.hi[j / (D / 32)], o[j % (D / 32)]);
+        o[j % (D / 32)] = mfma(vc, pB.lo[j / (D / 32)], o[j % (D / 32)]);
       }
     };
     if (alone) run(std::true_type{});

@@ -768,3 +768,23 @@ def test_decode_probabilities_keep_16_bits(ctx, nq, H, R, rise):
         rows = pool[table[s, np.arange(n) // P], np.arange(n) % P].double().numpy()
         want, spread = ol.absorbed_attention(f64(q[s]), rows, R, 0.125)
         close_bits(got[s], want, spread)
+
+
+@pytest.mark.parametrize("rise", [False, True])
+@pytest.mark.parametrize("ctx,new,H,d", [
+    ([1, 2, 3, 40, 300], [1, 2, 3, 7, 30], 4, 128),
+    ([290, 129], [1, 129], 5, 64),
+    ([280], [280], 16, 128),
+])
+def test_chunk_probabilities_keep_16_bits(ctx, new, H, d, rise):
+    start, rows = np.concatenate([[0], np.cumsum(new)]), np.concatenate([[0], np.cumsum(ctx)])
+    T, N = int(start[-1]), int(rows[-1])
+    kv = rand(H, N, H, 2 * d).to(BF)
+    kr = torch.cat([whole_parts(s, n, rise) for s, n in enumerate(ctx)]).to(BF)
+    q = torch.cat([torch.zeros(T, H, d), whole_queries(H, (T, H), rise)], -1).to(BF)
+    got, st = chunk(q.cuda(), kv.cuda(), kr.cuda(), start, rows, 0.125, F32)
+    assert st == 0
+    for s in range(len(ctx)):
+        r, t = slice(rows[s], rows[s + 1]), slice(start[s], start[s + 1])
+        want, spread = ol.expanded_attention(f64(q[t]), f64(kv[r, :, :d]), f64(kv[r, :, d:]), f64(kr[r]), 0.125)
+        close_bits(got[t], want, spread)
