@@ -693,3 +693,41 @@ def test_captured_step():
         for x, y in zip(got, (w, src, new, pool, vp)):
             assert torch.equal(x, y)
     assert int(st.item()) == 0
+
+
+# ----------------------------------------------------------------------- promises of the headers
+
+@pytest.mark.parametrize("m", [2, 40])
+@pytest.mark.parametrize("scale", [-0.05, 0.0])
+def test_weights_scales(m, scale):
+    ctx, P, hq, hkv, d = [300, 77], 16, 8, 2, 64
+    table, n_pages = layout(ctx, P, 1)
+    pool = key_pool(ctx, table, n_pages, P, hkv, d, 3)
+    q = rand(4, 2 * m, hq, d).to(BF)
+    got, st = weights(q.cuda(), pool.cuda(), table, [0, m, 2 * m], ctx, m, scale)
+    assert st == 0
+    for s, n in enumerate(ctx):
+        k = pool[table[s, np.arange(n) // P], np.arange(n) % P].double().numpy()
+        w = oe.row_weights(f64(q[s * m:(s + 1) * m]), k, scale)
+        assert (np.abs(f64(got[s, :n]) - w) <= tolerance(d) * w).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (16, 1, 576)])
+@pytest.mark.parametrize("m", [2, 70])
+@pytest.mark.parametrize("row", [3, 120, 231])
+def test_weights_beside_a_key_that_is_no_number(m, row, hq, hkv, d):
+    """Every row that a token sees beside it is NaN; what no such token sees, and the other sequences, are right."""
+    ctx, P = [232, 150, 90], 16
+    table, n_pages = layout(ctx, P, 1)
+    pool = key_pool(ctx, table, n_pages, P, hkv, d, 3)
+    pool[table[0, row // P], row % P, hkv - 1, 5] = float("nan")
+    q = (rand(4, 3 * m, hq, d) * spread_of(d)).to(BF)
+    gpool = pool.cuda() if d <= 128 else pool.cuda().view(n_pages, P, d)
+    got, st = weights(q.cuda(), gpool, table, [0, m, 2 * m, 3 * m], ctx, m, scale_of(d))
+    assert st == 0
+    assert torch.isnan(got[0, :232]).all() and (got[0, 232:] == 77.0).all()      # (the last token sees all)
+    for s in (1, 2):
+        n = ctx[s]
+        k = pool[table[s, np.arange(n) // P], np.arange(n) % P].double().numpy()
+        w = oe.row_weights(f64(q[s * m:(s + 1) * m]), k, scale_of(d))
+        assert (np.abs(f64(got[s, :n]) - w) <= tolerance(d) * w).all()

@@ -788,3 +788,36 @@ def test_chunk_probabilities_keep_16_bits(ctx, new, H, d, rise):
         r, t = slice(rows[s], rows[s + 1]), slice(start[s], start[s + 1])
         want, spread = ol.expanded_attention(f64(q[t]), f64(kv[r, :, :d]), f64(kv[r, :, d:]), f64(kr[r]), 0.125)
         close_bits(got[t], want, spread)
+
+
+# ----------------------------------------------------------------------- promises of the headers
+
+@pytest.mark.parametrize("scale", [-0.05, 0.0])
+def test_chunk_scales(scale):
+    n, m, H, d = [300, 40], [70, 40], 4, 64
+    start, rows = [0, 70, 110], [0, 300, 340]
+    kv, kr, q = rand(1, 340, H, 2 * d).to(BF), rand(2, 340, E).to(BF), rand(3, 110, H, d + E).to(BF)
+    got, st = chunk(q.cuda(), kv.cuda(), kr.cuda(), start, rows, scale, F32)
+    assert st == 0
+    for s in range(2):
+        r, t = slice(rows[s], rows[s + 1]), slice(start[s], start[s + 1])
+        want, spread = ol.expanded_attention(f64(q[t]), f64(kv[r, :, :d]), f64(kv[r, :, d:]), f64(kr[r]), scale)
+        near(got[t], want, spread, 2.0 ** -11, F32)
+
+
+def test_append_with_offsets_out_of_order():
+    """Tokens that lie in the offsets of a sequence go to their rows there, each once; no other row changes."""
+    from paper_2609_34653_amd import latent as la, paged as pg
+    ctx, P, R, start = [40, 33, 20], 16, 256, [0, 5, 3, 12]
+    kv = rand(1, 12, R + E).to(BF).cuda()
+    table, n_pages = layout(ctx, P, 3)
+    pool = torch.full((n_pages, P, R + E), 9.0, dtype=BF, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    la.omnitide_latent_append(kv[:, :R], kv[:, R:], pool, i32(table), i32(start), i32(ctx), d_status=st)
+    assert int(st.item()) == pg.E_PAGES
+    want = torch.full_like(pool, 9.0)
+    for t in range(12):
+        s = 0 if t < 5 else 2                                # the first sequence whose offsets hold the token
+        r = ctx[s] - (start[s + 1] - t)
+        want[int(table[s, r // P]), r % P] = kv[t]
+    assert torch.equal(pool, want)
