@@ -108,14 +108,14 @@ __device__ inline void report_weights(const AttnWeightsArgs& a) {
   if (__any(bad) && (threadIdx.x & (kWave - 1)) == 0) set_status(a.d_status, OMNITIDE_E_CAPACITY);
 }
 
-// What a call's passes hand on.  seqs: every sequence's first token, tokens (0: none, or malformed) and
-// context; part: (m, l) of each key chunk, KV head and query row; stats: (m, 1 / l) of each KV head and query
-// row (a sequence's rows are token by token the KV head's G query heads).
+// What a call's passes hand on.  seqs: every sequence's first token, tokens (0: none, or malformed),
+// context and the row chunks of those in front of it; part: (m, l) of each key chunk, KV head and query row; stats:
+// (m, 1 / l) of each KV head and query row (a sequence's rows are token by token the KV head's G query heads).
 struct WeightsWork {
   int4* seqs;
   float2* part;
   float2* stats;
-  float* sums;                           // [row chunk][KV head][sequence][max_ctx]
+  float* sums;                           // [row chunk, of all sequences][KV head][max_ctx]
   int chunk_keys, row_chunk;             // keys of an item of the first pass, query rows of one of the second
 };
 
@@ -174,9 +174,11 @@ __device__ inline int first_item() {
 }
 
 // Every sequence into LDS, by the whole workgroup: one that starts in front of an earlier offset has no tokens, nor
-// has one with more than max_q, or with fewer rows than tokens.
+// has one with more than max_q, or with fewer rows than tokens.  The row chunks in front of it are those of its 64
+// sequences; in_64: all of each 64.
 template <int SEQS>
-__device__ inline void read_seqs(const AttnWeightsArgs& a, int4 (&seqs)[SEQS]) {
+__device__ inline void read_seqs(const AttnWeightsArgs& a, int row_chunk, int4 (&seqs)[SEQS],
+                                 int (&in_64)[SEQS / kWave]) {
   const PagedBatch& b = a.batch;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(static_cast<int>(threadIdx.x / kWave));
   const int cap = b.max_pages << b.page_shift, chunks = (b.n_seq + kWave - 1) / kWave;
@@ -192,7 +194,10 @@ __device__ inline void read_seqs(const AttnWeightsArgs& a, int4 (&seqs)[SEQS]) {
     for (int j = lane; j < c * kWave; j += kWave) before = max(before, b.q_start[j]);
     front = max(front, wave_max_i32(before));
     const bool ok = s0 >= front && s1 > s0 && s1 <= b.n_tokens && s1 - s0 <= a.max_q && n >= s1 - s0 && n <= cap;
-    seqs[i] = make_int4(s0, ok ? s1 - s0 : 0, n, 0);
+    const int len = ok ? s1 - s0 : 0, mine = (len * (a.n_q_heads / a.n_kv_heads) + row_chunk - 1) / row_chunk;
+    const int inc = wave_scan_add_i32(mine);
+    seqs[i] = make_int4(s0, len, n, inc - mine);
+    if (lane == kWave - 1) in_64[c] = inc;
   }
   __syncthreads();
 }
@@ -213,6 +218,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void 
   constexpr float kSumLimit = 4294967296.f;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kRing * S::kBytes];
   __shared__ int4 seqs[SEQS];
+  __shared__ int chunks_in_64[SEQS / kWave];
   __shared__ Items<SEQS> items;
   const PagedBatch& b = a.batch;
   const int tid = threadIdx.x;
@@ -222,9 +228,14 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void 
   const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
 
   if (blockIdx.x == 0 && wave == 0) report_weights(a);
-  read_seqs(a, seqs);
-  if (blockIdx.x == 0)
-    for (int i = tid; i < b.n_seq; i += kThreads) ws.seqs[i] = seqs[i];
+  read_seqs(a, ws.row_chunk, seqs, chunks_in_64);
+  if (blockIdx.x == 0) {
+    for (int i = tid; i < b.n_seq; i += kThreads) {
+      int4 q = seqs[i];
+      for (int c = 0; c < i / kWave; ++c) q.w += chunks_in_64[c];
+      ws.seqs[i] = q;
+    }
+  }
   const int64_t total = items.make(b.n_seq, [&](int i) {
     const int4 q = seqs[i];
     if (q.y == 0) return int64_t{0};
@@ -548,7 +559,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? kWaves / 2 : kWaves / 4) void 
       }
       wait_vmcnt<0>();
       // over the 32 rows of a half, in a fixed order; lane e of half h then stores key e % 4 + 8 (e / 4) + 4 h
-      float* out = ws.sums + ((static_cast<size_t>(rc) * Hkv + g) * b.n_seq + s) * max_ctx;
+      float* out = ws.sums + (static_cast<size_t>(uniform(sq.w) + rc) * Hkv + g) * max_ctx;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         float v = acc[e];
@@ -575,15 +586,14 @@ __global__ __launch_bounds__(kSumThreads) void weights_add_kernel(const AttnWeig
   const int rc0 = first_row(tile * kItemKeys, kept, G) / ws.row_chunk, rc1 = (rows - 1) / ws.row_chunk;
   // [row chunk][KV head], eight of them on their way at once
   constexpr int kFlight = 8;
-  const int64_t first = static_cast<int64_t>(rc0) * a.n_kv_heads;
-  const int64_t last = (static_cast<int64_t>(rc1) + 1) * a.n_kv_heads - 1;
-  const size_t step = static_cast<size_t>(b.n_seq) * max_ctx;
-  const float* sums = ws.sums + static_cast<size_t>(s) * max_ctx + j;
+  const int64_t first = static_cast<int64_t>(q.w + rc0) * a.n_kv_heads;
+  const int64_t last = static_cast<int64_t>(q.w + rc1 + 1) * a.n_kv_heads - 1;
+  const float* sums = ws.sums + j;
   float sum = 0.f;
   for (int64_t i0 = first; i0 <= last; i0 += kFlight) {
     float x[kFlight];
 #pragma unroll
-    for (int i = 0; i < kFlight; ++i) x[i] = sums[static_cast<size_t>(min(i0 + i, last)) * step];
+    for (int i = 0; i < kFlight; ++i) x[i] = sums[static_cast<size_t>(min(i0 + i, last)) * max_ctx];
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) sum += i0 + i <= last ? x[i] : 0.f;
   }
@@ -620,7 +630,6 @@ Layout layout(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, in
   l.chunk_keys = static_cast<int>(((max_ctx + chunks - 1) / chunks + 63) / 64 * 64);
   const int64_t rows = (max_q < n_tokens ? max_q : n_tokens) * G;
   const int64_t key_items = static_cast<int64_t>((max_ctx + kItemKeys - 1) / kItemKeys) * n_kv_heads * n_seq;
-  auto row_chunks = [&](int64_t chunk) { return (rows + chunk - 1) / chunk; };
   l.row_chunk = kRowChunk;
   if (key_items <= wgs) {
     const int64_t n = wgs / key_items, chunk = ((rows + n - 1) / n + 63) / 64 * 64;
@@ -630,8 +639,13 @@ Layout layout(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, in
   l.part = n_seq * sizeof(int4);
   l.stats = l.part + most * vecs;
   l.sums = align16(l.stats + vecs);
-  // (with smaller chunks there are as many items of kItemKeys sums as workgroups at most)
-  const size_t sums = static_cast<size_t>(row_chunks(kRowChunk)) * n_kv_heads * n_seq * max_ctx;
+  // Row chunks of all sequences: at most as many of each as of the longest, and one for each beside those of all
+  // rows in one piece (a chunk of 4,096 tokens beside 1,023 single ones over 16,384 keys of 8 heads: 0.55 GB, not the
+  // 8.6 GB of as many chunks for all).  With smaller chunks there are as many items of kItemKeys sums as workgroups
+  // at most.
+  const int64_t seqs = n_seq < n_tokens ? n_seq : n_tokens;
+  const int64_t each = seqs * ((rows + kRowChunk - 1) / kRowChunk), piece = n_tokens * G / kRowChunk + seqs;
+  const size_t sums = static_cast<size_t>(each < piece ? each : piece) * n_kv_heads * max_ctx;
   const size_t few = static_cast<size_t>(wgs) * kItemKeys;
   l.bytes = l.sums + (sums > few ? sums : few) * sizeof(float);
   return l;

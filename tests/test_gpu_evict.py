@@ -695,6 +695,37 @@ def test_captured_step():
     assert int(st.item()) == 0
 
 
+# ------------------------------------------------------------------------------- mixed batches
+
+@pytest.mark.parametrize("hq,hkv,d,cap", [(16, 4, 64, 1 << 14), (16, 1, 320, 4096)])
+def test_weights_of_chunks_beside_single_tokens(hq, hkv, d, cap):
+    """Several row chunks of some sequences, one of most, none of a few; more sequences than are counted at once."""
+    new = [1] * 150
+    new[3], new[70], new[149] = 700, 300, 431
+    new[0], new[64], new[100] = 0, 0, 0
+    ctx = [max(m, 30 + 7 * i % 400) for i, m in enumerate(new)]
+    P = 16
+    table, n_pages = layout(ctx, P, 1)
+    wide = np.full((len(ctx), cap // P), -1)
+    wide[:, :table.shape[1]] = table
+    start = np.concatenate([[0], np.cumsum(new)])
+    pool = key_pool(ctx, table, n_pages, P, hkv, d, 1)
+    q = (rand(2, int(start[-1]), hq, d) * spread_of(d)).to(BF)
+    gpool = pool.cuda() if d <= 128 else pool.cuda().view(n_pages, P, d)
+    got, st = weights(q.cuda(), gpool, wide, start, ctx, 700, scale_of(d))
+    assert st == 0
+    for s, (n, m) in enumerate(zip(ctx, new)):
+        if m == 0:
+            assert (got[s] == 77.0).all()
+        elif m > 1 or s % 11 == 0:
+            k = pool[table[s, np.arange(n) // P], np.arange(n) % P].double().numpy()
+            w = oe.row_weights(f64(q[start[s]:start[s + 1]]), k, scale_of(d))
+            assert (np.abs(f64(got[s, :n]) - w) <= tolerance(d) * w).all()
+        else:
+            assert torch.isclose(got[s, :n].sum(), torch.tensor(float(hq)), rtol=1e-3)
+        assert (got[s, n:] == 77.0).all()
+
+
 # ----------------------------------------------------------------------- promises of the headers
 
 @pytest.mark.parametrize("m", [2, 40])

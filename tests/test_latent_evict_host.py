@@ -186,6 +186,14 @@ def test_weights_workspace():
         assert size(*bad) == 0
 
 
+def test_weights_workspace_of_mixed_batches():
+    """Partial sums are those of the tokens that there are, not of the longest chunk for every sequence."""
+    size = ev.omnitide_paged_attn_weights_workspace_bytes
+    # one chunk of 4,096 beside 1,023 single tokens: 16 + 1,023 row chunks of 8 heads of 16,384 sums
+    assert size(5119, 1024, 16384, 4096, 32, 8, 128) < (16 + 1023 + 3) * 8 * 16384 * 4 + (1 << 25)
+    assert size(2463, 64, 131072, 2400, 32, 8, 128) < (9 + 64 + 1) * 8 * 131072 * 4 + (1 << 25)
+
+
 def plan(L, **kw):
     a = dict(w=fake(0), ws=2000, ctx=fake(1), S=4, mc=1500, high=1000, budget=900, sink=4, recent=100,
              src=fake(2), ss=1000, new=fake(3), wo=fake(4), wos=1000, work=fake(5), wb=1 << 34, status=fake(6))
