@@ -28,15 +28,19 @@ extern "C" {
  *   k_pool      bf16 [n_pages][page_size][n_kv_heads][head_dim]; head_dim 64 or 128, or 320 or 576 with
  *               one KV head (a latent pool, with absorbed queries)
  *   max_q       the most tokens of one sequence in the call (a sequence with more: OMNITIDE_E_CAPACITY,
- *               as if its lengths were wrong)
+ *               as if its lengths were wrong).  It chooses the way of the whole call: with up to 32 query
+ *               vectors (max_q * n_q_heads / n_kv_heads; 64 of latents) the keys are read once, with more
+ *               twice, so a loose bound costs time, and single tokens beside a chunk are faster in a call of
+ *               their own.
  *   seen_len    int32 [n_seq]: rows that weight_in holds weights of (values outside [0, ctx_len] count as
  *               the nearer end), or NULL: all but the sequence's tokens of this call
  *   weight_in   or NULL: nothing accumulated yet (seen_len and decay are then ignored); may be weight_out
  *   weight_out  float [n_seq][weight_stride]: rows below ctx_len of sequences with tokens are written, the
  *               others left as they were
  *   workspace   device scratch of omnitide_paged_attn_weights_workspace_bytes() bytes, whose size
- *               never falls as n_tokens, n_seq or max_ctx grows; nothing in it is kept from call to call.
- *               Calls that overlap in time need a workspace each.
+ *               never falls as n_tokens, n_seq, max_ctx or max_q grows, so one for the largest of each
+ *               serves every call; nothing in it is kept from call to call.  Calls that overlap in time
+ *               need a workspace each.
  * The order of every sum is fixed by the call's arguments: equal calls give equal bits.  The weights of
  * the rows that a token sees beside one of a bad page (or a key of NaN) come out as NaN.
  * Numerics: bf16 products, all else in float.  Limits: n_q_heads a multiple of n_kv_heads, at most 4096;

@@ -690,16 +690,16 @@ hipError_t launch_d(const AttnWeightsArgs& a, hipStream_t stream) {
 
 size_t attn_weights_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads,
                                     int n_kv_heads, int head_dim) {
+  // the larger of both ways, so that a larger call's serves a smaller one: whatever max_q is, the call of fewer
+  // tokens per sequence may go the way of few
+  const size_t few = attn_weights_few_workspace_bytes(n_tokens, n_seq, max_ctx, max_q, n_q_heads, n_kv_heads, head_dim);
   const size_t n = layout(n_tokens, n_seq, max_ctx, max_q, n_q_heads, n_kv_heads, head_dim).bytes;
-  // (the larger of both ways where either may be taken, so that a larger call's serves a smaller one)
-  if (!attn_weights_few(1, 1, max_q, n_q_heads, n_kv_heads, head_dim)) return n;
-  const size_t few = attn_weights_few_workspace_bytes(n_tokens, n_seq, max_ctx, n_q_heads);
   return n > few ? n : few;
 }
 
 hipError_t launch_attn_weights(const AttnWeightsArgs& a, hipStream_t stream) {
   const int max_ctx = a.batch.max_pages << a.batch.page_shift;
-  if (attn_weights_few(a.batch.n_tokens, max_ctx, a.max_q, a.n_q_heads, a.n_kv_heads, a.head_dim))
+  if (attn_weights_few(a.batch.n_tokens, a.batch.n_seq, max_ctx, a.max_q, a.n_q_heads, a.n_kv_heads, a.head_dim))
     return launch_attn_weights_few(a, stream);
   switch (a.head_dim) {
     case 64: return launch_d<64>(a, stream);

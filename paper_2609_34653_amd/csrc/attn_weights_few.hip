@@ -17,6 +17,7 @@
 //   vectors   against the two passes: 24 x 8 tokens of 32 / 8 heads (32 vectors) 117 us, 137 there; 24 streams of
 //             latents with 32 heads 49 us, 97 there; with 64 heads 70 us, 105 there.  (More of them than that,
 //             and the scores outweigh the keys, or the queries the registers.)
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -45,10 +46,10 @@ template <int D>
 constexpr int wgs_of() { return D <= 128 ? kMaxWGs : kMaxWGs / 2; }
 
 // sequence i = 64 n + lane holds nb[n] blocks, work for kOverhead + nb[n] (none without blocks); first[n] is its KV
-// head's work before it, per_head all of it, `share` that of a workgroup.
+// head's work before it, per_head all of it, `share` that of a workgroup; rank[n]: the tokens of those in front of it.
 template <int NS>
 struct FewShares {
-  int nb[NS], first[NS], ctx[NS], q0[NS], len[NS];
+  int nb[NS], first[NS], ctx[NS], q0[NS], len[NS], rank[NS];
   int per_head, share;
 };
 
@@ -67,7 +68,7 @@ __device__ inline FewShares<NS> plan_few(const AttnWeightsArgs& a, int wgs) {
     s.ctx[n] = i < b.n_seq ? b.ctx_len[i] : -1;
   }
   s.per_head = 0;
-  int front = 0;
+  int front = 0, tokens = 0;
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
     const int q0 = s.q0[n], q1 = s.len[n];
@@ -81,6 +82,9 @@ __device__ inline FewShares<NS> plan_few(const AttnWeightsArgs& a, int wgs) {
     const int inc = wave_scan_add_i32(work);
     s.first[n] = s.per_head + inc - work;
     s.per_head += readlane(inc, kWave - 1);
+    const int upto = wave_scan_add_i32(s.len[n]);
+    s.rank[n] = tokens + upto - s.len[n];
+    tokens += readlane(upto, kWave - 1);
   }
   const int per = max(1, wgs / a.n_kv_heads);
   s.share = max(kMinShare, (s.per_head + per - 1) / per);
@@ -100,12 +104,14 @@ __device__ inline void wait_landed(int ahead, int stores) {
   wait_vmcnt<LOADS * AHEAD + STORES>();
 }
 
-// What the first kernel hands on.
+// What the first kernel hands on, of the tokens of sequences in the call, which padding and refused sequences are not
+// counted among: max_q of each at most.
 struct FewWork {
-  int4* seqs;                            // first token, tokens (0: none), context, its shares: first | count << 16
+  int4* seqs;                            // rank of the first token, tokens (0: none), context, its shares: first |
+                                         //   count << 16
   float2* part_ml;                       // [2 x workgroup][kCols]
-  float2* stats;                         // (m, 1 / l) [token][query head], of sequences in one share
-  float* scores;                         // [token][query head][max_ctx]
+  float2* stats;                         // (m, 1 / l) [token's rank][query head], of sequences in one share
+  float* scores;                         // [token's rank][query head][max_ctx]
 };
 
 // NC: tiles of query vectors.
@@ -139,7 +145,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
       if (i >= b.n_seq) continue;
       const int w0 = (sh.first[n] + kOverhead) / sh.share;
       const int w1 = (sh.first[n] + kOverhead + max(sh.nb[n], 1) - 1) / sh.share;
-      ws.seqs[i] = make_int4(sh.q0[n], sh.len[n], sh.ctx[n], w0 | (w1 - w0 + 1) << 16);
+      ws.seqs[i] = make_int4(sh.rank[n], sh.len[n], sh.ctx[n], w0 | (w1 - w0 + 1) << 16);
       const int s0 = b.q_start[i], s1 = b.q_start[i + 1];
       many |= s0 >= 0 && s1 >= s0 && s1 <= b.n_tokens && s1 - s0 > a.max_q;
     }
@@ -169,7 +175,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
 
   for (int pos = lo; pos < hi;) {
     // the part of one sequence that starts at pos; its overhead comes before its blocks
-    int seq = 0, u0 = 0, nb = 1, ctx = 1, q0 = 0, len = 1;
+    int seq = 0, u0 = 0, nb = 1, ctx = 1, q0 = 0, len = 1, rank = 0;
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
       const uint64_t hit = __ballot(sh.nb[n] > 0 && pos >= sh.first[n] &&
@@ -182,6 +188,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
         ctx = readlane(sh.ctx[n], l);
         q0 = readlane(sh.q0[n], l);
         len = readlane(sh.len[n], l);
+        rank = readlane(sh.rank[n], l);
       }
     }
     const int u1 = min(kOverhead + nb, u0 + (hi - pos));
@@ -194,8 +201,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
 
     // Q^T operand: column c = 16 ct + c16 = query vector (token c / G, head g*G + c % G)
     const int cols = len * G;
-    auto vec_of = [&](int c) {               // of a column in use
-      return static_cast<size_t>(q0 + c / G) * Hq + g * G + c % G;
+    auto vec_of = [&](int token, int c) {    // of a column in use, token: the sequence's first
+      return static_cast<size_t>(token + c / G) * Hq + g * G + c % G;
     };
     bool col_ok[NC];
     int lim[NC];                             // keys <= lim are visible
@@ -206,9 +213,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
       const int c = kTile * ct + c16;
       col_ok[ct] = c < cols;
       lim[ct] = ctx - len + (col_ok[ct] ? c / G : 0);
-      const size_t vec = vec_of(col_ok[ct] ? c : 0);
-      scores[ct] = ws.scores + vec * max_ctx + 4 * g4;
-      const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + vec * D;
+      scores[ct] = ws.scores + vec_of(rank, col_ok[ct] ? c : 0) * max_ctx + 4 * g4;
+      const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + vec_of(q0, col_ok[ct] ? c : 0) * D;
 #pragma unroll
       for (int kc = 0; kc < KC; ++kc)
         qf[ct][kc] = __builtin_bit_cast(bf16x8, ld16(qrow + 32 * kc + 8 * g4));
@@ -352,7 +358,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void weights_score_kern
       for (int w = 0; w < kWaves; ++w)
         if (sm[w][tid] != -INFINITY) l = fmaf(__builtin_amdgcn_exp2f(sm[w][tid] - M), sl[w][tid], l);
       if (!whole) ws.part_ml[static_cast<size_t>(slot) * kCols + tid] = make_float2(M, l);
-      else if (tid < cols) ws.stats[vec_of(tid)] = make_float2(M, 1.f / l);
+      else if (tid < cols) ws.stats[vec_of(rank, tid)] = make_float2(M, 1.f / l);
     }
   }
 }
@@ -483,9 +489,12 @@ __global__ __launch_bounds__(kSumThreads) void weights_few_add_kernel(const Attn
 struct Layout {
   size_t part_ml, stats, scores, bytes;
 };
-Layout layout(int n_tokens, int n_seq, int max_ctx, int n_q_heads) {
+// Query vectors whose scores are kept, of a call with at most max_q tokens of a sequence.
+size_t few_vecs(int n_tokens, int n_seq, int max_q, int n_q_heads) {
+  return static_cast<size_t>(std::min<int64_t>(n_tokens, static_cast<int64_t>(n_seq) * max_q)) * n_q_heads;
+}
+Layout layout(size_t vecs, int n_seq, int max_ctx) {
   Layout l;
-  const size_t vecs = static_cast<size_t>(n_tokens) * n_q_heads;
   l.part_ml = n_seq * sizeof(int4);
   l.stats = l.part_ml + 2 * kMaxWGs * kCols * sizeof(float2);
   l.scores = (l.stats + vecs * sizeof(float2) + 15) & ~static_cast<size_t>(15);
@@ -497,7 +506,7 @@ template <int D, int NS, int NC>
 hipError_t launch_t(const AttnWeightsArgs& a, hipStream_t stream) {
   const PagedBatch& b = a.batch;
   const int max_ctx = b.max_pages << b.page_shift;
-  const Layout l = layout(b.n_tokens, b.n_seq, max_ctx, a.n_q_heads);
+  const Layout l = layout(few_vecs(b.n_tokens, b.n_seq, a.max_q, a.n_q_heads), b.n_seq, max_ctx);
   uint8_t* base = static_cast<uint8_t*>(a.workspace);
   const FewWork ws{reinterpret_cast<int4*>(base), reinterpret_cast<float2*>(base + l.part_ml),
                    reinterpret_cast<float2*>(base + l.stats), reinterpret_cast<float*>(base + l.scores)};
@@ -527,20 +536,24 @@ hipError_t launch_d(const AttnWeightsArgs& a, hipStream_t stream) {
   return launch_n<D, 2>(a, stream);
 }
 
+// Query vectors of a sequence and KV head at most.
+int cols_of(int head_dim) { return head_dim > 128 ? kCols : kColsHeads; }
+
 }  // namespace
 
-bool attn_weights_few(int n_tokens, int max_ctx, int max_q, int n_q_heads, int n_kv_heads, int head_dim) {
-  return static_cast<int64_t>(max_q) * (n_q_heads / n_kv_heads) <= (head_dim > 128 ? kCols : kColsHeads) &&
-         n_kv_heads <= kMaxKvHeads &&
-         static_cast<size_t>(n_tokens) * n_q_heads * max_ctx <= kScoreBytes / sizeof(float);
+bool attn_weights_few(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, int n_kv_heads,
+                      int head_dim) {
+  return static_cast<int64_t>(max_q) * (n_q_heads / n_kv_heads) <= cols_of(head_dim) && n_kv_heads <= kMaxKvHeads &&
+         few_vecs(n_tokens, n_seq, max_q, n_q_heads) * max_ctx <= kScoreBytes / sizeof(float);
 }
 
-size_t attn_weights_few_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int n_q_heads) {
-  const size_t vecs = static_cast<size_t>(n_tokens) * n_q_heads;
-  const Layout l = layout(n_tokens, n_seq, max_ctx, n_q_heads);
+size_t attn_weights_few_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads,
+                                        int n_kv_heads, int head_dim) {
+  const int most = cols_of(head_dim) / (n_q_heads / n_kv_heads);         // tokens of a sequence
+  if (most < 1 || n_kv_heads > kMaxKvHeads) return 0;
+  const size_t vecs = few_vecs(n_tokens, n_seq, std::min(max_q, most), n_q_heads);
   // (of a call whose scores are too many to be kept: as many as are)
-  return l.scores + (vecs * max_ctx <= kScoreBytes / sizeof(float) ? vecs * max_ctx * sizeof(float)
-                                                                  : kScoreBytes);
+  return layout(vecs, n_seq, max_ctx).scores + std::min(vecs * max_ctx * sizeof(float), kScoreBytes);
 }
 
 hipError_t launch_attn_weights_few(const AttnWeightsArgs& a, hipStream_t stream) {

@@ -22,8 +22,10 @@ size_t attn_weights_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int ma
                                     int n_kv_heads, int head_dim);
 hipError_t launch_attn_weights(const AttnWeightsArgs& a, hipStream_t stream);
 // The same of few tokens per sequence (attn_weights_few.hip); whether a call's are.
-bool attn_weights_few(int n_tokens, int max_ctx, int max_q, int n_q_heads, int n_kv_heads, int head_dim);
-size_t attn_weights_few_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int n_q_heads);
+bool attn_weights_few(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads, int n_kv_heads,
+                      int head_dim);
+size_t attn_weights_few_workspace_bytes(int n_tokens, int n_seq, int max_ctx, int max_q, int n_q_heads,
+                                        int n_kv_heads, int head_dim);
 hipError_t launch_attn_weights_few(const AttnWeightsArgs& a, hipStream_t stream);
 
 struct EvictPlanArgs {

@@ -726,6 +726,36 @@ def test_weights_of_chunks_beside_single_tokens(hq, hkv, d, cap):
         assert (got[s, n:] == 77.0).all()
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (16, 1, 576), (70, 2, 64)])
+def test_weights_of_padded_batches(hq, hkv, d):
+    """Far more tokens than sequences may have, one refused in the middle: both ways stay within the workspace of the
+    call's own lengths, and one of the largest serves it with the same bits."""
+    from paper_2609_34653_amd import evict as ev, omnitide as ot
+    ctx, start, T, P, cap = [300, 200, 150, 90], [70, 72, 92, 93, 95], 300, 16, 512
+    table, n_pages = layout(ctx, P, 1, max_pages=cap // P)
+    pool = key_pool(ctx, table, n_pages, P, hkv, d, 1)
+    q = (rand(2, T, hq, d) * spread_of(d)).to(BF)
+    gpool = pool.cuda() if d <= 128 else pool.cuda().view(n_pages, P, d)
+    got = []
+    for size in ((T, 4, cap, 2), (T + 700, 9, 2 * cap, 400)):
+        nb = ev.omnitide_paged_attn_weights_workspace_bytes(*size, hq, hkv, d)
+        ws = torch.full((nb + 4096,), 0xff, dtype=torch.uint8, device="cuda")
+        out, st = torch.full((4, cap), 77.0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        ev.omnitide_paged_attn_weights(q.cuda(), gpool, i32(table), i32(start), i32(ctx), 2, scale_of(d), out,
+                                       workspace=ws[:nb], d_status=st)
+        assert int(st.item()) == ot.E_CAPACITY and (ws[nb:] == 0xff).all()
+        got.append(out)
+    assert torch.equal(got[0], got[1])
+    for s, n in enumerate(ctx):
+        if s == 1:
+            assert (got[0][s] == 77.0).all()
+            continue
+        k = pool[table[s, np.arange(n) // P], np.arange(n) % P].double().numpy()
+        w = oe.row_weights(f64(q[start[s]:start[s + 1]]), k, scale_of(d))
+        assert (np.abs(f64(got[0][s, :n]) - w) <= tolerance(d) * w).all()
+        assert (got[0][s, n:] == 77.0).all()
+
+
 # ----------------------------------------------------------------------- promises of the headers
 
 @pytest.mark.parametrize("m", [2, 40])

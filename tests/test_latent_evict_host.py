@@ -187,11 +187,32 @@ def test_weights_workspace():
 
 
 def test_weights_workspace_of_mixed_batches():
-    """Partial sums are those of the tokens that there are, not of the longest chunk for every sequence."""
+    """Partial sums are those of the tokens that there are, not of the longest chunk for every sequence; beside them
+    at most the 2^30 bytes of scores that calls of few tokens keep."""
     size = ev.omnitide_paged_attn_weights_workspace_bytes
     # one chunk of 4,096 beside 1,023 single tokens: 16 + 1,023 row chunks of 8 heads of 16,384 sums
-    assert size(5119, 1024, 16384, 4096, 32, 8, 128) < (16 + 1023 + 3) * 8 * 16384 * 4 + (1 << 25)
-    assert size(2463, 64, 131072, 2400, 32, 8, 128) < (9 + 64 + 1) * 8 * 131072 * 4 + (1 << 25)
+    assert size(5119, 1024, 16384, 4096, 32, 8, 128) < max(1 << 30, (16 + 1023 + 3) * 8 * 16384 * 4) + (1 << 25)
+    assert size(2463, 64, 131072, 2400, 32, 8, 128) < max(1 << 30, (9 + 64 + 1) * 8 * 131072 * 4) + (1 << 25)
+    # more query heads for a KV head than the way of few takes: the partial sums alone
+    assert size(5119, 1024, 16384, 4096, 264, 4, 64) < (330 + 1024) * 4 * 16384 * 4 + (1 << 28)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(32, 8, 128), (4, 1, 64), (16, 1, 576), (128, 1, 576), (65, 65, 64), (256, 2, 64)])
+def test_weights_workspace_never_falls(Hq, Hkv, d):
+    """In any of its lengths: a workspace for the largest calls serves every one of them, whichever way it goes."""
+    size = ev.omnitide_paged_attn_weights_workspace_bytes
+    T, S, M, Q = [1, 24, 192, 193, 665, 5000], [1, 7, 24, 300], [16, 256, 20096, 131072], [1, 2, 4, 8, 9, 64, 65, 4000]
+    for a in T:
+        for b in S:
+            for c in M:
+                for q in Q:
+                    base = size(a, b, c, q, Hq, Hkv, d)
+                    for k, more in enumerate((T, S, M, Q)):
+                        at = [a, b, c, q]
+                        i = more.index(at[k])
+                        if i + 1 < len(more):
+                            at[k] = more[i + 1]
+                            assert size(*at, Hq, Hkv, d) >= base, (a, b, c, q, at)
 
 
 def plan(L, **kw):
