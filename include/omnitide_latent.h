@@ -83,7 +83,8 @@ int omnitide_paged_rows(const void* pool, int n_pages, int page_size, int row_el
  *   q           bf16 [n_seq][n_q][n_heads][latent_dim + 64]: the absorbed queries (A_h^T n, r)
  *   out         [n_seq][n_q][n_heads][latent_dim] of out_dtype; a sequence with ctx_len 0 is idle: zeros
  *   workspace   device scratch of omnitide_latent_decode_workspace_bytes() bytes, as for
- *               omnitide_paged_decode_attn (its size depends on latent_dim and n_q * n_heads alone)
+ *               omnitide_paged_decode_attn (its size depends on latent_dim and n_q * n_heads alone, and
+ *               never falls as either grows)
  * Numerics: as omnitide_paged_decode_attn (bf16 inputs, float accumulation and softmax, probabilities with
  * 16 significant bits): out is off by at most 2^-16 sum_j p_j |c_j - out| for the probabilities' rounding.
  * Limits: n_q * n_heads <= 1024, n_seq <= 1024, n_seq * max_pages * page_size <= 2^34, |scale| <= 1e30.

@@ -630,8 +630,8 @@ hipError_t launch_r(const LatentDecodeArgs& a, hipStream_t stream) {
 }  // namespace
 
 size_t latent_decode_workspace_bytes(int n_q, int n_heads, int latent_dim) {
-  const int groups = groups_of(n_q * n_heads);
-  const size_t rows = static_cast<size_t>(2 * shares_of(groups) * groups) * part_rows(n_q * n_heads);
+  // (of kWGs workgroups, which some numbers of groups leave a few of: a larger call's serves a smaller one)
+  const size_t rows = static_cast<size_t>(2 * kWGs) * part_rows(n_q * n_heads);
   return rows * (static_cast<size_t>(latent_dim) + 2) * sizeof(float);
 }
 

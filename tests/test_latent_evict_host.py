@@ -124,6 +124,15 @@ def test_decode_workspace(L):
         assert size(*bad) == 0
 
 
+def test_decode_workspace_never_falls():
+    size = la.omnitide_latent_decode_workspace_bytes
+    for R in (256, 512):
+        got = [size(1, 1, 64, m, R) for m in range(1, 1025)]
+        assert got == sorted(got) and got[0] > 0
+        assert all(size(1, nq, 64, 16, R) == got[16 * nq - 1] for nq in range(1, 65))
+    assert size(1, 1, 64, 16, 256) < size(1, 1, 64, 16, 512)
+
+
 def chunk(L, **kw):
     a = dict(q=fake(0), k=fake(1), v=fake(1, 256), kr=fake(2), ks=4096, kh=256, vs=4096, vh=256, es=576,
              st=fake(3), kst=fake(4), S=4, n=50, N=900, H=16, d=128, scale=0.1, out=fake(5), od=0,
