@@ -110,7 +110,8 @@ size_t omnitide_latent_decode_workspace_bytes(int n_seq, int n_q, int max_ctx, i
  *               (v_head_stride) elements apart, so that parts of one projection can be passed
  *   k_rope      bf16 [n_rows][64], rows k_rope_stride elements apart (a part of omnitide_paged_rows'
  *               output), shared by the heads
- *   kv_start    int32 [n_seq + 1], as q_start with n_rows in place of n_tokens
+ *   kv_start    int32 [n_seq + 1], as q_start with n_rows in place of n_tokens (of n_rows 0, all tokens being
+ *               padding, k, v and k_rope may be NULL)
  *   out         [n_tokens][n_heads][head_dim] of out_dtype, contiguous
  *   workspace   device scratch of omnitide_latent_chunk_attn_workspace_bytes() bytes, as for
  *               omnitide_paged_chunk_attn

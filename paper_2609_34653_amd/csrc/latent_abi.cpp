@@ -198,7 +198,8 @@ int omnitide_latent_chunk_attn(const void* q, const void* k, const void* v, cons
                                int n_heads, int head_dim, float scale, void* out, int out_dtype,
                                void* workspace, size_t workspace_bytes, int32_t* d_status,
                                void* stream) {
-  if (!all_set({q_start, kv_start}) || (n_tokens != 0 && !all_set({q, k, v, k_rope, out})))
+  if (!all_set({q_start, kv_start}) || (n_tokens != 0 && !all_set({q, out})) ||
+      (n_tokens != 0 && n_rows != 0 && !all_set({k, v, k_rope})))
     return OMNITIDE_E_NULL;
   const int ob = elt_bytes(out_dtype);
   if (ob == 0) return OMNITIDE_E_DTYPE;
@@ -257,7 +258,7 @@ int omnitide_latent_chunk_attn(const void* q, const void* k, const void* v, cons
 
 size_t omnitide_latent_chunk_attn_workspace_bytes(int n_tokens, int n_seq, int n_rows, int n_heads,
                                                   int head_dim) {
-  if (n_tokens < 1 || n_tokens > kMaxTokens || n_seq < 1 || n_seq > kMaxAttnSeqs || n_rows < 1 ||
+  if (n_tokens < 1 || n_tokens > kMaxTokens || n_seq < 1 || n_seq > kMaxAttnSeqs || n_rows < 0 ||
       n_rows > kMaxRows || n_heads < 1 || n_heads > kMaxHeads || !head_dim_ok(head_dim))
     return 0;
   return omnitide::latent_chunk_workspace_bytes(head_dim);

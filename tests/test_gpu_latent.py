@@ -805,6 +805,16 @@ def test_chunk_scales(scale):
         near(got[t], want, spread, 2.0 ** -11, F32)
 
 
+@pytest.mark.parametrize("start,refused", [([0, 0, 0], False), ([3, 3, 3], False), ([0, 2, 2], True)])
+def test_chunk_of_padding_alone(start, refused):
+    """No rows: nothing is written, and a sequence that has tokens all the same is refused on the device."""
+    from paper_2609_34653_amd import omnitide as ot
+    H, d = 4, 64
+    none = torch.empty(0, H, 2 * d, dtype=BF, device="cuda")
+    got, st = chunk(rand(1, 5, H, d + E).to(BF).cuda(), none, none[:, 0, :E], start, [0, 0, 0], 0.1, F32)
+    assert st == (ot.E_CAPACITY if refused else 0) and torch.isnan(got).all()
+
+
 def test_append_with_offsets_out_of_order():
     """Tokens that lie in the offsets of a sequence go to their rows there, each once; no other row changes."""
     from paper_2609_34653_amd import latent as la, paged as pg

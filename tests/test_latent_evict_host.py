@@ -157,6 +157,13 @@ def test_chunk_refusals(L):
     assert chunk(L, n=0, q=None, k=None, v=None, kr=None, out=None, ws=None) == ot.OK
 
 
+def test_chunk_of_padding_alone():
+    """No rows at all is a call, with a workspace as large as any."""
+    size = la.omnitide_latent_chunk_attn_workspace_bytes
+    assert size(5, 2, 0, 4, 64) == size(5, 2, 100, 4, 64) > 0
+    assert size(5, 2, -1, 4, 64) == 0
+
+
 # --------------------------------------------------------------------------------- eviction
 
 def weights(L, **kw):
