@@ -18,6 +18,7 @@
 // lane and a pair per lane.  An item is 16 bytes next to each other, but of the rotated dimensions in the style that
 // pairs the halves, twice four values, so that both members of a pair sit in one lane.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "evict.h"
@@ -362,18 +363,20 @@ __global__ __launch_bounds__(kPlanThreads) void evict_place_kernel(const EvictPl
 // ---------------------------------------------------------------------------------------------
 
 constexpr int kMoveThreads = 256;
-constexpr int kMoveFlight = 2;           // items of a thread on their way at once
+constexpr int kMoveFlight = 2;           // items of a thread, on their way at once
 constexpr int kMoveRows = 16;            // rows of a workgroup at most
 constexpr int kMoveGrid = 1 << 20;       // workgroups along x at most (2^32 threads are not launched)
 
-// How a workgroup's items are numbered: `rows` rows of `per` items, `per_head` of each head; quotients of numbers
-// below 1,024 by multiplication (x * magic >> 20: exact, as 1,024 x 1,024 = 2^20).
+// How a workgroup's items are numbered: `rows` rows of `per` items, `per_head` of each head, kMoveFlight for each thread
+// at most; quotients of numbers below 1,024 by multiplication (x * magic >> 20: exact, as 1,024 x 1,024 = 2^20).
+static_assert(OMNITIDE_MAX_ROW_ELEMS / 8 <= kMoveFlight * kMoveThreads, "a workgroup holds a row");
 struct MoveItems {
   int rows, per, per_head;
   uint32_t by_per, by_head;
 };
 
-template <bool HALF, bool TURN>
+// VALUES: a pool of values beside that of keys.
+template <bool HALF, bool TURN, bool VALUES>
 __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const PagedCompactArgs a,
                                                                    const MoveItems items) {
   __shared__ __attribute__((aligned(16))) float2 cs[kMoveRows][kMaxRopePairs];
@@ -414,55 +417,51 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
   const int all = items.rows * items.per, R = TURN ? a.rope_dims : 0;
   const size_t row_bytes = static_cast<size_t>(a.row_elems) * 2;
 
-  u32x2 ka[kMoveFlight], kb[kMoveFlight];
-  u32x4 v[kMoveFlight];
+  u32x4 kv[kMoveFlight], v[kMoveFlight];  // four values from da on and four from db on; eight
   int row[kMoveFlight], piece[kMoveFlight], da[kMoveFlight], db[kMoveFlight], pair[kMoveFlight];
   bool on[kMoveFlight];
-  auto load = [&](int it0) {
 #pragma unroll
-    for (int f = 0; f < kMoveFlight; ++f) {
-      const int it = it0 + f * kMoveThreads + tid;
-      const bool in = it < all;
-      row[f] = in ? static_cast<int>((static_cast<uint32_t>(it) * items.by_per) >> 20) : 0;
-      piece[f] = in ? it - row[f] * items.per : 0;
-      const int64_t at = __shfl(static_cast<long long>(from), row[f], kWave);
-      on[f] = in && at >= 0;
-      pair[f] = -1;
-      da[f] = 8 * piece[f];
-      db[f] = 8 * piece[f] + 4;
-      if constexpr (TURN) {
-        // of each head first the rotated items, then the other dimensions
-        const int head = static_cast<int>((static_cast<uint32_t>(piece[f]) * items.by_head) >> 20);
-        const int x = piece[f] - head * items.per_head;
-        if (8 * x < R) {
-          pair[f] = 4 * x;
-          da[f] = a.rope_offset + (HALF ? 4 * x : 8 * x);
-          db[f] = a.rope_offset + (HALF ? R / 2 + 4 * x : 8 * x + 4);
-        } else {
-          const int d = 8 * x - R;
-          da[f] = d < a.rope_offset ? d : d + R;
-          db[f] = da[f] + 4;
-        }
-        da[f] += head * a.head_dim;
-        db[f] += head * a.head_dim;
+  for (int f = 0; f < kMoveFlight; ++f) {
+    const int it = f * kMoveThreads + tid;
+    const bool in = it < all;
+    row[f] = in ? static_cast<int>((static_cast<uint32_t>(it) * items.by_per) >> 20) : 0;
+    piece[f] = in ? it - row[f] * items.per : 0;
+    const int64_t at = __shfl(static_cast<long long>(from), row[f], kWave);
+    on[f] = in && at >= 0;
+    pair[f] = -1;
+    da[f] = 8 * piece[f];
+    db[f] = 8 * piece[f] + 4;
+    if constexpr (TURN) {
+      // of each head first the rotated items, then the other dimensions
+      const int head = static_cast<int>((static_cast<uint32_t>(piece[f]) * items.by_head) >> 20);
+      const int x = piece[f] - head * items.per_head;
+      if (8 * x < R) {
+        pair[f] = 4 * x;
+        da[f] = a.rope_offset + (HALF ? 4 * x : 8 * x);
+        db[f] = a.rope_offset + (HALF ? R / 2 + 4 * x : 8 * x + 4);
+      } else {
+        const int d = 8 * x - R;
+        da[f] = d < a.rope_offset ? d : d + R;
+        db[f] = da[f] + 4;
       }
-      if (on[f]) {
-        const uint8_t* k = static_cast<const uint8_t*>(a.k) + at * row_bytes;
-        if (!HALF || pair[f] < 0) {        // next to each other
-          const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + 2 * da[f]));
-          ka[f] = u32x2{x[0], x[1]};
-          kb[f] = u32x2{x[2], x[3]};
-        } else {
-          ka[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * da[f]));
-          kb[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * db[f]));
-        }
-        if (a.v != nullptr)
-          v[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
-              static_cast<const uint8_t*>(a.v) + at * row_bytes + 16 * piece[f]));
-      }
+      da[f] += head * a.head_dim;
+      db[f] += head * a.head_dim;
     }
-  };
-  load(0);
+    // (an item that does not move reads the pool's first row: no branch around the loads, whose results would be
+    // copied, and so waited for one by one, where its ways meet: 41 us in place of 38 for 24 streams, plan and move)
+    const size_t byte = on[f] ? at * row_bytes : 0;
+    const uint8_t* k = static_cast<const uint8_t*>(a.k) + byte;
+    if (!HALF || pair[f] < 0) {            // next to each other
+      kv[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + 2 * da[f]));
+    } else {
+      const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * da[f]));
+      const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(k + 2 * db[f]));
+      kv[f] = u32x4{x[0], x[1], y[0], y[1]};
+    }
+    if constexpr (VALUES)
+      v[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.v) + byte +
+                                                                       16 * piece[f]));
+  }
   if constexpr (TURN) {                  // the angles, while the first rows are on their way
     for (int x = tid; x < kMoveRows * kMaxRopePairs; x += kMoveThreads) {
       const int r = x / kMaxRopePairs, p = x % kMaxRopePairs;
@@ -476,38 +475,34 @@ __global__ __launch_bounds__(kMoveThreads) void paged_compact_kernel(const Paged
     }
     __syncthreads();
   }
-  for (int it0 = 0; it0 < all; it0 += kMoveFlight * kMoveThreads) {
-    if (it0 > 0) load(it0);
 #pragma unroll
-    for (int f = 0; f < kMoveFlight; ++f) {
-      const int64_t at = __shfl(static_cast<long long>(to), row[f], kWave);
-      if constexpr (TURN) {
-        const int d = __shfl(shift, row[f], kWave);
-        if (on[f] && pair[f] >= 0 && d != 0) {
-          floatx4 x = unpack_quad<false>(u32x4{ka[f][0], ka[f][1], 0, 0});
-          floatx4 y = unpack_quad<false>(u32x4{kb[f][0], kb[f][1], 0, 0}), c, sn;
+  for (int f = 0; f < kMoveFlight; ++f) {
+    const int64_t at = __shfl(static_cast<long long>(to), row[f], kWave);
+    if constexpr (TURN) {
+      const int d = __shfl(shift, row[f], kWave);
+      if (on[f] && pair[f] >= 0 && d != 0) {
+        floatx4 x = unpack_quad<false>(u32x4{kv[f][0], kv[f][1], 0, 0});
+        floatx4 y = unpack_quad<false>(u32x4{kv[f][2], kv[f][3], 0, 0}), c, sn;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 t = cs[row[f]][pair[f] + e];
-            c[e] = t.x;
-            sn[e] = t.y;
-          }
-          turn_quads<HALF>(x, y, c, sn);
-          ka[f] = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-          kb[f] = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        for (int e = 0; e < 4; ++e) {
+          const float2 t = cs[row[f]][pair[f] + e];
+          c[e] = t.x;
+          sn[e] = t.y;
         }
+        turn_quads<HALF>(x, y, c, sn);
+        kv[f] = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
       }
-      if (!on[f]) continue;
-      uint8_t* k = static_cast<uint8_t*>(a.k) + at * row_bytes;
-      if (!HALF || pair[f] < 0) {
-        *reinterpret_cast<u32x4*>(k + 2 * da[f]) = u32x4{ka[f][0], ka[f][1], kb[f][0], kb[f][1]};
-      } else {
-        *reinterpret_cast<u32x2*>(k + 2 * da[f]) = ka[f];
-        *reinterpret_cast<u32x2*>(k + 2 * db[f]) = kb[f];
-      }
-      if (a.v != nullptr)
-        *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.v) + at * row_bytes + 16 * piece[f]) = v[f];
     }
+    if (!on[f]) continue;
+    uint8_t* k = static_cast<uint8_t*>(a.k) + at * row_bytes;
+    if (!HALF || pair[f] < 0) {
+      *reinterpret_cast<u32x4*>(k + 2 * da[f]) = kv[f];
+    } else {
+      *reinterpret_cast<u32x2*>(k + 2 * da[f]) = u32x2{kv[f][0], kv[f][1]};
+      *reinterpret_cast<u32x2*>(k + 2 * db[f]) = u32x2{kv[f][2], kv[f][3]};
+    }
+    if constexpr (VALUES)
+      *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.v) + at * row_bytes + 16 * piece[f]) = v[f];
   }
 }
 
@@ -594,12 +589,18 @@ hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream) {
   const int64_t gx = std::min(blocks, static_cast<int64_t>(kMoveGrid));
   const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>(a.batch.n_seq),
                   static_cast<unsigned>((blocks + gx - 1) / gx));
-  if (a.rope_dims == 0)
-    hipLaunchKernelGGL((paged_compact_kernel<false, false>), grid, dim3(kMoveThreads), 0, stream, a, items);
-  else if (a.rope_half)
-    hipLaunchKernelGGL((paged_compact_kernel<true, true>), grid, dim3(kMoveThreads), 0, stream, a, items);
-  else
-    hipLaunchKernelGGL((paged_compact_kernel<false, true>), grid, dim3(kMoveThreads), 0, stream, a, items);
+  const dim3 block(kMoveThreads);
+  auto launch = [&](auto values) {
+    constexpr bool V = decltype(values)::value;
+    if (a.rope_dims == 0)
+      hipLaunchKernelGGL((paged_compact_kernel<false, false, V>), grid, block, 0, stream, a, items);
+    else if (a.rope_half)
+      hipLaunchKernelGGL((paged_compact_kernel<true, true, V>), grid, block, 0, stream, a, items);
+    else
+      hipLaunchKernelGGL((paged_compact_kernel<false, true, V>), grid, block, 0, stream, a, items);
+  };
+  if (a.v != nullptr) launch(std::true_type{});
+  else launch(std::false_type{});
   return hipGetLastError();
 }
 
