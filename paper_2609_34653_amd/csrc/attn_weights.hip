@@ -69,7 +69,6 @@ struct Stage {
       oct[i] = call / kOctCalls;
       row[i] = at / kChunks;
       piece[i] = 16u * ((at % kChunks) ^ (swz(8 * oct[i] + row[i]) & (kChunks - 1)));
-      if (D > 128) piece[i] = 16u * ((at % kChunks) ^ swz(8 * oct[i] + row[i]));
     }
   }
   // where load i of the ring's entry e goes
