@@ -15,10 +15,10 @@
 //             workgroups as the chip holds take them in turn, two on a CU for d <= 128, so that one's vector work
 //             hides what the other waits for.
 //   sums      no atomics: every item owns its place in a buffer of partial sums, added in a fixed order.
-//   measured  665 tokens of 32 heads over 17,048 keys of 8 x 128: 139 us and 143 us for the passes (91 GFLOP each), 5
-//             us for each of the other two kernels.  Matrix cores busy 0.41 and 0.36, vector units 0.64 and 0.61: what
-//             one waits for, the other does, most of the time.  In the first pass the products of the next keys
-//             stand between the exponentials of these (whole row tiles in turn, without: 170 us); in the second
+//   measured  665 tokens of 32 heads over 17,048 keys of 8 x 128: 137 to 145 us and 140 to 148 us by card for the passes
+//             (91 GFLOP each), 5 us for each of the other two kernels.  Matrix cores busy 0.41 and 0.36, vector units
+//             0.64 and 0.61: they work in turn, so their times add up.  In the first pass the products of the next
+//             keys stand between the exponentials of these (whole row tiles in turn, without: 170 us); in the second
 //             that takes the registers that a second workgroup of the CU needs (191 us and more).
 #include <type_traits>
 

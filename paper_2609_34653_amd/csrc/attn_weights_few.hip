@@ -15,8 +15,8 @@
 //   products  S^T (16 keys x 16 vectors) = K Q^T with v_mfma_f32_16x16x32_bf16, for one, two or four tiles of
 //             vectors: a lane holds four consecutive keys of a vector, stored as 16 bytes.
 //   vectors   against the two passes: 24 x 8 tokens of 32 / 8 heads (32 vectors) 117 us, 137 there; 24 streams of
-//             latents with 32 heads 49 us, 97 there; with 64 heads 70 us, 105 there.  (More of them than that,
-//             and the scores outweigh the keys, or the queries the registers.)
+//             latents with 32 heads 49 us, 97 there; with 64 heads 70 us, 105 there (128 heads, there alone: 113 us).
+//             More of them than that, and the scores outweigh the keys, or the queries the registers.
 #include <algorithm>
 #include <type_traits>
 

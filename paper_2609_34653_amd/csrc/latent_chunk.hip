@@ -14,9 +14,9 @@
 // Each probability enters the value products as its bf16 rounding and the rounding of the remainder (16 significant
 // bits, as in paged decode and the absorbed form, so that both forms of one cache agree); the sum takes the same two.
 // Rounded once, as paged_chunk.hip does, a float output was off by 1.5e-3 of itself and a bf16 one by a third more
-// than its own rounding, for 131 us a call in place of 171 (665 tokens over 17,048 keys, 16 heads of 128).
+// than its own rounding, for 131 us a call in place of 171 to 174 (665 tokens over 17,048 keys, 16 heads of 128).
 //
-// Those 171 us, 8 of them the merge: 114 GFLOP, 159 executed (0.67 and 0.93 PFLOP/s; matrix cores busy 0.51, as in
+// Of those, 8 us are the merge: 114 GFLOP, 159 executed (0.67 and 0.93 PFLOP/s; matrix cores busy 0.50, as in
 // paged_chunk.hip, at the clock that power allows); 89 tokens over 601, 4 heads of 64: 13.5 us, latency.
 #include <type_traits>
 
