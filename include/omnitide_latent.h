@@ -20,7 +20,9 @@
  * The conventions of omnitide_paged.h hold (page_table, ctx_len, q_start and their device checks, a
  * padded batch, bad pages, limits).  The pool is bf16 [n_pages][page_size][latent_dim + 64]: latent_dim
  * (256 or 512) values of the latent, then the 64 of the key part.  To the calls of omnitide_evict.h it
- * is a pool of one KV head of latent_dim + 64.
+ * is a pool of one KV head of latent_dim + 64.  As there, the values of rows in use are finite numbers to the
+ * attention calls (a token whose row lies in front of one that is not may come out as NaN too); those of other
+ * rows may be anything.
  */
 #ifndef OMNITIDE_LATENT_H
 #define OMNITIDE_LATENT_H

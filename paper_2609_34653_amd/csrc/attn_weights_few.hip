@@ -9,7 +9,7 @@
 //             equal shares, one per workgroup and KV head, a fixed cost counted for each sequence.
 //   waves     each takes every fourth block of its workgroup's part and owns a ring of LDS buffers filled by
 //             direct loads marked as read once; no barrier until the waves merge.
-//   measured  24 tokens of 32 heads over 119,095 keys of 8 x 128 in all: 50 us for the scores (244 MB read and 15
+//   measured  24 tokens of 32 heads over 119,095 keys of 8 x 128 in all: 51 us for the scores (244 MB read and 15
 //             written, 5.2 TB/s, a copy's rate; without the stores 42 us; with non-temporal ones 54 us) and
 //             9 us for the sum (7 us and a kernel of 4.6 us for the join, when that was one).
 //   products  S^T (16 keys x 16 vectors) = K Q^T with v_mfma_f32_16x16x32_bf16, for one, two or four tiles of

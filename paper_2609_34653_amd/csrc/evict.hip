@@ -12,8 +12,8 @@
 //
 // The move is a copy: each kept row is read and written once, behind a chain of four loads (length, row, page,
 // values).  So a workgroup takes only as many rows as its threads hold in two items of eight values each, and
-// many of them run at once: 4 (key, value) rows of 1,024 or 7 latent rows of 576.  16,384 of the former: 29 us (134
-// MB, 4.7 TB/s; 35 us with waves of their own of four items a lane), 55,939 of the latter: 29 us (129 MB, 4.4 TB/s; 44
+// many of them run at once: 4 (key, value) rows of 1,024 or 7 latent rows of 576.  16,384 of the former: 28 us (134
+// MB, 4.8 TB/s; 35 us with waves of their own of four items a lane), 55,939 of the latter: 29 us (129 MB, 4.4 TB/s; 44
 // us with one item a thread, 34 with all items in two halves).  Pages and angles are worked out a row per
 // lane and a pair per lane.  An item is 16 bytes next to each other, but of the rotated dimensions in the style that
 // pairs the halves, twice four values, so that both members of a pair sit in one lane.

@@ -30,12 +30,12 @@
 //             the second product as it stands.  Each probability enters it as its bf16 rounding and the rounding of
 //             the remainder (16 significant bits, as in paged decode); the sum takes the same two.  Rounded to bf16
 //             once, float outputs were off by 1e-3 of themselves and bf16 ones by a fifth more than their own
-//             rounding, for 53 us in place of 64 below (14.7 in place of 15.9 for 16 vectors).  The roundings cross
+//             rounding, for 52 us in place of 65 below (14.7 in place of 15.5 for 16 vectors).  The roundings cross
 //             before the value products; the remainders, for which no LDS is left, in their middle, in the part of
 //             the keys that the values do not have.
-//   measured  24 x 128 vectors over 119,095 rows of 576 in all: 64 us and 10 us for the merge (33 GFLOP, 49 executed;
+//   measured  24 x 128 vectors over 119,095 rows of 576 in all: 65 us and 10 us for the merge (33 GFLOP, 49 executed;
 //             matrix cores busy 0.40; the start of a part takes 5 us and its end 4, which writes 37 MB).
-//             16 vectors over 16,948 rows: 15.9 and 7 us, all of it latency (pages, first keys, two steps, parts).
+//             16 vectors over 16,948 rows: 15.5 and 7 us, all of it latency (pages, first keys, two steps, parts).
 #include "common.h"
 #include "latent.h"
 #include "mfma_tile.h"

@@ -4,7 +4,7 @@
 // pieces, so that its loads are full whatever the row's width; the page of each row is looked up by a lane of
 // its own, and the pieces fetch it from there.  Offsets are searched once per sequence that a wave's rows are
 // of, not once per row.  Eight streams' 47,341 rows of 1,024 values: 36 us (194 MB, 5.3 TB/s, a large
-// copy's rate; 46 us with a search per row, 44 us with stores through the cache); 17,048 rows of 576: 8.4 us
+// copy's rate; 46 us with a search per row, 44 us with stores through the cache); 17,048 rows of 576: 7.8 to 8.5 us
 // (10.8 us with non-temporal loads, which pass by the caches that hold a pool just written).
 #include "common.h"
 #include "latent.h"
