@@ -30,13 +30,11 @@ __device__ inline int scalar_entry(const int32_t* table, int i) {
   return reinterpret_cast<const_i32>(reinterpret_cast<uintptr_t>(table))[__builtin_amdgcn_readfirstlane(i)];
 }
 
-// The sequence whose offsets hold wave-uniform token t: 64 sequences per step, one per lane.  Malformed offsets
-// match no token (report_batch tells of them); fits: its rows are at least its tokens, and its table holds them.
-struct TokenSeq {
-  int seq, s0, s1, ctx;                  // seq < 0: none
-  bool fits;
-};
-__device__ inline TokenSeq find_seq(const PagedBatch& b, int t) {
+// The sequence whose offsets hold wave-uniform token t, 64 sequences per step, one per lane: hit(sequence, its first
+// token, the one behind its last, its rows, whether these are fewer than its tokens or more than its table holds), or none.
+// Malformed offsets match no token (report_batch tells of them).
+template <class T, class Hit>
+__device__ inline T find_seq(const PagedBatch& b, int t, T none, Hit hit) {
   const int lane = threadIdx.x & (kWave - 1);
   for (int i0 = 0; i0 < b.n_seq; i0 += kWave) {
     const int i = i0 + lane;
@@ -46,16 +44,16 @@ __device__ inline TokenSeq find_seq(const PagedBatch& b, int t) {
       s1 = b.q_start[i + 1];
       c = b.ctx_len[i];
     }
-    const uint64_t hit = __ballot(s0 >= 0 && s0 <= t && t < s1 && s1 <= b.n_tokens);
-    if (hit != 0) {
-      const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+    const uint64_t at = __ballot(s0 >= 0 && s0 <= t && t < s1 && s1 <= b.n_tokens);
+    if (at != 0) {
+      const int l = __ffsll(static_cast<unsigned long long>(at)) - 1;
       s0 = readlane(s0, l);
       s1 = readlane(s1, l);
       c = readlane(c, l);
-      return {i0 + l, s0, s1, c, c >= s1 - s0 && c <= (b.max_pages << b.page_shift)};
+      return hit(i0 + l, s0, s1, c, c < s1 - s0 || c > (b.max_pages << b.page_shift));
     }
   }
-  return {-1, 0, 0, 0, false};
+  return none;
 }
 
 // Sequence and row of a token: in [0, ctx_len) of a sequence whose ctx_len fits its table.
@@ -63,9 +61,10 @@ struct TokenRow {
   int seq, row;                          // seq < 0: the token belongs to no (valid) sequence
 };
 __device__ inline TokenRow find_token(const PagedBatch& b, int t) {
-  const TokenSeq q = find_seq(b, t);
-  if (q.seq < 0 || !q.fits) return {-1, 0};
-  return {q.seq, q.ctx - (q.s1 - t)};
+  return find_seq(b, t, TokenRow{-1, 0}, [&](int seq, int, int s1, int ctx, bool bad) {
+    if (bad) return TokenRow{-1, 0};
+    return TokenRow{seq, ctx - (s1 - t)};
+  });
 }
 
 // One wave reports what is wrong with a batch's offsets and lengths.
@@ -95,10 +94,10 @@ struct RowRun {
   int seq, row, left;
 };
 __device__ inline RowRun find_rows(const PagedBatch& b, int t) {
-  const TokenSeq q = find_seq(b, t);
-  if (q.seq < 0) return {-1, 0, 1};
-  if (!q.fits) return {-1, 0, q.s1 - t};
-  return {q.seq, t - q.s0, q.s1 - t};
+  return find_seq(b, t, RowRun{-1, 0, 1}, [&](int seq, int s0, int s1, int, bool bad) {
+    if (bad) return RowRun{-1, 0, s1 - t};
+    return RowRun{seq, t - s0, s1 - t};
+  });
 }
 
 }  // namespace omnitide
